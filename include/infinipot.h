@@ -204,6 +204,128 @@ CCD_API int ccd_score_lse(const ccd_shape_t* shape, const void* Q_cat, const voi
 CCD_API int ccd_compress_lse(const ccd_shape_t* shape, const void* Q_cat, void* K, void* V, const float* lse, float* novelty,
                      float* scores_opt, int32_t* keep_idx, void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- Several sequences at once: a paged cache ---------------------------------------------------------------------
+ *
+ * The cache of one layer is n_pages pages of `page` tokens each, K_pages and V_pages [n_pages, Hkv, page, d] (any order of
+ * the outer three dimensions in memory: the strides say).  Row b of a block table names the pages of sequence b: its
+ * token at position t stands in row t % page of page block_table[b][t / page].  A step adds new tokens to some of the
+ * sequences; they are numbered sequence after sequence, those of sequence b being q_start[b] .. q_start[b + 1] - 1.
+ *
+ *   ccd_paged_plan    which pages the sequences take or give back, which row every new token's key and value go to
+ *   ccd_rope          rotary embedding of the new tokens' queries and keys at their positions
+ *   ccd_paged_append  writes the new keys and values to their rows (the keys embedded on the way, if asked for)
+ *   ccd_paged_attend  attention of the new tokens over what their sequences have cached, with the rows' log-sum-exps
+ *
+ * A memory pot is such a cache: one page of n_cap tokens per (sequence, layer).  The log-sum-exps of the catalyst
+ * prompt's rows over a pot (`behind` = 1) are the `lse` of ccd_score_lse and ccd_compress_lse.
+ * Lengths, block tables, slots and positions are read on the device; what they say is checked there: a page outside
+ * 0 .. n_pages - 1 holds no tokens, a slot outside the cache is not written, rows beyond `tokens` are not touched. */
+typedef struct {
+  int32_t B;                  /* sequences (rows of the block table)                                               */
+  int32_t tokens;             /* rows of Q, out, lse, K_new, V_new, slots, positions: the step's new tokens and any  */
+                              /* padding behind the last sequence's, which is left as it is                         */
+  int32_t Hq, Hkv, d;         /* query heads, KV heads (Hq % Hkv == 0), head dimension 64 or 128                    */
+  int32_t dtype;              /* CCD_FP32 or CCD_BF16, for Q, out, K, V                                             */
+  int32_t page, n_pages;      /* tokens per page, pages of the cache; page * n_pages < 2^31                         */
+  int32_t table_width;        /* entries per row of the block table; page * table_width < 2^31                      */
+  int32_t window;             /* sliding attention window in tokens, 0 = none: a query at position p sees the       */
+                              /* positions p - window + 1 .. p only                                                 */
+  int32_t behind;             /* 0: the new tokens are the last ones of kv_len, and see the keys up to their own;   */
+                              /* 1: they stand behind the kv_len cached ones, whose keys they all see, and their    */
+                              /* own keys are not in the cache (the catalyst prompt over a pot)                     */
+  int32_t max_new, max_len;   /* the largest number of new tokens of a sequence and the largest kv_len, as far as   */
+                              /* the host knows (0: it does not).  They choose kernels and how the work is cut;     */
+                              /* results do not depend on them beyond rounding.                                     */
+  float scale;                /* logit scale; 0 means 1/sqrt(d)                                                     */
+  int64_t page_stride, head_stride, row_stride;      /* K_pages, V_pages, in elements                                */
+  int64_t new_stride_t, new_stride_h;                /* K_new, V_new [tokens, Hkv, d]                                */
+  int64_t q_stride_b, q_stride_t, q_stride_h;        /* new token i of sequence b, head h: at b * q_stride_b         */
+                              /* + (q_start[b] + i) * q_stride_t + h * q_stride_h of Q.  Q [tokens, Hq, d]: stride_b 0;  */
+                              /* m tokens of every sequence as [B, Hq, m, d]: stride_t d, stride_b (Hq - 1) * m * d  */
+  int64_t o_stride_b, o_stride_t, o_stride_h;        /* out, likewise                                                */
+  int64_t lse_stride_b, lse_stride_t, lse_stride_h;  /* lse, likewise                                                */
+} ccd_paged_t;
+
+/* Plans a step: lengths before and after it (len_before, len_after int32 [B]; negative counts as 0) to pages and rows.
+ * Sequence b needs ceil(len / page) pages, at most table_width.  One that grows takes pages from a ring of free ones, in
+ * the order of the sequences; one that shrinks (a finished request: to 0; a distilled one) gives its last pages back, behind
+ * those in the ring: a page given back in this call is handed out by the next one at the earliest.
+ *   block_table       int32 [B, table_width], the pages now held: ceil(len_before / page) in front of every row
+ *   block_table_next  int32 [B, table_width], the pages held after the step, -1 behind them.  May be block_table: then only
+ *                     the entries taken or given back are written.
+ *   free_pages        int32 [n_pages], the ring: pages given back are written behind the others
+ *   cursor            int32 [4]: place of the first free page in the ring, number of free pages, pages that were asked for
+ *                     and not there (output only), and 0.  cursor_next takes the values after the step and may be cursor.
+ *   q_start           int32 [B + 1]: number of the first new token of every sequence, and of all
+ *   slots, positions  int32 [tokens] each: of every new token the row page_id * page + row_in_page it goes to and its
+ *                     position in its sequence; -1 both behind the last one.  A token whose page was not there has slot -1
+ *                     and no page has an entry of -1 in the table.
+ * Reads B, tokens, page, n_pages, table_width of the descriptor; B <= 4096 (CCD_EUNSUPPORTED).  No other two of the buffers
+ * may overlap.  Two calls at once need two rings. */
+CCD_API int ccd_paged_plan(const ccd_paged_t* paged, const int32_t* len_before, const int32_t* len_after, const int32_t* block_table,
+                   int32_t* block_table_next, int32_t* free_pages, int32_t* cursor, int32_t* cursor_next, int32_t* q_start,
+                   int32_t* slots, int32_t* positions, void* hip_stream);
+
+/* Rotary positions.  Pair i of the first `rot` elements of a head is turned by the angle position * f_i:
+ *   y_1 = a * (x_1 cos - x_2 sin),  y_2 = a * (x_2 cos + x_1 sin)
+ * (x_1, x_2) being elements (i, i + rot/2) with CCD_ROPE_HALF and (2 i, 2 i + 1) with CCD_ROPE_PAIRS, a = amplitude; elements
+ * from rot on are copied.  `inverse` turns the other way: the embedding taken off again, and the gradient of the embedding.
+ * Frequencies, in radians per position: f_i = base^(-2 i / rot), and for contexts longer than the trained one
+ *   CCD_ROPE_LINEAR  f_i / factor
+ *   CCD_ROPE_NTK     with base * factor^(rot / (rot - 2)) as the base (rot = 2: unchanged)
+ *   CCD_ROPE_PARTS   f_i * (keep_i + (1 - keep_i) / factor), keep_i = (r_i - low) / (high - low) within 0 .. 1, r_i = context * f_i
+ *                    / 2 pi: pairs that turn `high` times or more within the trained context stay, those below `low` turns
+ *                    are stretched by the factor.
+ * Angles are exact at any position: frequencies are kept as 64-bit fractions of a turn, and whole turns drop out of the
+ * product with the position.  Cosine, sine and the rotation are fp32, rounded once to the type. */
+enum { CCD_ROPE_HALF = 0, CCD_ROPE_PAIRS = 1 };
+enum { CCD_ROPE_PLAIN = 0, CCD_ROPE_LINEAR = 1, CCD_ROPE_NTK = 2, CCD_ROPE_PARTS = 3 };
+typedef struct {
+  int32_t tokens, heads, d;   /* X, Y [tokens, heads, d]; d a multiple of 16 bytes, at most 1024                    */
+  int32_t rot;                /* elements of a head that are turned: even, 2 .. d                                   */
+  int32_t dtype;              /* CCD_FP32 or CCD_BF16                                                               */
+  int32_t layout, inverse;    /* CCD_ROPE_HALF or CCD_ROPE_PAIRS; 0 or 1                                            */
+  float amplitude;            /* 0 means 1                                                                          */
+  int64_t x_stride_t, x_stride_h, y_stride_t, y_stride_h;       /* in elements                                      */
+  int32_t scaling, context;   /* CCD_ROPE_PLAIN .. _PARTS; trained context in tokens (PARTS)                        */
+  double base, factor, low, high;
+} ccd_rope_t;
+
+/* The frequencies of a descriptor as ccd_rope and ccd_paged_append take them: turns[i] = f_i / 2 pi as a fraction of 2^64,
+ * i < rot / 2.  HOST memory; the caller copies it to the device once.  (Frequencies of one's own may be written so, too.)
+ * Reads rot, scaling, context, base, factor, low, high: base > 1 (at most 2^64), factor >= 1, PARTS: context >= 1, low < high. */
+CCD_API int ccd_rope_turns(const ccd_rope_t* rope, uint64_t* turns);
+
+/* Y = X with every head of token t embedded at positions[t] (device int32 [tokens]); a row whose position is negative is
+ * padding and its row of Y is left as it is.  Y may be X (with the same strides); other overlap is not allowed.  turns:
+ * device, [rot / 2].  The queries and keys of one projection are one tensor of Hq + Hkv heads: one call embeds both. */
+CCD_API int ccd_rope(const ccd_rope_t* rope, const void* X, const int32_t* positions, const uint64_t* turns, void* Y,
+             void* hip_stream);
+
+/* Key and value of new token t (K_new, V_new [tokens, Hkv, d]) go to row slots[t] % page of page slots[t] / page; a slot
+ * outside 0 .. page * n_pages - 1 (the plan's -1) is not written.  Two tokens must not have the same slot.  rope (nullable):
+ * the keys are embedded on the way at positions[t], with turns as in ccd_rope (rot, layout, inverse and amplitude of rope are
+ * read; a token with a negative position is not written); without it positions and turns are not read. */
+CCD_API int ccd_paged_append(const ccd_paged_t* paged, const ccd_rope_t* rope, const void* K_new, const void* V_new,
+                     const int32_t* slots, const int32_t* positions, const uint64_t* turns, void* K_pages, void* V_pages,
+                     void* hip_stream);
+
+/* Bytes of scratch ccd_paged_attend needs for this descriptor (0 if it is invalid; a valid one needs 256 at least).  The
+ * workspace must be 256-byte aligned; its contents need not survive between calls, nor start at any value. */
+CCD_API size_t ccd_paged_workspace_bytes(const ccd_paged_t* paged);
+
+/* Attention of the new tokens of every sequence over its cached ones: with n = kv_len[b] (device int32 [B]; what the table
+ * cannot hold is cut off) and m = q_start[b + 1] - q_start[b] (device int32 [B + 1], not descending), token i < m stands at
+ * position p = n - m + i (behind: n + i) and
+ *   out = sum_t w_t v_t / sum_t w_t,  w_t = exp(scale * <q, k_t>),  lse = log sum_t w_t
+ * over the positions t < n with t <= p, t > p - window if there is one, and a page in the table.  A row that sees nothing has
+ * out = 0 and lse = -inf.  out must not overlap Q; lse (fp32) may be NULL.  Rows of no sequence are left as they are.
+ * Logits, softmax and sums are fp32; with a bf16 cache the weights of a tile of tokens are rounded to bf16 for their product
+ * with the values. */
+CCD_API int ccd_paged_attend(const ccd_paged_t* paged, const void* Q, const void* K_pages, const void* V_pages,
+                     const int32_t* block_table, const int32_t* q_start, const int32_t* kv_len, void* out, float* lse,
+                     void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Per-kernel timing of ccd_compress for benchmarks: a host-side aid, off by default, and the only state the library
  * keeps between calls (process-wide: enable it from one thread, for calls on one stream).  While enabled, each
  * kernel of ccd_compress is launched with two HIP events attached that take the kernel's own begin and end time

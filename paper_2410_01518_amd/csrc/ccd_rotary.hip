@@ -1,0 +1,173 @@
+// ccd_rope: rotary embedding of the queries and keys of a step, and ccd_paged_append, which embeds keys on their way into the
+// pages.  Both move their rows once in and once out and are bound by memory; what could be in the way is the arithmetic of
+// cosine and sine (about 35 instructions a pair), so a wave works them out once for a token and takes all its heads.
+#include "ccd_paged.h"
+#include "ccd_rotary.h"
+
+namespace ccd {
+
+// where row h of a token goes: heads of a dense or strided tensor, or of a page
+template <class T>
+struct Rows {
+  const T* src;
+  T* dst;
+  int64_t src_h, dst_h;
+};
+
+// The heads h0, h0 + 1 .. of one token by one wave, in pieces of 16 bytes: `R.rot` elements turned, the rest copied.  A piece index
+// runs over the turned pieces and then over the tail; 64 / pieces heads at a time.
+template <class T, bool HALF>
+__device__ __forceinline__ void rotate_heads(const Rotary& R, const Rows<T>& rows, int h_begin, int h_end, int lane, int position,
+                                             const uint64_t* __restrict__ turns, bool copy_tail) {
+  constexpr int kEPL = 16 / sizeof(T);
+  const int turned = R.rot / (HALF ? 2 * kEPL : kEPL);
+  const int pieces = turned + (copy_tail ? (R.d - R.rot) / kEPL : 0);
+  // more than 64 pieces (rows of more than 1 KiB): several rounds of lanes
+  for (int p0 = 0; p0 < pieces; p0 += 64) {
+    const int width = pieces - p0 < 64 ? pieces - p0 : 64, side = 64 / width;
+    const int piece = p0 + lane % width, h_lane = lane / width;
+    if (h_lane >= side) continue;
+    if (piece < turned) {
+      RotaryLane<T, HALF> rot;
+      rot.angles(R, piece, position, turns);
+      const int e = piece * kEPL, e2 = e + R.rot / 2;
+#pragma unroll 4
+      for (int h = h_begin + h_lane; h < h_end; h += side) {
+        const T* s = rows.src + h * rows.src_h;
+        T* o = rows.dst + h * rows.dst_h;
+        uint4 a = *reinterpret_cast<const uint4*>(s + e), b{};
+        if constexpr (HALF) b = *reinterpret_cast<const uint4*>(s + e2);
+        rot.rotate(a, b);
+        *reinterpret_cast<uint4*>(o + e) = a;
+        if constexpr (HALF) *reinterpret_cast<uint4*>(o + e2) = b;
+      }
+    } else {
+      const int e = R.rot + (piece - turned) * kEPL;
+#pragma unroll 4
+      for (int h = h_begin + h_lane; h < h_end; h += side)
+        *reinterpret_cast<uint4*>(rows.dst + h * rows.dst_h + e) = *reinterpret_cast<const uint4*>(rows.src + h * rows.src_h + e);
+    }
+  }
+}
+
+// The same pair by pair, for a turned part that does not come in whole pieces of 16 bytes
+template <class T>
+__device__ __forceinline__ void rotate_heads_pairwise(const Rotary& R, const Rows<T>& rows, int h_begin, int h_end, int lane, int position,
+                                                      const uint64_t* __restrict__ turns, bool copy_tail) {
+  const int pairs = R.rot / 2;
+  for (int i = lane; i < pairs; i += 64) {
+    float c, s;
+    cos_sin_of_phase((uint64_t)(uint32_t)position * turns[i], c, s);
+    c *= R.amplitude;
+    s *= R.inverse ? -R.amplitude : R.amplitude;
+    const int e1 = R.half ? i : 2 * i, e2 = R.half ? i + pairs : 2 * i + 1;
+    for (int h = h_begin; h < h_end; ++h) {
+      const float x = load_elem(rows.src + h * rows.src_h + e1), z = load_elem(rows.src + h * rows.src_h + e2);
+      store_elem(rows.dst + h * rows.dst_h + e1, fmaf(-z, s, x * c));
+      store_elem(rows.dst + h * rows.dst_h + e2, fmaf(x, s, z * c));
+    }
+  }
+  if (!copy_tail) return;
+  for (int e = R.rot + lane; e < R.d; e += 64)
+    for (int h = h_begin; h < h_end; ++h) rows.dst[h * rows.dst_h + e] = rows.src[h * rows.src_h + e];
+}
+
+enum { kHalves = 0, kPairsNext = 1, kPairwise = 2 };
+
+template <class T, int KIND>
+__device__ __forceinline__ void rotate_any(const Rotary& R, const Rows<T>& rows, int h_begin, int h_end, int lane, int position,
+                                           const uint64_t* __restrict__ turns, bool copy_tail) {
+  if constexpr (KIND == kHalves) rotate_heads<T, true>(R, rows, h_begin, h_end, lane, position, turns, copy_tail);
+  else if constexpr (KIND == kPairsNext) rotate_heads<T, false>(R, rows, h_begin, h_end, lane, position, turns, copy_tail);
+  else rotate_heads_pairwise<T>(R, rows, h_begin, h_end, lane, position, turns, copy_tail);
+}
+
+// a wave per (token, group of heads)
+template <class T, int KIND>
+__global__ __launch_bounds__(256) void rotary_kernel(Rotary R, const T* X, const int32_t* __restrict__ positions,
+                                                     const uint64_t* __restrict__ turns, T* Y, int heads_per_wave) {
+  const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (t >= R.tokens) return;
+  const int position = positions[t];
+  if (position < 0) return;
+  const int h_begin = blockIdx.y * heads_per_wave;
+  const int h_end = h_begin + heads_per_wave < R.heads ? h_begin + heads_per_wave : R.heads;
+  const Rows<T> rows{X + t * R.x_t, Y + t * R.y_t, R.x_h, R.y_h};
+  rotate_any<T, KIND>(R, rows, h_begin, h_end, lane, position, turns, (const void*)X != (const void*)Y);
+}
+
+// a wave per token: its keys (turned, or copied) and values into the row of its slot
+template <class T, int KIND>
+__global__ __launch_bounds__(256) void paged_append_kernel(Paged P, Rotary R, bool rope, const T* __restrict__ K_new, const T* __restrict__ V_new,
+                                                           const int32_t* __restrict__ slots, const int32_t* __restrict__ positions,
+                                                           const uint64_t* __restrict__ turns, T* K, T* V) {
+  const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (t >= P.tokens) return;
+  const int slot = slots[t], position = rope ? positions[t] : 0;
+  if (slot < 0 || position < 0) return;
+  const int page = page_of(P.div, slot), row = slot - page * P.div.page;
+  if (page >= P.n_pages) return;
+  const int64_t to = page * P.page_stride + row * P.row_stride, from = t * P.new_t;
+  constexpr int kEPL = 16 / sizeof(T);
+  const int pieces = P.d / kEPL;                       // 8, 16 or 32
+  const int piece = lane % pieces, side = 64 / pieces;
+#pragma unroll 4
+  for (int h = lane / pieces; h < P.Hkv; h += side)
+    *reinterpret_cast<uint4*>(V + to + h * P.head_stride + piece * kEPL) = *reinterpret_cast<const uint4*>(V_new + from + h * P.new_h + piece * kEPL);
+  if (rope) {
+    const Rows<T> rows{K_new + from, K + to, P.new_h, P.head_stride};
+    rotate_any<T, KIND>(R, rows, 0, P.Hkv, lane, position, turns, true);
+    return;
+  }
+#pragma unroll 4
+  for (int h = lane / pieces; h < P.Hkv; h += side)
+    *reinterpret_cast<uint4*>(K + to + h * P.head_stride + piece * kEPL) = *reinterpret_cast<const uint4*>(K_new + from + h * P.new_h + piece * kEPL);
+}
+
+template <class T, int KIND>
+static void rotary_launch(const Rotary& R, const void* X, const int32_t* positions, const uint64_t* turns, void* Y, hipStream_t s) {
+  // few tokens: the heads of a token are shared out until about 1024 waves are under way
+  int groups = 1;
+  while (groups * 2 <= R.heads && (int64_t)R.tokens * groups < 1024) groups *= 2;
+  const int per = (R.heads + groups - 1) / groups;
+  launch(rotary_kernel<T, KIND>, dim3((R.tokens + 3) / 4, (R.heads + per - 1) / per), dim3(256), s, R, static_cast<const T*>(X), positions, turns,
+         static_cast<T*>(Y), per);
+}
+
+void launch_rotary(const Rotary& R, int dtype, const void* X, const int32_t* positions, const uint64_t* turns, void* Y, hipStream_t s) {
+  const bool f32 = dtype == 0;
+  const bool whole = rotary_by_pieces(R.rot, R.half, f32 ? 4 : 2);
+  if (f32) {
+    if (!whole)      rotary_launch<float, kPairwise>(R, X, positions, turns, Y, s);
+    else if (R.half) rotary_launch<float, kHalves>(R, X, positions, turns, Y, s);
+    else             rotary_launch<float, kPairsNext>(R, X, positions, turns, Y, s);
+  } else {
+    if (!whole)      rotary_launch<uint16_t, kPairwise>(R, X, positions, turns, Y, s);
+    else if (R.half) rotary_launch<uint16_t, kHalves>(R, X, positions, turns, Y, s);
+    else             rotary_launch<uint16_t, kPairsNext>(R, X, positions, turns, Y, s);
+  }
+}
+
+template <class T, int KIND>
+static void append_launch(const Paged& P, const Rotary* rope, const void* K_new, const void* V_new, const int32_t* slots, const int32_t* positions,
+                          const uint64_t* turns, void* K, void* V, hipStream_t s) {
+  launch(paged_append_kernel<T, KIND>, dim3((P.tokens + 3) / 4), dim3(256), s, P, rope ? *rope : Rotary{}, rope != nullptr, static_cast<const T*>(K_new),
+         static_cast<const T*>(V_new), slots, positions, turns, static_cast<T*>(K), static_cast<T*>(V));
+}
+
+void launch_paged_append(const Paged& P, int dtype, const Rotary* rope, const void* K_new, const void* V_new, const int32_t* slots,
+                         const int32_t* positions, const uint64_t* turns, void* K, void* V, hipStream_t s) {
+  const bool f32 = dtype == 0;
+  const bool whole = rope == nullptr || rotary_by_pieces(rope->rot, rope->half, f32 ? 4 : 2), half = rope == nullptr || rope->half;
+  if (f32) {
+    if (!whole)    append_launch<float, kPairwise>(P, rope, K_new, V_new, slots, positions, turns, K, V, s);
+    else if (half) append_launch<float, kHalves>(P, rope, K_new, V_new, slots, positions, turns, K, V, s);
+    else           append_launch<float, kPairsNext>(P, rope, K_new, V_new, slots, positions, turns, K, V, s);
+  } else {
+    if (!whole)    append_launch<uint16_t, kPairwise>(P, rope, K_new, V_new, slots, positions, turns, K, V, s);
+    else if (half) append_launch<uint16_t, kHalves>(P, rope, K_new, V_new, slots, positions, turns, K, V, s);
+    else           append_launch<uint16_t, kPairsNext>(P, rope, K_new, V_new, slots, positions, turns, K, V, s);
+  }
+}
+
+}  // namespace ccd

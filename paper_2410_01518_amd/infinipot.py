@@ -21,11 +21,14 @@ CCD_EINVAL, CCD_EUNSUPPORTED, CCD_EALIGN, CCD_EWORKSPACE, CCD_ELAUNCH = -1, -2, 
 CCD_FP32, CCD_BF16 = 0, 1
 CCD_POOL_NONE, CCD_POOL_MAX, CCD_POOL_AVG = 0, 1, 2
 CCD_PATH_AUTO, CCD_PATH_VALU, CCD_PATH_MFMA_SLICES, CCD_PATH_MFMA_UNIT = 0, 1, 2, 3
+CCD_ROPE_HALF, CCD_ROPE_PAIRS = 0, 1
+CCD_ROPE_PLAIN, CCD_ROPE_LINEAR, CCD_ROPE_NTK, CCD_ROPE_PARTS = 0, 1, 2, 3
 
 EXPORTS = ("ccd_workspace_bytes", "ccd_score", "ccd_select", "ccd_compact", "ccd_compress", "ccd_append", "ccd_cr_rope",
            "ccd_compress_rope", "ccd_score_kcat", "ccd_compress_kcat", "ccd_score_lse", "ccd_compress_lse",
            "ccd_nuc_from_logits", "ccd_compress_noalloc", "ccd_profile_enable", "ccd_profile_stages", "ccd_profile_stage_name",
-           "ccd_profile_collect", "ccd_strerror")
+           "ccd_profile_collect", "ccd_strerror", "ccd_paged_plan", "ccd_rope_turns", "ccd_rope", "ccd_paged_append",
+           "ccd_paged_workspace_bytes", "ccd_paged_attend")
 
 
 class ccd_shape_t(ctypes.Structure):
@@ -35,6 +38,23 @@ class ccd_shape_t(ctypes.Structure):
     _fields_ += [(n, ctypes.c_int64) for n in
                  ("kv_stride_b", "kv_stride_l", "kv_stride_h", "q_stride_b", "q_stride_l", "q_stride_h",
                   "nov_stride_b", "nov_stride_l", "nov_stride_h")]
+
+
+class ccd_paged_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in
+                ("B", "tokens", "Hq", "Hkv", "d", "dtype", "page", "n_pages", "table_width", "window", "behind", "max_new", "max_len")]
+    _fields_ += [("scale", ctypes.c_float)]
+    _fields_ += [(n, ctypes.c_int64) for n in
+                 ("page_stride", "head_stride", "row_stride", "new_stride_t", "new_stride_h", "q_stride_b", "q_stride_t", "q_stride_h",
+                  "o_stride_b", "o_stride_t", "o_stride_h", "lse_stride_b", "lse_stride_t", "lse_stride_h")]
+
+
+class ccd_rope_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("tokens", "heads", "d", "rot", "dtype", "layout", "inverse")]
+    _fields_ += [("amplitude", ctypes.c_float)]
+    _fields_ += [(n, ctypes.c_int64) for n in ("x_stride_t", "x_stride_h", "y_stride_t", "y_stride_h")]
+    _fields_ += [("scaling", ctypes.c_int32), ("context", ctypes.c_int32)]
+    _fields_ += [(n, ctypes.c_double) for n in ("base", "factor", "low", "high")]
 
 
 class CCDError(RuntimeError):
@@ -84,6 +104,19 @@ def lib() -> ctypes.CDLL:
         L.ccd_compress_kcat.argtypes = [sp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
         L.ccd_nuc_from_logits.restype = ctypes.c_int
         L.ccd_nuc_from_logits.argtypes = [vp, vp, vp, ctypes.c_int64, ctypes.c_int32, ctypes.c_int64, ctypes.c_int32, vp]
+        cp, rp = ctypes.POINTER(ccd_paged_t), ctypes.POINTER(ccd_rope_t)
+        L.ccd_paged_plan.restype = ctypes.c_int
+        L.ccd_paged_plan.argtypes = [cp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.ccd_rope_turns.restype = ctypes.c_int
+        L.ccd_rope_turns.argtypes = [rp, vp]
+        L.ccd_rope.restype = ctypes.c_int
+        L.ccd_rope.argtypes = [rp, vp, vp, vp, vp, vp]
+        L.ccd_paged_append.restype = ctypes.c_int
+        L.ccd_paged_append.argtypes = [cp, rp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.ccd_paged_workspace_bytes.restype = ctypes.c_size_t
+        L.ccd_paged_workspace_bytes.argtypes = [cp]
+        L.ccd_paged_attend.restype = ctypes.c_int
+        L.ccd_paged_attend.argtypes = [cp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
         L.ccd_profile_enable.restype = ctypes.c_int
         L.ccd_profile_enable.argtypes = [ctypes.c_int]
         L.ccd_profile_stages.restype = ctypes.c_int
@@ -263,6 +296,121 @@ def ccd_compress_kcat(shape, Q_cat, K, V, K_cap, novelty, keep_idx, workspace, s
     return _check(lib().ccd_compress_kcat(ctypes.byref(shape), _ptr(Q_cat), _ptr(K), _ptr(V), _ptr(K_cap), _ptr(novelty),
                                           _ptr(scores), _ptr(keep_idx), _ptr(workspace),
                                           0 if workspace is None else workspace.numel(), _stream(stream)))
+
+
+# ---- paged caches
+
+def _int32(**tensors):
+    for name, t in tensors.items():
+        assert t.dtype == torch.int32 and t.is_contiguous(), f"{name}: contiguous int32 needed"
+
+
+def make_plan(block_table, *, tokens, page, n_pages) -> ccd_paged_t:
+    """Descriptor of a step's plan alone: block_table [B, table_width], a cache of n_pages pages of `page` tokens, `tokens` entries in
+    the slot map."""
+    B, W = block_table.shape
+    return ccd_paged_t(B=B, tokens=tokens, page=page, n_pages=n_pages, table_width=W)
+
+
+def make_paged(K_pages, *, tokens, block_table=None, Q=None, out=None, lse=None, K_new=None, window=0, behind=False, max_new=0,
+               max_len=0, scale=0.0) -> ccd_paged_t:
+    """Descriptor from tensor geometry: K_pages (and V_pages) [n_pages, Hkv, page, d] in any order of the outer three
+    dimensions, block_table [B, table_width].  Q and out are [tokens, Hq, d] with lse [tokens, Hq], or, `tokens` = B m,
+    [B, Hq, m, d] with lse [B, Hq, m]; K_new (and V_new) [tokens, Hkv, d]."""
+    n_pages, Hkv, page, d = K_pages.shape
+    ps, hs, rs, es = K_pages.stride()
+    assert es == 1, "rows of the cache must be contiguous"
+    p = ccd_paged_t(B=1, tokens=tokens, Hq=Hkv, Hkv=Hkv, d=d, dtype=_dtype_code(K_pages), page=page, n_pages=n_pages, table_width=1,
+                    window=window, behind=int(behind), max_new=max_new, max_len=max_len, scale=scale, page_stride=ps, head_stride=hs,
+                    row_stride=rs, new_stride_t=Hkv * d, new_stride_h=d)
+    if block_table is not None:
+        p.B, p.table_width = block_table.shape
+    if K_new is not None:
+        assert tuple(K_new.shape) == (tokens, Hkv, d) and K_new.stride(2) == 1 and K_new.dtype == K_pages.dtype
+        p.new_stride_t, p.new_stride_h = K_new.stride(0), K_new.stride(1)
+    p.Hq = Hkv if Q is None else Q.shape[1]
+    for t, name, batched in ((Q, "q", 4), (out, "o", 4), (lse, "lse", 3)):
+        if t is None:
+            strides = (0, p.Hq, 1) if name == "lse" else (0, p.Hq * d, d)
+        else:
+            if name == "lse":
+                assert t.dtype == torch.float32
+            else:
+                assert t.shape[-1] == d and t.stride(-1) == 1 and t.dtype == K_pages.dtype
+            assert t.shape[1] == p.Hq
+            if t.dim() == batched:
+                m = t.shape[2]
+                assert t.shape[0] == p.B and p.B * m == tokens
+                strides = (t.stride(0) - m * t.stride(2), t.stride(2), t.stride(1))
+            else:
+                assert t.shape[0] == tokens
+                strides = (0, t.stride(0), t.stride(1))
+        for axis, v in zip("bth", strides):
+            setattr(p, f"{name}_stride_{axis}", v)
+    return p
+
+
+def make_rope(X, Y=None, *, rot=None, layout=CCD_ROPE_HALF, base=10000.0, scaling=CCD_ROPE_PLAIN, factor=1.0, context=0, low=1.0, high=4.0,
+              amplitude=0.0, inverse=False) -> ccd_rope_t:
+    """Descriptor from tensor geometry: X and Y [tokens, heads, d] with contiguous heads (Y: X where none is given)."""
+    Y = X if Y is None else Y
+    T, H, d = X.shape
+    assert tuple(Y.shape) == (T, H, d) and X.stride(2) == 1 and Y.stride(2) == 1 and X.dtype == Y.dtype
+    return ccd_rope_t(tokens=T, heads=H, d=d, rot=d if rot is None else rot, dtype=_dtype_code(X), layout=layout, inverse=int(inverse),
+                      amplitude=amplitude, x_stride_t=X.stride(0), x_stride_h=X.stride(1), y_stride_t=Y.stride(0), y_stride_h=Y.stride(1),
+                      scaling=scaling, context=context, base=base, factor=factor, low=low, high=high)
+
+
+def rope_turns(rope: ccd_rope_t, device="cuda") -> torch.Tensor:
+    """The descriptor's frequencies for ccd_rope and ccd_paged_append, int64 [rot / 2] on the device (fractions of 2^64)."""
+    host = torch.empty(max(rope.rot, 2) // 2, dtype=torch.int64)
+    _check(lib().ccd_rope_turns(ctypes.byref(rope), host.data_ptr()))
+    return host.to(device)
+
+
+def alloc_paged_workspace(paged: ccd_paged_t, device="cuda") -> torch.Tensor:
+    nbytes = ccd_paged_workspace_bytes(paged)
+    if nbytes == 0:
+        raise CCDError(CCD_EINVAL, "invalid descriptor")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def ccd_paged_workspace_bytes(paged: ccd_paged_t) -> int:
+    return int(lib().ccd_paged_workspace_bytes(ctypes.byref(paged)))
+
+
+def ccd_paged_plan(paged, len_before, len_after, block_table, block_table_next, free_pages, cursor, cursor_next, q_start, slots, positions,
+                   stream=None) -> int:
+    """len_before, len_after [B], block_table and block_table_next [B, table_width] (may be one), free_pages [n_pages], cursor and
+    cursor_next [4] (may be one), q_start [B + 1], slots and positions [tokens]: int32."""
+    _int32(len_before=len_before, len_after=len_after, block_table=block_table, block_table_next=block_table_next, free_pages=free_pages,
+           cursor=cursor, cursor_next=cursor_next, q_start=q_start, slots=slots, positions=positions)
+    return _check(lib().ccd_paged_plan(ctypes.byref(paged), _ptr(len_before), _ptr(len_after), _ptr(block_table), _ptr(block_table_next),
+                                       _ptr(free_pages), _ptr(cursor), _ptr(cursor_next), _ptr(q_start), _ptr(slots), _ptr(positions),
+                                       _stream(stream)))
+
+
+def ccd_rope(rope, X, positions, turns, Y, stream=None) -> int:
+    """positions int32 [tokens]; turns as rope_turns gives them; Y may be X."""
+    _int32(positions=positions)
+    return _check(lib().ccd_rope(ctypes.byref(rope), _ptr(X), _ptr(positions), _ptr(turns), _ptr(Y), _stream(stream)))
+
+
+def ccd_paged_append(paged, K_new, V_new, slots, K_pages, V_pages, rope=None, positions=None, turns=None, stream=None) -> int:
+    """K_new and V_new have the same strides, as have K_pages and V_pages; with a rope descriptor the keys are embedded at `positions`."""
+    _int32(slots=slots)
+    assert K_new.stride() == V_new.stride() and K_pages.stride() == V_pages.stride()
+    return _check(lib().ccd_paged_append(ctypes.byref(paged), None if rope is None else ctypes.byref(rope), _ptr(K_new), _ptr(V_new), _ptr(slots),
+                                         _ptr(positions), _ptr(turns), _ptr(K_pages), _ptr(V_pages), _stream(stream)))
+
+
+def ccd_paged_attend(paged, Q, K_pages, V_pages, block_table, q_start, kv_len, out, lse, workspace, stream=None) -> int:
+    """block_table [B, table_width], q_start [B + 1], kv_len [B]: int32; lse fp32 or None."""
+    _int32(block_table=block_table, q_start=q_start, kv_len=kv_len)
+    assert K_pages.stride() == V_pages.stride()
+    return _check(lib().ccd_paged_attend(ctypes.byref(paged), _ptr(Q), _ptr(K_pages), _ptr(V_pages), _ptr(block_table), _ptr(q_start), _ptr(kv_len),
+                                         _ptr(out), _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel(),
+                                         _stream(stream)))
 
 
 def ccd_profile_enable(on: bool) -> int:
