@@ -1,0 +1,100 @@
+// What the attention kernels share: how a call is cut, the tokens a block of rows sees, rows of pages, the running softmax.
+//
+//   out = sum_t w_t v_t / sum_t w_t,   w_t = 2^(scale log2(e) <q, k_t> - m)
+// in one pass over the tokens.  m is a reference that only follows the largest logit at a distance: it is raised, and the sums so far
+// scaled down by 2^(old - new), when a logit lies more than kRaise above it.  Weights are then at most 2^kRaise, far inside fp32, and most
+// tiles cost no rescaling and no exchange between lanes.
+//
+// The rows of a unit (sequence, KV head) are its new tokens times the G query heads that share the head, row r = token r / G, head r % G:
+// heads of one token lie side by side and see the same keys, and a block of rows is a narrow band of positions.
+#pragma once
+#include "ccd_common.h"
+#include "ccd_paged.h"
+
+namespace ccd {
+
+constexpr float kRaise = 8.f;
+
+typedef short v4s __attribute__((ext_vector_type(4)));
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+
+// How a call is cut: blocks of `rows` rows, each over at most `parts` stretches of its tokens.  chunk: tokens per stretch, doubled or more where
+// that gives more than `parts` (so the host's idea of the lengths only decides how well the work is spread).
+struct AttendPlan {
+  int kernel, rows, row_blocks, parts, chunk;
+};
+
+// what a workgroup knows of its sequence
+struct Sequence {
+  int first, m, n, base;           // number of its first new token, new tokens, cached tokens, position of its first new token
+};
+__device__ __forceinline__ Sequence load_sequence(const Paged& P, int b, const int32_t* __restrict__ q_start, const int32_t* __restrict__ kv_len) {
+  Sequence s;
+  s.first = q_start[b];
+  const int end = q_start[b + 1];
+  int m = (end < P.tokens ? end : P.tokens) - s.first;         // rows that exist
+  s.m = s.first < 0 || m < 0 ? 0 : m;
+  const int n = kv_len[b];
+  s.n = n < 0 ? 0 : n < P.max_len ? n : P.max_len;
+  s.base = P.behind ? s.n : s.n - (end - s.first);
+  return s;
+}
+// the first position that a query at position pos sees
+__device__ __forceinline__ int first_seen(const Paged& P, int pos) {
+  const int64_t low = (int64_t)pos - P.window + 1;
+  return P.window > 0 && low > 0 ? (int)low : 0;
+}
+// the tokens begin .. end - 1 that some row of r0 .. r1 - 1 sees, and how they are cut
+struct Stretch {
+  int begin, end, parts, chunk;
+};
+__device__ __forceinline__ Stretch cut_rows(const Paged& P, const Sequence& s, int r0, int r1, int parts, int chunk) {
+  Stretch c;
+  const int64_t last = (int64_t)s.base + (r1 - 1) / P.G;
+  const int first = first_seen(P, s.base + r0 / P.G);
+  c.end = last + 1 < s.n ? (int)(last + 1) : s.n;
+  if (c.end < 0) c.end = 0;
+  c.begin = first < c.end ? first : c.end;
+  const int len = c.end - c.begin;
+  c.parts = (len + chunk - 1) / chunk;
+  c.chunk = chunk;
+  if (c.parts > parts) {
+    const int per = (len + parts - 1) / parts;
+    c.chunk = (per + 127) / 128 * 128;
+    c.parts = (len + c.chunk - 1) / c.chunk;
+  }
+  if (c.parts < 1) c.parts = 1;
+  return c;
+}
+
+// 16 bytes of zeros: where rows that are not there are read
+constexpr int kZeroBytes = 512;
+extern __device__ const uint4 g_zero_row[kZeroBytes / 16];
+
+// where part p of row `row` (number of the new token), head h stands in the workspace
+struct Partials {
+  float* o;                        // [parts][tokens * Hq][d], scaled to the reference in ml
+  float2* ml;                      // [parts][tokens * Hq]: reference, sum of weights
+};
+
+__device__ __forceinline__ float to_natural_lse(float m, float l) {
+  return l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f : l == l ? -INFINITY : l;
+}
+// 1 / sum of weights; a row that sees nothing has 0, one that sees a NaN keeps it
+__device__ __forceinline__ float inverse_sum(float l) { return l > 0.f ? 1.f / l : l == l ? 0.f : l; }
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+  const v2bf r = {(__bf16)a, (__bf16)b};
+  return __builtin_bit_cast(uint32_t, r);
+}
+
+// split kernel: a workgroup per (unit, block of rows, stretch of tokens), its waves deal the stretch's tiles among themselves
+AttendPlan plan_split_attend(const Paged& P, int dtype, int max_new, int max_len);
+void launch_attend_split(const Paged& P, const AttendPlan& pl, int dtype, const void* Q, const void* K, const void* V, const int32_t* table,
+                         const int32_t* q_start, const int32_t* kv_len, void* out, float* lse, Partials part, hipStream_t s);
+
+}  // namespace ccd

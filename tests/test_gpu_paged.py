@@ -322,7 +322,7 @@ def _check_attend(p, out, lse, dtype, *, window=0, behind=False, scale=0.0, sent
         assert (gl[T:] == sentinel).all()
         assert (np.isneginf(gl[:T]) == np.isneginf(wl[:T])).all()
         fin = np.isfinite(wl[:T])
-        assert (np.abs(gl[:T] - wl[:T])[fin] <= (e + n + 2.0 ** -20 + 2.0 ** -22 * np.abs(np.where(np.isfinite(wl), wl, 0.0)))[:T][fin]).all()
+        assert (np.abs(gl[:T][fin] - wl[:T][fin]) <= (e + n + 2.0 ** -20 + 2.0 ** -22 * np.abs(np.where(np.isfinite(wl), wl, 0.0)))[:T][fin]).all()
 
 
 def _run_attend(p, *, window=0, behind=False, scale=0.0, with_lse=True, max_new=None, max_len=None, stream=None):
