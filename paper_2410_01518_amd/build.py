@@ -12,7 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libinfinipot.so")
 SOURCES = ["infinipot_api.hip", "ccd_score_valu.hip", "ccd_score_mfma.hip", "ccd_score_unit.hip", "ccd_score_unit_1.hip", "ccd_score_unit_2.hip",
            "ccd_score_unit_4.hip", "ccd_score_split.hip", "ccd_score_direct.hip", "ccd_select.hip", "ccd_compact.hip",
-           "ccd_nuc.hip", "ccd_paged_api.hip", "ccd_paged_plan.hip", "ccd_rotary.hip", "ccd_attend.hip"]
+           "ccd_nuc.hip", "ccd_paged_api.hip", "ccd_paged_plan.hip", "ccd_rotary.hip", "ccd_attend.hip",
+           "ccd_attend_rows.hip"]
 # The unit kernel (ccd_score_unit.h) keeps its query fragments at fixed places in the accumulation registers (named in its inline
 # assembly): the compiler must put nothing of its own there, so matrix-instruction results go to vector registers and
 # the generated code is checked for accumulation registers outside the assembly statements.

@@ -24,7 +24,7 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 // How a call is cut: blocks of `rows` rows, each over at most `parts` stretches of its tokens.  chunk: tokens per stretch, doubled or more where
 // that gives more than `parts` (so the host's idea of the lengths only decides how well the work is spread).
 struct AttendPlan {
-  int kernel, rows, row_blocks, parts, chunk;
+  int by_rows, rows, row_blocks, parts, chunk;
 };
 
 // what a workgroup knows of its sequence
@@ -70,9 +70,9 @@ __device__ __forceinline__ Stretch cut_rows(const Paged& P, const Sequence& s, i
   return c;
 }
 
-// 16 bytes of zeros: where rows that are not there are read
+// A row of zeros: where rows that are not there are read (weights of 0 do not make good what a NaN beside them does to a product)
 constexpr int kZeroBytes = 512;
-extern __device__ const uint4 g_zero_row[kZeroBytes / 16];
+static __device__ const uint4 g_zero_row[kZeroBytes / 16] = {};
 
 // where part p of row `row` (number of the new token), head h stands in the workspace
 struct Partials {
@@ -93,8 +93,13 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 }
 
 // split kernel: a workgroup per (unit, block of rows, stretch of tokens), its waves deal the stretch's tiles among themselves
-AttendPlan plan_split_attend(const Paged& P, int dtype, int max_new, int max_len);
 void launch_attend_split(const Paged& P, const AttendPlan& pl, int dtype, const void* Q, const void* K, const void* V, const int32_t* table,
                          const int32_t* q_start, const int32_t* kv_len, void* out, float* lse, Partials part, hipStream_t s);
+
+// rows kernel (bf16): a workgroup per (unit, block of 128 rows, stretch), its waves share the tiles
+void launch_attend_rows(const Paged& P, const AttendPlan& pl, const void* Q, const void* K, const void* V, const int32_t* table,
+                        const int32_t* q_start, const int32_t* kv_len, void* out, float* lse, Partials part, hipStream_t s);
+void launch_attend_join(const Paged& P, const AttendPlan& pl, int dtype, Partials part, const int32_t* q_start, const int32_t* kv_len, void* out,
+                        float* lse, hipStream_t s);
 
 }  // namespace ccd

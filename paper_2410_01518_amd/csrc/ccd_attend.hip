@@ -12,8 +12,6 @@
 
 namespace ccd {
 
-__device__ const uint4 g_zero_row[kZeroBytes / 16] = {};
-
 constexpr int kWaves = 4;
 
 template <class T, int D>
@@ -390,26 +388,6 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Paged P, AttendPlan pl
   if (lse != nullptr && lane == 0) lse[lo * P.l_b + row * P.l_t + head * P.l_h] = to_natural_lse(top, sum);
 }
 
-AttendPlan plan_split_attend(const Paged& P, int dtype, int max_new, int max_len) {
-  AttendPlan pl{};
-  const int64_t rows = (int64_t)max_new * P.G;
-  pl.rows = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
-  pl.row_blocks = (int)((rows + pl.rows - 1) / pl.rows);
-  const int64_t units = (int64_t)P.B * P.Hkv * pl.row_blocks;
-  int64_t len = max_len;
-  if (P.window > 0 && len > (int64_t)P.window + max_new) len = (int64_t)P.window + max_new;
-  // stretches: until some 1024 workgroups are under way, of 256 tokens at least
-  int64_t parts = (1024 + units - 1) / units;
-  const int64_t most = (len + 255) / 256;
-  if (parts > most) parts = most;
-  if (parts > 64) parts = 64;
-  if (parts < 1) parts = 1;
-  pl.chunk = (int)(((len + parts - 1) / parts + 127) / 128 * 128);
-  pl.parts = (int)((len + pl.chunk - 1) / pl.chunk);
-  if (pl.parts < 1) pl.parts = 1;
-  return pl;
-}
-
 template <class T, int D>
 static void split_launch(const Paged& P, const AttendPlan& pl, const void* Q, const void* K, const void* V, const int32_t* table,
                          const int32_t* q_start, const int32_t* kv_len, void* out, float* lse, Partials part, hipStream_t s) {
@@ -419,8 +397,6 @@ static void split_launch(const Paged& P, const AttendPlan& pl, const void* Q, co
   if (pl.rows == 16)      launch(attend_split_kernel<T, D, 1>, grid, block, s, P, pl, q, k, v, table, q_start, kv_len, o, lse, part);
   else if (pl.rows == 32) launch(attend_split_kernel<T, D, 2>, grid, block, s, P, pl, q, k, v, table, q_start, kv_len, o, lse, part);
   else                    launch(attend_split_kernel<T, D, 4>, grid, block, s, P, pl, q, k, v, table, q_start, kv_len, o, lse, part);
-  if (pl.parts > 1)
-    launch(attend_join_kernel<T, D>, dim3((unsigned)(((int64_t)P.tokens * P.Hq + 3) / 4)), dim3(256), s, P, pl, part, q_start, kv_len, o, lse);
 }
 
 void launch_attend_split(const Paged& P, const AttendPlan& pl, int dtype, const void* Q, const void* K, const void* V, const int32_t* table,
@@ -434,7 +410,40 @@ void launch_attend_split(const Paged& P, const AttendPlan& pl, int dtype, const 
   }
 }
 
-static AttendPlan plan_attend(const Paged& P, int dtype, int max_new, int max_len) { return plan_split_attend(P, dtype, max_new, max_len); }
+template <class T>
+static void join_launch(const Paged& P, const AttendPlan& pl, Partials part, const int32_t* q_start, const int32_t* kv_len, void* out, float* lse,
+                        hipStream_t s) {
+  const dim3 grid((unsigned)(((int64_t)P.tokens * P.Hq + 3) / 4));
+  if (P.d == 64) launch(attend_join_kernel<T, 64>, grid, dim3(256), s, P, pl, part, q_start, kv_len, static_cast<T*>(out), lse);
+  else           launch(attend_join_kernel<T, 128>, grid, dim3(256), s, P, pl, part, q_start, kv_len, static_cast<T*>(out), lse);
+}
+
+void launch_attend_join(const Paged& P, const AttendPlan& pl, int dtype, Partials part, const int32_t* q_start, const int32_t* kv_len, void* out,
+                        float* lse, hipStream_t s) {
+  if (dtype == 0) join_launch<float>(P, pl, part, q_start, kv_len, out, lse, s);
+  else            join_launch<uint16_t>(P, pl, part, q_start, kv_len, out, lse, s);
+}
+
+static AttendPlan plan_attend(const Paged& P, int dtype, int max_new, int max_len) {
+  AttendPlan pl{};
+  const int64_t rows = (int64_t)max_new * P.G;
+  pl.by_rows = dtype != 0 && rows > 64;
+  pl.rows = pl.by_rows ? 128 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  pl.row_blocks = (int)((rows + pl.rows - 1) / pl.rows);
+  const int64_t units = (int64_t)P.B * P.Hkv * pl.row_blocks;
+  int64_t len = max_len;
+  if (P.window > 0 && len > (int64_t)P.window + max_new) len = (int64_t)P.window + max_new;
+  // stretches: until some 1024 workgroups are under way (512 of the rows kernel), of 256 tokens at least
+  int64_t parts = ((pl.by_rows ? 512 : 1024) + units - 1) / units;
+  const int64_t most = (len + 255) / 256;
+  if (parts > most) parts = most;
+  if (parts > 64) parts = 64;
+  if (parts < 1) parts = 1;
+  pl.chunk = (int)(((len + parts - 1) / parts + 127) / 128 * 128);
+  pl.parts = (int)((len + pl.chunk - 1) / pl.chunk);
+  if (pl.parts < 1) pl.parts = 1;
+  return pl;
+}
 
 size_t attend_workspace_bytes(const Paged& P, int dtype, int max_new, int max_len) {
   const AttendPlan pl = plan_attend(P, dtype, max_new, max_len);
@@ -449,7 +458,9 @@ void launch_attend(const Paged& P, int dtype, int max_new, int max_len, const vo
   const size_t rows = (size_t)P.tokens * P.Hq * pl.parts;
   Partials part{static_cast<float*>(workspace),
                 reinterpret_cast<float2*>(static_cast<char*>(workspace) + (rows * P.d * sizeof(float) + 255) / 256 * 256)};
-  launch_attend_split(P, pl, dtype, Q, K, V, table, q_start, kv_len, out, lse, part, s);
+  if (pl.by_rows) launch_attend_rows(P, pl, Q, K, V, table, q_start, kv_len, out, lse, part, s);
+  else            launch_attend_split(P, pl, dtype, Q, K, V, table, q_start, kv_len, out, lse, part, s);
+  if (pl.parts > 1) launch_attend_join(P, pl, dtype, part, q_start, kv_len, out, lse, s);
 }
 
 }  // namespace ccd
