@@ -21,10 +21,12 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 
-// How a call is cut: blocks of `rows` rows, each over at most `parts` stretches of its tokens.  chunk: tokens per stretch, doubled or more where
-// that gives more than `parts` (so the host's idea of the lengths only decides how well the work is spread).
+// How a call is cut.  On a grid: blocks of `rows` rows, each over at most `parts` stretches of its tokens; chunk: tokens per stretch, made longer where
+// that gives more than `parts` (so the host's idea of the lengths only decides how well the work is spread); sequences of `few` rows or less
+// are left to the even cut.  Evenly: `parts` workgroups, at most `rows` rows per unit; only_few: sequences of more than `few` rows are left to the grid.
+// turn: blocks of rows of the first half of one round (rows kernel), 0: the call is more than one round.
 struct AttendPlan {
-  int by_rows, rows, row_blocks, parts, chunk;
+  int by_rows, rows, row_blocks, parts, chunk, few, only_few, turn;
 };
 
 // what a workgroup knows of its sequence
@@ -74,10 +76,12 @@ __device__ __forceinline__ Stretch cut_rows(const Paged& P, const Sequence& s, i
 constexpr int kZeroBytes = 512;
 static __device__ const uint4 g_zero_row[kZeroBytes / 16] = {};
 
-// where part p of row `row` (number of the new token), head h stands in the workspace
+// Sums of stretches in the workspace, scaled to their own references.  Entries: on a grid [parts][tokens * Hq]; of the even cut
+// [workgroups][2][rows], the second for a unit that begins in the workgroup, the first for one that began before.
 struct Partials {
-  float* o;                        // [parts][tokens * Hq][d], scaled to the reference in ml
-  float2* ml;                      // [parts][tokens * Hq]: reference, sum of weights
+  float* o;                        // [entries][d]
+  float2* ml;                      // [entries]: reference, sum of weights
+  int2* meta;                      // even cut, per unit: the first workgroup that has some of it, how many have
 };
 
 __device__ __forceinline__ float to_natural_lse(float m, float l) {
@@ -92,14 +96,8 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, r);
 }
 
-// split kernel: a workgroup per (unit, block of rows, stretch of tokens), its waves deal the stretch's tiles among themselves
-void launch_attend_split(const Paged& P, const AttendPlan& pl, int dtype, const void* Q, const void* K, const void* V, const int32_t* table,
-                         const int32_t* q_start, const int32_t* kv_len, void* out, float* lse, Partials part, hipStream_t s);
-
 // rows kernel (bf16): a workgroup per (unit, block of 128 rows, stretch), its waves share the tiles
 void launch_attend_rows(const Paged& P, const AttendPlan& pl, const void* Q, const void* K, const void* V, const int32_t* table,
                         const int32_t* q_start, const int32_t* kv_len, void* out, float* lse, Partials part, hipStream_t s);
-void launch_attend_join(const Paged& P, const AttendPlan& pl, int dtype, Partials part, const int32_t* q_start, const int32_t* kv_len, void* out,
-                        float* lse, hipStream_t s);
 
 }  // namespace ccd

@@ -48,17 +48,14 @@ struct Tile<uint16_t, D> {
     }
   }
   // 16-byte pieces of a row, exchanged in pairs by the row's number so that the rows a transposing read takes together (16 rows, one pair
-  // of pieces) lie in different banks
-  __device__ static int piece_at(int row, int piece) {
-    const int swap = D == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1;
-    return row * (D * 2) + ((piece ^ swap) << 4);
-  }
+  // of pieces) lie in different banks.  An exchange is an exclusive or of the piece's number, so a lane's places in a row differ by one, too.
+  __device__ static int swap_of(int row) { return D == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1; }
   __device__ static void store_values(const Values& r, char* lds, int lane) {
+    const int at = (lane & 15) * (D * 2) + (((lane >> 4) ^ swap_of(lane & 15)) << 4);
 #pragma unroll
     for (int h = 0; h < kHalves; ++h)
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s)
-        *reinterpret_cast<v4u*>(lds + piece_at(16 * h + (lane & 15), 4 * s + (lane >> 4))) = r.v[h][s];
+      for (int s = 0; s < kSteps; ++s) *reinterpret_cast<v4u*>(lds + ((at ^ (s << 6)) + 16 * h * (D * 2))) = r.v[h][s];
   }
   // x[h][i]: logit of token 16 h + 4 (lane >> 4) + i for row lane & 15
   __device__ static void logits(v4f (&x)[kHalves], const Keys& r, const Query& q) {
@@ -78,14 +75,13 @@ struct Tile<uint16_t, D> {
   template <int NQ>
   __device__ static void add_values(v4f (&o)[NQ][kBlocks], const Weights (&w)[NQ], const Values&, const char* lds, int lane) {
     const int row = 4 * (lane >> 4) + ((lane & 15) >> 2);
+    const int at = row * (D * 2) + ((((lane & 3) >> 1) ^ swap_of(row)) << 4) + (lane & 1) * 8;
 #pragma unroll
     for (int c = 0; c < kBlocks; ++c) {
       v4s t[2];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const char* p = lds + piece_at(16 * h + row, 2 * c + ((lane & 3) >> 1)) + (lane & 1) * 8;
-        t[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(p));
-      }
+      for (int h = 0; h < 2; ++h)
+        t[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(lds + ((at ^ (c << 5)) + 16 * h * (D * 2))));
       const v8bf a = __builtin_bit_cast(v8bf, __builtin_shufflevector(t[0], t[1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
       for (int j = 0; j < NQ; ++j) o[j][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[j].w, o[j][c], 0, 0, 0);
@@ -158,6 +154,18 @@ struct Tile<float, D> {
   __device__ static int element(int c, int lane, int i) { return 64 * (c >> 2) + 4 * (4 * (lane >> 4) + i) + (c & 3); }
 };
 
+__device__ __forceinline__ void store_piece(float* to, const float (&x)[4]) { *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]); }
+__device__ __forceinline__ void store_piece(float* to, const float (&x)[8]) {
+  *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]);
+  *reinterpret_cast<float4*>(to + 4) = make_float4(x[4], x[5], x[6], x[7]);
+}
+__device__ __forceinline__ void store_piece(uint16_t* to, const float (&x)[4]) {
+  *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
+}
+__device__ __forceinline__ void store_piece(uint16_t* to, const float (&x)[8]) {
+  *reinterpret_cast<uint4*>(to) = make_uint4(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7]));
+}
+
 // over the four lanes that hold a row
 __device__ __forceinline__ float row_max(float x) {
   x = fmaxf(x, __shfl_xor(x, 16));
@@ -168,299 +176,565 @@ __device__ __forceinline__ float row_sum(float x) {
   return x + __shfl_xor(x, 32);
 }
 
-// waves per SIMD that the registers are cut for: what the rows of queries and of sums leave room for
+// workgroups per compute unit, and so waves per SIMD, that the registers are cut for: what the rows of queries and of sums leave room for
 template <class T, int D, int NQ>
-constexpr int split_waves() { return NQ == 4 ? 1 : NQ == 2 || (sizeof(T) == 4 && D == 128) ? 2 : D == 128 ? 3 : 4; }
+constexpr int split_waves() { return NQ == 4 ? 1 : NQ == 2 || D == 128 ? 2 : 3; }
+
+struct AttendArgs {
+  const void *Q, *K, *V;
+  const int32_t *table, *q_start, *kv_len;
+  void* out;
+  float* lse;
+  Partials part;
+};
 
 template <class T, int D, int NQ>
-__global__ __launch_bounds__(64 * kWaves, (split_waves<T, D, NQ>())) void attend_split_kernel(Paged P, AttendPlan pl, const T* __restrict__ Q, const T* __restrict__ K, const T* __restrict__ V,
-                                                                     const int32_t* __restrict__ table, const int32_t* __restrict__ q_start,
-                                                                     const int32_t* __restrict__ kv_len, T* __restrict__ out, float* __restrict__ lse,
-                                                                     Partials part) {
+struct SplitLds {
+  static constexpr int kRows = 16 * NQ, kPitch = D + 4;
+  static constexpr int kWaveBytes = Tile<T, D>::kLdsBytes > 16 * kPitch * 4 ? Tile<T, D>::kLdsBytes : 16 * kPitch * 4;
+  __align__(16) char wave[kWaves][kWaveBytes];
+  float m[kWaves][kRows], l[kWaves][kRows];
+};
+
+// Rows r0 .. r1 - 1 of unit (b, hkv) over the tokens t_begin .. t_end - 1, by the workgroup.  whole_row: these are all tokens the rows see, the result
+// is written; else (o, m, l) of row r go to entry part0 + (r - r0) of the workspace, or, part0 < 0, to those of part_no by the row's number.
+template <class T, int D, int NQ>
+__device__ __forceinline__ void attend_stretch(const Paged& P, const AttendArgs& A, SplitLds<T, D, NQ>& L, const Sequence& sq, int b, int hkv, int r0, int r1,
+                                               int t_begin, int t_end, bool whole_row, int64_t part0, int part_no) {
   using Tl = Tile<T, D>;
-  constexpr int kRows = 16 * NQ, kPitch = D + 4;
-  constexpr int kWaveBytes = Tl::kLdsBytes > 16 * kPitch * 4 ? Tl::kLdsBytes : 16 * kPitch * 4;
-  __shared__ __align__(16) char lds[kWaves][kWaveBytes];
-  __shared__ float wave_m[kWaves][kRows], wave_l[kWaves][kRows];
+  constexpr int kPitch = SplitLds<T, D, NQ>::kPitch, kStride = kWaves * Tl::kTokens;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int32_t* pages = A.table + (int64_t)b * P.table_width;
+  const T* Kh = static_cast<const T*>(A.K) + hkv * P.head_stride;
+  const T* Vh = static_cast<const T*>(A.V) + hkv * P.head_stride;
+  // Keys and values of a tile are asked for a tile ahead, the pages they are in two tiles ahead: a chain of two loads from memory
+  // would not hide behind one tile's work.
+  typename Tl::Keys keys;
+  typename Tl::Values values;
+  int64_t off[Tl::kHalves];
+  int id[Tl::kHalves];
+  auto look_up = [&](int t0) {
+#pragma unroll
+    for (int h = 0; h < Tl::kHalves; ++h) {
+      const int t = t0 + 16 * h + (lane & 15);
+      id[h] = t < t_end ? pages[page_of(P.div, t)] : -1;
+    }
+  };
+  auto offsets = [&](int t0) {
+#pragma unroll
+    for (int h = 0; h < Tl::kHalves; ++h) {
+      const int t = t0 + 16 * h + (lane & 15);
+      off[h] = id[h] >= 0 && id[h] < P.n_pages ? id[h] * P.page_stride + (int64_t)(t - page_of(P.div, t) * P.div.page) * P.row_stride : -1;
+    }
+  };
+  int t0 = t_begin + wave * Tl::kTokens;
+  if (t0 < t_end) {
+    look_up(t0);
+    offsets(t0);
+    Tl::load_keys(keys, Kh, off, lane);
+    Tl::load_values(values, Vh, off, lane);
+    look_up(t0 + kStride);
+  }
+  // the lane's rows
+  typename Tl::Query q[NQ];
+  int pos[NQ], low[NQ];                                    // position of the row, first position it sees
+  const int pos_min = sq.base + r0 / P.G, low_max = first_seen(P, sq.base + (r1 - 1) / P.G);
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    const int r = r0 + 16 * j + (lane & 15), i = r / P.G;
+    pos[j] = sq.base + i;
+    low[j] = first_seen(P, pos[j]);
+    Tl::load_query(q[j], static_cast<const T*>(A.Q) + b * P.q_b + (int64_t)(sq.first + i) * P.q_t + (int64_t)(hkv * P.G + r - i * P.G) * P.q_h, lane, r < r1);
+  }
+  float m[NQ], l[NQ];
+  v4f o[NQ][Tl::kBlocks];
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    m[j] = -INFINITY; l[j] = 0.f;
+#pragma unroll
+    for (int c = 0; c < Tl::kBlocks; ++c) o[j][c] = v4f{0.f, 0.f, 0.f, 0.f};
+  }
+  for (; t0 < t_end; t0 += kStride) {
+    uint32_t there = (uint32_t)__ballot(off[0] >= 0) & 0xFFFFu;
+    if constexpr (Tl::kHalves == 2) there |= (uint32_t)__ballot(off[Tl::kHalves - 1] >= 0) << 16;
+    const bool more = t0 + kStride < t_end;
+    if (more) offsets(t0 + kStride);
+    // the next tile's rows are asked for as soon as this one's are out of their registers
+    Tl::store_values(values, L.wave[wave], lane);
+    if (more && !Tl::kValuesLate) Tl::load_values(values, Vh, off, lane);
+    v4f x[NQ][Tl::kHalves];
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) Tl::logits(x[j], keys, q[j]);
+    if (more) {
+      Tl::load_keys(keys, Kh, off, lane);
+      if (!Tl::kValuesLate) look_up(t0 + 2 * kStride);
+    }
+    const bool whole = there == (Tl::kHalves == 2 ? 0xFFFFFFFFu : 0xFFFFu) && t0 + Tl::kTokens - 1 <= pos_min && t0 >= low_max;
+    typename Tl::Weights w[NQ];
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+      if (!whole) {
+#pragma unroll
+        for (int h = 0; h < Tl::kHalves; ++h)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int at = 16 * h + 4 * (lane >> 4) + i, t = t0 + at;
+            if (!((there >> at) & 1u) || t > pos[j] || t < low[j]) x[j][h][i] = -INFINITY;
+          }
+      }
+      float top = x[j][0][0];
+#pragma unroll
+      for (int h = 0; h < Tl::kHalves; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, x[j][h][i]);
+      top *= P.scale_log2;
+      if (__any(top > m[j] + kRaise)) {
+        const float next = fmaxf(m[j], row_max(top));
+        const float keep = next == -INFINITY ? 1.f : fast_exp2(m[j] - next);
+        m[j] = next;
+        l[j] *= keep;
+#pragma unroll
+        for (int c = 0; c < Tl::kBlocks; ++c) o[j][c] *= keep;
+      }
+      const float ref = m[j] == -INFINITY ? 0.f : m[j];
+      float sum = 0.f;
+#pragma unroll
+      for (int h = 0; h < Tl::kHalves; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float e = fast_exp2(fmaf(x[j][h][i], P.scale_log2, -ref));
+          x[j][h][i] = e;
+          sum += e;
+        }
+      l[j] += sum;
+      w[j] = Tl::weights(x[j]);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    Tl::add_values(o, w, values, L.wave[wave], lane);
+    __builtin_amdgcn_wave_barrier();
+    if (more && Tl::kValuesLate) {
+      Tl::load_values(values, Vh, off, lane);
+      look_up(t0 + 2 * kStride);
+    }
+  }
+
+  // the waves' sums together: all to the largest reference, 16 rows at a time through LDS
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    l[j] = row_sum(l[j]);
+    if (lane < 16) { L.m[wave][16 * j + lane] = m[j]; L.l[wave][16 * j + lane] = l[j]; }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    float all = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) all = fmaxf(all, L.m[w][16 * j + (lane & 15)]);
+    const float keep = m[j] == -INFINITY ? (l[j] == l[j] ? 0.f : l[j]) : fast_exp2(m[j] - all);
+    float* mine = reinterpret_cast<float*>(L.wave[wave]) + (lane & 15) * kPitch;
+    if (j > 0) __syncthreads();
+#pragma unroll
+    for (int c = 0; c < Tl::kBlocks; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mine[Tl::element(c, lane, i)] = o[j][c][i] * keep;
+    __syncthreads();
+    // 16 rows of D elements by 256 threads
+    constexpr int kPer = 16 * D / (64 * kWaves);           // 4 or 8 elements a thread
+    const int q_row = tid / (D / kPer), e0 = tid % (D / kPer) * kPer, r = r0 + 16 * j + q_row;
+    float acc[kPer] = {}, top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float* from = reinterpret_cast<const float*>(L.wave[w]) + q_row * kPitch + e0;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) acc[e] += from[e];
+      top = fmaxf(top, L.m[w][16 * j + q_row]);
+    }
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float mw = L.m[w][16 * j + q_row], lw = L.l[w][16 * j + q_row];
+      sum += mw == -INFINITY ? (lw == lw ? 0.f : lw) : lw * fast_exp2(mw - top);
+    }
+    if (r < r1) {
+      const int i = r / P.G, head = hkv * P.G + r - i * P.G;
+      const int64_t row = sq.first + i;
+      if (whole_row) {
+        const float inv = inverse_sum(sum);
+        T* to = static_cast<T*>(A.out) + b * P.o_b + row * P.o_t + head * P.o_h + e0;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) acc[e] *= inv;
+        store_piece(to, acc);
+        if (A.lse != nullptr && e0 == 0) A.lse[b * P.l_b + row * P.l_t + head * P.l_h] = to_natural_lse(top, sum);
+      } else {
+        const int64_t at = part0 >= 0 ? part0 + (r - r0) : ((int64_t)part_no * P.tokens + row) * P.Hq + head;
+        float* to = A.part.o + at * D + e0;
+#pragma unroll
+        for (int e = 0; e < kPer; e += 4) *reinterpret_cast<float4*>(to + e) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+        if (e0 == 0) A.part.ml[at] = make_float2(top, sum);
+      }
+    }
+  }
+  __syncthreads();
+}
+
+// the call cut on a grid: (unit, block of rows, stretch)
+template <class T, int D, int NQ>
+__global__ __launch_bounds__(64 * kWaves, (split_waves<T, D, NQ>())) void attend_split_kernel(Paged P, AttendPlan pl, AttendArgs A) {
+  __shared__ SplitLds<T, D, NQ> L;
+  constexpr int kRows = 16 * NQ;
   const int units = P.B * P.Hkv;
   int idx = blockIdx.x;
   const int unit = idx % units;
   idx /= units;
   const int part_no = idx % pl.parts, block0 = pl.row_blocks - 1 - idx / pl.parts;       // the last rows see most: first
   const int b = unit / P.Hkv, hkv = unit % P.Hkv;
-  const Sequence sq = load_sequence(P, b, q_start, kv_len);
+  const Sequence sq = load_sequence(P, b, A.q_start, A.kv_len);
   const int rows_all = sq.m * P.G;
-  const int32_t* pages = table + (int64_t)b * P.table_width;
-  const T* Kh = K + hkv * P.head_stride;
-  const T* Vh = V + hkv * P.head_stride;
-
+  if (rows_all <= pl.few) return;
   for (int r0 = block0 * kRows; r0 < rows_all; r0 += pl.row_blocks * kRows) {
     const int r1 = r0 + kRows < rows_all ? r0 + kRows : rows_all;
     const Stretch st = cut_rows(P, sq, r0, r1, pl.parts, pl.chunk);
     if (part_no >= st.parts) continue;
     const int t_begin = st.begin + part_no * st.chunk, t_end = t_begin + st.chunk < st.end ? t_begin + st.chunk : st.end;
-    // the lane's rows
-    typename Tl::Query q[NQ];
-    int pos[NQ], low[NQ];                                    // position of the row, first position it sees
-    const int pos_min = sq.base + r0 / P.G, low_max = first_seen(P, sq.base + (r1 - 1) / P.G);
-#pragma unroll
-    for (int j = 0; j < NQ; ++j) {
-      const int r = r0 + 16 * j + (lane & 15), i = r / P.G;
-      pos[j] = sq.base + i;
-      low[j] = first_seen(P, pos[j]);
-      Tl::load_query(q[j], Q + b * P.q_b + (int64_t)(sq.first + i) * P.q_t + (int64_t)(hkv * P.G + r - i * P.G) * P.q_h, lane, r < r1);
-    }
-    float m[NQ], l[NQ];
-    v4f o[NQ][Tl::kBlocks];
-#pragma unroll
-    for (int j = 0; j < NQ; ++j) {
-      m[j] = -INFINITY; l[j] = 0.f;
-#pragma unroll
-      for (int c = 0; c < Tl::kBlocks; ++c) o[j][c] = v4f{0.f, 0.f, 0.f, 0.f};
-    }
-    auto offsets = [&](int t0, int64_t (&off)[Tl::kHalves]) {
-#pragma unroll
-      for (int h = 0; h < Tl::kHalves; ++h) {
-        const int t = t0 + 16 * h + (lane & 15);
-        off[h] = -1;
-        if (t < t_end) {
-          const int c = page_of(P.div, t), id = pages[c];
-          if (id >= 0 && id < P.n_pages) off[h] = id * P.page_stride + (int64_t)(t - c * P.div.page) * P.row_stride;
-        }
-      }
-    };
-    typename Tl::Keys keys;
-    typename Tl::Values values;
-    int64_t off[Tl::kHalves];
-    int t0 = t_begin + wave * Tl::kTokens;
-    if (t0 < t_end) {
-      offsets(t0, off);
-      Tl::load_keys(keys, Kh, off, lane);
-      Tl::load_values(values, Vh, off, lane);
-    }
-    for (; t0 < t_end; t0 += kWaves * Tl::kTokens) {
-      uint32_t there = (uint32_t)__ballot(off[0] >= 0) & 0xFFFFu;
-      if constexpr (Tl::kHalves == 2) there |= (uint32_t)__ballot(off[Tl::kHalves - 1] >= 0) << 16;
-      const bool more = t0 + kWaves * Tl::kTokens < t_end;
-      if (more) offsets(t0 + kWaves * Tl::kTokens, off);
-      // the next tile's rows are asked for as soon as this one's are out of their registers
-      Tl::store_values(values, lds[wave], lane);
-      if (more && !Tl::kValuesLate) Tl::load_values(values, Vh, off, lane);
-      v4f x[NQ][Tl::kHalves];
-#pragma unroll
-      for (int j = 0; j < NQ; ++j) Tl::logits(x[j], keys, q[j]);
-      if (more) Tl::load_keys(keys, Kh, off, lane);
-      const bool whole = there == (Tl::kHalves == 2 ? 0xFFFFFFFFu : 0xFFFFu) && t0 + Tl::kTokens - 1 <= pos_min && t0 >= low_max;
-      typename Tl::Weights w[NQ];
-#pragma unroll
-      for (int j = 0; j < NQ; ++j) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int h = 0; h < Tl::kHalves; ++h)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            float y = x[j][h][i] * P.scale_log2;
-            if (!whole) {
-              const int at = 16 * h + 4 * (lane >> 4) + i, t = t0 + at;
-              if (!((there >> at) & 1u) || t > pos[j] || t < low[j]) y = -INFINITY;
-            }
-            x[j][h][i] = y;
-            top = fmaxf(top, y);
-          }
-        if (__any(top > m[j] + kRaise)) {
-          const float next = fmaxf(m[j], row_max(top));
-          const float keep = next == -INFINITY ? 1.f : fast_exp2(m[j] - next);
-          m[j] = next;
-          l[j] *= keep;
-#pragma unroll
-          for (int c = 0; c < Tl::kBlocks; ++c) o[j][c] *= keep;
-        }
-        const float ref = m[j] == -INFINITY ? 0.f : m[j];
-#pragma unroll
-        for (int h = 0; h < Tl::kHalves; ++h)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float e = fast_exp2(x[j][h][i] - ref);
-            x[j][h][i] = e;
-            l[j] += e;
-          }
-        w[j] = Tl::weights(x[j]);
-      }
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      Tl::add_values(o, w, values, lds[wave], lane);
-      __builtin_amdgcn_wave_barrier();
-      if (more && Tl::kValuesLate) Tl::load_values(values, Vh, off, lane);
-    }
-
-    // the waves' sums together: all to the largest reference, 16 rows at a time through LDS
-#pragma unroll
-    for (int j = 0; j < NQ; ++j) {
-      l[j] = row_sum(l[j]);
-      if (lane < 16) { wave_m[wave][16 * j + lane] = m[j]; wave_l[wave][16 * j + lane] = l[j]; }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < NQ; ++j) {
-      float all = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) all = fmaxf(all, wave_m[w][16 * j + (lane & 15)]);
-      const float keep = m[j] == -INFINITY ? (l[j] == l[j] ? 0.f : l[j]) : fast_exp2(m[j] - all);
-      float* mine = reinterpret_cast<float*>(lds[wave]) + (lane & 15) * kPitch;
-      if (j > 0) __syncthreads();
-#pragma unroll
-      for (int c = 0; c < Tl::kBlocks; ++c)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) mine[Tl::element(c, lane, i)] = o[j][c][i] * keep;
-      __syncthreads();
-      // 16 rows of D elements by 256 threads
-      constexpr int kPer = 16 * D / (64 * kWaves);           // 4 or 8 elements a thread
-      const int q_row = tid / (D / kPer), e0 = tid % (D / kPer) * kPer, r = r0 + 16 * j + q_row;
-      float acc[kPer] = {}, top = -INFINITY, sum = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float* from = reinterpret_cast<const float*>(lds[w]) + q_row * kPitch + e0;
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) acc[e] += from[e];
-        top = fmaxf(top, wave_m[w][16 * j + q_row]);
-      }
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        const float mw = wave_m[w][16 * j + q_row], lw = wave_l[w][16 * j + q_row];
-        sum += mw == -INFINITY ? (lw == lw ? 0.f : lw) : lw * fast_exp2(mw - top);
-      }
-      if (r < r1) {
-        const int i = r / P.G, head = hkv * P.G + r - i * P.G;
-        const int64_t row = sq.first + i;
-        if (st.parts == 1) {
-          const float inv = inverse_sum(sum);
-          T* to = out + b * P.o_b + row * P.o_t + head * P.o_h + e0;
-#pragma unroll
-          for (int e = 0; e < kPer; ++e) store_elem(to + e, acc[e] * inv);
-          if (lse != nullptr && e0 == 0) lse[b * P.l_b + row * P.l_t + head * P.l_h] = to_natural_lse(top, sum);
-        } else {
-          const int64_t at = ((int64_t)part_no * P.tokens + row) * P.Hq + head;
-          float* to = part.o + at * D + e0;
-#pragma unroll
-          for (int e = 0; e < kPer; ++e) to[e] = acc[e];
-          if (e0 == 0) part.ml[at] = make_float2(top, sum);
-        }
-      }
-    }
-    __syncthreads();
+    attend_stretch<T, D, NQ>(P, A, L, sq, b, hkv, r0, r1, t_begin, t_end, st.parts == 1, -1, part_no);
   }
 }
 
-// joins the stretches of a row: one wave per (new token, query head)
-template <class T, int D>
-__global__ __launch_bounds__(256) void attend_join_kernel(Paged P, AttendPlan pl, Partials part, const int32_t* __restrict__ q_start,
-                                                          const int32_t* __restrict__ kv_len, T* __restrict__ out, float* __restrict__ lse) {
-  const int64_t at0 = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  const int row = (int)(at0 / P.Hq), head = (int)(at0 % P.Hq);
-  if (row >= P.tokens || row < q_start[0] || row >= q_start[P.B]) return;
-  int lo = 0, hi = P.B;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (q_start[mid] <= row) lo = mid; else hi = mid;
-  }
-  const Sequence sq = load_sequence(P, lo, q_start, kv_len);
-  const int r = (row - sq.first) * P.G + head % P.G, r0 = r / pl.rows * pl.rows;
-  const int rows_all = sq.m * P.G;
-  if (r < 0 || r >= rows_all) return;
-  const Stretch st = cut_rows(P, sq, r0, r0 + pl.rows < rows_all ? r0 + pl.rows : rows_all, pl.parts, pl.chunk);
-  if (st.parts < 2) return;
-  const int64_t step = (int64_t)P.tokens * P.Hq;
-  float top = -INFINITY, sum = 0.f;
-  for (int p = 0; p < st.parts; ++p) top = fmaxf(top, part.ml[at0 + p * step].x);
-  float acc[D / 64] = {};
-  for (int p = 0; p < st.parts; ++p) {
-    const float2 ml = part.ml[at0 + p * step];
-    const float keep = ml.x == -INFINITY ? (ml.y == ml.y ? 0.f : ml.y) : fast_exp2(ml.x - top);
-    sum += ml.x == -INFINITY ? keep : ml.y * keep;
+// The call cut evenly: the tokens of all units, one after the other, are dealt to the workgroups in equal stretches, so that one round of the chip
+// has the same to read everywhere whatever the lengths.  A workgroup's stretch can end in one unit and go on in the next; a unit's rows are
+// joined from the stretches of the workgroups `first` .. that share it.  Every workgroup sums up the lengths for itself.
+constexpr int kEvenLeast = 256;          // tokens of a stretch, at least
+constexpr int kShortChunk = 512;
+
+// what sequence b has to read per KV head, to whole tiles: nothing if its rows are not for this kernel or see nothing
+struct Span {
+  int begin, end, padded;
+};
+__device__ __forceinline__ Span span_of(const Paged& P, const AttendPlan& pl, const Sequence& sq) {
+  Span s{0, 0, 0};
+  if (sq.m < 1 || (pl.only_few && sq.m * P.G > pl.few)) return s;
+  const int64_t end = (int64_t)sq.base + sq.m;
+  s.end = end < 0 ? 0 : end < sq.n ? (int)end : sq.n;
+  const int low = first_seen(P, sq.base);
+  s.begin = low < s.end ? low : s.end;
+  s.padded = (s.end - s.begin + 31) & ~31;
+  return s;
+}
+
+template <class T, int D, int NQ>
+__global__ __launch_bounds__(64 * kWaves, (split_waves<T, D, NQ>())) void attend_even_kernel(Paged P, AttendPlan pl, AttendArgs A) {
+  __shared__ SplitLds<T, D, NQ> L;
+  __shared__ int64_t wave_sum[kWaves];
+  __shared__ int64_t found_at;
+  __shared__ int found_b;
+  constexpr int kRows = 16 * NQ, kThreads = 64 * kWaves;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, me = blockIdx.x;
+  auto length = [&](int b) { return b < P.B ? span_of(P, pl, load_sequence(P, b, A.q_start, A.kv_len)).padded : 0; };
+  // all tokens; with few sequences also where each begins
+  const int mine = length(tid);
+  int64_t run = 0;
+  for (int b = tid + kThreads; b < P.B; b += kThreads) run += length(b);
+  run += mine;
+  int64_t to = run;
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) acc[j] = fmaf(part.o[(at0 + p * step) * D + j * 64 + lane], keep, acc[j]);
+  for (int s = 1; s < 64; s <<= 1) {
+    const int64_t y = __shfl_up(to, s);
+    if (lane >= s) to += y;
+  }
+  if (lane == 63) wave_sum[wave] = to;
+  if (tid == 0) found_b = -1;
+  __syncthreads();
+  int64_t all = 0, before = to - run;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) { if (w < wave) before += wave_sum[w]; all += wave_sum[w]; }
+  all *= P.Hkv;
+  int64_t per = (all + gridDim.x - 1) / gridDim.x;
+  per = per < kEvenLeast ? kEvenLeast : (per + 127) / 128 * 128;
+  int64_t at = me * per;
+  const int64_t stop = at + per < all ? at + per : all;
+  // the sequence that the stretch begins in, and where that begins
+  if (P.B <= kThreads) {
+    if (at < stop && mine > 0 && before * P.Hkv <= at && at < (before + mine) * P.Hkv) { found_b = tid; found_at = before * P.Hkv; }
+  } else if (tid == 0 && at < stop) {
+    int64_t sum = 0;
+    for (int b = 0; b < P.B; ++b) {
+      const int64_t n = (int64_t)length(b) * P.Hkv;
+      if (sum + n > at) { found_b = b; found_at = sum; break; }
+      sum += n;
+    }
+  }
+  // rows that see nothing
+  int2* meta = A.part.meta;
+  for (int b = me; b < P.B; b += gridDim.x) {
+    const Sequence sq = load_sequence(P, b, A.q_start, A.kv_len);
+    const bool mine_too = sq.m > 0 && !(pl.only_few && sq.m * P.G > pl.few);
+    if (!mine_too || span_of(P, pl, sq).padded > 0) continue;
+    for (int h = tid; h < P.Hkv; h += kThreads) meta[b * P.Hkv + h] = make_int2(0, 1);
+    for (int64_t x = tid; x < (int64_t)sq.m * P.Hq * (D / 4); x += kThreads) {
+      const int e = (int)(x % (D / 4)) * 4, head = (int)(x / (D / 4) % P.Hq), i = (int)(x / (D / 4) / P.Hq);
+      const float none[4] = {0.f, 0.f, 0.f, 0.f};
+      store_piece(static_cast<T*>(A.out) + b * P.o_b + (int64_t)(sq.first + i) * P.o_t + head * P.o_h + e, none);
+      if (A.lse != nullptr && e == 0) A.lse[b * P.l_b + (int64_t)(sq.first + i) * P.l_t + head * P.l_h] = -INFINITY;
+    }
+  }
+  __syncthreads();
+  int b = found_b;
+  int64_t b_at = found_at;
+  while (b >= 0 && at < stop) {
+    const Sequence sq = load_sequence(P, b, A.q_start, A.kv_len);
+    const Span sp = span_of(P, pl, sq);
+    if (sp.padded == 0) { ++b; continue; }
+    const int64_t b_end = b_at + (int64_t)sp.padded * P.Hkv;
+    while (at < stop && at < b_end) {
+      const int h = (int)((at - b_at) / sp.padded);
+      const int64_t unit_at = b_at + (int64_t)h * sp.padded, unit_end = unit_at + sp.padded;
+      const int64_t until = unit_end < stop ? unit_end : stop;
+      const int first = (int)(unit_at / per), last = (int)((unit_end - 1) / per);
+      const int rows_all = sq.m * P.G;
+      // More rows than the host expected of any sequence: block after block and whole, by the workgroup that the unit begins in.
+      const bool alone = rows_all > kRows;
+      if (tid == 0 && first == me) meta[b * P.Hkv + h] = make_int2(first, alone ? 1 : last - first + 1);
+      const int t_begin = sp.begin + (int)(at - unit_at), t_stop = sp.begin + (int)(until - unit_at);
+      if (!alone || first == me)
+        for (int r0 = 0; r0 < rows_all; r0 += kRows)
+          attend_stretch<T, D, NQ>(P, A, L, sq, b, h, r0, r0 + kRows < rows_all ? r0 + kRows : rows_all, alone ? sp.begin : t_begin,
+                                   alone || t_stop > sp.end ? sp.end : t_stop, alone || first == last, (int64_t)(2 * me + (first == me)) * kRows, 0);
+      at = until;
+    }
+    b_at = b_end;
+    ++b;
+  }
+}
+
+// Joins the stretches of a row: WAVES waves per (new token, query head).  A lane has the reference and the sum of one stretch, so 64 of them are
+// there at once and their largest costs no chain of loads; the waves then take the stretches' sums in turn.  EVEN: the stretches of
+// attend_even_kernel, else those of a grid.
+template <class T, int D, int WAVES, bool EVEN>
+__global__ __launch_bounds__(256) void attend_join_kernel(Paged P, AttendPlan pl, AttendArgs A) {
+  constexpr int kPer = D / 64;
+  __shared__ float sums[WAVES > 1 ? WAVES : 1][D];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t at0 = WAVES > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
+  const int row = (int)(at0 / P.Hq), head = (int)(at0 % P.Hq);
+  if (row >= P.tokens) return;
+  int lo = 0;                                          // sequences that end at or before the row: counted, no chain of loads
+  for (int b0 = 1; b0 <= P.B; b0 += 64) lo += __popcll(__ballot(b0 + lane <= P.B && A.q_start[b0 + lane <= P.B ? b0 + lane : P.B] <= row));
+  if (lo >= P.B || row < A.q_start[0]) return;
+  const Sequence sq = load_sequence(P, lo, A.q_start, A.kv_len);
+  const int r = (row - sq.first) * P.G + head % P.G, rows_all = sq.m * P.G;
+  if (r < 0 || r >= rows_all) return;
+  int parts;
+  int64_t part_first, part_0, part_step;              // entry of the first stretch, of the second less a step, distance of the others
+  if (EVEN) {
+    if (pl.only_few && rows_all > pl.few) return;
+    const int2 unit = A.part.meta[lo * P.Hkv + head / P.G];
+    parts = unit.y;
+    part_step = 2 * pl.rows;
+    part_0 = (int64_t)unit.x * part_step + r;
+    part_first = part_0 + pl.rows;
+  } else {
+    if (rows_all <= pl.few) return;
+    const int r0 = r / pl.rows * pl.rows;
+    parts = cut_rows(P, sq, r0, r0 + pl.rows < rows_all ? r0 + pl.rows : rows_all, pl.parts, pl.chunk).parts;
+    part_step = (int64_t)P.tokens * P.Hq;
+    part_0 = part_first = at0;
+  }
+  if (parts < 2) return;
+  auto entry = [&](int p) { return p == 0 ? part_first : part_0 + p * part_step; };
+  float top = -INFINITY, sum = 0.f, acc[kPer] = {};
+  for (int p0 = 0; p0 < parts; p0 += 64) {
+    const int here = parts - p0 < 64 ? parts - p0 : 64;
+    const float2 ml = lane < here ? A.part.ml[entry(p0 + lane)] : make_float2(-INFINITY, 0.f);
+    float next = fmaxf(top, ml.x);
+#pragma unroll
+    for (int s = 32; s; s >>= 1) next = fmaxf(next, __shfl_xor(next, s));
+    const float keep = ml.x == -INFINITY ? (ml.y == ml.y ? 0.f : ml.y) : fast_exp2(ml.x - next);
+    float more = ml.x == -INFINITY ? keep : ml.y * keep;
+#pragma unroll
+    for (int s = 32; s; s >>= 1) more += __shfl_xor(more, s);
+    const float old = next == -INFINITY ? 1.f : fast_exp2(top - next);
+    top = next;
+    sum = sum * old + more;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) acc[j] *= old;
+    for (int p = WAVES > 1 ? wave : 0; p < here; p += 8 * WAVES) {
+      float v[8][kPer];
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) v[u][j] = p + u * WAVES < here ? A.part.o[entry(p0 + p + u * WAVES) * D + j * 64 + lane] : 0.f;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const float k = __shfl(keep, (p + u * WAVES) & 63);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) acc[j] = p + u * WAVES < here ? fmaf(v[u][j], k, acc[j]) : acc[j];
+      }
+    }
+  }
+  if (WAVES > 1) {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) sums[wave][j * 64 + lane] = acc[j];
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      acc[j] = 0.f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) acc[j] += sums[w][j * 64 + lane];
+    }
   }
   const float inv = inverse_sum(sum);
 #pragma unroll
-  for (int j = 0; j < D / 64; ++j) store_elem(out + lo * P.o_b + row * P.o_t + head * P.o_h + j * 64 + lane, acc[j] * inv);
-  if (lse != nullptr && lane == 0) lse[lo * P.l_b + row * P.l_t + head * P.l_h] = to_natural_lse(top, sum);
+  for (int j = 0; j < kPer; ++j) store_elem(static_cast<T*>(A.out) + lo * P.o_b + row * P.o_t + head * P.o_h + j * 64 + lane, acc[j] * inv);
+  if (A.lse != nullptr && lane == 0) A.lse[lo * P.l_b + row * P.l_t + head * P.l_h] = to_natural_lse(top, sum);
 }
+
+// ---- host side
+
+// How a call is cut.  Few rows in every sequence (decoding, at most 64 rows per unit): evenly.  More: on a grid, with the sequences of
+// few rows among them (a batch of chunks and single tokens) evenly by kernels of their own, as a block of 128 rows would walk their long
+// caches alone.
+struct AttendCuts {
+  AttendPlan even, grid;           // rows == 0: not used
+};
 
 template <class T, int D>
-static void split_launch(const Paged& P, const AttendPlan& pl, const void* Q, const void* K, const void* V, const int32_t* table,
-                         const int32_t* q_start, const int32_t* kv_len, void* out, float* lse, Partials part, hipStream_t s) {
-  const T *q = static_cast<const T*>(Q), *k = static_cast<const T*>(K), *v = static_cast<const T*>(V);
-  T* o = static_cast<T*>(out);
-  const dim3 grid((unsigned)((int64_t)P.B * P.Hkv * pl.parts * pl.row_blocks)), block(64 * kWaves);
-  if (pl.rows == 16)      launch(attend_split_kernel<T, D, 1>, grid, block, s, P, pl, q, k, v, table, q_start, kv_len, o, lse, part);
-  else if (pl.rows == 32) launch(attend_split_kernel<T, D, 2>, grid, block, s, P, pl, q, k, v, table, q_start, kv_len, o, lse, part);
-  else                    launch(attend_split_kernel<T, D, 4>, grid, block, s, P, pl, q, k, v, table, q_start, kv_len, o, lse, part);
-}
+static int even_waves(int rows) { return rows == 16 ? split_waves<T, D, 1>() : rows == 32 ? split_waves<T, D, 2>() : split_waves<T, D, 4>(); }
 
-void launch_attend_split(const Paged& P, const AttendPlan& pl, int dtype, const void* Q, const void* K, const void* V, const int32_t* table,
-                         const int32_t* q_start, const int32_t* kv_len, void* out, float* lse, Partials part, hipStream_t s) {
-  if (dtype == 0) {
-    if (P.d == 64) split_launch<float, 64>(P, pl, Q, K, V, table, q_start, kv_len, out, lse, part, s);
-    else           split_launch<float, 128>(P, pl, Q, K, V, table, q_start, kv_len, out, lse, part, s);
-  } else {
-    if (P.d == 64) split_launch<uint16_t, 64>(P, pl, Q, K, V, table, q_start, kv_len, out, lse, part, s);
-    else           split_launch<uint16_t, 128>(P, pl, Q, K, V, table, q_start, kv_len, out, lse, part, s);
-  }
-}
+int attend_compute_units();
 
-template <class T>
-static void join_launch(const Paged& P, const AttendPlan& pl, Partials part, const int32_t* q_start, const int32_t* kv_len, void* out, float* lse,
-                        hipStream_t s) {
-  const dim3 grid((unsigned)(((int64_t)P.tokens * P.Hq + 3) / 4));
-  if (P.d == 64) launch(attend_join_kernel<T, 64>, grid, dim3(256), s, P, pl, part, q_start, kv_len, static_cast<T*>(out), lse);
-  else           launch(attend_join_kernel<T, 128>, grid, dim3(256), s, P, pl, part, q_start, kv_len, static_cast<T*>(out), lse);
-}
-
-void launch_attend_join(const Paged& P, const AttendPlan& pl, int dtype, Partials part, const int32_t* q_start, const int32_t* kv_len, void* out,
-                        float* lse, hipStream_t s) {
-  if (dtype == 0) join_launch<float>(P, pl, part, q_start, kv_len, out, lse, s);
-  else            join_launch<uint16_t>(P, pl, part, q_start, kv_len, out, lse, s);
-}
-
-static AttendPlan plan_attend(const Paged& P, int dtype, int max_new, int max_len) {
-  AttendPlan pl{};
-  const int64_t rows = (int64_t)max_new * P.G;
-  pl.by_rows = dtype != 0 && rows > 64;
-  pl.rows = pl.by_rows ? 128 : rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
-  pl.row_blocks = (int)((rows + pl.rows - 1) / pl.rows);
-  const int64_t units = (int64_t)P.B * P.Hkv * pl.row_blocks;
+static AttendCuts plan_attend(const Paged& P, int dtype, int max_new, int max_len) {
+  AttendCuts c{};
+  const int64_t rows = (int64_t)max_new * P.G, cus = attend_compute_units();
+  const bool many = rows > 64;
   int64_t len = max_len;
   if (P.window > 0 && len > (int64_t)P.window + max_new) len = (int64_t)P.window + max_new;
-  // stretches: until some 1024 workgroups are under way (512 of the rows kernel), of 256 tokens at least
-  int64_t parts = ((pl.by_rows ? 512 : 1024) + units - 1) / units;
-  const int64_t most = (len + 255) / 256;
-  if (parts > most) parts = most;
-  if (parts > 64) parts = 64;
-  if (parts < 1) parts = 1;
-  pl.chunk = (int)(((len + parts - 1) / parts + 127) / 128 * 128);
-  pl.parts = (int)((len + pl.chunk - 1) / pl.chunk);
-  if (pl.parts < 1) pl.parts = 1;
-  return pl;
+  if (!many || P.B > 1) {
+    AttendPlan& e = c.even;
+    const int64_t most = many ? P.G : rows;
+    e.rows = most <= 16 ? 16 : most <= 32 ? 32 : 64;
+    e.only_few = many;
+    e.few = e.rows;
+    const int waves = dtype == 0 ? (P.d == 64 ? even_waves<float, 64>(e.rows) : even_waves<float, 128>(e.rows))
+                                 : (P.d == 64 ? even_waves<uint16_t, 64>(e.rows) : even_waves<uint16_t, 128>(e.rows));
+    const int64_t units = (int64_t)P.B * P.Hkv;
+    int64_t wgs = (units * len + kEvenLeast - 1) / kEvenLeast;
+    if (wgs > cus * waves) wgs = cus * waves;
+    e.parts = (int)(wgs < 1 ? 1 : wgs);
+    // Short caches: a workgroup per unit and 512 tokens fits one round of the chip, then nobody has to go on in a second unit.
+    const int64_t chunks = (len + kShortChunk - 1) / kShortChunk;
+    if (!many && units * chunks <= cus * waves && chunks <= 64) {
+      c.grid = e;
+      c.grid.few = 0;
+      c.grid.row_blocks = (int)((rows + e.rows - 1) / e.rows);
+      c.grid.chunk = kShortChunk;
+      c.grid.parts = (int)(chunks < 1 ? 1 : chunks);
+      c.even.rows = 0;
+    }
+  }
+  if (many) {
+    AttendPlan& g = c.grid;
+    g.by_rows = dtype != 0;
+    g.rows = g.by_rows ? 128 : 64;
+    g.few = P.B > 1 ? c.even.few : 0;
+    g.row_blocks = (int)((rows + g.rows - 1) / g.rows);
+    const int64_t units = (int64_t)P.B * P.Hkv * g.row_blocks;
+    // stretches: until one round of the chip is full, of 256 tokens at least
+    int64_t parts = (cus * (g.by_rows ? 2 : 4) + units - 1) / units;
+    const int64_t most = (len + 255) / 256;
+    if (parts > most) parts = most;
+    if (parts > 64) parts = 64;
+    if (parts < 1) parts = 1;
+    g.chunk = (int)(((len + parts - 1) / parts + 127) / 128 * 128);
+    g.parts = (int)((len + g.chunk - 1) / g.chunk);
+    if (g.parts < 1) g.parts = 1;
+    if (g.by_rows && units * g.parts <= 2 * cus) g.turn = (g.row_blocks + 1) / 2;
+  }
+  return c;
+}
+
+int attend_compute_units() {
+  static int cus = 0;             // (the answer of the first device serves all: one GPU model per node)
+  if (cus == 0) {
+    int dev = 0, n = 0;
+    if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) n = 256;
+    cus = n;
+  }
+  return cus;
+}
+
+// the workspace: entries of the even cut and of the grid, (o, m, l) each, and the even cut's units
+struct AttendSpace {
+  size_t even_o, even_ml, meta, grid_o, grid_ml, total;
+};
+static AttendSpace lay_out(const Paged& P, const AttendCuts& c) {
+  AttendSpace w{};
+  auto take = [&](size_t bytes) { const size_t at = w.total; w.total += (bytes + 255) / 256 * 256; return at; };
+  if (c.even.rows > 0) {
+    const size_t entries = (size_t)c.even.parts * 2 * c.even.rows;
+    w.even_o = take(entries * P.d * sizeof(float));
+    w.even_ml = take(entries * sizeof(float2));
+    w.meta = take((size_t)P.B * P.Hkv * sizeof(int2));
+  }
+  if (c.grid.rows > 0 && c.grid.parts > 1) {
+    const size_t entries = (size_t)P.tokens * P.Hq * c.grid.parts;
+    w.grid_o = take(entries * P.d * sizeof(float));
+    w.grid_ml = take(entries * sizeof(float2));
+  }
+  if (w.total == 0) w.total = 256;
+  return w;
 }
 
 size_t attend_workspace_bytes(const Paged& P, int dtype, int max_new, int max_len) {
-  const AttendPlan pl = plan_attend(P, dtype, max_new, max_len);
-  if (pl.parts < 2) return 256;
-  const size_t rows = (size_t)P.tokens * P.Hq * pl.parts;
-  return (rows * P.d * sizeof(float) + 255) / 256 * 256 + (rows * sizeof(float2) + 255) / 256 * 256;
+  return lay_out(P, plan_attend(P, dtype, max_new, max_len)).total;
+}
+
+template <class T, int D, bool EVEN>
+static void join_launch(const Paged& P, const AttendPlan& pl, const AttendArgs& A, hipStream_t s) {
+  const int64_t rows = (int64_t)P.tokens * P.Hq;
+  // (few rows: four waves each)
+  if (rows <= 2048) launch(attend_join_kernel<T, D, 4, EVEN>, dim3((unsigned)rows), dim3(256), s, P, pl, A);
+  else              launch(attend_join_kernel<T, D, 1, EVEN>, dim3((unsigned)((rows + 3) / 4)), dim3(256), s, P, pl, A);
+}
+
+template <class T, int D>
+static void attend_launch(const Paged& P, int dtype, const AttendCuts& c, const AttendArgs& even, const AttendArgs& grid, hipStream_t s) {
+  const dim3 block(64 * kWaves);
+  if (c.grid.rows > 0) {
+    const AttendPlan& pl = c.grid;
+    if (pl.by_rows) {
+      launch_attend_rows(P, pl, grid.Q, grid.K, grid.V, grid.table, grid.q_start, grid.kv_len, grid.out, grid.lse, grid.part, s);
+    } else {
+      const dim3 wgs((unsigned)((int64_t)P.B * P.Hkv * pl.parts * pl.row_blocks));
+      if (pl.rows == 16)      launch(attend_split_kernel<T, D, 1>, wgs, block, s, P, pl, grid);
+      else if (pl.rows == 32) launch(attend_split_kernel<T, D, 2>, wgs, block, s, P, pl, grid);
+      else                    launch(attend_split_kernel<T, D, 4>, wgs, block, s, P, pl, grid);
+    }
+    if (pl.parts > 1) join_launch<T, D, false>(P, pl, grid, s);
+  }
+  if (c.even.rows > 0) {
+    const AttendPlan& pl = c.even;
+    const dim3 wgs((unsigned)pl.parts);
+    if (pl.rows == 16)      launch(attend_even_kernel<T, D, 1>, wgs, block, s, P, pl, even);
+    else if (pl.rows == 32) launch(attend_even_kernel<T, D, 2>, wgs, block, s, P, pl, even);
+    else                    launch(attend_even_kernel<T, D, 4>, wgs, block, s, P, pl, even);
+    if (pl.parts > 1) join_launch<T, D, true>(P, pl, even, s);
+  }
 }
 
 void launch_attend(const Paged& P, int dtype, int max_new, int max_len, const void* Q, const void* K, const void* V, const int32_t* table,
                    const int32_t* q_start, const int32_t* kv_len, void* out, float* lse, void* workspace, hipStream_t s) {
-  const AttendPlan pl = plan_attend(P, dtype, max_new, max_len);
-  const size_t rows = (size_t)P.tokens * P.Hq * pl.parts;
-  Partials part{static_cast<float*>(workspace),
-                reinterpret_cast<float2*>(static_cast<char*>(workspace) + (rows * P.d * sizeof(float) + 255) / 256 * 256)};
-  if (pl.by_rows) launch_attend_rows(P, pl, Q, K, V, table, q_start, kv_len, out, lse, part, s);
-  else            launch_attend_split(P, pl, dtype, Q, K, V, table, q_start, kv_len, out, lse, part, s);
-  if (pl.parts > 1) launch_attend_join(P, pl, dtype, part, q_start, kv_len, out, lse, s);
+  const AttendCuts c = plan_attend(P, dtype, max_new, max_len);
+  const AttendSpace w = lay_out(P, c);
+  char* ws = static_cast<char*>(workspace);
+  AttendArgs even{Q, K, V, table, q_start, kv_len, out, lse,
+                  {reinterpret_cast<float*>(ws + w.even_o), reinterpret_cast<float2*>(ws + w.even_ml), reinterpret_cast<int2*>(ws + w.meta)}};
+  AttendArgs grid = even;
+  grid.part = {reinterpret_cast<float*>(ws + w.grid_o), reinterpret_cast<float2*>(ws + w.grid_ml), nullptr};
+  if (dtype == 0 && P.d == 64) attend_launch<float, 64>(P, dtype, c, even, grid, s);
+  else if (dtype == 0)         attend_launch<float, 128>(P, dtype, c, even, grid, s);
+  else if (P.d == 64)          attend_launch<uint16_t, 64>(P, dtype, c, even, grid, s);
+  else                         attend_launch<uint16_t, 128>(P, dtype, c, even, grid, s);
 }
 
 }  // namespace ccd

@@ -37,10 +37,15 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_kernel(Paged P,
   int idx = blockIdx.x;
   const int unit = idx % units;
   idx /= units;
-  const int part_no = idx % pl.parts, block0 = pl.row_blocks - 1 - idx / pl.parts;
+  // The last rows see most and come first.  Where the call is one round of two workgroups per compute unit, its second half runs the other way, so that
+  // a compute unit has a long one and a short one.
+  int turn = idx / pl.parts;
+  if (pl.turn > 0 && turn >= pl.turn) turn = pl.row_blocks - 1 - (turn - pl.turn);
+  const int part_no = idx % pl.parts, block0 = pl.row_blocks - 1 - turn;
   const int b = unit / P.Hkv, hkv = unit % P.Hkv;
   const Sequence sq = load_sequence(P, b, q_start, kv_len);
   const int rows_all = sq.m * P.G;
+  if (rows_all <= pl.few) return;
   const int32_t* pages = table + (int64_t)b * P.table_width;
   const uint16_t* Kh = K + hkv * P.head_stride;
   const uint16_t* Vh = V + hkv * P.head_stride;
