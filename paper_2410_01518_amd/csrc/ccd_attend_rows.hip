@@ -12,6 +12,7 @@
 namespace ccd {
 
 constexpr int kRowWaves = 4, kTile = 64;
+enum { kKeys = 1, kValues = 2 };
 
 // 64 lanes x 16 bytes from memory into LDS, at lds_addr + 16 * lane
 __device__ __forceinline__ void load_to_lds(uint32_t lds_addr, const void* p) {
@@ -19,6 +20,13 @@ __device__ __forceinline__ void load_to_lds(uint32_t lds_addr, const void* p) {
 }
 __device__ __forceinline__ void load_to_lds(uint32_t lds_addr, uint32_t offset, const void* base) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_addr), "v"(offset), "s"(base) : "memory");
+}
+
+__device__ __forceinline__ float largest(const v16f& x) {
+  float top = x[0];
+#pragma unroll
+  for (int e = 1; e < 16; ++e) top = fmaxf(top, x[e]);
+  return top;
 }
 
 // BANDED: pages of whole runs of 16 rows, so that a wave's 16 rows of a tile lie in one page
@@ -60,7 +68,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_kernel(Paged P,
   // what the lane reads: keys, row (lane & 31), piece 2 s + half; values, 4 tokens at 4 half + .., 16 elements at 16 ((lane >> 4) & 1)
   const int key_at = (lane & 31) * kRowB + ((half ^ key_swap(lane & 31)) << 4);
   const int value_row = 4 * half + ((lane & 15) >> 2);
-  const int value_piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+  const int value_at = value_row * kRowB + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ value_swap(value_row)) << 4) + (lane & 1) * 8;
 
   for (int r0 = block0 * kRows; r0 < rows_all; r0 += pl.row_blocks * kRows) {
     const int r1 = r0 + kRows < rows_all ? r0 + kRows : rows_all;
@@ -72,8 +80,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_kernel(Paged P,
     const int r = r0 + 32 * wave + (lane & 31), i = r / P.G, head = hkv * P.G + r - i * P.G;
     const int pos = r < r1 ? sq.base + i : -1, low_row = first_seen(P, pos), low = low_row > t_begin ? low_row : t_begin;
     const int w0 = r0 + 32 * wave, w1 = w0 + 32 < r1 ? w0 + 32 : r1;   // the wave's rows (none if w0 >= r1)
-    const int pos_min = sq.base + w0 / P.G, pos_max = w0 < r1 ? sq.base + (w1 - 1) / P.G : -1;
-    const int low_min = first_seen(P, pos_min), low_all = first_seen(P, pos_max) > t_begin ? first_seen(P, pos_max) : t_begin;
+    const int pos_min = sq.base + w0 / P.G, low_max = w0 < r1 ? first_seen(P, sq.base + (w1 - 1) / P.G) : 0, low_all = low_max > t_begin ? low_max : t_begin;
     v8bf q[kSteps];
     {
       const uint16_t* row = Q + b * P.q_b + (int64_t)(sq.first + i) * P.q_t + (int64_t)head * P.q_h;
@@ -96,7 +103,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_kernel(Paged P,
       const int tw = t0 + 16 * wave;
       return BANDED && tw + 16 <= t_end ? pages[page_of(P.div, tw)] : -1;
     };
-    auto request = [&](int t0, int buf, int page_id) {
+    auto request = [&](int t0, int buf, int what, int page_id) {
       const int tw = t0 + 16 * wave;
       const uint32_t kd = lds0 + (buf * 2) * kTileB + 16 * wave * kRowB, vd = kd + kTileB;
       if (BANDED && page_id >= 0 && page_id < P.n_pages) {
@@ -105,10 +112,10 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_kernel(Paged P,
 #pragma unroll
         for (int k = 0; k < kLoads; ++k) {
           const int row = kPerLoad * k + load_row;
-          load_to_lds(kd + k * 1024, (uint32_t)(row * (int)P.row_stride + ((place ^ key_swap(row)) << 3)) * 2u, kb);
-          load_to_lds(vd + k * 1024, (uint32_t)(row * (int)P.row_stride + ((place ^ value_swap(row)) << 3)) * 2u, vb);
+          if (what & kKeys) load_to_lds(kd + k * 1024, (uint32_t)(row * (int)P.row_stride + ((place ^ key_swap(row)) << 3)) * 2u, kb);
+          if (what & kValues) load_to_lds(vd + k * 1024, (uint32_t)(row * (int)P.row_stride + ((place ^ value_swap(row)) << 3)) * 2u, vb);
         }
-        if (lane == 0) here[buf][wave] = 0xFFFFu;
+        if ((what & kKeys) && lane == 0) here[buf][wave] = 0xFFFFu;
         return;
       }
       auto row_at = [&](int t) -> int64_t {
@@ -116,98 +123,175 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_kernel(Paged P,
         const int c = page_of(P.div, t), id = pages[c];
         return id >= 0 && id < P.n_pages ? id * P.page_stride + (int64_t)(t - c * P.div.page) * P.row_stride : -1;
       };
+      const uint16_t* zero = reinterpret_cast<const uint16_t*>(g_zero_row);
 #pragma unroll
       for (int k = 0; k < kLoads; ++k) {
         const int row = kPerLoad * k + load_row;
         const int64_t at = row_at(tw + row);
-        const uint16_t* zero = reinterpret_cast<const uint16_t*>(g_zero_row);
-        load_to_lds(kd + k * 1024, (at >= 0 ? Kh + at : zero) + ((place ^ key_swap(row)) << 3));
-        load_to_lds(vd + k * 1024, (at >= 0 ? Vh + at : zero) + ((place ^ value_swap(row)) << 3));
+        if (what & kKeys) load_to_lds(kd + k * 1024, (at >= 0 ? Kh + at : zero) + ((place ^ key_swap(row)) << 3));
+        if (what & kValues) load_to_lds(vd + k * 1024, (at >= 0 ? Vh + at : zero) + ((place ^ value_swap(row)) << 3));
       }
-      const uint32_t mine = (uint32_t)__ballot(row_at(tw + (lane & 15)) >= 0) & 0xFFFFu;
-      if (lane == 0) here[buf][wave] = mine;
+      if (what & kKeys) {
+        const uint32_t mine = (uint32_t)__ballot(row_at(tw + (lane & 15)) >= 0) & 0xFFFFu;
+        if (lane == 0) here[buf][wave] = mine;
+      }
     };
 
-    if (tile0 < t_end) request(tile0, 0, __builtin_amdgcn_readfirstlane(look_up(tile0)));
-    int page_id = __builtin_amdgcn_readfirstlane(look_up(tile0 + kTile));
-    int buf = 0;
-    for (int t0 = tile0; t0 < t_end; t0 += kTile, buf ^= 1) {
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      if (t0 + kTile < t_end) {
-        request(t0 + kTile, buf ^ 1, page_id);
-        page_id = __builtin_amdgcn_readfirstlane(look_up(t0 + 2 * kTile));     // (a tile ahead: its latency is not waited for)
-      }
-      if (t0 > pos_max || t0 + kTile <= low_min) continue;              // no row of this wave sees any of it
-      const char *kt = lds[buf][0], *vt = lds[buf][1];
-      const uint32_t there_lo = __builtin_amdgcn_readfirstlane(here[buf][0] | here[buf][1] << 16);
-      const uint32_t there_hi = __builtin_amdgcn_readfirstlane(here[buf][2] | here[buf][3] << 16);
-      const uint64_t there = (uint64_t)there_hi << 32 | there_lo;
-      v16f x[2];
-#pragma unroll
-      for (int tb = 0; tb < 2; ++tb) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[tb][e] = 0.f;
-#pragma unroll
-        for (int s = 0; s < kSteps; ++s) {
-          const v4u k = *reinterpret_cast<const v4u*>(kt + ((key_at ^ (s << 5)) + tb * 32 * kRowB));
-          x[tb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, k), q[s], x[tb], 0, 0, 0);
-        }
-      }
-      const bool whole = there == ~0ull && t0 + kTile - 1 <= pos_min && t0 >= low_all;
+    // The wave's pipeline, a step per 32 tokens (two steps a tile): while the weights of block j are worked out (vector ALUs), the matrix cores compute the
+    // logits of block j + 1 and add the values of block j - 1; the three do not depend on each other.  Keys run a block ahead and values a block behind, so
+    // tile t's second step needs the keys of tile t + 1 and the values of tile t, and one barrier a tile, before that step, is enough:
+    // behind it the keys of tile t and the values of tile t - 1 are done with, and their buffers take those of t + 2 and t + 1.
+    v16f x;                                                  // logits of block j, then of block j + 1
+    v8bf w[2];                                               // weights of block j - 1, then of block j
+    // masks block `at` (its first token) where not all of it is seen, and raises the reference where a logit calls for it
+    auto settle = [&](int at, int buf, int sub, float top) {
+      const uint32_t there = (uint32_t)__builtin_amdgcn_readfirstlane(here[buf][2 * sub] | here[buf][2 * sub + 1] << 16);
+      const bool whole = there == ~0u && at + 31 <= pos_min && at >= low_all;
       if (!whole) {
 #pragma unroll
-        for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int at = 32 * tb + 8 * (e >> 2) + 4 * half + (e & 3), t = t0 + at;
-            if (!((there >> at) & 1ull) || t > pos || t < low) x[tb][e] = -INFINITY;
-          }
+        for (int e = 0; e < 16; ++e) {
+          const int off = 8 * (e >> 2) + 4 * half + (e & 3), t = at + off;
+          if (!((there >> off) & 1u) || t > pos || t < low) x[e] = -INFINITY;
+        }
+        top = largest(x);
       }
-      float top = x[0][0];
-#pragma unroll
-      for (int tb = 0; tb < 2; ++tb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) top = fmaxf(top, x[tb][e]);
-      if (__any(top * P.scale_log2 > m + kRaise)) {
-        const float next = fmaxf(m, fmaxf(top, __shfl_xor(top, 32)) * P.scale_log2);
+      top *= P.scale_log2;
+      if (__any(top > m + kRaise)) {
+        // (a whole number: the weights in w, bf16 by now, are scaled without rounding)
+        const float next = fmaxf(m, ceilf(fmaxf(top, __shfl_xor(top, 32))));
         const float keep = next == -INFINITY ? 1.f : fast_exp2(m - next);
         m = next;
         l *= keep;
 #pragma unroll
         for (int c = 0; c < kBlocks; ++c) o[c] *= keep;
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w[s][e] = (__bf16)((float)w[s][e] * keep);
       }
+    };
+    auto key_of = [&](const char* kt, int sub, int s) {
+      return __builtin_bit_cast(v8bf, *reinterpret_cast<const v4u*>(kt + ((key_at ^ (s << 5)) + sub * 32 * kRowB)));
+    };
+    auto value_of = [&](const char* vt, int sub, int s, int c) {
+      v4s t[2];
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+        t[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(vt + ((value_at ^ (c << 6)) + (32 * sub + 16 * s + 8 * u) * kRowB)));
+      return __builtin_bit_cast(v8bf, __builtin_shufflevector(t[0], t[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    auto logits = [&](const char* kt, int sub) {
+      v16f y;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) y[e] = 0.f;
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_of(kt, sub, s), q[s], y, 0, 0, 0);
+      return y;
+    };
+    auto add_values = [&](const char* vt, int sub) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int c = 0; c < kBlocks; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value_of(vt, sub, s, c), w[s], o[c], 0, 0, 0);
+    };
+    auto weights = [&](v8bf (&to)[2]) {
       const float ref = m == -INFINITY ? 0.f : m;
-      v8bf w[4];
+      float sum = 0.f;
 #pragma unroll
-      for (int tb = 0; tb < 2; ++tb) {
-        float part_l = 0.f;
+      for (int s = 0; s < 2; ++s) {
+        float y[8];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          x[tb][e] = fast_exp2(fmaf(x[tb][e], P.scale_log2, -ref));
-          part_l += x[tb][e];
+        for (int e = 0; e < 8; ++e) {
+          y[e] = fast_exp2(fmaf(x[8 * s + e], P.scale_log2, -ref));
+          sum += y[e];
         }
-        l += part_l;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const v4u p = {pack_bf16(x[tb][8 * s], x[tb][8 * s + 1]), pack_bf16(x[tb][8 * s + 2], x[tb][8 * s + 3]),
-                         pack_bf16(x[tb][8 * s + 4], x[tb][8 * s + 5]), pack_bf16(x[tb][8 * s + 6], x[tb][8 * s + 7])};
-          w[2 * tb + s] = __builtin_bit_cast(v8bf, p);
-        }
+        const v4u p = {pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])};
+        to[s] = __builtin_bit_cast(v8bf, p);
       }
+      l += sum;
+    };
+    // One step: weights of block j, logits of block j + 1 (keys: buffer kbuf, half sub), values of block j - 1 (buffer vbuf).  Left to itself the compiler puts
+    // the three one after the other and waits for every read from LDS where it is used.  So the order is laid down: reads run kAhead products ahead,
+    // and behind every product stands its share of the vector work, which the products cover (a product takes the matrix core 32 clocks and the issue
+    // port 4).
+    auto step = [&](int kbuf, int vbuf, int sub, int next_at) {
+      constexpr int kProducts = kSteps + 2 * kBlocks, kAhead = 3;
+      const char *kt = lds[kbuf][0], *vt = lds[vbuf][1];
+      auto operand = [&](int i) { return i < kSteps ? key_of(kt, sub, i) : value_of(vt, sub, (i - kSteps) / kBlocks, (i - kSteps) % kBlocks); };
+      const float ref = m == -INFINITY ? 0.f : m;
+      v8bf f[kAhead + 1];
+      v4u now[2];
+      v16f y;
 #pragma unroll
-      for (int s = 0; s < 4; ++s)
+      for (int e = 0; e < 16; ++e) y[e] = 0.f;
+      float sum = 0.f, top = -INFINITY;
 #pragma unroll
-        for (int c = 0; c < kBlocks; ++c) {
-          v4s t[2];
+      for (int i = 0; i < kAhead; ++i) f[i] = operand(i);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            const char* p = vt + (16 * s + 8 * u + value_row) * kRowB + (((4 * c + value_piece) ^ value_swap(value_row + 8 * u)) << 4) + (lane & 1) * 8;
-            t[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(p));
-          }
-          const v8bf a = __builtin_bit_cast(v8bf, __builtin_shufflevector(t[0], t[1], 0, 1, 2, 3, 4, 5, 6, 7));
-          o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, w[s], o[c], 0, 0, 0);
+      for (int i = 0; i < kProducts; ++i) {
+        if (i + kAhead < kProducts) f[(i + kAhead) % (kAhead + 1)] = operand(i + kAhead);
+        const v8bf a = f[i % (kAhead + 1)];
+        if (i < kSteps) y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[i], y, 0, 0, 0);
+        else o[(i - kSteps) % kBlocks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, w[(i - kSteps) / kBlocks], o[(i - kSteps) % kBlocks], 0, 0, 0);
+        constexpr int kPairs = 8;                            // pairs of logits of block j
+#pragma unroll
+        for (int p = i * kPairs / kProducts; p < (i + 1) * kPairs / kProducts; ++p) {
+          const float e0 = fast_exp2(fmaf(x[2 * p], P.scale_log2, -ref)), e1 = fast_exp2(fmaf(x[2 * p + 1], P.scale_log2, -ref));
+          uint32_t packed = pack_bf16(e0, e1);
+          sum += e0 + e1;
+          asm volatile("" : "+v"(packed), "+v"(sum));
+          now[p / 4][p % 4] = packed;
         }
+        // block j + 1's largest logit, a few products behind its last one
+        constexpr int kFrom = kSteps + 1, kLeft = kProducts - kFrom;
+        if (i >= kFrom) {
+#pragma unroll
+          for (int e = (i - kFrom) * 16 / kLeft; e < (i - kFrom + 1) * 16 / kLeft; ++e) top = fmaxf(top, y[e]);
+          asm volatile("" : "+v"(top));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      l += sum;
+      w[0] = __builtin_bit_cast(v8bf, now[0]);
+      w[1] = __builtin_bit_cast(v8bf, now[1]);
+      x = y;
+      settle(next_at, kbuf, sub, top);
+    };
+
+    const int tiles = (t_end - tile0 + kTile - 1) / kTile;
+    if (tiles > 0) {
+      request(tile0, 0, kKeys | kValues, __builtin_amdgcn_readfirstlane(look_up(tile0)));
+      int id1 = __builtin_amdgcn_readfirstlane(look_up(tile0 + kTile)), id2 = __builtin_amdgcn_readfirstlane(look_up(tile0 + 2 * kTile));
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      if (tiles > 1) request(tile0 + kTile, 1, kKeys, id1);
+#pragma unroll
+      for (int s = 0; s < 2; ++s)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[s][e] = (__bf16)0.f;
+      x = logits(lds[0][0], 0);
+      settle(tile0, 0, 0, largest(x));
+      weights(w);
+      x = logits(lds[0][0], 1);
+      settle(tile0 + 32, 0, 1, largest(x));
+      for (int t = 0; t + 1 < tiles; ++t) {
+        const int at = tile0 + t * kTile, buf = t & 1;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        request(at + kTile, buf ^ 1, kValues, id1);
+        if (t + 2 < tiles) request(at + 2 * kTile, buf, kKeys, id2);
+        id1 = id2;
+        id2 = __builtin_amdgcn_readfirstlane(look_up(at + 3 * kTile));        // (used a tile later: its latency is not waited for)
+        step(buf ^ 1, buf, 0, at + kTile);
+        step(buf ^ 1, buf, 1, at + kTile + 32);
+      }
+      const char* vt = lds[(tiles - 1) & 1][1];
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      add_values(vt, 0);
+      weights(w);
+      add_values(vt, 1);
     }
 
     l += __shfl_xor(l, 32);
