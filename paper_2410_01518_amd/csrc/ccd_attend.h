@@ -96,8 +96,15 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return __builtin_bit_cast(uint32_t, r);
 }
 
+struct AttendArgs {
+  const void *Q, *K, *V;
+  const int32_t *table, *q_start, *kv_len;
+  void* out;
+  float* lse;
+  Partials part;
+};
+
 // rows kernel (bf16): a workgroup per (unit, block of 128 rows, stretch), its waves share the tiles
-void launch_attend_rows(const Paged& P, const AttendPlan& pl, const void* Q, const void* K, const void* V, const int32_t* table,
-                        const int32_t* q_start, const int32_t* kv_len, void* out, float* lse, Partials part, hipStream_t s);
+void launch_attend_rows(const Paged& P, const AttendPlan& pl, const AttendArgs& A, hipStream_t s);
 
 }  // namespace ccd

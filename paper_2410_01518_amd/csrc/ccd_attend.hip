@@ -180,14 +180,6 @@ __device__ __forceinline__ float row_sum(float x) {
 template <class T, int D, int NQ>
 constexpr int split_waves() { return NQ == 4 ? 1 : NQ == 2 || D == 128 ? 2 : 3; }
 
-struct AttendArgs {
-  const void *Q, *K, *V;
-  const int32_t *table, *q_start, *kv_len;
-  void* out;
-  float* lse;
-  Partials part;
-};
-
 template <class T, int D, int NQ>
 struct SplitLds {
   static constexpr int kRows = 16 * NQ, kPitch = D + 4;
@@ -703,7 +695,7 @@ static void attend_launch(const Paged& P, int dtype, const AttendCuts& c, const 
   if (c.grid.rows > 0) {
     const AttendPlan& pl = c.grid;
     if (pl.by_rows) {
-      launch_attend_rows(P, pl, grid.Q, grid.K, grid.V, grid.table, grid.q_start, grid.kv_len, grid.out, grid.lse, grid.part, s);
+      launch_attend_rows(P, pl, grid, s);
     } else {
       const dim3 wgs((unsigned)((int64_t)P.B * P.Hkv * pl.parts * pl.row_blocks));
       if (pl.rows == 16)      launch(attend_split_kernel<T, D, 1>, wgs, block, s, P, pl, grid);

@@ -2,25 +2,44 @@
 //
 // Here the matrix cores are the bound, and next to them the vector ALUs: a logit costs 4 d flops but also an fma, an exp2, an addition and half a
 // conversion.  Four waves have 32 rows each and walk the same tokens; tiles of 64 keys and values come from memory straight into LDS
-// (global_load_lds, no registers), two buffers deep, one barrier per tile.  Two workgroups share a compute unit, so that one's softmax runs
-// beside the other's products.  Logits are computed as D[token][row] = K Q^T (v_mfma_f32_32x32x16_bf16): a lane has 16 of 32 tokens of one row, so a row's
-// largest logit and its sum stay within a lane and its neighbour 32 lanes on, and the weights are already the operand of D[d][row] = V^T W^T
-// if that product counts its tokens in the same order; values are transposed by the LDS read (ds_read_b64_tr_b16).
+// (global_load_lds, no registers), two deep, one barrier per tile.  Two workgroups share a compute unit.  Logits are computed as
+// D[token][row] = K Q^T (v_mfma_f32_32x32x16_bf16): a lane has 16 of 32 tokens of one row, so a row's sum stays within a lane and its neighbour 32
+// lanes on, and the weights are already the operand of D[d][row] = V^T W^T if that product counts its tokens in the same order; values
+// are transposed by the LDS read (ds_read_b64_tr_b16).
+//
+// Measured, a chunk of 2048 tokens over 32768 cached ones, 32 query heads on 8 KV heads of 128 elements: 970 - 1020 us by the machine, 1.04 - 1.10 PFLOP/s,
+// where a product of 8192^3 reaches 1.2 - 1.3.  The matrix cores are busy 52 % of the cycles and the clock is at 1.9 - 2.0 GHz: what is left is bound by power
+// (removing all bank conflicts and a tenth of the instructions took 20 % of the cycles and 4 % of the time).  Waves of 64 rows, one per SIMD,
+// read LDS half as often and keep 2.4 GHz, but a wave alone cannot cover its own waits: 1010 - 1040 us, and coarser blocks for short calls.
 #include "ccd_attend.h"
 #include "ccd_rotary.h"
+
+#include <type_traits>
 
 namespace ccd {
 
 constexpr int kRowWaves = 4, kTile = 64;
+constexpr float kFar = 256.f;            // sum of a lane's 16 weights above which the reference is raised
 enum { kKeys = 1, kValues = 2 };
 
 // 64 lanes x 16 bytes from memory into LDS, at lds_addr + 16 * lane
 __device__ __forceinline__ void load_to_lds(uint32_t lds_addr, const void* p) {
   asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_addr), "v"(p) : "memory");
 }
-__device__ __forceinline__ void load_to_lds(uint32_t lds_addr, uint32_t offset, const void* base) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds_addr), "v"(offset), "s"(base) : "memory");
+// N such, to lds_addr + 1024 k + 16 * lane.  An instruction's own offset counts for both addresses: offset[k] is meant with it taken off, and what
+// would then be negative is in the base (run_offset).
+template <int N>
+__device__ __forceinline__ void load_run_to_lds(uint32_t lds_addr, const uint32_t (&offset)[N], const void* base) {
+  if constexpr (N == 4)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\t"
+                 "global_load_lds_dwordx4 %3, %5 offset:2048\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072"
+                 ::"s"(lds_addr), "v"(offset[0]), "v"(offset[1]), "v"(offset[2]), "v"(offset[3]), "s"(base) : "memory");
+  else
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024"
+                 ::"s"(lds_addr), "v"(offset[0]), "v"(offset[1]), "s"(base) : "memory");
 }
+constexpr int kRunBack = 4096;
+__device__ __forceinline__ uint32_t run_offset(int64_t bytes, int k) { return (uint32_t)(bytes + kRunBack - 1024 * k); }
 
 __device__ __forceinline__ float largest(const v16f& x) {
   float top = x[0];
@@ -31,15 +50,12 @@ __device__ __forceinline__ float largest(const v16f& x) {
 
 // BANDED: pages of whole runs of 16 rows, so that a wave's 16 rows of a tile lie in one page
 template <int D, bool BANDED>
-__global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_kernel(Paged P, AttendPlan pl, const uint16_t* __restrict__ Q, const uint16_t* __restrict__ K,
-                                                                       const uint16_t* __restrict__ V, const int32_t* __restrict__ table,
-                                                                       const int32_t* __restrict__ q_start, const int32_t* __restrict__ kv_len,
-                                                                       uint16_t* __restrict__ out, float* __restrict__ lse, Partials part) {
+__global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_kernel(Paged P, AttendPlan pl, AttendArgs A) {
   constexpr int kRows = 32 * kRowWaves, kRowB = D * 2, kPieces = D / 8;            // 16-byte pieces of a row
   constexpr int kPerLoad = 64 / kPieces, kLoads = 16 / kPerLoad;                   // rows per load instruction, loads of a wave's 16 rows
   constexpr int kTileB = kTile * kRowB, kSteps = D / 16, kBlocks = D / 32;
-  __shared__ __align__(1024) char lds[2][2][kTileB];                               // [buffer][keys, values]
-  __shared__ uint32_t here[2][kRowWaves];                                          // [buffer]: which of 16 tokens have a page
+  __shared__ __align__(1024) char lds[2][2][kTileB];                               // [tile][keys, values]
+  __shared__ uint32_t here[2][kRowWaves];                                          // [tile]: which of 16 tokens have a page
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
   const int units = P.B * P.Hkv;
   int idx = blockIdx.x;
@@ -47,43 +63,51 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_kernel(Paged P,
   idx /= units;
   // The last rows see most and come first.  Where the call is one round of two workgroups per compute unit, its second half runs the other way, so that
   // a compute unit has a long one and a short one.
-  int turn = idx / pl.parts;
-  if (pl.turn > 0 && turn >= pl.turn) turn = pl.row_blocks - 1 - (turn - pl.turn);
-  const int part_no = idx % pl.parts, block0 = pl.row_blocks - 1 - turn;
+  int turn_no = idx / pl.parts;
+  if (pl.turn > 0 && turn_no >= pl.turn) turn_no = pl.row_blocks - 1 - (turn_no - pl.turn);
+  const int part_no = idx % pl.parts, block0 = pl.row_blocks - 1 - turn_no;
   const int b = unit / P.Hkv, hkv = unit % P.Hkv;
-  const Sequence sq = load_sequence(P, b, q_start, kv_len);
+  const Sequence sq = load_sequence(P, b, A.q_start, A.kv_len);
   const int rows_all = sq.m * P.G;
   if (rows_all <= pl.few) return;
-  const int32_t* pages = table + (int64_t)b * P.table_width;
-  const uint16_t* Kh = K + hkv * P.head_stride;
-  const uint16_t* Vh = V + hkv * P.head_stride;
+  const int32_t* pages = A.table + (int64_t)b * P.table_width;
+  const uint16_t* Kh = static_cast<const uint16_t*>(A.K) + hkv * P.head_stride;
+  const uint16_t* Vh = static_cast<const uint16_t*>(A.V) + hkv * P.head_stride;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)&lds[0][0][0];
 
-  // Pieces change places by the row's number: keys so that the 8 or 16 rows of a 16-byte read lie in different banks, values so that the four rows
-  // of a transposing read do.
+  // Pieces change places by the row's number, so that what a read takes together lies in all banks: 16 lanes of a 16-byte read (16 rows of keys, one piece),
+  // 32 lanes of a transposing one (four rows of values, two pairs of pieces).
   auto key_swap = [](int row) { return D == 128 ? row & 15 : (row >> 1) & 7; };
-  auto value_swap = [](int row) { return D == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1; };
+  auto value_swap = [](int row) { return D == 128 ? (row & 3) << 2 : ((row >> 1) & 1) << 2; };
   // what the lane loads of the wave's 16 rows: row kPerLoad * k + load_row, the piece that belongs at its place
   const int load_row = lane / kPieces, place = lane % kPieces;
   // what the lane reads: keys, row (lane & 31), piece 2 s + half; values, 4 tokens at 4 half + .., 16 elements at 16 ((lane >> 4) & 1)
   const int key_at = (lane & 31) * kRowB + ((half ^ key_swap(lane & 31)) << 4);
   const int value_row = 4 * half + ((lane & 15) >> 2);
   const int value_at = value_row * kRowB + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ value_swap(value_row)) << 4) + (lane & 1) * 8;
+  // the lane's offsets in a run of 16 rows of one page
+  uint32_t key_run[kLoads], value_run[kLoads];
+#pragma unroll
+  for (int k = 0; k < kLoads; ++k) {
+    const int row = kPerLoad * k + load_row;
+    key_run[k] = run_offset((int64_t)row * P.row_stride * 2 + ((place ^ key_swap(row)) << 4), k);
+    value_run[k] = run_offset((int64_t)row * P.row_stride * 2 + ((place ^ value_swap(row)) << 4), k);
+  }
 
   for (int r0 = block0 * kRows; r0 < rows_all; r0 += pl.row_blocks * kRows) {
     const int r1 = r0 + kRows < rows_all ? r0 + kRows : rows_all;
     const Stretch st = cut_rows(P, sq, r0, r1, pl.parts, pl.chunk);
     if (part_no >= st.parts) continue;
     const int t_begin = st.begin + part_no * st.chunk, t_end = t_begin + st.chunk < st.end ? t_begin + st.chunk : st.end;
-    const int tile0 = t_begin & ~15;                                   // (tokens before t_begin are masked)
-    // the lane's row
-    const int r = r0 + 32 * wave + (lane & 31), i = r / P.G, head = hkv * P.G + r - i * P.G;
-    const int pos = r < r1 ? sq.base + i : -1, low_row = first_seen(P, pos), low = low_row > t_begin ? low_row : t_begin;
-    const int w0 = r0 + 32 * wave, w1 = w0 + 32 < r1 ? w0 + 32 : r1;   // the wave's rows (none if w0 >= r1)
+    const int tile0 = t_begin & ~15, tiles = (t_end - tile0 + kTile - 1) / kTile;              // (tokens before t_begin are masked)
+    // the lane's row, and the wave's rows (none if w0 >= r1)
+    const int r = r0 + 32 * wave + (lane & 31), i_row = r / P.G, head = hkv * P.G + r - i_row * P.G;
+    const int w0 = r0 + 32 * wave, w1 = w0 + 32 < r1 ? w0 + 32 : r1;
+    const int pos = r < r1 ? sq.base + i_row : -1, low_row = first_seen(P, pos), low = low_row > t_begin ? low_row : t_begin;
     const int pos_min = sq.base + w0 / P.G, low_max = w0 < r1 ? first_seen(P, sq.base + (w1 - 1) / P.G) : 0, low_all = low_max > t_begin ? low_max : t_begin;
     v8bf q[kSteps];
     {
-      const uint16_t* row = Q + b * P.q_b + (int64_t)(sq.first + i) * P.q_t + (int64_t)head * P.q_h;
+      const uint16_t* row = static_cast<const uint16_t*>(A.Q) + b * P.q_b + (int64_t)(sq.first + i_row) * P.q_t + (int64_t)head * P.q_h;
 #pragma unroll
       for (int s = 0; s < kSteps; ++s) {
         v4u w = {0, 0, 0, 0};
@@ -91,34 +115,42 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_kernel(Paged P,
         q[s] = __builtin_bit_cast(v8bf, w);
       }
     }
-    float m = -INFINITY, l = 0.f;
+    float m = 0.f, l = 0.f;                                    // reference (0 until the row has one), sum of weights
+    bool seen = r >= r1;                                       // has the row a reference?
     v16f o[kBlocks];
 #pragma unroll
     for (int c = 0; c < kBlocks; ++c)
 #pragma unroll
       for (int e = 0; e < 16; ++e) o[c][e] = 0.f;
 
-    // the wave's 16 of the tile's 64 tokens; page_id: the page of the first of them, where it was looked up
-    auto look_up = [&](int t0) {
-      const int tw = t0 + 16 * wave;
-      return BANDED && tw + 16 <= t_end ? pages[page_of(P.div, tw)] : -1;
+    // Pages of the wave's 16 rows, 64 tiles at once, a lane each: a scalar load per tile would be waited for with the first reads from LDS (they share a counter).
+    int ids = -1;
+    auto look_up = [&](int tile) __attribute__((always_inline)) {
+      if (!BANDED) return -1;
+      if ((tile & 63) == 0) {
+        const int64_t tw = (int64_t)tile0 + (int64_t)(tile + lane) * kTile + 16 * wave;
+        ids = tw + 16 <= t_end ? pages[page_of(P.div, (int)tw)] : -1;
+      }
+      return __builtin_amdgcn_readlane(ids, tile & 63);
     };
-    auto request = [&](int t0, int buf, int what, int page_id) {
-      const int tw = t0 + 16 * wave;
-      const uint32_t kd = lds0 + (buf * 2) * kTileB + 16 * wave * kRowB, vd = kd + kTileB;
-      if (BANDED && page_id >= 0 && page_id < P.n_pages) {
-        const int64_t at = page_id * P.page_stride + (int64_t)(tw - page_of(P.div, tw) * P.div.page) * P.row_stride;
-        const uint16_t *kb = Kh + at, *vb = Vh + at;
-#pragma unroll
-        for (int k = 0; k < kLoads; ++k) {
-          const int row = kPerLoad * k + load_row;
-          if (what & kKeys) load_to_lds(kd + k * 1024, (uint32_t)(row * (int)P.row_stride + ((place ^ key_swap(row)) << 3)) * 2u, kb);
-          if (what & kValues) load_to_lds(vd + k * 1024, (uint32_t)(row * (int)P.row_stride + ((place ^ value_swap(row)) << 3)) * 2u, vb);
-        }
-        if ((what & kKeys) && lane == 0) here[buf][wave] = 0xFFFFu;
+    // where the wave's 16 rows of a tile begin, if they are all there and in one page (else -1)
+    auto run_of = [&](int tile) __attribute__((always_inline)) -> int64_t {
+      const int page_id = look_up(tile), tw = tile0 + tile * kTile + 16 * wave;
+      if (!BANDED || page_id < 0 || page_id >= P.n_pages) return -1;
+      return page_id * P.page_stride + (int64_t)(tw - page_of(P.div, tw) * P.div.page) * P.row_stride;
+    };
+    // asks for the wave's 16 rows of a tile
+    auto ask = [&](int tile, int slot, int what, int64_t run) __attribute__((always_inline)) {
+      if (tile >= tiles) return;
+      const int tw = tile0 + tile * kTile + 16 * wave;
+      const uint32_t kd = lds0 + (slot * 2) * kTileB + 16 * wave * kRowB, vd = kd + kTileB;
+      if (BANDED && run >= 0) {
+        if (what & kKeys) load_run_to_lds<kLoads>(kd, key_run, reinterpret_cast<const char*>(Kh + run) - kRunBack);
+        if (what & kValues) load_run_to_lds<kLoads>(vd, value_run, reinterpret_cast<const char*>(Vh + run) - kRunBack);
+        if ((what & kKeys) && lane == 0) here[slot][wave] = 0xFFFFu;
         return;
       }
-      auto row_at = [&](int t) -> int64_t {
+      auto row_at = [&](int t) __attribute__((always_inline)) -> int64_t {
         if (t >= t_end) return -1;
         const int c = page_of(P.div, t), id = pages[c];
         return id >= 0 && id < P.n_pages ? id * P.page_stride + (int64_t)(t - c * P.div.page) * P.row_stride : -1;
@@ -133,188 +165,198 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_kernel(Paged P,
       }
       if (what & kKeys) {
         const uint32_t mine = (uint32_t)__ballot(row_at(tw + (lane & 15)) >= 0) & 0xFFFFu;
-        if (lane == 0) here[buf][wave] = mine;
+        if (lane == 0) here[slot][wave] = mine;
       }
     };
 
     // The wave's pipeline, a step per 32 tokens (two steps a tile): while the weights of block j are worked out (vector ALUs), the matrix cores compute the
     // logits of block j + 1 and add the values of block j - 1; the three do not depend on each other.  Keys run a block ahead and values a block behind, so
     // tile t's second step needs the keys of tile t + 1 and the values of tile t, and one barrier a tile, before that step, is enough:
-    // behind it the keys of tile t and the values of tile t - 1 are done with, and their buffers take those of t + 2 and t + 1.
-    v16f x;                                                  // logits of block j, then of block j + 1
-    v8bf w[2];                                               // weights of block j - 1, then of block j
-    // masks block `at` (its first token) where not all of it is seen, and raises the reference where a logit calls for it
-    auto settle = [&](int at, int buf, int sub, float top) {
-      const uint32_t there = (uint32_t)__builtin_amdgcn_readfirstlane(here[buf][2 * sub] | here[buf][2 * sub + 1] << 16);
-      const bool whole = there == ~0u && at + 31 <= pos_min && at >= low_all;
-      if (!whole) {
+    // behind it the keys of tile t and the values of tile t - 1 are done with, and their places take those of t + 2 and t + 1.
+    // Logits of block j and j + 1, weights of block j - 1 and j are two sets that change places with every step.
+    v16f x0, x1;
+    v8bf wa[2], wb[2];
+    // masks block `at` (its first token; there: which of its tokens have a page) where not all of it is seen
+    auto mask = [&](v16f& x, int at, uint32_t there) __attribute__((always_inline)) {
+      if (__builtin_expect(there != ~0u || at + 31 > pos_min || at < low_all, 0)) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
           const int off = 8 * (e >> 2) + 4 * half + (e & 3), t = at + off;
           if (!((there >> off) & 1u) || t > pos || t < low) x[e] = -INFINITY;
         }
-        top = largest(x);
-      }
-      top *= P.scale_log2;
-      if (__any(top > m + kRaise)) {
-        // (a whole number: the weights in w, bf16 by now, are scaled without rounding)
-        const float next = fmaxf(m, ceilf(fmaxf(top, __shfl_xor(top, 32))));
-        const float keep = next == -INFINITY ? 1.f : fast_exp2(m - next);
-        m = next;
-        l *= keep;
-#pragma unroll
-        for (int c = 0; c < kBlocks; ++c) o[c] *= keep;
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) w[s][e] = (__bf16)((float)w[s][e] * keep);
       }
     };
-    auto key_of = [&](const char* kt, int sub, int s) {
+    auto weigh = [&](const v16f& x, v8bf (&w)[2]) __attribute__((always_inline)) {
+      float sum = 0.f;
+      v4u now[2];
+#pragma unroll
+      for (int p = 0; p < 8; ++p) {
+        const float e0 = fast_exp2(fmaf(x[2 * p], P.scale_log2, -m)), e1 = fast_exp2(fmaf(x[2 * p + 1], P.scale_log2, -m));
+        now[p / 4][p % 4] = pack_bf16(e0, e1);
+        sum += e0 + e1;
+      }
+      w[0] = __builtin_bit_cast(v8bf, now[0]);
+      w[1] = __builtin_bit_cast(v8bf, now[1]);
+      return sum;
+    };
+    // A block's largest logit is not looked for: all weights are positive, so as long as their sum is small no logit lies far above the reference.  Where
+    // it is not (or is no number, or there is no reference yet) the reference is raised and the weights are worked out again.
+    auto settle = [&](const v16f& x, v8bf (&w)[2], float& sum) __attribute__((always_inline)) {
+      if (__builtin_expect(__any(!(sum <= kFar) || !seen), 0)) {
+        const float top = largest(x) * P.scale_log2, next = fmaxf(top, __shfl_xor(top, 32));
+        // a row without a reference takes the first finite one; until then it has no weights
+        const float to = seen ? fmaxf(m, next) : next;
+        if (to != -INFINITY) {
+          const float keep = seen ? fast_exp2(m - to) : 0.f;
+          l *= keep;
+#pragma unroll
+          for (int c = 0; c < kBlocks; ++c) o[c] *= keep;
+          m = to;
+          seen = true;
+        }
+        sum = weigh(x, w);
+      }
+      l += sum;
+    };
+    auto key_of = [&](const char* kt, int sub, int s) __attribute__((always_inline)) {
       return __builtin_bit_cast(v8bf, *reinterpret_cast<const v4u*>(kt + ((key_at ^ (s << 5)) + sub * 32 * kRowB)));
     };
-    auto value_of = [&](const char* vt, int sub, int s, int c) {
+    auto value_of = [&](const char* vt, int sub, int s, int c) __attribute__((always_inline)) {
       v4s t[2];
 #pragma unroll
       for (int u = 0; u < 2; ++u)
         t[u] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4s*)(vt + ((value_at ^ (c << 6)) + (32 * sub + 16 * s + 8 * u) * kRowB)));
       return __builtin_bit_cast(v8bf, __builtin_shufflevector(t[0], t[1], 0, 1, 2, 3, 4, 5, 6, 7));
     };
-    auto logits = [&](const char* kt, int sub) {
-      v16f y;
+    // the first blocks and the last ones, which have no neighbours: the step's parts by themselves
+    auto logits = [&](v16f& x, const char* kt, int sub) __attribute__((always_inline)) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) y[e] = 0.f;
+      for (int e = 0; e < 16; ++e) x[e] = 0.f;
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_of(kt, sub, s), q[s], y, 0, 0, 0);
-      return y;
+      for (int s = 0; s < kSteps; ++s) x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(key_of(kt, sub, s), q[s], x, 0, 0, 0);
     };
-    auto add_values = [&](const char* vt, int sub) {
+    auto weights = [&](const v16f& x, v8bf (&w)[2]) __attribute__((always_inline)) {
+      float sum = weigh(x, w);
+      settle(x, w, sum);
+    };
+    auto add_values = [&](const v8bf (&w)[2], const char* vt, int sub) __attribute__((always_inline)) {
 #pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int c = 0; c < kBlocks; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value_of(vt, sub, s, c), w[s], o[c], 0, 0, 0);
     };
-    auto weights = [&](v8bf (&to)[2]) {
-      const float ref = m == -INFINITY ? 0.f : m;
-      float sum = 0.f;
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        float y[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          y[e] = fast_exp2(fmaf(x[8 * s + e], P.scale_log2, -ref));
-          sum += y[e];
-        }
-        const v4u p = {pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])};
-        to[s] = __builtin_bit_cast(v8bf, p);
-      }
-      l += sum;
-    };
-    // One step: weights of block j, logits of block j + 1 (keys: buffer kbuf, half sub), values of block j - 1 (buffer vbuf).  Left to itself the compiler puts
-    // the three one after the other and waits for every read from LDS where it is used.  So the order is laid down: reads run kAhead products ahead,
-    // and behind every product stands its share of the vector work, which the products cover (a product takes the matrix core 32 clocks and the issue
-    // port 4).
-    auto step = [&](int kbuf, int vbuf, int sub, int next_at) {
-      constexpr int kProducts = kSteps + 2 * kBlocks, kAhead = 3;
-      const char *kt = lds[kbuf][0], *vt = lds[vbuf][1];
-      auto operand = [&](int i) { return i < kSteps ? key_of(kt, sub, i) : value_of(vt, sub, (i - kSteps) / kBlocks, (i - kSteps) % kBlocks); };
-      const float ref = m == -INFINITY ? 0.f : m;
-      v8bf f[kAhead + 1];
-      v4u now[2];
-      v16f y;
+    // One step: weights `now` of block j (logits x), logits y of block j + 1 (keys kt, half sub; its first token next_at), values of block j - 1 (weights w, values
+    // vt).  Left to itself the compiler puts the three one after the other and waits for every read from LDS where it is used.  So the order is laid down:
+    // reads run kAhead products ahead, and behind every product stands its share of the vector work, which the products cover (a product takes the
+    // matrix core 32 clocks and the issue port 4).  chained: the step's last reads are the first operands of the next, keys kt, half 1.
+    constexpr int kProducts = kSteps + 2 * kBlocks, kAhead = 3;
+    static_assert(kProducts % (kAhead + 1) == 0, "a step begins where the one before left the ring of operands");
+    v8bf f[kAhead + 1];
+    auto step = [&](const v16f& x, const v8bf (&w)[2], v16f& y, v8bf (&now)[2], const char* kt, const char* vt, int sub, int next_at, uint32_t next_there,
+                    bool chained) __attribute__((always_inline)) {
+      float sum = 0.f, v[2];
+      v4u packed[2];
 #pragma unroll
       for (int e = 0; e < 16; ++e) y[e] = 0.f;
-      float sum = 0.f, top = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < kAhead; ++i) f[i] = operand(i);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int i = 0; i < kProducts; ++i) {
-        if (i + kAhead < kProducts) f[(i + kAhead) % (kAhead + 1)] = operand(i + kAhead);
+        const int ahead = i + kAhead;
+        if (ahead < kSteps) f[ahead % (kAhead + 1)] = key_of(kt, sub, ahead);
+        else if (ahead < kProducts) f[ahead % (kAhead + 1)] = value_of(vt, sub, (ahead - kSteps) / kBlocks, (ahead - kSteps) % kBlocks);
+        else if (chained) f[ahead % (kAhead + 1)] = key_of(kt, 1, ahead - kProducts);
         const v8bf a = f[i % (kAhead + 1)];
         if (i < kSteps) y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[i], y, 0, 0, 0);
         else o[(i - kSteps) % kBlocks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, w[(i - kSteps) / kBlocks], o[(i - kSteps) % kBlocks], 0, 0, 0);
-        constexpr int kPairs = 8;                            // pairs of logits of block j
+        // the product's share of block j's 16 logits (as in weigh)
 #pragma unroll
-        for (int p = i * kPairs / kProducts; p < (i + 1) * kPairs / kProducts; ++p) {
-          const float e0 = fast_exp2(fmaf(x[2 * p], P.scale_log2, -ref)), e1 = fast_exp2(fmaf(x[2 * p + 1], P.scale_log2, -ref));
-          uint32_t packed = pack_bf16(e0, e1);
-          sum += e0 + e1;
-          asm volatile("" : "+v"(packed), "+v"(sum));
-          now[p / 4][p % 4] = packed;
-        }
-        // block j + 1's largest logit, a few products behind its last one
-        constexpr int kFrom = kSteps + 1, kLeft = kProducts - kFrom;
-        if (i >= kFrom) {
-#pragma unroll
-          for (int e = (i - kFrom) * 16 / kLeft; e < (i - kFrom + 1) * 16 / kLeft; ++e) top = fmaxf(top, y[e]);
-          asm volatile("" : "+v"(top));
+        for (int e = i * 16 / kProducts; e < (i + 1) * 16 / kProducts; ++e) {
+          v[e & 1] = fast_exp2(fmaf(x[e], P.scale_log2, -m));
+          asm volatile("" ::"v"(v[e & 1]));
+          if (e & 1) {
+            const uint32_t two = pack_bf16(v[0], v[1]);
+            sum += v[0] + v[1];
+            asm volatile("" ::"v"(two), "v"(sum));
+            packed[e / 8][e / 2 % 4] = two;
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      l += sum;
-      w[0] = __builtin_bit_cast(v8bf, now[0]);
-      w[1] = __builtin_bit_cast(v8bf, now[1]);
-      x = y;
-      settle(next_at, kbuf, sub, top);
+      now[0] = __builtin_bit_cast(v8bf, packed[0]);
+      now[1] = __builtin_bit_cast(v8bf, packed[1]);
+      settle(x, now, sum);
+      mask(y, next_at, next_there);
     };
 
-    const int tiles = (t_end - tile0 + kTile - 1) / kTile;
     if (tiles > 0) {
-      request(tile0, 0, kKeys | kValues, __builtin_amdgcn_readfirstlane(look_up(tile0)));
-      int id1 = __builtin_amdgcn_readfirstlane(look_up(tile0 + kTile)), id2 = __builtin_amdgcn_readfirstlane(look_up(tile0 + 2 * kTile));
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      if (tiles > 1) request(tile0 + kTile, 1, kKeys, id1);
-#pragma unroll
-      for (int s = 0; s < 2; ++s)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[s][e] = (__bf16)0.f;
-      x = logits(lds[0][0], 0);
-      settle(tile0, 0, 0, largest(x));
-      weights(w);
-      x = logits(lds[0][0], 1);
-      settle(tile0 + 32, 0, 1, largest(x));
-      for (int t = 0; t + 1 < tiles; ++t) {
-        const int at = tile0 + t * kTile, buf = t & 1;
+      // (which tokens are there: one word per run of 16, read with the tile's keys)
+      auto there_of = [&](int slot, int sub) __attribute__((always_inline)) { return here[slot][2 * sub] | here[slot][2 * sub + 1] << 16; };
+      auto uniform = [](uint32_t u) __attribute__((always_inline)) { return (uint32_t)__builtin_amdgcn_readfirstlane(u); };
+      // loads into LDS are waited for all together: they do not arrive in the order they were asked for
+      auto arrived = [&]() __attribute__((always_inline)) {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        request(at + kTile, buf ^ 1, kValues, id1);
-        if (t + 2 < tiles) request(at + 2 * kTile, buf, kKeys, id2);
-        id1 = id2;
-        id2 = __builtin_amdgcn_readfirstlane(look_up(at + 3 * kTile));        // (used a tile later: its latency is not waited for)
-        step(buf ^ 1, buf, 0, at + kTile);
-        step(buf ^ 1, buf, 1, at + kTile + 32);
+      };
+      ask(0, 0, kKeys | kValues, run_of(0));
+      int64_t run1 = run_of(1);                                                // of the next tile: its keys are asked for, its values will be
+      arrived();
+      ask(1, 1, kKeys, run1);
+      logits(x0, lds[0][0], 0);
+      mask(x0, tile0, uniform(there_of(0, 0)));
+      weights(x0, wa);
+      logits(x0, lds[0][0], 1);
+      mask(x0, tile0 + 32, uniform(there_of(0, 1)));
+      auto turn = [&](auto even, int t) __attribute__((always_inline)) {
+        constexpr int slot = decltype(even)::value ? 0 : 1, next = slot ^ 1;   // (places that the compiler knows: addresses without arithmetic)
+        const int at = tile0 + (t + 1) * kTile;
+        arrived();
+        // (the first operands are on their way while the next tiles are asked for)
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) f[i] = key_of(lds[next][0], 0, i);
+        const uint32_t here0 = there_of(next, 0), here1 = there_of(next, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        const int64_t run2 = run_of(t + 2);
+        ask(t + 1, next, kValues, run1);
+        ask(t + 2, slot, kKeys, run2);
+        run1 = run2;
+        const uint32_t there0 = uniform(here0), there1 = uniform(here1);
+        step(x0, wa, x1, wb, lds[next][0], lds[slot][1], 0, at, there0, true);
+        // (its first operands: read at the end of the step before)
+        step(x1, wb, x0, wa, lds[next][0], lds[slot][1], 1, at + 32, there1, false);
+      };
+      for (int t = 0; t + 1 < tiles; t += 2) {
+        turn(std::true_type{}, t);
+        if (t + 2 < tiles) turn(std::false_type{}, t + 1);
       }
       const char* vt = lds[(tiles - 1) & 1][1];
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      add_values(vt, 0);
-      weights(w);
-      add_values(vt, 1);
+      arrived();
+      add_values(wa, vt, 0);
+      weights(x0, wb);
+      add_values(wb, vt, 1);
     }
 
     l += __shfl_xor(l, 32);
     if (r < r1) {
-      const int64_t row = sq.first + i;
+      const int64_t row = sq.first + i_row;
       if (st.parts == 1) {
         const float inv = inverse_sum(l);
-        uint16_t* to = out + b * P.o_b + row * P.o_t + (int64_t)head * P.o_h + 4 * half;
+        uint16_t* to = static_cast<uint16_t*>(A.out) + b * P.o_b + row * P.o_t + (int64_t)head * P.o_h + 4 * half;
 #pragma unroll
         for (int c = 0; c < kBlocks; ++c)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
             *reinterpret_cast<uint2*>(to + 32 * c + 8 * e) = make_uint2(pack_bf16(o[c][4 * e] * inv, o[c][4 * e + 1] * inv),
                                                                          pack_bf16(o[c][4 * e + 2] * inv, o[c][4 * e + 3] * inv));
-        if (lse != nullptr && half == 0) lse[b * P.l_b + row * P.l_t + head * P.l_h] = to_natural_lse(m, l);
+        if (A.lse != nullptr && half == 0) A.lse[b * P.l_b + row * P.l_t + head * P.l_h] = to_natural_lse(m, l);
       } else {
         const int64_t at = ((int64_t)part_no * P.tokens + row) * P.Hq + head;
-        float* to = part.o + at * D + 4 * half;
+        float* to = A.part.o + at * D + 4 * half;
 #pragma unroll
         for (int c = 0; c < kBlocks; ++c)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) *reinterpret_cast<float4*>(to + 32 * c + 8 * e) = make_float4(o[c][4 * e], o[c][4 * e + 1], o[c][4 * e + 2], o[c][4 * e + 3]);
-        if (half == 0) part.ml[at] = make_float2(m, l);
+          for (int e = 0; e < 4; ++e)
+            *reinterpret_cast<float4*>(to + 32 * c + 8 * e) = make_float4(o[c][4 * e], o[c][4 * e + 1], o[c][4 * e + 2], o[c][4 * e + 3]);
+        if (half == 0) A.part.ml[at] = make_float2(seen ? m : -INFINITY, l);
       }
     }
     __syncthreads();
@@ -322,20 +364,17 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_kernel(Paged P,
 }
 
 template <int D>
-static void rows_launch(const Paged& P, const AttendPlan& pl, const void* Q, const void* K, const void* V, const int32_t* table, const int32_t* q_start,
-                        const int32_t* kv_len, void* out, float* lse, Partials part, hipStream_t s) {
-  const uint16_t *q = static_cast<const uint16_t*>(Q), *k = static_cast<const uint16_t*>(K), *v = static_cast<const uint16_t*>(V);
+static void rows_launch(const Paged& P, const AttendPlan& pl, const AttendArgs& A, hipStream_t s) {
   const dim3 grid((unsigned)((int64_t)P.B * P.Hkv * pl.parts * pl.row_blocks)), block(64 * kRowWaves);
   // (a lane's offset within the 16 rows of a run is 32 bits)
   const bool banded = P.div.page % 16 == 0 && P.row_stride * 2 * 16 < (int64_t)1 << 31;
-  if (banded) launch(attend_rows_kernel<D, true>, grid, block, s, P, pl, q, k, v, table, q_start, kv_len, static_cast<uint16_t*>(out), lse, part);
-  else        launch(attend_rows_kernel<D, false>, grid, block, s, P, pl, q, k, v, table, q_start, kv_len, static_cast<uint16_t*>(out), lse, part);
+  if (banded) launch(attend_rows_kernel<D, true>, grid, block, s, P, pl, A);
+  else        launch(attend_rows_kernel<D, false>, grid, block, s, P, pl, A);
 }
 
-void launch_attend_rows(const Paged& P, const AttendPlan& pl, const void* Q, const void* K, const void* V, const int32_t* table,
-                        const int32_t* q_start, const int32_t* kv_len, void* out, float* lse, Partials part, hipStream_t s) {
-  if (P.d == 64) rows_launch<64>(P, pl, Q, K, V, table, q_start, kv_len, out, lse, part, s);
-  else           rows_launch<128>(P, pl, Q, K, V, table, q_start, kv_len, out, lse, part, s);
+void launch_attend_rows(const Paged& P, const AttendPlan& pl, const AttendArgs& A, hipStream_t s) {
+  if (P.d == 64) rows_launch<64>(P, pl, A, s);
+  else           rows_launch<128>(P, pl, A, s);
 }
 
 }  // namespace ccd
