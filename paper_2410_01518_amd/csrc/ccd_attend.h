@@ -24,9 +24,10 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 // How a call is cut.  On a grid: blocks of `rows` rows, each over at most `parts` stretches of its tokens; chunk: tokens per stretch, made longer where
 // that gives more than `parts` (so the host's idea of the lengths only decides how well the work is spread); sequences of `few` rows or less
 // are left to the even cut.  Evenly: `parts` workgroups, at most `rows` rows per unit; only_few: sequences of more than `few` rows are left to the grid.
+// join: rows of a unit, as far as the host knows.
 // turn: blocks of rows of the first half of one round (rows kernel), 0: the call is more than one round.
 struct AttendPlan {
-  int by_rows, rows, row_blocks, parts, chunk, few, only_few, turn;
+  int by_rows, rows, row_blocks, parts, chunk, few, only_few, turn, join;
 };
 
 // what a workgroup knows of its sequence

@@ -360,8 +360,7 @@ __device__ __forceinline__ void attend_stretch(const Paged& P, const AttendArgs&
       } else {
         const int64_t at = part0 >= 0 ? part0 + (r - r0) : ((int64_t)part_no * P.tokens + row) * P.Hq + head;
         float* to = A.part.o + at * D + e0;
-#pragma unroll
-        for (int e = 0; e < kPer; e += 4) *reinterpret_cast<float4*>(to + e) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+        store_piece(to, acc);
         if (e0 == 0) A.part.ml[at] = make_float2(top, sum);
       }
     }
@@ -396,7 +395,6 @@ __global__ __launch_bounds__(64 * kWaves, (split_waves<T, D, NQ>())) void attend
 // has the same to read everywhere whatever the lengths.  A workgroup's stretch can end in one unit and go on in the next; a unit's rows are
 // joined from the stretches of the workgroups `first` .. that share it.  Every workgroup sums up the lengths for itself.
 constexpr int kEvenLeast = 256;          // tokens of a stretch, at least
-constexpr int kShortChunk = 512;
 
 // what sequence b has to read per KV head, to whole tiles: nothing if its rows are not for this kernel or see nothing
 struct Span {
@@ -500,85 +498,88 @@ __global__ __launch_bounds__(64 * kWaves, (split_waves<T, D, NQ>())) void attend
 
 // Joins the stretches of a row: WAVES waves per (new token, query head).  A lane has the reference and the sum of one stretch, so 64 of them are
 // there at once and their largest costs no chain of loads; the waves then take the stretches' sums in turn.  EVEN: the stretches of
-// attend_even_kernel, else those of a grid.
+// attend_even_kernel, `join` rows of every unit side by side; else those of a grid, rows counted through the call.
 template <class T, int D, int WAVES, bool EVEN>
 __global__ __launch_bounds__(256) void attend_join_kernel(Paged P, AttendPlan pl, AttendArgs A) {
   constexpr int kPer = D / 64;
   __shared__ float sums[WAVES > 1 ? WAVES : 1][D];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t at0 = WAVES > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
-  const int row = (int)(at0 / P.Hq), head = (int)(at0 % P.Hq);
-  if (row >= P.tokens) return;
-  int lo = 0;                                          // sequences that end at or before the row: counted, no chain of loads
-  for (int b0 = 1; b0 <= P.B; b0 += 64) lo += __popcll(__ballot(b0 + lane <= P.B && A.q_start[b0 + lane <= P.B ? b0 + lane : P.B] <= row));
-  if (lo >= P.B || row < A.q_start[0]) return;
-  const Sequence sq = load_sequence(P, lo, A.q_start, A.kv_len);
-  const int r = (row - sq.first) * P.G + head % P.G, rows_all = sq.m * P.G;
-  if (r < 0 || r >= rows_all) return;
-  int parts;
-  int64_t part_first, part_0, part_step;              // entry of the first stretch, of the second less a step, distance of the others
-  if (EVEN) {
-    if (pl.only_few && rows_all > pl.few) return;
-    const int2 unit = A.part.meta[lo * P.Hkv + head / P.G];
-    parts = unit.y;
-    part_step = 2 * pl.rows;
-    part_0 = (int64_t)unit.x * part_step + r;
-    part_first = part_0 + pl.rows;
-  } else {
-    if (rows_all <= pl.few) return;
-    const int r0 = r / pl.rows * pl.rows;
-    parts = cut_rows(P, sq, r0, r0 + pl.rows < rows_all ? r0 + pl.rows : rows_all, pl.parts, pl.chunk).parts;
-    part_step = (int64_t)P.tokens * P.Hq;
-    part_0 = part_first = at0;
-  }
-  if (parts < 2) return;
-  auto entry = [&](int p) { return p == 0 ? part_first : part_0 + p * part_step; };
-  float top = -INFINITY, sum = 0.f, acc[kPer] = {};
-  for (int p0 = 0; p0 < parts; p0 += 64) {
-    const int here = parts - p0 < 64 ? parts - p0 : 64;
-    const float2 ml = lane < here ? A.part.ml[entry(p0 + lane)] : make_float2(-INFINITY, 0.f);
-    float next = fmaxf(top, ml.x);
+  // entry of the first stretch, of the second less a step, distance of the others
+  auto join = [&](int b, int row, int head, int parts, int64_t part_first, int64_t part_0, int64_t part_step) __attribute__((always_inline)) {
+    auto entry = [&](int p) { return p == 0 ? part_first : part_0 + p * part_step; };
+    float top = -INFINITY, sum = 0.f, acc[kPer] = {};
+    for (int p0 = 0; p0 < parts; p0 += 64) {
+      const int here = parts - p0 < 64 ? parts - p0 : 64;
+      const float2 ml = lane < here ? A.part.ml[entry(p0 + lane)] : make_float2(-INFINITY, 0.f);
+      float next = fmaxf(top, ml.x);
 #pragma unroll
-    for (int s = 32; s; s >>= 1) next = fmaxf(next, __shfl_xor(next, s));
-    const float keep = ml.x == -INFINITY ? (ml.y == ml.y ? 0.f : ml.y) : fast_exp2(ml.x - next);
-    float more = ml.x == -INFINITY ? keep : ml.y * keep;
+      for (int s = 32; s; s >>= 1) next = fmaxf(next, __shfl_xor(next, s));
+      const float keep = ml.x == -INFINITY ? (ml.y == ml.y ? 0.f : ml.y) : fast_exp2(ml.x - next);
+      float more = ml.x == -INFINITY ? keep : ml.y * keep;
 #pragma unroll
-    for (int s = 32; s; s >>= 1) more += __shfl_xor(more, s);
-    const float old = next == -INFINITY ? 1.f : fast_exp2(top - next);
-    top = next;
-    sum = sum * old + more;
+      for (int s = 32; s; s >>= 1) more += __shfl_xor(more, s);
+      const float old = next == -INFINITY ? 1.f : fast_exp2(top - next);
+      top = next;
+      sum = sum * old + more;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) acc[j] *= old;
-    for (int p = WAVES > 1 ? wave : 0; p < here; p += 8 * WAVES) {
-      float v[8][kPer];
+      for (int j = 0; j < kPer; ++j) acc[j] *= old;
+      for (int p = WAVES > 1 ? wave : 0; p < here; p += 8 * WAVES) {
+        float v[8][kPer];
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
+        for (int u = 0; u < 8; ++u)
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) v[u][j] = p + u * WAVES < here ? A.part.o[entry(p0 + p + u * WAVES) * D + j * 64 + lane] : 0.f;
+          for (int j = 0; j < kPer; ++j) v[u][j] = p + u * WAVES < here ? A.part.o[entry(p0 + p + u * WAVES) * D + j * 64 + lane] : 0.f;
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const float k = __shfl(keep, (p + u * WAVES) & 63);
+        for (int u = 0; u < 8; ++u) {
+          const float k = __shfl(keep, (p + u * WAVES) & 63);
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) acc[j] = p + u * WAVES < here ? fmaf(v[u][j], k, acc[j]) : acc[j];
+          for (int j = 0; j < kPer; ++j) acc[j] = p + u * WAVES < here ? fmaf(v[u][j], k, acc[j]) : acc[j];
+        }
       }
     }
-  }
-  if (WAVES > 1) {
+    if (WAVES > 1) {
+      __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) sums[wave][j * 64 + lane] = acc[j];
-    __syncthreads();
-    if (wave != 0) return;
+      for (int j = 0; j < kPer; ++j) sums[wave][j * 64 + lane] = acc[j];
+      __syncthreads();
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      acc[j] = 0.f;
+      for (int j = 0; j < kPer; ++j) {
+        acc[j] = 0.f;
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) acc[j] += sums[w][j * 64 + lane];
+        for (int w = 0; w < WAVES; ++w) acc[j] += sums[w][j * 64 + lane];
+      }
+      if (wave != 0) return;
     }
-  }
-  const float inv = inverse_sum(sum);
+    const float inv = inverse_sum(sum);
 #pragma unroll
-  for (int j = 0; j < kPer; ++j) store_elem(static_cast<T*>(A.out) + lo * P.o_b + row * P.o_t + head * P.o_h + j * 64 + lane, acc[j] * inv);
-  if (A.lse != nullptr && lane == 0) A.lse[lo * P.l_b + row * P.l_t + head * P.l_h] = to_natural_lse(top, sum);
+    for (int j = 0; j < kPer; ++j) store_elem(static_cast<T*>(A.out) + b * P.o_b + row * P.o_t + head * P.o_h + j * 64 + lane, acc[j] * inv);
+    if (A.lse != nullptr && lane == 0) A.lse[b * P.l_b + row * P.l_t + head * P.l_h] = to_natural_lse(top, sum);
+  };
+
+  if constexpr (EVEN) {
+    const int unit = (int)(at0 / pl.join), hkv = unit % P.Hkv, b = unit / P.Hkv;
+    if (b >= P.B) return;
+    const Sequence sq = load_sequence(P, b, A.q_start, A.kv_len);
+    const int rows_all = sq.m * P.G;
+    if (rows_all < 1 || rows_all > pl.rows) return;                     // (more rows: not cut)
+    const int2 cut = A.part.meta[unit];
+    if (cut.y < 2) return;
+    for (int r = (int)(at0 % pl.join); r < rows_all; r += pl.join)
+      join(b, sq.first + r / P.G, hkv * P.G + r % P.G, cut.y, (int64_t)(2 * cut.x + 1) * pl.rows + r, (int64_t)(2 * cut.x) * pl.rows + r, 2 * pl.rows);
+  } else {
+    const int row = (int)(at0 / P.Hq), head = (int)(at0 % P.Hq);
+    if (row >= P.tokens) return;
+    int b = 0;                                                          // sequences that end at or before the row: counted, no chain of loads
+    for (int b0 = 1; b0 <= P.B; b0 += 64) b += __popcll(__ballot(b0 + lane <= P.B && A.q_start[b0 + lane <= P.B ? b0 + lane : P.B] <= row));
+    if (b >= P.B || row < A.q_start[0]) return;
+    const Sequence sq = load_sequence(P, b, A.q_start, A.kv_len);
+    const int r = (row - sq.first) * P.G + head % P.G, rows_all = sq.m * P.G;
+    if (r < 0 || r >= rows_all || rows_all <= pl.few) return;
+    const int r0 = r / pl.rows * pl.rows;
+    const int parts = cut_rows(P, sq, r0, r0 + pl.rows < rows_all ? r0 + pl.rows : rows_all, pl.parts, pl.chunk).parts;
+    if (parts > 1) join(b, row, head, parts, at0, at0, (int64_t)P.tokens * P.Hq);
+  }
 }
 
 // ---- host side
@@ -607,27 +608,33 @@ static AttendCuts plan_attend(const Paged& P, int dtype, int max_new, int max_le
     e.rows = most <= 16 ? 16 : most <= 32 ? 32 : 64;
     e.only_few = many;
     e.few = e.rows;
+    e.join = (int)(most < e.rows ? most : e.rows);
     const int waves = dtype == 0 ? (P.d == 64 ? even_waves<float, 64>(e.rows) : even_waves<float, 128>(e.rows))
                                  : (P.d == 64 ? even_waves<uint16_t, 64>(e.rows) : even_waves<uint16_t, 128>(e.rows));
     const int64_t units = (int64_t)P.B * P.Hkv;
     int64_t wgs = (units * len + kEvenLeast - 1) / kEvenLeast;
     if (wgs > cus * waves) wgs = cus * waves;
     e.parts = (int)(wgs < 1 ? 1 : wgs);
-    // Short caches: a workgroup per unit and 512 tokens fits one round of the chip, then nobody has to go on in a second unit.
-    const int64_t chunks = (len + kShortChunk - 1) / kShortChunk;
-    if (!many && units * chunks <= cus * waves && chunks <= 64) {
+    // Short caches: where a workgroup per unit and stretch fits one round of the chip, nobody has to go on in a second unit.  A compute unit reads some
+    // 25 GB/s whatever its waves do, so stretches are short while there are compute units to spare; up to 512 tokens (1024, where the units alone
+    // fill half of the chip) they are not cut at all, which saves the second kernel.
+    const int64_t whole = 2 * units >= cus ? 1024 : 512;
+    for (int chunk = len <= whole ? (int)whole : 256; !many && chunk <= 1024; chunk *= 2) {
+      const int64_t chunks = (len + chunk - 1) / chunk;
+      if (chunks > 64 || units * chunks > (chunk == 256 ? cus : cus * waves) || (chunk == 1024 && len > 1024)) continue;
       c.grid = e;
       c.grid.few = 0;
       c.grid.row_blocks = (int)((rows + e.rows - 1) / e.rows);
-      c.grid.chunk = kShortChunk;
+      c.grid.chunk = chunk;
       c.grid.parts = (int)(chunks < 1 ? 1 : chunks);
-      c.even.rows = 0;
+      c.even.rows = c.even.parts = 0;
+      break;
     }
   }
   if (many) {
     AttendPlan& g = c.grid;
     g.by_rows = dtype != 0;
-    g.rows = g.by_rows ? 128 : 64;
+    g.rows = g.by_rows ? 128 : 32;
     g.few = P.B > 1 ? c.even.few : 0;
     g.row_blocks = (int)((rows + g.rows - 1) / g.rows);
     const int64_t units = (int64_t)P.B * P.Hkv * g.row_blocks;
@@ -683,30 +690,26 @@ size_t attend_workspace_bytes(const Paged& P, int dtype, int max_new, int max_le
 
 template <class T, int D, bool EVEN>
 static void join_launch(const Paged& P, const AttendPlan& pl, const AttendArgs& A, hipStream_t s) {
-  const int64_t rows = (int64_t)P.tokens * P.Hq;
-  // (few rows: four waves each)
-  if (rows <= 2048) launch(attend_join_kernel<T, D, 4, EVEN>, dim3((unsigned)rows), dim3(256), s, P, pl, A);
+  const int64_t rows = EVEN ? (int64_t)P.B * P.Hkv * pl.join : (int64_t)P.tokens * P.Hq;
+  // (few rows, or many stretches: four waves each)
+  if (rows <= 1024) launch(attend_join_kernel<T, D, 4, EVEN>, dim3((unsigned)rows), dim3(256), s, P, pl, A);
   else              launch(attend_join_kernel<T, D, 1, EVEN>, dim3((unsigned)((rows + 3) / 4)), dim3(256), s, P, pl, A);
 }
 
 template <class T, int D>
-static void attend_launch(const Paged& P, int dtype, const AttendCuts& c, const AttendArgs& even, const AttendArgs& grid, hipStream_t s) {
-  const dim3 block(64 * kWaves);
+static void attend_launch(const Paged& P, const AttendCuts& c, const AttendArgs& even, const AttendArgs& grid, hipStream_t s) {
   if (c.grid.rows > 0) {
     const AttendPlan& pl = c.grid;
-    if (pl.by_rows) {
-      launch_attend_rows(P, pl, grid, s);
-    } else {
-      const dim3 wgs((unsigned)((int64_t)P.B * P.Hkv * pl.parts * pl.row_blocks));
-      if (pl.rows == 16)      launch(attend_split_kernel<T, D, 1>, wgs, block, s, P, pl, grid);
-      else if (pl.rows == 32) launch(attend_split_kernel<T, D, 2>, wgs, block, s, P, pl, grid);
-      else                    launch(attend_split_kernel<T, D, 4>, wgs, block, s, P, pl, grid);
-    }
+    const dim3 wgs((unsigned)((int64_t)P.B * P.Hkv * pl.parts * pl.row_blocks)), block(64 * kWaves);
+    if (pl.by_rows)         launch_attend_rows(P, pl, grid, s);
+    else if (pl.rows == 16) launch(attend_split_kernel<T, D, 1>, wgs, block, s, P, pl, grid);
+    else if (pl.rows == 32) launch(attend_split_kernel<T, D, 2>, wgs, block, s, P, pl, grid);
+    else                    launch(attend_split_kernel<T, D, 4>, wgs, block, s, P, pl, grid);
     if (pl.parts > 1) join_launch<T, D, false>(P, pl, grid, s);
   }
   if (c.even.rows > 0) {
     const AttendPlan& pl = c.even;
-    const dim3 wgs((unsigned)pl.parts);
+    const dim3 wgs((unsigned)pl.parts), block(64 * kWaves);
     if (pl.rows == 16)      launch(attend_even_kernel<T, D, 1>, wgs, block, s, P, pl, even);
     else if (pl.rows == 32) launch(attend_even_kernel<T, D, 2>, wgs, block, s, P, pl, even);
     else                    launch(attend_even_kernel<T, D, 4>, wgs, block, s, P, pl, even);
@@ -723,10 +726,10 @@ void launch_attend(const Paged& P, int dtype, int max_new, int max_len, const vo
                   {reinterpret_cast<float*>(ws + w.even_o), reinterpret_cast<float2*>(ws + w.even_ml), reinterpret_cast<int2*>(ws + w.meta)}};
   AttendArgs grid = even;
   grid.part = {reinterpret_cast<float*>(ws + w.grid_o), reinterpret_cast<float2*>(ws + w.grid_ml), nullptr};
-  if (dtype == 0 && P.d == 64) attend_launch<float, 64>(P, dtype, c, even, grid, s);
-  else if (dtype == 0)         attend_launch<float, 128>(P, dtype, c, even, grid, s);
-  else if (P.d == 64)          attend_launch<uint16_t, 64>(P, dtype, c, even, grid, s);
-  else                         attend_launch<uint16_t, 128>(P, dtype, c, even, grid, s);
+  if (dtype == 0 && P.d == 64) attend_launch<float, 64>(P, c, even, grid, s);
+  else if (dtype == 0)         attend_launch<float, 128>(P, c, even, grid, s);
+  else if (P.d == 64)          attend_launch<uint16_t, 64>(P, c, even, grid, s);
+  else                         attend_launch<uint16_t, 128>(P, c, even, grid, s);
 }
 
 }  // namespace ccd
