@@ -1,4 +1,4 @@
-// ccd_paged_attend, few rows per unit and fp32 caches: a workgroup per (unit, block of 16, 32 or 64 rows, stretch of tokens).
+// ccd_paged_attend, few rows per unit and fp32 caches: a workgroup per (unit, block of 16 or 32 rows, stretch of tokens).
 //
 // Decoding reads every key and value once for a handful of rows and is bound by memory.  So the work is cut along the tokens, fine
 // enough to fill the chip evenly whatever the lengths, and a workgroup's waves go their own ways: wave w takes tiles w, w + 4, ... of the
@@ -178,7 +178,7 @@ __device__ __forceinline__ float row_sum(float x) {
 
 // workgroups per compute unit, and so waves per SIMD, that the registers are cut for: what the rows of queries and of sums leave room for
 template <class T, int D, int NQ>
-constexpr int split_waves() { return NQ == 4 ? 1 : NQ == 2 || D == 128 ? 2 : 3; }
+constexpr int split_waves() { return NQ == 2 || D == 128 ? 2 : 3; }
 
 template <class T, int D, int NQ>
 struct SplitLds {
@@ -584,7 +584,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Paged P, AttendPlan pl
 
 // ---- host side
 
-// How a call is cut.  Few rows in every sequence (decoding, at most 64 rows per unit): evenly.  More: on a grid, with the sequences of
+// How a call is cut.  Few rows in every sequence (decoding, at most 32 rows per unit): evenly.  More: on a grid, with the sequences of
 // few rows among them (a batch of chunks and single tokens) evenly by kernels of their own, as a block of 128 rows would walk their long
 // caches alone.
 struct AttendCuts {
@@ -592,20 +592,20 @@ struct AttendCuts {
 };
 
 template <class T, int D>
-static int even_waves(int rows) { return rows == 16 ? split_waves<T, D, 1>() : rows == 32 ? split_waves<T, D, 2>() : split_waves<T, D, 4>(); }
+static int even_waves(int rows) { return rows == 16 ? split_waves<T, D, 1>() : split_waves<T, D, 2>(); }
 
 int attend_compute_units();
 
 static AttendCuts plan_attend(const Paged& P, int dtype, int max_new, int max_len) {
   AttendCuts c{};
   const int64_t rows = (int64_t)max_new * P.G, cus = attend_compute_units();
-  const bool many = rows > 64;
+  const bool many = rows > 32;
   int64_t len = max_len;
   if (P.window > 0 && len > (int64_t)P.window + max_new) len = (int64_t)P.window + max_new;
-  if (!many || P.B > 1) {
+  if (!many || (P.B > 1 && P.G <= 32)) {
     AttendPlan& e = c.even;
     const int64_t most = many ? P.G : rows;
-    e.rows = most <= 16 ? 16 : most <= 32 ? 32 : 64;
+    e.rows = most <= 16 ? 16 : 32;
     e.only_few = many;
     e.few = e.rows;
     e.join = (int)(most < e.rows ? most : e.rows);
@@ -635,7 +635,7 @@ static AttendCuts plan_attend(const Paged& P, int dtype, int max_new, int max_le
     AttendPlan& g = c.grid;
     g.by_rows = dtype != 0;
     g.rows = g.by_rows ? 128 : 32;
-    g.few = P.B > 1 ? c.even.few : 0;
+    g.few = c.even.few;
     g.row_blocks = (int)((rows + g.rows - 1) / g.rows);
     const int64_t units = (int64_t)P.B * P.Hkv * g.row_blocks;
     // stretches: until one round of the chip is full, of 256 tokens at least
@@ -703,16 +703,14 @@ static void attend_launch(const Paged& P, const AttendCuts& c, const AttendArgs&
     const dim3 wgs((unsigned)((int64_t)P.B * P.Hkv * pl.parts * pl.row_blocks)), block(64 * kWaves);
     if (pl.by_rows)         launch_attend_rows(P, pl, grid, s);
     else if (pl.rows == 16) launch(attend_split_kernel<T, D, 1>, wgs, block, s, P, pl, grid);
-    else if (pl.rows == 32) launch(attend_split_kernel<T, D, 2>, wgs, block, s, P, pl, grid);
-    else                    launch(attend_split_kernel<T, D, 4>, wgs, block, s, P, pl, grid);
+    else                    launch(attend_split_kernel<T, D, 2>, wgs, block, s, P, pl, grid);
     if (pl.parts > 1) join_launch<T, D, false>(P, pl, grid, s);
   }
   if (c.even.rows > 0) {
     const AttendPlan& pl = c.even;
     const dim3 wgs((unsigned)pl.parts), block(64 * kWaves);
     if (pl.rows == 16)      launch(attend_even_kernel<T, D, 1>, wgs, block, s, P, pl, even);
-    else if (pl.rows == 32) launch(attend_even_kernel<T, D, 2>, wgs, block, s, P, pl, even);
-    else                    launch(attend_even_kernel<T, D, 4>, wgs, block, s, P, pl, even);
+    else                    launch(attend_even_kernel<T, D, 2>, wgs, block, s, P, pl, even);
     if (pl.parts > 1) join_launch<T, D, true>(P, pl, even, s);
   }
 }
