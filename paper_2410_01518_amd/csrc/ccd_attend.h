@@ -10,6 +10,7 @@
 #pragma once
 #include "ccd_common.h"
 #include "ccd_paged.h"
+#include "ccd_rotary.h"
 
 namespace ccd {
 
@@ -17,7 +18,6 @@ constexpr float kRaise = 8.f;
 
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
-typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef float v16f __attribute__((ext_vector_type(16)));
 
@@ -90,12 +90,6 @@ __device__ __forceinline__ float to_natural_lse(float m, float l) {
 }
 // 1 / sum of weights; a row that sees nothing has 0, one that sees a NaN keeps it
 __device__ __forceinline__ float inverse_sum(float l) { return l > 0.f ? 1.f / l : l == l ? 0.f : l; }
-
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-  typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
-  const v2bf r = {(__bf16)a, (__bf16)b};
-  return __builtin_bit_cast(uint32_t, r);
-}
 
 struct AttendArgs {
   const void *Q, *K, *V;

@@ -8,7 +8,6 @@
 // needed.  Weights need not move at all: a lane holds those of tokens 4g .. 4g + 3 of its row, which is an operand if the tokens of the
 // product are counted in that order.  The waves join their sums at the end; stretches are joined by a second kernel.
 #include "ccd_attend.h"
-#include "ccd_rotary.h"
 
 namespace ccd {
 

@@ -12,7 +12,6 @@
 // (removing all bank conflicts and a tenth of the instructions took 20 % of the cycles and 4 % of the time).  Waves of 64 rows, one per SIMD,
 // read LDS half as often and keep 2.4 GHz, but a wave alone cannot cover its own waits: 1010 - 1040 us, and coarser blocks for short calls.
 #include "ccd_attend.h"
-#include "ccd_rotary.h"
 
 #include <type_traits>
 

@@ -3,7 +3,8 @@
 // Everything follows from three prefix sums over the sequences: pages taken, pages given back, new tokens.  A few thousand
 // lengths are read and summed in about the time a second launch would take, so every workgroup does it for itself and then deals with its
 // share of the tokens and of the table: one launch, and no workgroup waits for another.  Only what is given back needs an order
-// of its own (entries that name no page are left out), which the first workgroup walks.  Bound by latency: a few dependent loads.
+// of its own (entries that name no page are left out), which the first workgroup walks.  Bound by latency, a few dependent loads; so
+// no workgroup has two kinds of work after one another: the first what is given back and the sums, others the table, others the tokens.
 #include "ccd_common.h"
 #include "ccd_paged.h"
 
@@ -44,8 +45,9 @@ struct PlanArgs {
 };
 
 // CAP: sequences the workgroup's arrays hold
+// table_wgs: workgroups that write the table; those behind them have the tokens
 template <int CAP>
-__global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(Paged P, PlanArgs A) {
+__global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(Paged P, PlanArgs A, int table_wgs) {
   __shared__ int first_page[CAP + 1], first_gone[CAP + 1], first_token[CAP + 1];     // before sequence b: pages taken, given back, new tokens
   __shared__ int wave_take[kPlanWaves], wave_give[kPlanWaves];
   __shared__ int64_t wave_new[kPlanWaves];
@@ -153,9 +155,9 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(Paged P, PlanA
   }
 
   // the table: a wave per piece of 256 entries of a row
-  const int gwave = blockIdx.x * kPlanWaves + wave, waves = gridDim.x * kPlanWaves;
+  const int wg = (int)blockIdx.x - 1, waves = table_wgs * kPlanWaves;
   const int pieces = (W + 255) / 256;
-  for (int64_t it = gwave; it < (int64_t)B * pieces; it += waves) {
+  for (int64_t it = wg * kPlanWaves + wave; wg >= 0 && wg < table_wgs && it < (int64_t)B * pieces; it += waves) {
     const int b = (int)(it / pieces), c0 = (int)(it % pieces) * 256;
     const int p0 = p_before(b), n_take = first_page[b + 1] - first_page[b], n_give = first_gone[b + 1] - first_gone[b];
     const int keep = p0 - n_give, p1 = p0 + n_take - n_give;
@@ -175,12 +177,13 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(Paged P, PlanA
   }
 
   // the new tokens
-  for (int i = blockIdx.x * kPlanThreads + tid; i < P.tokens; i += gridDim.x * kPlanThreads) {
+  const int token_wgs = (int)gridDim.x - 1 - table_wgs;
+  for (int64_t i = (int64_t)(wg - table_wgs) * kPlanThreads + tid; i >= 0 && i < P.tokens; i += (int64_t)token_wgs * kPlanThreads) {
     int slot = -1, pos = -1;
     if (i < all_new) {
-      const int b = find_sequence(first_token, B, i);
+      const int b = find_sequence(first_token, B, (int)i);
       const int len0 = A.before[b] > 0 ? A.before[b] : 0;
-      pos = len0 + (i - first_token[b]);
+      pos = len0 + ((int)i - first_token[b]);
       const int c = page_of(P.div, pos), p0 = p_before(b);
       const int id = c >= W ? -1 : c < p0 ? A.table[(int64_t)b * W + c] : page_taken(first_page[b] + c - p0);
       if (id >= 0 && id < P.n_pages) slot = id * P.div.page + (pos - c * P.div.page);
@@ -211,12 +214,12 @@ void launch_paged_plan(const Paged& P, const int32_t* before, const int32_t* aft
                        int32_t* ring, int32_t* cursor, int32_t* cursor_next, int32_t* q_start, int32_t* slots, int32_t* positions,
                        hipStream_t s) {
   const PlanArgs A{before, after, table, table_next, ring, cursor, cursor_next, q_start, slots, positions};
-  const int64_t table_wgs = ((int64_t)P.B * ((P.table_width + 255) / 256) + kPlanWaves - 1) / kPlanWaves;
-  const int64_t token_wgs = ((int64_t)P.tokens + kPlanThreads - 1) / kPlanThreads;
-  int64_t wgs = table_wgs > token_wgs ? table_wgs : token_wgs;
-  wgs = wgs < 1 ? 1 : wgs > 256 ? 256 : wgs;
-  if (P.B <= 512) launch(paged_plan_kernel<512>, dim3((unsigned)wgs), dim3(kPlanThreads), s, P, A);
-  else            launch(paged_plan_kernel<kPlanMaxSequences>, dim3((unsigned)wgs), dim3(kPlanThreads), s, P, A);
+  const int64_t rows_wgs = ((int64_t)P.B * ((P.table_width + 255) / 256) + kPlanWaves - 1) / kPlanWaves;
+  const int64_t tokens_wgs = ((int64_t)P.tokens + kPlanThreads - 1) / kPlanThreads;
+  const int table_wgs = (int)(rows_wgs > 128 ? 128 : rows_wgs), token_wgs = (int)(tokens_wgs > 256 ? 256 : tokens_wgs);
+  const dim3 grid((unsigned)(1 + table_wgs + token_wgs));
+  if (P.B <= 512) launch(paged_plan_kernel<512>, grid, dim3(kPlanThreads), s, P, A, table_wgs);
+  else            launch(paged_plan_kernel<kPlanMaxSequences>, grid, dim3(kPlanThreads), s, P, A, table_wgs);
 }
 
 }  // namespace ccd

@@ -32,22 +32,30 @@ __device__ __forceinline__ void cos_sin_of_phase(uint64_t phase, float& c, float
   s = (q & 2u) ? -b : b;                           // quarters 2 and 3
 }
 
-__device__ __forceinline__ void load_f32(const uint4& w, float (&x)[4], const float*) {
-  x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
+
+// rounded to nearest even (v_cvt_pk_bf16_f32)
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+  const v2bf r = {(__bf16)a, (__bf16)b};
+  return __builtin_bit_cast(uint32_t, r);
 }
-__device__ __forceinline__ void load_f32(const uint4& w, float (&x)[8], const uint16_t*) {
-  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+
+__device__ __forceinline__ void load_f32(const v4u& w, float (&x)[4], const float*) {
+  x[0] = __uint_as_float(w[0]); x[1] = __uint_as_float(w[1]); x[2] = __uint_as_float(w[2]); x[3] = __uint_as_float(w[3]);
+}
+__device__ __forceinline__ void load_f32(const v4u& w, float (&x)[8], const uint16_t*) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u); }
+  for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
 }
-__device__ __forceinline__ uint4 store_bits(const float (&y)[4], const float*) {
-  return make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]));
+__device__ __forceinline__ v4u store_bits(const float (&y)[4], const float*) {
+  return {__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3])};
 }
-__device__ __forceinline__ uint4 store_bits(const float (&y)[8], const uint16_t*) {
-  uint32_t u[4];
+__device__ __forceinline__ v4u store_bits(const float (&y)[8], const uint16_t*) {
+  v4u u;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) u[i] = f32_to_bf16_bits(y[2 * i]) | (f32_to_bf16_bits(y[2 * i + 1]) << 16);
-  return make_uint4(u[0], u[1], u[2], u[3]);
+  for (int i = 0; i < 4; ++i) u[i] = pack_bf16(y[2 * i], y[2 * i + 1]);
+  return u;
 }
 __device__ __forceinline__ void store_elem(float* p, float v) { *p = v; }
 __device__ __forceinline__ void store_elem(uint16_t* p, float v) { *p = (uint16_t)f32_to_bf16_bits(v); }
@@ -68,7 +76,7 @@ struct RotaryLane {
       s[i] *= R.inverse ? -R.amplitude : R.amplitude;
     }
   }
-  __device__ __forceinline__ void rotate(uint4& lo, uint4& hi) const {      // HALF: both pieces; else `hi` is not used
+  __device__ __forceinline__ void rotate(v4u& lo, v4u& hi) const {      // HALF: both pieces; else `hi` is not used
     const T* tag = nullptr;
     float x[kEPL];
     load_f32(lo, x, tag);

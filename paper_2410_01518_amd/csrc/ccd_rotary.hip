@@ -7,12 +7,28 @@
 namespace ccd {
 
 // where row h of a token goes: heads of a dense or strided tensor, or of a page
+constexpr int kBatch = 4;
+
 template <class T>
 struct Rows {
   const T* src;
   T* dst;
   int64_t src_h, dst_h;
 };
+
+// one piece of the heads h, h + side, ... below h_end
+template <class T>
+__device__ __forceinline__ void copy_pieces(const Rows<T>& rows, int h, int h_end, int side, int e) {
+  for (; h < h_end; h += kBatch * side) {
+    v4u a[kBatch] = {};
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      if (h + u * side < h_end) a[u] = *reinterpret_cast<const v4u*>(rows.src + (h + u * side) * rows.src_h + e);
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u)
+      if (h + u * side < h_end) *reinterpret_cast<v4u*>(rows.dst + (h + u * side) * rows.dst_h + e) = a[u];
+  }
+}
 
 // The heads h0, h0 + 1 .. of one token by one wave, in pieces of 16 bytes: `R.rot` elements turned, the rest copied.  A piece index
 // runs over the turned pieces and then over the tail; 64 / pieces heads at a time.
@@ -27,25 +43,32 @@ __device__ __forceinline__ void rotate_heads(const Rotary& R, const Rows<T>& row
     const int width = pieces - p0 < 64 ? pieces - p0 : 64, side = 64 / width;
     const int piece = p0 + lane % width, h_lane = lane / width;
     if (h_lane >= side) continue;
+    // (kBatch heads are read before the first is written: dst may be src, so the compiler would not move a load over a store)
     if (piece < turned) {
-      RotaryLane<T, HALF> rot;
-      rot.angles(R, piece, position, turns);
       const int e = piece * kEPL, e2 = e + R.rot / 2;
-#pragma unroll 4
-      for (int h = h_begin + h_lane; h < h_end; h += side) {
-        const T* s = rows.src + h * rows.src_h;
-        T* o = rows.dst + h * rows.dst_h;
-        uint4 a = *reinterpret_cast<const uint4*>(s + e), b{};
-        if constexpr (HALF) b = *reinterpret_cast<const uint4*>(s + e2);
-        rot.rotate(a, b);
-        *reinterpret_cast<uint4*>(o + e) = a;
-        if constexpr (HALF) *reinterpret_cast<uint4*>(o + e2) = b;
+      RotaryLane<T, HALF> rot;
+      for (int h0 = h_begin + h_lane; h0 < h_end; h0 += kBatch * side) {
+        v4u a[kBatch] = {}, b[kBatch] = {};
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          if (h0 + u * side >= h_end) continue;
+          const T* s = rows.src + (h0 + u * side) * rows.src_h;
+          a[u] = *reinterpret_cast<const v4u*>(s + e);
+          if constexpr (HALF) b[u] = *reinterpret_cast<const v4u*>(s + e2);
+        }
+        if (h0 == h_begin + h_lane) rot.angles(R, piece, position, turns);           // (while the first heads are on their way)
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          rot.rotate(a[u], b[u]);
+          if (h0 + u * side < h_end) {
+            T* o = rows.dst + (h0 + u * side) * rows.dst_h;
+            *reinterpret_cast<v4u*>(o + e) = a[u];
+            if constexpr (HALF) *reinterpret_cast<v4u*>(o + e2) = b[u];
+          }
+        }
       }
     } else {
-      const int e = R.rot + (piece - turned) * kEPL;
-#pragma unroll 4
-      for (int h = h_begin + h_lane; h < h_end; h += side)
-        *reinterpret_cast<uint4*>(rows.dst + h * rows.dst_h + e) = *reinterpret_cast<const uint4*>(rows.src + h * rows.src_h + e);
+      copy_pieces(rows, h_begin + h_lane, h_end, side, R.rot + (piece - turned) * kEPL);
     }
   }
 }
@@ -111,17 +134,10 @@ __global__ __launch_bounds__(256) void paged_append_kernel(Paged P, Rotary R, bo
   constexpr int kEPL = 16 / sizeof(T);
   const int pieces = P.d / kEPL;                       // 8, 16 or 32
   const int piece = lane % pieces, side = 64 / pieces;
-#pragma unroll 4
-  for (int h = lane / pieces; h < P.Hkv; h += side)
-    *reinterpret_cast<uint4*>(V + to + h * P.head_stride + piece * kEPL) = *reinterpret_cast<const uint4*>(V_new + from + h * P.new_h + piece * kEPL);
-  if (rope) {
-    const Rows<T> rows{K_new + from, K + to, P.new_h, P.head_stride};
-    rotate_any<T, KIND>(R, rows, 0, P.Hkv, lane, position, turns, true);
-    return;
-  }
-#pragma unroll 4
-  for (int h = lane / pieces; h < P.Hkv; h += side)
-    *reinterpret_cast<uint4*>(K + to + h * P.head_stride + piece * kEPL) = *reinterpret_cast<const uint4*>(K_new + from + h * P.new_h + piece * kEPL);
+  copy_pieces(Rows<T>{V_new + from, V + to, P.new_h, P.head_stride}, lane / pieces, P.Hkv, side, piece * kEPL);
+  const Rows<T> rows{K_new + from, K + to, P.new_h, P.head_stride};
+  if (rope) rotate_any<T, KIND>(R, rows, 0, P.Hkv, lane, position, turns, true);
+  else      copy_pieces(rows, lane / pieces, P.Hkv, side, piece * kEPL);
 }
 
 template <class T, int KIND>
