@@ -300,9 +300,17 @@ def ccd_compress_kcat(shape, Q_cat, K, V, K_cap, novelty, keep_idx, workspace, s
 
 # ---- paged caches
 
-def _int32(**tensors):
-    for name, t in tensors.items():
-        assert t.dtype == torch.int32 and t.is_contiguous(), f"{name}: contiguous int32 needed"
+def _here(*tensors):
+    """The call runs on the current device's stream: its tensors must be there."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t.device.index != device:
+            raise ValueError(f"a tensor on {t.device}, and the current device is cuda:{device}")
+
+
+def _int32(*tensors):
+    for t in tensors:
+        assert t.dtype is torch.int32 and t.is_contiguous(), "contiguous int32 needed"
 
 
 def make_plan(block_table, *, tokens, page, n_pages) -> ccd_paged_t:
@@ -383,8 +391,8 @@ def ccd_paged_plan(paged, len_before, len_after, block_table, block_table_next, 
                    stream=None) -> int:
     """len_before, len_after [B], block_table and block_table_next [B, table_width] (may be one), free_pages [n_pages], cursor and
     cursor_next [4] (may be one), q_start [B + 1], slots and positions [tokens]: int32."""
-    _int32(len_before=len_before, len_after=len_after, block_table=block_table, block_table_next=block_table_next, free_pages=free_pages,
-           cursor=cursor, cursor_next=cursor_next, q_start=q_start, slots=slots, positions=positions)
+    _int32(len_before, len_after, block_table, block_table_next, free_pages, cursor, cursor_next, q_start, slots, positions)
+    _here(block_table)
     return _check(lib().ccd_paged_plan(ctypes.byref(paged), _ptr(len_before), _ptr(len_after), _ptr(block_table), _ptr(block_table_next),
                                        _ptr(free_pages), _ptr(cursor), _ptr(cursor_next), _ptr(q_start), _ptr(slots), _ptr(positions),
                                        _stream(stream)))
@@ -392,21 +400,25 @@ def ccd_paged_plan(paged, len_before, len_after, block_table, block_table_next, 
 
 def ccd_rope(rope, X, positions, turns, Y, stream=None) -> int:
     """positions int32 [tokens]; turns as rope_turns gives them; Y may be X."""
-    _int32(positions=positions)
+    _int32(positions)
+    _here(X, positions)
     return _check(lib().ccd_rope(ctypes.byref(rope), _ptr(X), _ptr(positions), _ptr(turns), _ptr(Y), _stream(stream)))
 
 
 def ccd_paged_append(paged, K_new, V_new, slots, K_pages, V_pages, rope=None, positions=None, turns=None, stream=None) -> int:
     """K_new and V_new have the same strides, as have K_pages and V_pages; with a rope descriptor the keys are embedded at `positions`."""
-    _int32(slots=slots)
+    _int32(slots)
+    _here(K_pages, slots)
     assert K_new.stride() == V_new.stride() and K_pages.stride() == V_pages.stride()
+    assert rope is None or (positions is not None and turns is not None)
     return _check(lib().ccd_paged_append(ctypes.byref(paged), None if rope is None else ctypes.byref(rope), _ptr(K_new), _ptr(V_new), _ptr(slots),
                                          _ptr(positions), _ptr(turns), _ptr(K_pages), _ptr(V_pages), _stream(stream)))
 
 
 def ccd_paged_attend(paged, Q, K_pages, V_pages, block_table, q_start, kv_len, out, lse, workspace, stream=None) -> int:
     """block_table [B, table_width], q_start [B + 1], kv_len [B]: int32; lse fp32 or None."""
-    _int32(block_table=block_table, q_start=q_start, kv_len=kv_len)
+    _int32(block_table, q_start, kv_len)
+    _here(Q, K_pages, block_table)
     assert K_pages.stride() == V_pages.stride()
     return _check(lib().ccd_paged_attend(ctypes.byref(paged), _ptr(Q), _ptr(K_pages), _ptr(V_pages), _ptr(block_table), _ptr(q_start), _ptr(kv_len),
                                          _ptr(out), _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel(),

@@ -5,8 +5,11 @@ full; then the catalyst-prompt queries of that moment score the cache and ccd_co
 head in place, after which appending continues behind them.  Novelty is carried per head, because after
 the first distillation heads no longer hold the same tokens in the same slots (Sec. 3.3.1).
 
-Only buffer bookkeeping happens here; appending, scoring, selection and compaction all run in the library's kernels
+Only buffer bookkeeping happens here; appending, attention, scoring, selection and compaction all run in the library's kernels
 (the append stands in for the model forward that would write new keys and values).
+
+`MemoryPot` is one pot per sequence, all filled alike.  `PagedPots` serves sequences of different lengths from one pool of pages; where a
+page is a whole pot, a sequence's pot is distilled as soon as it is full, whatever the others hold.
 """
 from __future__ import annotations
 
@@ -27,6 +30,9 @@ class MemoryPot:
         self.n_valid = 0
         self.calls = 0
         self._ws = None
+        self._attn_ws = None
+        self._attn_len = (None, None)           # kv_len as last written, and the number it holds
+        self._attn_rows = {}                    # (pages, tokens) -> block table, q_start
 
     @property
     def room(self) -> int:
@@ -41,16 +47,133 @@ class MemoryPot:
         assert rc == ip.CCD_OK, rc
         self.n_valid += m
 
-    def distill(self, Q_cat, scores=None) -> int:
-        """One CCD compression if the pot is full; returns the library's code (CCD_OK or CCD_NOOP)."""
+    def attend(self, Q, *, layer=None, behind=False, window=0, K=None, out=None, lse=None):
+        """Attention of m query tokens over the pot: Q [B, L, Hq, m, d], or [B, Hq, m, d] of one layer.  The tokens are the pot's last m (already
+        appended: each sees what stands before it and itself) or, with `behind`, stand behind it and see all of it (the catalyst prompt).
+        K: other keys than the stored ones (the embedded ones of CR-RoPE).  Returns (out, lse) like Q and Q without its last axis; the
+        catalyst prompt's lse is what `distill` can take."""
+        K = self.K if K is None else K
+        one = layer is not None
+        keys, values = (K[:, layer], self.V[:, layer]) if one else (K.view(-1, *K.shape[2:]), self.V.view(-1, *K.shape[2:]))
+        pages, (Hq, m) = keys.shape[0], Q.shape[-3:-1]
+        q = Q if one else Q.reshape(-1, *Q.shape[2:])
+        out = torch.empty_like(Q, memory_format=torch.contiguous_format) if out is None else out
+        lse = torch.empty(Q.shape[:-1], dtype=torch.float32, device=Q.device) if lse is None else lse
+        if (pages, m) not in self._attn_rows:
+            self._attn_rows[pages, m] = (torch.arange(pages, dtype=torch.int32, device=Q.device)[:, None].contiguous(),
+                                         torch.arange(pages + 1, dtype=torch.int32, device=Q.device) * m)
+        table, q_start = self._attn_rows[pages, m]
+        kv_len, held = self._attn_len
+        if kv_len is None:
+            kv_len = torch.empty(self.B * self.L, dtype=torch.int32, device=Q.device)
+        if held != self.n_valid:
+            kv_len.fill_(self.n_valid)
+            self._attn_len = (kv_len, self.n_valid)
+        o, s = (out, lse) if one else (out.view(-1, *out.shape[2:]), lse.view(-1, *lse.shape[2:]))
+        paged = ip.make_paged(keys, tokens=pages * m, block_table=table, Q=q, out=o, lse=s, window=window, behind=behind, max_new=m, max_len=max(1, self.n_valid))
+        need = ip.ccd_paged_workspace_bytes(paged)
+        if self._attn_ws is None or self._attn_ws.numel() < need:
+            self._attn_ws = ip.alloc_paged_workspace(paged, Q.device)
+        rc = ip.ccd_paged_attend(paged, q, keys, values, table, q_start, kv_len[:pages], o, s, self._attn_ws)
+        assert rc == ip.CCD_OK, rc
+        return out, lse
+
+    def distill(self, Q_cat, scores=None, lse=None) -> int:
+        """One CCD compression if the pot is full; returns the library's code (CCD_OK or CCD_NOOP).  lse: the catalyst rows' log-sum-exps, as
+        `attend` returns them (one pass over the keys instead of two)."""
         shape = ip.make_shape(Q_cat, self.K, self.novelty, k=self.k, T=self.T, pool_w=self.pool_w,
                               pool_mode=self.pool_mode, n_valid=self.n_valid)
         if self._ws is None:
             full = ip.make_shape(Q_cat, self.K, self.novelty, k=self.k, T=self.T, pool_w=self.pool_w,
                                  pool_mode=self.pool_mode, n_valid=self.n_cap)
             self._ws = ip.alloc_workspace(full)
-        rc = ip.ccd_compress(shape, Q_cat, self.K, self.V, self.novelty, self.keep_idx, self._ws, scores=scores)
+        if lse is not None:
+            rc = ip.ccd_compress_lse(shape, Q_cat, self.K, self.V, lse, self.novelty, self.keep_idx, self._ws, scores=scores)
+        else:
+            rc = ip.ccd_compress(shape, Q_cat, self.K, self.V, self.novelty, self.keep_idx, self._ws, scores=scores)
         if rc == ip.CCD_OK:
             self.n_valid = self.k
             self.calls += 1
+        return rc
+
+
+class PagedPots:
+    """Sequences of different lengths over one pool of pages, for all layers.
+
+    A step of a serving loop: `step(lengths)` says how many tokens every sequence holds after it (one that shrinks gives pages back, 0 ends it)
+    and plans where the new ones go; then, in every layer, `append` writes their keys and values and `attend` lets them attend.  The new
+    tokens are numbered sequence after sequence; tensors may have more rows than that, which are left alone.  A pool whose pages
+    are as long as the longest sequence is a pool of memory pots: `distill` compresses the pot of one sequence.
+    """
+
+    def __init__(self, sequences, n_pages, page, max_len, step_tokens, L, Hq, Hkv, d, *, dtype=torch.bfloat16, window=0, device="cuda"):
+        self.page, self.L, self.Hq, self.window, self.step_tokens = page, L, Hq, window, step_tokens
+        self.K = torch.zeros((n_pages, L, Hkv, page, d), dtype=dtype, device=device)
+        self.V = torch.zeros_like(self.K)
+        ints = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=device)            # noqa: E731
+        self.table = torch.full((sequences, -(-max_len // page)), -1, dtype=torch.int32, device=device)
+        self.free_pages = torch.arange(n_pages, dtype=torch.int32, device=device)
+        self.cursor = torch.tensor([0, n_pages, 0, 0], dtype=torch.int32, device=device)
+        self.before, self.after, self.q_start = ints(sequences), ints(sequences), ints(sequences + 1)
+        self.slots, self.positions = ints(step_tokens), ints(step_tokens)
+        self.lengths = [0] * sequences                  # on the host, as of the last step
+        self.new = [0] * sequences
+        self._plan = ip.make_plan(self.table, tokens=step_tokens, page=page, n_pages=n_pages)
+        self._ws = None
+
+    def pages(self, length) -> int:
+        return -(-length // self.page)
+
+    def step(self, lengths) -> int:
+        """Plans the step that leaves sequence b with lengths[b] tokens; returns the number of new ones."""
+        lengths = [int(n) for n in lengths]
+        new = [max(0, n - o) for o, n in zip(self.lengths, lengths)]
+        if len(lengths) != len(self.lengths) or min(lengths) < 0 or self.pages(max(lengths)) > self.table.shape[1] or sum(new) > self.step_tokens:
+            raise ValueError("a length, or the number of new tokens, beyond what the pool was made for")
+        held = sum(map(self.pages, self.lengths))
+        if held + sum(max(0, self.pages(n) - self.pages(o)) for o, n in zip(self.lengths, lengths)) > self.K.shape[0]:
+            raise ValueError("not enough free pages (those given back in a step are free from the next one on)")
+        both = torch.tensor([self.lengths, lengths], dtype=torch.int32).to(self.table.device)
+        self.before.copy_(both[0])
+        self.after.copy_(both[1])
+        rc = ip.ccd_paged_plan(self._plan, self.before, self.after, self.table, self.table, self.free_pages, self.cursor, self.cursor, self.q_start,
+                               self.slots, self.positions)
+        assert rc == ip.CCD_OK, rc
+        self.lengths, self.new = lengths, new
+        return sum(new)
+
+    def _paged(self, layer, tokens, **kw):
+        return ip.make_paged(self.K[:, layer], tokens=tokens, block_table=self.table, window=self.window, max_new=max(1, *self.new), max_len=max(1, *self.lengths), **kw)
+
+    def append(self, layer, K_new, V_new, rope=None, turns=None) -> None:
+        """Keys and values of the step's new tokens, [rows, Hkv, d]; rope and turns (as of rope_turns): the keys are embedded at their positions."""
+        rows = K_new.shape[0]
+        rc = ip.ccd_paged_append(self._paged(layer, rows, K_new=K_new), K_new, V_new, self.slots[:rows], self.K[:, layer], self.V[:, layer], rope=rope,
+                                 positions=None if rope is None else self.positions[:rows], turns=turns)
+        assert rc == ip.CCD_OK, rc
+
+    def attend(self, layer, Q, out=None, lse=None):
+        """Q [rows, Hq, d] of the step's new tokens, their keys and values appended; returns (out, lse)."""
+        out = torch.empty_like(Q, memory_format=torch.contiguous_format) if out is None else out
+        lse = torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device) if lse is None else lse
+        paged = self._paged(layer, Q.shape[0], Q=Q, out=out, lse=lse)
+        need = ip.ccd_paged_workspace_bytes(paged)
+        if self._ws is None or self._ws.numel() < need:
+            self._ws = ip.alloc_paged_workspace(paged, Q.device)
+        rc = ip.ccd_paged_attend(paged, Q, self.K[:, layer], self.V[:, layer], self.table, self.q_start, self.after, out, lse, self._ws)
+        assert rc == ip.CCD_OK, rc
+        return out, lse
+
+    def distill(self, b, page_id, Q_cat, novelty, keep_idx, workspace, *, k, T, pool_w=7, pool_mode=ip.CCD_POOL_MAX, lse=None) -> int:
+        """Compresses the pot of sequence b, the page page_id that it holds (one page per sequence), if it is full: Q_cat [1, L, Hq, P, d], novelty
+        [1, page] or [1, L, Hkv, page], keep_idx [1, L, Hkv, k].  Returns the library's code; after CCD_OK the sequence has k tokens."""
+        assert self.table.shape[1] == 1, "distillation needs pages that are whole pots"
+        K, V = self.K[page_id: page_id + 1], self.V[page_id: page_id + 1]
+        shape = ip.make_shape(Q_cat, K, novelty, k=k, T=T, pool_w=pool_w, pool_mode=pool_mode, n_valid=max(1, self.lengths[b]))
+        if lse is not None:
+            rc = ip.ccd_compress_lse(shape, Q_cat, K, V, lse, novelty, keep_idx, workspace)
+        else:
+            rc = ip.ccd_compress(shape, Q_cat, K, V, novelty, keep_idx, workspace)
+        if rc == ip.CCD_OK:
+            self.lengths[b] = k
         return rc
