@@ -99,6 +99,58 @@ struct AttendArgs {
   Partials part;
 };
 
+// A weight of 0 takes a token out of a product only if its value is a number.  Where some rows see a token and others do not, and its value is infinite
+// or NaN, the products carry NaN into rows that do not see it.  Sums that come out as NaN where the rows are of several new tokens are therefore
+// taken once more, by a wave a row, over those of the tokens t_begin .. t_end - 1 alone that it sees.  They are the result (whole_row) or
+// the stretch's `entry` of the workspace.
+template <class T, int D>
+__device__ __forceinline__ void redo_row(const Paged& P, const AttendArgs& A, const Sequence& sq, int b, int hkv, int r, int t_begin, int t_end,
+                                         bool whole_row, int64_t entry) {
+  constexpr int kPer = D / 64;
+  const int lane = threadIdx.x & 63;
+  const int32_t* pages = A.table + (int64_t)b * P.table_width;
+  const T* K = static_cast<const T*>(A.K) + hkv * P.head_stride;
+  const T* V = static_cast<const T*>(A.V) + hkv * P.head_stride;
+  const int i = r / P.G, head = hkv * P.G + r - i * P.G, pos = sq.base + i, low = first_seen(P, pos);
+  const int64_t row = sq.first + i;
+  const T* q = static_cast<const T*>(A.Q) + b * P.q_b + row * P.q_t + head * P.q_h;
+  const int begin = low > t_begin ? low : t_begin, end = pos + 1 < t_end ? pos + 1 : t_end;
+  float m = -INFINITY, l = 0.f, o[kPer] = {};
+  for (int t = begin; t < end; ++t) {
+    const int c = page_of(P.div, t), id = pages[c];
+    if (id < 0 || id >= P.n_pages) continue;
+    const int64_t at = id * P.page_stride + (int64_t)(t - c * P.div.page) * P.row_stride;
+    float x = 0.f;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) x = fmaf(load_elem(q + j * 64 + lane), load_elem(K + at + j * 64 + lane), x);
+#pragma unroll
+    for (int s = 32; s; s >>= 1) x += __shfl_xor(x, s);
+    x *= P.scale_log2;
+    const float next = fmaxf(m, x), keep = next == -INFINITY ? 1.f : fast_exp2(m - next), w = next == -INFINITY && x == x ? 0.f : fast_exp2(x - next);
+    m = next;
+    l = l * keep + w;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) o[j] = o[j] * keep + (w != 0.f ? w * load_elem(V + at + j * 64 + lane) : 0.f);
+  }
+  if (whole_row) {
+    const float inv = inverse_sum(l);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) store_elem(static_cast<T*>(A.out) + b * P.o_b + row * P.o_t + head * P.o_h + j * 64 + lane, o[j] * inv);
+    if (A.lse != nullptr && lane == 0) A.lse[b * P.l_b + row * P.l_t + head * P.l_h] = to_natural_lse(m, l);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) A.part.o[entry * D + j * 64 + lane] = o[j];
+    if (lane == 0) A.part.ml[entry] = make_float2(m, l);
+  }
+}
+// rows r0, r0 + step .. of those before r1, in a grid's stretch part_no, by the wave
+template <class T, int D>
+__device__ __forceinline__ void redo_rows(const Paged& P, const AttendArgs& A, const Sequence& sq, int b, int hkv, int r0, int r1, int step, int t_begin, int t_end,
+                                          bool whole_row, int part_no) {
+  for (int r = r0; r < r1; r += step)
+    redo_row<T, D>(P, A, sq, b, hkv, r, t_begin, t_end, whole_row, ((int64_t)part_no * P.tokens + sq.first + r / P.G) * P.Hq + hkv * P.G + r % P.G);
+}
+
 // rows kernel (bf16): a workgroup per (unit, block of 128 rows, stretch), its waves share the tiles
 void launch_attend_rows(const Paged& P, const AttendPlan& pl, const AttendArgs& A, hipStream_t s);
 

@@ -189,8 +189,9 @@ struct SplitLds {
 
 // Rows r0 .. r1 - 1 of unit (b, hkv) over the tokens t_begin .. t_end - 1, by the workgroup.  whole_row: these are all tokens the rows see, the result
 // is written; else (o, m, l) of row r go to entry part0 + (r - r0) of the workspace, or, part0 < 0, to those of part_no by the row's number.
+// Returns whether the rows have to be done again (redo_rows).
 template <class T, int D, int NQ>
-__device__ __forceinline__ void attend_stretch(const Paged& P, const AttendArgs& A, SplitLds<T, D, NQ>& L, const Sequence& sq, int b, int hkv, int r0, int r1,
+__device__ __forceinline__ bool attend_stretch(const Paged& P, const AttendArgs& A, SplitLds<T, D, NQ>& L, const Sequence& sq, int b, int hkv, int r0, int r1,
                                                int t_begin, int t_end, bool whole_row, int64_t part0, int part_no) {
   using Tl = Tile<T, D>;
   constexpr int kPitch = SplitLds<T, D, NQ>::kPitch, kStride = kWaves * Tl::kTokens;
@@ -248,6 +249,7 @@ __device__ __forceinline__ void attend_stretch(const Paged& P, const AttendArgs&
   for (; t0 < t_end; t0 += kStride) {
     uint32_t there = (uint32_t)__ballot(off[0] >= 0) & 0xFFFFu;
     if constexpr (Tl::kHalves == 2) there |= (uint32_t)__ballot(off[Tl::kHalves - 1] >= 0) << 16;
+    const bool whole = there == (Tl::kHalves == 2 ? 0xFFFFFFFFu : 0xFFFFu) && t0 + Tl::kTokens - 1 <= pos_min && t0 >= low_max;
     const bool more = t0 + kStride < t_end;
     if (more) offsets(t0 + kStride);
     // the next tile's rows are asked for as soon as this one's are out of their registers
@@ -260,7 +262,6 @@ __device__ __forceinline__ void attend_stretch(const Paged& P, const AttendArgs&
       Tl::load_keys(keys, Kh, off, lane);
       if (!Tl::kValuesLate) look_up(t0 + 2 * kStride);
     }
-    const bool whole = there == (Tl::kHalves == 2 ? 0xFFFFFFFFu : 0xFFFFu) && t0 + Tl::kTokens - 1 <= pos_min && t0 >= low_max;
     typename Tl::Weights w[NQ];
 #pragma unroll
     for (int j = 0; j < NQ; ++j) {
@@ -317,6 +318,7 @@ __device__ __forceinline__ void attend_stretch(const Paged& P, const AttendArgs&
     if (lane < 16) { L.m[wave][16 * j + lane] = m[j]; L.l[wave][16 * j + lane] = l[j]; }
   }
   __syncthreads();
+  bool none = false;                                        // sums that are no numbers
 #pragma unroll
   for (int j = 0; j < NQ; ++j) {
     float all = -INFINITY;
@@ -347,6 +349,8 @@ __device__ __forceinline__ void attend_stretch(const Paged& P, const AttendArgs&
       sum += mw == -INFINITY ? (lw == lw ? 0.f : lw) : lw * fast_exp2(mw - top);
     }
     if (r < r1) {
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) none = none || acc[e] != acc[e];
       const int i = r / P.G, head = hkv * P.G + r - i * P.G;
       const int64_t row = sq.first + i;
       if (whole_row) {
@@ -364,7 +368,8 @@ __device__ __forceinline__ void attend_stretch(const Paged& P, const AttendArgs&
       }
     }
   }
-  __syncthreads();
+  // one new token alone sees all tokens of the stretch: what it has is its own
+  return __syncthreads_or(none && r0 / P.G != (r1 - 1) / P.G);
 }
 
 // the call cut on a grid: (unit, block of rows, stretch)
@@ -381,13 +386,26 @@ __global__ __launch_bounds__(64 * kWaves, (split_waves<T, D, NQ>())) void attend
   const Sequence sq = load_sequence(P, b, A.q_start, A.kv_len);
   const int rows_all = sq.m * P.G;
   if (rows_all <= pl.few) return;
-  for (int r0 = block0 * kRows; r0 < rows_all; r0 += pl.row_blocks * kRows) {
-    const int r1 = r0 + kRows < rows_all ? r0 + kRows : rows_all;
-    const Stretch st = cut_rows(P, sq, r0, r1, pl.parts, pl.chunk);
-    if (part_no >= st.parts) continue;
-    const int t_begin = st.begin + part_no * st.chunk, t_end = t_begin + st.chunk < st.end ? t_begin + st.chunk : st.end;
-    attend_stretch<T, D, NQ>(P, A, L, sq, b, hkv, r0, r1, t_begin, t_end, st.parts == 1, -1, part_no);
+  // (once more over all of it, row by row, if need be)
+  bool again = false;
+  for (int pass = 0; pass < 2; ++pass) {
+    for (int r0 = block0 * kRows; r0 < rows_all; r0 += pl.row_blocks * kRows) {
+      const int r1 = r0 + kRows < rows_all ? r0 + kRows : rows_all;
+      const Stretch st = cut_rows(P, sq, r0, r1, pl.parts, pl.chunk);
+      if (part_no >= st.parts) continue;
+      const int t_begin = st.begin + part_no * st.chunk, t_end = t_begin + st.chunk < st.end ? t_begin + st.chunk : st.end;
+      if (pass == 0) again = attend_stretch<T, D, NQ>(P, A, L, sq, b, hkv, r0, r1, t_begin, t_end, st.parts == 1, -1, part_no) || again;
+      else           redo_rows<T, D>(P, A, sq, b, hkv, r0 + (int)(threadIdx.x >> 6), r1, kWaves, t_begin, t_end, st.parts == 1, part_no);
+    }
+    if (__builtin_expect(!again, 1)) break;
   }
+}
+
+constexpr int kAgain = -1;                                  // for a unit's number of stretches: its rows have to be done again
+
+// What all lanes have alike, into scalar registers (what comes from LDS the compiler takes to differ by lane).
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  return (int64_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
 }
 
 // The call cut evenly: the tokens of all units, one after the other, are dealt to the workgroups in equal stretches, so that one round of the chip
@@ -436,7 +454,7 @@ __global__ __launch_bounds__(64 * kWaves, (split_waves<T, D, NQ>())) void attend
   int64_t all = 0, before = to - run;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) { if (w < wave) before += wave_sum[w]; all += wave_sum[w]; }
-  all *= P.Hkv;
+  all = uniform(all) * P.Hkv;
   int64_t per = (all + gridDim.x - 1) / gridDim.x;
   per = per < kEvenLeast ? kEvenLeast : (per + 127) / 128 * 128;
   int64_t at = me * per;
@@ -467,8 +485,8 @@ __global__ __launch_bounds__(64 * kWaves, (split_waves<T, D, NQ>())) void attend
     }
   }
   __syncthreads();
-  int b = found_b;
-  int64_t b_at = found_at;
+  int b = __builtin_amdgcn_readfirstlane(found_b);
+  int64_t b_at = uniform(found_at);
   while (b >= 0 && at < stop) {
     const Sequence sq = load_sequence(P, b, A.q_start, A.kv_len);
     const Span sp = span_of(P, pl, sq);
@@ -485,9 +503,12 @@ __global__ __launch_bounds__(64 * kWaves, (split_waves<T, D, NQ>())) void attend
       if (tid == 0 && first == me) meta[b * P.Hkv + h] = make_int2(first, alone ? 1 : last - first + 1);
       const int t_begin = sp.begin + (int)(at - unit_at), t_stop = sp.begin + (int)(until - unit_at);
       if (!alone || first == me)
-        for (int r0 = 0; r0 < rows_all; r0 += kRows)
-          attend_stretch<T, D, NQ>(P, A, L, sq, b, h, r0, r0 + kRows < rows_all ? r0 + kRows : rows_all, alone ? sp.begin : t_begin,
-                                   alone || t_stop > sp.end ? sp.end : t_stop, alone || first == last, (int64_t)(2 * me + (first == me)) * kRows, 0);
+        for (int r0 = 0; r0 < rows_all; r0 += kRows) {
+          const bool again = attend_stretch<T, D, NQ>(P, A, L, sq, b, h, r0, r0 + kRows < rows_all ? r0 + kRows : rows_all, alone ? sp.begin : t_begin,
+                                                      alone || t_stop > sp.end ? sp.end : t_stop, alone || first == last, (int64_t)(2 * me + (first == me)) * kRows, 0);
+          // (the kernel that joins does them again, those of several stretches without being told)
+          if (again && (alone || first == last) && tid == 0) meta[b * P.Hkv + h].y = kAgain;
+        }
       at = until;
     }
     b_at = b_end;
@@ -505,7 +526,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Paged P, AttendPlan pl
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t at0 = WAVES > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
   // entry of the first stretch, of the second less a step, distance of the others
-  auto join = [&](int b, int row, int head, int parts, int64_t part_first, int64_t part_0, int64_t part_step) __attribute__((always_inline)) {
+  auto join = [&](const Sequence& sq, int b, int hkv, int r, int parts, int64_t part_first, int64_t part_0, int64_t part_step) __attribute__((always_inline)) {
     auto entry = [&](int p) { return p == 0 ? part_first : part_0 + p * part_step; };
     float top = -INFINITY, sum = 0.f, acc[kPer] = {};
     for (int p0 = 0; p0 < parts; p0 += 64) {
@@ -550,6 +571,14 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Paged P, AttendPlan pl
       }
       if (wave != 0) return;
     }
+    bool none = false;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) none = none || acc[j] != acc[j];
+    if (EVEN && sq.m > 1 && __builtin_expect(__any(none), 0)) {
+      redo_row<T, D>(P, A, sq, b, hkv, r, 0, sq.n, true, 0);
+      return;
+    }
+    const int row = sq.first + r / P.G, head = hkv * P.G + r % P.G;
     const float inv = inverse_sum(sum);
 #pragma unroll
     for (int j = 0; j < kPer; ++j) store_elem(static_cast<T*>(A.out) + b * P.o_b + row * P.o_t + head * P.o_h + j * 64 + lane, acc[j] * inv);
@@ -561,11 +590,13 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Paged P, AttendPlan pl
     if (b >= P.B) return;
     const Sequence sq = load_sequence(P, b, A.q_start, A.kv_len);
     const int rows_all = sq.m * P.G;
-    if (rows_all < 1 || rows_all > pl.rows) return;                     // (more rows: not cut)
+    if (rows_all < 1 || (pl.only_few && rows_all > pl.few)) return;
     const int2 cut = A.part.meta[unit];
-    if (cut.y < 2) return;
-    for (int r = (int)(at0 % pl.join); r < rows_all; r += pl.join)
-      join(b, sq.first + r / P.G, hkv * P.G + r % P.G, cut.y, (int64_t)(2 * cut.x + 1) * pl.rows + r, (int64_t)(2 * cut.x) * pl.rows + r, 2 * pl.rows);
+    if (cut.y == 1 || (cut.y == kAgain && WAVES > 1 && wave != 0)) return;
+    for (int r = (int)(at0 % pl.join); r < rows_all; r += pl.join) {
+      if (cut.y == kAgain) { redo_row<T, D>(P, A, sq, b, hkv, r, 0, sq.n, true, 0); continue; }
+      join(sq, b, hkv, r, cut.y, (int64_t)(2 * cut.x + 1) * pl.rows + r, (int64_t)(2 * cut.x) * pl.rows + r, 2 * pl.rows);
+    }
   } else {
     const int row = (int)(at0 / P.Hq), head = (int)(at0 % P.Hq);
     if (row >= P.tokens) return;
@@ -577,7 +608,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Paged P, AttendPlan pl
     if (r < 0 || r >= rows_all || rows_all <= pl.few) return;
     const int r0 = r / pl.rows * pl.rows;
     const int parts = cut_rows(P, sq, r0, r0 + pl.rows < rows_all ? r0 + pl.rows : rows_all, pl.parts, pl.chunk).parts;
-    if (parts > 1) join(b, row, head, parts, at0, at0, (int64_t)P.tokens * P.Hq);
+    if (parts > 1) join(sq, b, head / P.G, r, parts, at0, at0, (int64_t)P.tokens * P.Hq);
   }
 }
 
@@ -710,7 +741,7 @@ static void attend_launch(const Paged& P, const AttendCuts& c, const AttendArgs&
     const dim3 wgs((unsigned)pl.parts), block(64 * kWaves);
     if (pl.rows == 16)      launch(attend_even_kernel<T, D, 1>, wgs, block, s, P, pl, even);
     else                    launch(attend_even_kernel<T, D, 2>, wgs, block, s, P, pl, even);
-    if (pl.parts > 1) join_launch<T, D, true>(P, pl, even, s);
+    join_launch<T, D, true>(P, pl, even, s);
   }
 }
 

@@ -335,7 +335,14 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_kernel(Paged P,
     }
 
     l += __shfl_xor(l, 32);
-    if (r < r1) {
+    bool none = false;                                                         // (also from tokens of its tiles that no row sees)
+#pragma unroll
+    for (int c = 0; c < kBlocks; ++c)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) none = none || o[c][e] != o[c][e];
+    if (__builtin_expect(__any(none && r < r1), 0)) {
+      redo_rows<uint16_t, D>(P, A, sq, b, hkv, w0, w1, 1, t_begin, t_end, st.parts == 1, part_no);
+    } else if (r < r1) {
       const int64_t row = sq.first + i_row;
       if (st.parts == 1) {
         const float inv = inverse_sum(l);

@@ -583,3 +583,55 @@ def test_a_serving_loop(dtype, layout):
         assert (np.abs(_f64(lse)[:starts[-1]] - want_lse) <= slack).all()
         assert (out[starts[-1]:] == 5.0).all() and (lse[starts[-1]:] == 5.0).all()
         lens = nxt
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("new,window", [(3, 0), (8, 0), (70, 0), (200, 0), (40, 25), (1, 30)])
+@pytest.mark.parametrize("bad", ["nan", "inf"])
+def test_what_a_row_does_not_see_does_not_reach_it(dtype, new, window, bad):
+    """Keys and values of a token are NaN or infinite: rows before it, and rows whose window has passed it, are as if it were not there."""
+    p = _attend_problem(12, dtype, [330, 90], [new, 1], 4, 2, 64, 16)
+    first = 330 - new
+    for pos in (first - 40, first + new // 2, first + new - 1) if window else (first + new // 2, first + new - 1):
+        page, row = int(p["table"][0, pos // 16]), pos % 16
+        p["K"][page, :, row] = float("nan")
+        p["V"][page, :, row] = float("nan") if bad == "nan" else float("inf")
+    p["V"][int(p["table"][1, 0]), 0, 3, 5] = float(bad)
+    out, lse = _run_attend(p, window=window)
+    K, V = _f64(p["K"]), _f64(p["V"])
+    with np.errstate(invalid="ignore"):
+        want, want_lse, _, logit = O.attend(_f64(p["Q"]), K, V, p["table"], p["q_start"], p["lens"], window=window)
+    got, got_lse = _f64(out), _f64(lse)
+    seen = np.isnan(want_lse)                                       # rows that see a NaN key: NaN throughout
+    assert np.isnan(got[seen]).all() and np.isnan(got_lse[seen]).all()
+    ok = ~seen
+    assert ok[:new // 2].all()
+    assert (np.abs(got_lse[ok] - want_lse[ok]) <= 1e-4).all()
+    fin = np.isfinite(want) & ok[..., None]
+    assert (np.isfinite(got) == np.isfinite(want))[ok].all()
+    A = np.nan_to_num(np.abs(V), nan=0.0, posinf=0.0).max()
+    assert (np.abs(got[fin] - want[fin]) <= (2.0 ** -6 if dtype == "bf16" else 2.0 ** -16) * A).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("new", [[3, 3, 2], [3, 40, 2], [16, 2, 1]])
+def test_what_a_row_does_not_see_in_long_caches(dtype, new):
+    """The same where sequences share workgroups and rows are joined from many stretches, among chunks too."""
+    lens = [20000, 700, 5000]
+    p = _attend_problem(13, dtype, lens, new, 4, 2, 64, 16)
+    for b, n in enumerate(lens):
+        page, row = int(p["table"][b, (n - 1) // 16]), (n - 1) % 16
+        p["K"][page, :, row] = float("nan")
+        p["V"][page, :, row] = float("nan")
+    out, lse = _run_attend(p)
+    with np.errstate(invalid="ignore"):
+        want, want_lse, _, _ = O.attend(_f64(p["Q"]), _f64(p["K"]), _f64(p["V"]), p["table"], p["q_start"], p["lens"])
+    got, got_lse = _f64(out), _f64(lse)
+    seen = np.isnan(want_lse)
+    last = np.zeros(sum(new), dtype=bool)
+    last[np.cumsum(new) - 1] = True
+    assert (seen == last[:, None]).all()                            # the last rows alone see the last tokens
+    assert np.isnan(got[seen]).all() and np.isnan(got_lse[seen]).all()
+    assert (np.abs(got_lse[~seen] - want_lse[~seen]) <= 1e-4).all()
+    A = np.nan_to_num(np.abs(_f64(p["V"])), nan=0.0).max()
+    assert (np.abs(got[~seen] - want[~seen]) <= (2.0 ** -6 if dtype == "bf16" else 2.0 ** -16) * A).all()
