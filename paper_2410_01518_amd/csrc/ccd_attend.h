@@ -26,8 +26,9 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 // are left to the even cut.  Evenly: `parts` workgroups, at most `rows` rows per unit; only_few: sequences of more than `few` rows are left to the grid.
 // join: rows of a unit, as far as the host knows.
 // turn: blocks of rows of the first half of one round (rows kernel), 0: the call is more than one round.
+// blocks: 0: the grid has row_blocks blocks of rows for every sequence; else it has these for all (find_block).
 struct AttendPlan {
-  int by_rows, rows, row_blocks, parts, chunk, few, only_few, turn, join;
+  int by_rows, rows, row_blocks, blocks, parts, chunk, few, only_few, turn, join;
 };
 
 // what a workgroup knows of its sequence
@@ -63,13 +64,11 @@ __device__ __forceinline__ Stretch cut_rows(const Paged& P, const Sequence& s, i
   c.begin = first < c.end ? first : c.end;
   const int len = c.end - c.begin;
   c.parts = (len + chunk - 1) / chunk;
-  c.chunk = chunk;
-  if (c.parts > parts) {
-    const int per = (len + parts - 1) / parts;
-    c.chunk = (per + 127) / 128 * 128;
-    c.parts = (len + c.chunk - 1) / c.chunk;
-  }
+  if (c.parts > parts) c.parts = parts;
   if (c.parts < 1) c.parts = 1;
+  // (alike, but for whole tiles of the kernels)
+  c.chunk = ((len + c.parts - 1) / c.parts + 63) / 64 * 64;
+  if (c.chunk > 0) c.parts = (len + c.chunk - 1) / c.chunk;
   return c;
 }
 
@@ -98,6 +97,31 @@ struct AttendArgs {
   float* lse;
   Partials part;
 };
+
+// Block k of the call's blocks of rows, counted from the last sequence's last: where the sequences' new tokens differ, a grid for the most of any
+// would be workgroups without rows for the largest part.  By a wave: 64 sequences at a time.
+__device__ __forceinline__ bool find_block(const Paged& P, const AttendPlan& pl, const AttendArgs& A, int k, int& b, int& r0) {
+  const int lane = threadIdx.x & 63;
+  for (int b0 = 0; b0 < P.B; b0 += 64) {
+    const int mine = P.B - 1 - (b0 + lane), rows = mine >= 0 ? load_sequence(P, mine, A.q_start, A.kv_len).m * P.G : 0;
+    const int n = rows > pl.few ? (rows + pl.rows - 1) / pl.rows : 0;
+    int to = n;
+#pragma unroll
+    for (int s = 1; s < 64; s <<= 1) {
+      const int y = __shfl_up(to, s);
+      if (lane >= s) to += y;
+    }
+    const uint64_t past = __ballot(to > k);
+    if (past != 0) {
+      const int at = __builtin_ctzll(past);
+      b = P.B - 1 - (b0 + at);
+      r0 = (__builtin_amdgcn_readlane(to, at) - 1 - k) * pl.rows;
+      return true;
+    }
+    k -= __builtin_amdgcn_readlane(to, 63);
+  }
+  return false;
+}
 
 // A weight of 0 takes a token out of a product only if its value is a number.  Where some rows see a token and others do not, and its value is infinite
 // or NaN, the products carry NaN into rows that do not see it.  Sums that come out as NaN where the rows are of several new tokens are therefore
@@ -149,6 +173,10 @@ __device__ __forceinline__ void redo_rows(const Paged& P, const AttendArgs& A, c
                                           bool whole_row, int part_no) {
   for (int r = r0; r < r1; r += step)
     redo_row<T, D>(P, A, sq, b, hkv, r, t_begin, t_end, whole_row, ((int64_t)part_no * P.tokens + sq.first + r / P.G) * P.Hq + hkv * P.G + r % P.G);
+}
+
+inline unsigned grid_size(const Paged& P, const AttendPlan& pl) {
+  return (unsigned)((int64_t)P.Hkv * pl.parts * (pl.blocks > 0 ? pl.blocks : (int64_t)P.B * pl.row_blocks));
 }
 
 // rows kernel (bf16): a workgroup per (unit, block of 128 rows, stretch), its waves share the tiles

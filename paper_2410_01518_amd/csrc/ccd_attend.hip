@@ -372,30 +372,33 @@ __device__ __forceinline__ bool attend_stretch(const Paged& P, const AttendArgs&
   return __syncthreads_or(none && r0 / P.G != (r1 - 1) / P.G);
 }
 
-// the call cut on a grid: (unit, block of rows, stretch)
-template <class T, int D, int NQ>
+// the call cut on a grid: (head, sequence, stretch, block of rows), or (head, stretch, block of the call)
+// LISTED: the latter (a kernel of its own: the search costs the others 0.9 of 13 us).
+template <class T, int D, int NQ, bool LISTED>
 __global__ __launch_bounds__(64 * kWaves, (split_waves<T, D, NQ>())) void attend_split_kernel(Paged P, AttendPlan pl, AttendArgs A) {
   __shared__ SplitLds<T, D, NQ> L;
   constexpr int kRows = 16 * NQ;
-  const int units = P.B * P.Hkv;
   int idx = blockIdx.x;
-  const int unit = idx % units;
-  idx /= units;
-  const int part_no = idx % pl.parts, block0 = pl.row_blocks - 1 - idx / pl.parts;       // the last rows see most: first
-  const int b = unit / P.Hkv, hkv = unit % P.Hkv;
-  const Sequence sq = load_sequence(P, b, A.q_start, A.kv_len);
-  const int rows_all = sq.m * P.G;
-  if (rows_all <= pl.few) return;
-  // (once more over all of it, row by row, if need be)
+  const int hkv = idx % P.Hkv;
+  idx /= P.Hkv;
+  const int own_b = idx % P.B;
+  if (!LISTED) idx /= P.B;
+  const int part_no = idx % pl.parts, turn_no = idx / pl.parts;
   bool again = false;
-  for (int pass = 0; pass < 2; ++pass) {
-    for (int r0 = block0 * kRows; r0 < rows_all; r0 += pl.row_blocks * kRows) {
+  for (int pass = 0; pass < 2; ++pass) {                   // (once more over all of it, row by row, if need be)
+    int b = own_b, r0 = (pl.row_blocks - 1 - turn_no) * kRows, k = turn_no;              // the last rows see most: first
+    while (!LISTED || find_block(P, pl, A, k, b, r0)) {
+      const Sequence sq = load_sequence(P, b, A.q_start, A.kv_len);
+      const int rows_all = sq.m * P.G;
+      if (rows_all <= pl.few || r0 >= rows_all) break;
       const int r1 = r0 + kRows < rows_all ? r0 + kRows : rows_all;
       const Stretch st = cut_rows(P, sq, r0, r1, pl.parts, pl.chunk);
-      if (part_no >= st.parts) continue;
       const int t_begin = st.begin + part_no * st.chunk, t_end = t_begin + st.chunk < st.end ? t_begin + st.chunk : st.end;
-      if (pass == 0) again = attend_stretch<T, D, NQ>(P, A, L, sq, b, hkv, r0, r1, t_begin, t_end, st.parts == 1, -1, part_no) || again;
-      else           redo_rows<T, D>(P, A, sq, b, hkv, r0 + (int)(threadIdx.x >> 6), r1, kWaves, t_begin, t_end, st.parts == 1, part_no);
+      if (part_no >= st.parts) {}
+      else if (pass == 0) again = attend_stretch<T, D, NQ>(P, A, L, sq, b, hkv, r0, r1, t_begin, t_end, st.parts == 1, -1, part_no) || again;
+      else                redo_rows<T, D>(P, A, sq, b, hkv, r0 + (int)(threadIdx.x >> 6), r1, kWaves, t_begin, t_end, st.parts == 1, part_no);
+      r0 += pl.row_blocks * kRows;                         // (more rows than the host expected)
+      k += pl.blocks;
     }
     if (__builtin_expect(!again, 1)) break;
   }
@@ -626,6 +629,20 @@ static int even_waves(int rows) { return rows == 16 ? split_waves<T, D, 1>() : s
 
 int attend_compute_units();
 
+// About the time (ns) of a grid that cuts `units` blocks of rows and heads into `parts` stretches each.  A workgroup takes `token` ns a token where it has a
+// compute unit alone, and 250 tokens' time for itself; two that share one take `shared` times that (in between, while some have one alone:
+// the rows kernel is bound by power).  Sums of stretches are written and read again by one more kernel.  What was measured in us:
+//   rows kernel, d 128, 32 heads of 8 groups, 8192 tokens, for 1, 2, 3, 4 stretches:  512 new tokens 160, 102, 101, 91;  1024: 162, 160, 168, 167;
+//   1536: 213, 235, 250, 237;  64 new tokens, for 4, 8, 16, 32: 52, 35, 29, 33
+//   fp32, 16 heads of 4 groups, 4096 tokens, for 1, 2, 3, 4, 6, 8:  d 64, 256 new tokens 111, 64, 71, 58, 77, 64;  d 128, 300: 167, 174, 128, 139, 140, 133
+static double grid_time(const Paged& P, int by_rows, int64_t units, int64_t len, int64_t parts, int64_t cus) {
+  const double token = by_rows ? (P.d == 64 ? 12 : 20) : (P.d == 64 ? 26 : 40), shared = by_rows || P.d == 64 ? 1.6 : 2.0;
+  const int64_t wgs = units * parts, rounds = wgs / (2 * cus), rest = wgs % (2 * cus);
+  const double last = rest == 0 ? 0 : rest <= cus ? 1 : by_rows && 2 * rest <= 3 * cus ? (1 + 3 * shared) / 4 : shared;
+  const double sums = parts == 1 ? 0 : 8000 + (double)wgs * (by_rows ? 128 : 32) * P.d * 8 / 4000;
+  return (rounds * shared + last) * ((double)len / parts + 250) * token + sums;
+}
+
 static AttendCuts plan_attend(const Paged& P, int dtype, int max_new, int max_len) {
   AttendCuts c{};
   const int64_t rows = (int64_t)max_new * P.G, cus = attend_compute_units();
@@ -667,17 +684,22 @@ static AttendCuts plan_attend(const Paged& P, int dtype, int max_new, int max_le
     g.rows = g.by_rows ? 128 : 32;
     g.few = c.even.few;
     g.row_blocks = (int)((rows + g.rows - 1) / g.rows);
-    const int64_t units = (int64_t)P.B * P.Hkv * g.row_blocks;
-    // stretches: until one round of the chip is full, of 256 tokens at least
-    int64_t parts = (cus * (g.by_rows ? 2 : 4) + units - 1) / units;
-    const int64_t most = (len + 255) / 256;
-    if (parts > most) parts = most;
-    if (parts > 64) parts = 64;
-    if (parts < 1) parts = 1;
+    // What the rows of all sequences fill, and one more block for each, is all that there can be.
+    const int64_t filled = ((int64_t)P.tokens * P.G + g.rows - 1) / g.rows, of_all = (int64_t)P.B * g.row_blocks;
+    if (of_all > filled + P.B) g.blocks = (int)(filled + P.B);
+    const int64_t units = P.Hkv * (filled < 1 ? 1 : filled < of_all ? filled : of_all);
+    if (P.window > 0 && len > (int64_t)P.window + g.rows / P.G + 1) len = (int64_t)P.window + g.rows / P.G + 1;      // of one block
+    const int64_t most = len < 256 * 64 ? (len + 255) / 256 : 64;
+    int64_t parts = 1;
+    double least = 0;
+    for (int64_t p = 1; p <= most; ++p) {
+      const double t = grid_time(P, g.by_rows, units, len, p, cus);
+      if (p == 1 || t < least) { least = t; parts = p; }
+    }
     g.chunk = (int)(((len + parts - 1) / parts + 127) / 128 * 128);
     g.parts = (int)((len + g.chunk - 1) / g.chunk);
     if (g.parts < 1) g.parts = 1;
-    if (g.by_rows && units * g.parts <= 2 * cus) g.turn = (g.row_blocks + 1) / 2;
+    if (g.by_rows && g.blocks == 0 && units * g.parts <= 2 * cus) g.turn = (g.row_blocks + 1) / 2;
   }
   return c;
 }
@@ -730,10 +752,11 @@ template <class T, int D>
 static void attend_launch(const Paged& P, const AttendCuts& c, const AttendArgs& even, const AttendArgs& grid, hipStream_t s) {
   if (c.grid.rows > 0) {
     const AttendPlan& pl = c.grid;
-    const dim3 wgs((unsigned)((int64_t)P.B * P.Hkv * pl.parts * pl.row_blocks)), block(64 * kWaves);
+    const dim3 wgs(grid_size(P, pl)), block(64 * kWaves);
     if (pl.by_rows)         launch_attend_rows(P, pl, grid, s);
-    else if (pl.rows == 16) launch(attend_split_kernel<T, D, 1>, wgs, block, s, P, pl, grid);
-    else                    launch(attend_split_kernel<T, D, 2>, wgs, block, s, P, pl, grid);
+    else if (pl.rows == 16) launch(attend_split_kernel<T, D, 1, false>, wgs, block, s, P, pl, grid);
+    else if (pl.blocks == 0) launch(attend_split_kernel<T, D, 2, false>, wgs, block, s, P, pl, grid);
+    else if constexpr (sizeof(T) == 4) launch(attend_split_kernel<T, D, 2, true>, wgs, block, s, P, pl, grid);
     if (pl.parts > 1) join_launch<T, D, false>(P, pl, grid, s);
   }
   if (c.even.rows > 0) {

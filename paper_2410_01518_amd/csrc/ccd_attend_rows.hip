@@ -56,20 +56,16 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_kernel(Paged P,
   __shared__ __align__(1024) char lds[2][2][kTileB];                               // [tile][keys, values]
   __shared__ uint32_t here[2][kRowWaves];                                          // [tile]: which of 16 tokens have a page
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-  const int units = P.B * P.Hkv;
   int idx = blockIdx.x;
-  const int unit = idx % units;
-  idx /= units;
+  const int hkv = idx % P.Hkv;
+  idx /= P.Hkv;
+  int b = idx % P.B;
+  if (pl.blocks == 0) idx /= P.B;
+  const int part_no = idx % pl.parts;
   // The last rows see most and come first.  Where the call is one round of two workgroups per compute unit, its second half runs the other way, so that
   // a compute unit has a long one and a short one.
   int turn_no = idx / pl.parts;
   if (pl.turn > 0 && turn_no >= pl.turn) turn_no = pl.row_blocks - 1 - (turn_no - pl.turn);
-  const int part_no = idx % pl.parts, block0 = pl.row_blocks - 1 - turn_no;
-  const int b = unit / P.Hkv, hkv = unit % P.Hkv;
-  const Sequence sq = load_sequence(P, b, A.q_start, A.kv_len);
-  const int rows_all = sq.m * P.G;
-  if (rows_all <= pl.few) return;
-  const int32_t* pages = A.table + (int64_t)b * P.table_width;
   const uint16_t* Kh = static_cast<const uint16_t*>(A.K) + hkv * P.head_stride;
   const uint16_t* Vh = static_cast<const uint16_t*>(A.V) + hkv * P.head_stride;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)&lds[0][0][0];
@@ -93,7 +89,13 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_kernel(Paged P,
     value_run[k] = run_offset((int64_t)row * P.row_stride * 2 + ((place ^ value_swap(row)) << 4), k);
   }
 
-  for (int r0 = block0 * kRows; r0 < rows_all; r0 += pl.row_blocks * kRows) {
+  // (beyond row_blocks, or blocks: more rows than the host expected)
+  for (int r0 = (pl.row_blocks - 1 - turn_no) * kRows;; r0 += pl.row_blocks * kRows, turn_no += pl.blocks) {
+    if (pl.blocks > 0 && !find_block(P, pl, A, turn_no, b, r0)) break;
+    const Sequence sq = load_sequence(P, b, A.q_start, A.kv_len);
+    const int rows_all = sq.m * P.G;
+    if (rows_all <= pl.few || r0 >= rows_all) break;
+    const int32_t* pages = A.table + (int64_t)b * P.table_width;
     const int r1 = r0 + kRows < rows_all ? r0 + kRows : rows_all;
     const Stretch st = cut_rows(P, sq, r0, r1, pl.parts, pl.chunk);
     if (part_no >= st.parts) continue;
@@ -371,7 +373,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_kernel(Paged P,
 
 template <int D>
 static void rows_launch(const Paged& P, const AttendPlan& pl, const AttendArgs& A, hipStream_t s) {
-  const dim3 grid((unsigned)((int64_t)P.B * P.Hkv * pl.parts * pl.row_blocks)), block(64 * kRowWaves);
+  const dim3 grid(grid_size(P, pl)), block(64 * kRowWaves);
   // (a lane's offset within the 16 rows of a run is 32 bits)
   const bool banded = P.div.page % 16 == 0 && P.row_stride * 2 * 16 < (int64_t)1 << 31;
   if (banded) launch(attend_rows_kernel<D, true>, grid, block, s, P, pl, A);

@@ -635,3 +635,20 @@ def test_what_a_row_does_not_see_in_long_caches(dtype, new):
     assert (np.abs(got_lse[~seen] - want_lse[~seen]) <= 1e-4).all()
     A = np.nan_to_num(np.abs(_f64(p["V"])), nan=0.0).max()
     assert (np.abs(got[~seen] - want[~seen]) <= (2.0 ** -6 if dtype == "bf16" else 2.0 ** -16) * A).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("heads", [(4, 2), (40, 1)])
+@pytest.mark.parametrize("option", ["plain", "window", "behind", "max_new"])
+def test_chunks_among_many_sequences(dtype, heads, option):
+    """More than 64 sequences of very different numbers of new tokens, none among them: blocks of rows are found from their sums.  max_new: fewer
+    expected than there are."""
+    rng = np.random.default_rng(14)
+    news = [int(x) for x in rng.choice([0, 1, 1, 1, 2, 9, 17, 40], 150)]
+    news[70], news[149], news[0] = 300, 70, 129
+    lens = [n + int(rng.integers(0, 260)) for n in news]
+    lens[3] = 0
+    p = _attend_problem(15, dtype, lens, news, heads[0], heads[1], 64, 16, pad=9)
+    kw = dict(window=50) if option == "window" else dict(behind=True) if option == "behind" else {}
+    out, lse = _run_attend(p, max_new=33 if option == "max_new" else None, **kw)
+    _check_attend(p, out, lse, dtype, **kw)
