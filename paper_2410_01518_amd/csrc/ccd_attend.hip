@@ -13,6 +13,49 @@ namespace ccd {
 
 constexpr int kWaves = 4;
 
+// Rows are read by quads of lanes, 64 bytes of a row each: a compute unit takes 125 bytes/ns of what L2 has so, but 38 where the matrix instructions'
+// operand is read as it is, 16 bytes of 16 rows side by side (76 by pairs of lanes, 32 bytes).  Register s of lane j of N (4, or 2) lanes
+// then has piece j of their row s, and has to have piece s of row j.
+template <int CTRL>
+__device__ __forceinline__ uint32_t from_lane(uint32_t x) { return (uint32_t)__builtin_amdgcn_mov_dpp((int)x, CTRL, 0xF, 0xF, true); }
+template <int CTRL>
+__device__ __forceinline__ void exchange(v4u& a, v4u& b, bool second) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t of_a = from_lane<CTRL>(a[e]), of_b = from_lane<CTRL>(b[e]);
+    a[e] = second ? of_b : a[e];
+    b[e] = second ? b[e] : of_a;
+  }
+}
+template <int N>
+__device__ __forceinline__ void turn(v4u* r, int lane) {
+  constexpr int kNext = 0xB1, kOver = 0x4E;                // quad_perm 1 0 3 2, 2 3 0 1
+#pragma unroll
+  for (int s = 0; s < N; s += 2) exchange<kNext>(r[s], r[s + 1], lane & 1);
+  if constexpr (N == 4) {
+    exchange<kOver>(r[0], r[2], lane & 2);
+    exchange<kOver>(r[1], r[3], lane & 2);
+  }
+}
+// the address that the s-th of the N lanes has
+template <int N, int S>
+__device__ __forceinline__ const char* of_row(const char* p) {
+  constexpr int kCtrl = N == 4 ? 0x55 * S : 0xA0 + 0x55 * S;
+  const uint64_t x = (uint64_t)p;
+  return (const char*)((uint64_t)from_lane<kCtrl>((uint32_t)(x >> 32)) << 32 | from_lane<kCtrl>((uint32_t)x));
+}
+// N registers of 16 bytes: pieces first + (lane % N) of the rows of the N lanes, whose own row is at p
+template <int N>
+__device__ __forceinline__ void load_rows(v4u* r, const char* p, int first, int lane) {
+  const int at = 16 * (first + (lane & (N - 1)));
+  r[0] = *reinterpret_cast<const v4u*>(of_row<N, 0>(p) + at);
+  r[1] = *reinterpret_cast<const v4u*>(of_row<N, 1>(p) + at);
+  if constexpr (N == 4) {
+    r[2] = *reinterpret_cast<const v4u*>(of_row<N, 2>(p) + at);
+    r[3] = *reinterpret_cast<const v4u*>(of_row<N, 3>(p) + at);
+  }
+}
+
 template <class T, int D>
 struct Tile;
 
@@ -31,7 +74,7 @@ struct Tile<uint16_t, D> {
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
       v4u w = {0, 0, 0, 0};
-      if (there) w = *reinterpret_cast<const v4u*>(row + 32 * s + 8 * (lane >> 4));
+      if (there) w = *reinterpret_cast<const v4u*>(row + 8 * (kSteps * (lane >> 4) + s));
       q.f[s] = __builtin_bit_cast(v8bf, w);
     }
   }
@@ -42,19 +85,23 @@ struct Tile<uint16_t, D> {
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) {
       const T* x = off[h] >= 0 ? X + off[h] : reinterpret_cast<const T*>(g_zero_row);
-#pragma unroll
-      for (int s = 0; s < kSteps; ++s) r[h][s] = *reinterpret_cast<const v4u*>(x + 32 * s + 8 * (lane >> 4));
+      load_rows<kSteps>(r[h], reinterpret_cast<const char*>(x), kSteps * (lane >> 4), lane);
     }
   }
   // 16-byte pieces of a row, exchanged in pairs by the row's number so that the rows a transposing read takes together (16 rows, one pair
   // of pieces) lie in different banks.  An exchange is an exclusive or of the piece's number, so a lane's places in a row differ by one, too.
   __device__ static int swap_of(int row) { return D == 128 ? (row & 7) << 1 : ((row >> 1) & 3) << 1; }
   __device__ static void store_values(const Values& r, char* lds, int lane) {
-    const int at = (lane & 15) * (D * 2) + (((lane >> 4) ^ swap_of(lane & 15)) << 4);
+    const int row = lane & 15 & ~(kSteps - 1), piece = kSteps * (lane >> 4) + (lane & (kSteps - 1));
+    const int at = row * (D * 2) + ((piece ^ swap_of(row)) << 4);
 #pragma unroll
     for (int h = 0; h < kHalves; ++h)
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) *reinterpret_cast<v4u*>(lds + ((at ^ (s << 6)) + 16 * h * (D * 2))) = r.v[h][s];
+      for (int s = 0; s < kSteps; ++s) *reinterpret_cast<v4u*>(lds + ((at ^ (swap_of(s) << 4)) + (16 * h + s) * (D * 2))) = r.v[h][s];
+  }
+  __device__ static void turn_keys(Keys& r, int lane) {
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) turn<kSteps>(r.k[h], lane);
   }
   // x[h][i]: logit of token 16 h + 4 (lane >> 4) + i for row lane & 15
   __device__ static void logits(v4f (&x)[kHalves], const Keys& r, const Query& q) {
@@ -90,7 +137,8 @@ struct Tile<uint16_t, D> {
 };
 
 // fp32: 16 tokens (v_mfma_f32_16x16x4_f32).  Elements of a row are counted in the products so that a lane's share of a row is 16 bytes:
-// step (j, i) takes element 16 j + 4 g + i of lane group g.
+// step (j, i) takes element 16 j + 4 g + i of lane group g.  (Read as the products take them: those take longer than the reading does.  By quads a
+// step of ragged chunks took 60.5 us, not 57.6.)
 template <int D>
 struct Tile<float, D> {
   using T = float;
@@ -113,6 +161,7 @@ struct Tile<float, D> {
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) r.k[s] = *reinterpret_cast<const float4*>(k + 16 * s + 4 * (lane >> 4));
   }
+  __device__ static void turn_keys(Keys&, int) {}
   // token 4 g + i, elements 64 c + 4 (lane & 15) ..
   __device__ static void load_values(Values& r, const T* V, const int64_t (&off)[kHalves], int lane) {
 #pragma unroll
@@ -256,6 +305,7 @@ __device__ __forceinline__ bool attend_stretch(const Paged& P, const AttendArgs&
     Tl::store_values(values, L.wave[wave], lane);
     if (more && !Tl::kValuesLate) Tl::load_values(values, Vh, off, lane);
     v4f x[NQ][Tl::kHalves];
+    Tl::turn_keys(keys, lane);
 #pragma unroll
     for (int j = 0; j < NQ; ++j) Tl::logits(x[j], keys, q[j]);
     if (more) {
@@ -662,13 +712,16 @@ static AttendCuts plan_attend(const Paged& P, int dtype, int max_new, int max_le
     int64_t wgs = (units * len + kEvenLeast - 1) / kEvenLeast;
     if (wgs > cus * waves) wgs = cus * waves;
     e.parts = (int)(wgs < 1 ? 1 : wgs);
-    // Short caches: where a workgroup per unit and stretch fits one round of the chip, nobody has to go on in a second unit.  A compute unit reads some
-    // 25 GB/s whatever its waves do, so stretches are short while there are compute units to spare; up to 512 tokens (1024, where the units alone
-    // fill half of the chip) they are not cut at all, which saves the second kernel.
-    const int64_t whole = 2 * units >= cus ? 1024 : 512;
-    for (int chunk = len <= whole ? (int)whole : 256; !many && chunk <= 1024; chunk *= 2) {
+    // Short caches: workgroups that stay with one unit.  Not cut at all, which saves the second kernel, where one workgroup reads its unit, at 50 bytes/ns
+    // (d 64 32, fp32 35), in the time that the second kernel costs and half of all units take at 5100 (half: lengths differ, and the host knows the
+    // longest alone).  Else cut as finely as there are compute units to spare.  32 query heads of 8 groups, d 128, us uncut / by 128 / by 256 /
+    // evenly: one sequence of 400 tokens 10.9 / 12.1 / 13.2 / 17.9, of 1000 16.1 / 12.8 / 13.6 / 14.6, of 4000 30.6 / 13.6 / 14.0 / 18.3;
+    // 16 of 1000 17.8 / 23.8 / 20.8 / 25.6; 32 of 2000 51 / 78 / 63 / 62; 256 of 100 .. 512 60 / 107 / 81 / 80.
+    const int64_t row = 2 * (int64_t)P.d * (dtype == 0 ? 4 : 2);
+    const bool uncut = len <= 2048 && len * row / (dtype == 0 ? 35 : P.d == 64 ? 32 : 50) <= 6000 + units * len * row / 10200;
+    for (int chunk = uncut ? 2048 : 128; !many && chunk <= 2048; chunk *= 2) {
       const int64_t chunks = (len + chunk - 1) / chunk;
-      if (chunks > 64 || units * chunks > (chunk == 256 ? cus : cus * waves) || (chunk == 1024 && len > 1024)) continue;
+      if (!uncut && (chunks > 64 || units * chunks > (chunk <= 256 ? cus : cus * waves) || chunk > 512)) continue;
       c.grid = e;
       c.grid.few = 0;
       c.grid.row_blocks = (int)((rows + e.rows - 1) / e.rows);
