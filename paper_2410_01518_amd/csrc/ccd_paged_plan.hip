@@ -81,7 +81,9 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(Paged P, PlanA
   __syncthreads();
   int take_at = take_to - take, give_at = give_to - give;
   int64_t new_at = new_to - fresh;
-  for (int w = 0; w < wave; ++w) { take_at += wave_take[w]; give_at += wave_give[w]; new_at += wave_new[w]; }
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w)
+    if (w < wave) { take_at += wave_take[w]; give_at += wave_give[w]; new_at += wave_new[w]; }
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
     const int b = tid * kPer + j;
@@ -104,25 +106,40 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(Paged P, PlanA
     const int64_t at = (int64_t)start + i;
     return (int)(at < P.n_pages ? at : at - P.n_pages);
   };
+  auto ring_behind = [&](int i) {                                    // of the free pages; more than the ring holds only where a table names pages twice
+    int64_t at = (int64_t)ring_at(free_now) + i;
+    if (at >= P.n_pages) at -= P.n_pages;
+    return (int)(at < P.n_pages ? at : at % P.n_pages);
+  };
   auto page_taken = [&](int rank) { return rank < free_now ? A.ring[ring_at(rank)] : -1; };
   auto p_before = [&](int b) { const int p = pages(A.before[b]); return p < W ? p : W; };
 
   if (blockIdx.x == 0) {
     for (int b = tid; b <= B; b += kPlanThreads) A.q_start[b] = first_token[b];
     // what is given back goes behind the free pages, in order, entries that name no page left out
-    for (int r0 = 0; r0 < all_gone; r0 += kPlanThreads * kPlanGive) {
-      const int r_mine = r0 + tid * kPlanGive;
-      int ids[kPlanGive], n = 0;
+    // (as few to a thread as they are: entries that follow one another, all searched for at once)
+    const int each = (all_gone + kPlanThreads - 1) / kPlanThreads, per = each < kPlanGive ? each : kPlanGive;
+    for (int r0 = 0; r0 < all_gone; r0 += kPlanThreads * per) {
+      const int r_mine = r0 + tid * per, mine = all_gone - r_mine < per ? all_gone - r_mine : per;
+      int ids[kPlanGive], of[kPlanGive] = {}, n = 0;
+#pragma unroll
+      for (int step = CAP / 2; step > 0; step >>= 1)
+#pragma unroll
+        for (int j = 0; j < kPlanGive; ++j) {
+          const int next = of[j] + step;
+          if (next < B && first_gone[next] <= r_mine + j) of[j] = next;
+        }
 #pragma unroll
       for (int j = 0; j < kPlanGive; ++j) {
-        const int r = r_mine + j;
         ids[j] = -1;
-        if (r < all_gone) {
-          const int b = find_sequence(first_gone, B, r);
-          const int64_t e = (int64_t)b * W + p_before(b) - (first_gone[b + 1] - r);
+        if (j < mine) {
+          const int64_t e = (int64_t)of[j] * W + p_before(of[j]) - (first_gone[of[j] + 1] - (r_mine + j));
           ids[j] = A.table[e];
           if (in_place) A.table_next[e] = -1;
         }
+      }
+#pragma unroll
+      for (int j = 0; j < kPlanGive; ++j) {
         if (ids[j] < 0 || ids[j] >= P.n_pages) ids[j] = -1;
         n += ids[j] >= 0;
       }
@@ -130,10 +147,11 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(Paged P, PlanA
       if (lane == 63) wave_give[wave] = to;
       __syncthreads();
       int at = given + to - n, sum = 0;
+#pragma unroll
       for (int w = 0; w < kPlanWaves; ++w) { if (w < wave) at += wave_give[w]; sum += wave_give[w]; }
 #pragma unroll
       for (int j = 0; j < kPlanGive; ++j)
-        if (ids[j] >= 0) A.ring[((int64_t)start + free_now + at++) % P.n_pages] = ids[j];
+        if (ids[j] >= 0) A.ring[ring_behind(at++)] = ids[j];
       __syncthreads();
       if (tid == 0) given += sum;
       __syncthreads();
