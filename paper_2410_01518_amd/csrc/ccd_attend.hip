@@ -490,11 +490,10 @@ __global__ __launch_bounds__(64 * kWaves, (split_waves<T, D, NQ>())) void attend
   constexpr int kRows = 16 * NQ, kThreads = 64 * kWaves;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, me = blockIdx.x;
   auto length = [&](int b) { return b < P.B ? span_of(P, pl, load_sequence(P, b, A.q_start, A.kv_len)).padded : 0; };
-  // all tokens; with few sequences also where each begins
-  const int mine = length(tid);
+  // all tokens, and how many stand before the thread's sequences, which are neighbours
+  const int each = (P.B + kThreads - 1) / kThreads, b_first = tid * each;
   int64_t run = 0;
-  for (int b = tid + kThreads; b < P.B; b += kThreads) run += length(b);
-  run += mine;
+  for (int j = 0; j < each; ++j) run += length(b_first + j);
   int64_t to = run;
 #pragma unroll
   for (int s = 1; s < 64; s <<= 1) {
@@ -513,15 +512,11 @@ __global__ __launch_bounds__(64 * kWaves, (split_waves<T, D, NQ>())) void attend
   int64_t at = me * per;
   const int64_t stop = at + per < all ? at + per : all;
   // the sequence that the stretch begins in, and where that begins
-  if (P.B <= kThreads) {
-    if (at < stop && mine > 0 && before * P.Hkv <= at && at < (before + mine) * P.Hkv) { found_b = tid; found_at = before * P.Hkv; }
-  } else if (tid == 0 && at < stop) {
-    int64_t sum = 0;
-    for (int b = 0; b < P.B; ++b) {
-      const int64_t n = (int64_t)length(b) * P.Hkv;
-      if (sum + n > at) { found_b = b; found_at = sum; break; }
-      sum += n;
-    }
+  if (at < stop && run > 0 && before * P.Hkv <= at && at < (before + run) * P.Hkv) {
+    int b = b_first;
+    for (int n = length(b); at >= (before + n) * P.Hkv; n = length(++b)) before += n;
+    found_b = b;
+    found_at = before * P.Hkv;
   }
   // rows that see nothing
   int2* meta = A.part.meta;

@@ -652,3 +652,17 @@ def test_chunks_among_many_sequences(dtype, heads, option):
     kw = dict(window=50) if option == "window" else dict(behind=True) if option == "behind" else {}
     out, lse = _run_attend(p, max_new=33 if option == "max_new" else None, **kw)
     _check_attend(p, out, lse, dtype, **kw)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_decoding_of_many_sequences_cut_evenly(dtype):
+    """More sequences than a workgroup has threads, a few of them long, some without a token."""
+    rng = np.random.default_rng(16)
+    lens = [int(x) for x in rng.integers(0, 60, 700)]
+    for b, n in ((0, 2300), (255, 1), (256, 1700), (511, 0), (699, 2500)):
+        lens[b] = n
+    news = [min(1, n) if b % 7 else 0 for b, n in enumerate(lens)]
+    news[699] = news[256] = 1
+    p = _attend_problem(17, dtype, lens, news, 4, 2, 64, 16, pad=2)
+    out, lse = _run_attend(p)
+    _check_attend(p, out, lse, dtype)
