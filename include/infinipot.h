@@ -224,7 +224,8 @@ typedef struct {
   int32_t B;                  /* sequences (rows of the block table)                                               */
   int32_t tokens;             /* rows of Q, out, lse, K_new, V_new, slots, positions: the step's new tokens and any  */
                               /* padding behind the last sequence's, which is left as it is                         */
-  int32_t Hq, Hkv, d;         /* query heads, KV heads (Hq % Hkv == 0), head dimension 64 or 128                    */
+  int32_t Hq, Hkv, d;         /* query heads, KV heads (Hq % Hkv == 0; tokens * Hq and B * Hkv < 2^31), head       */
+                              /* dimension 64 or 128                                                                */
   int32_t dtype;              /* CCD_FP32 or CCD_BF16, for Q, out, K, V                                             */
   int32_t page, n_pages;      /* tokens per page, pages of the cache; page * n_pages < 2^31                         */
   int32_t table_width;        /* entries per row of the block table; page * table_width < 2^31                      */

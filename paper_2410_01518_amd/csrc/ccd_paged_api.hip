@@ -40,7 +40,7 @@ static int check_paged(const ccd_paged_t* c, int need) {
   if (need & kNew) { strides[n++] = {c->new_stride_t, c->d}; strides[n++] = {c->new_stride_h, c->d}; }
   if (need & kAttend) {
     if (c->Hq < 1 || c->Hq % c->Hkv != 0) return CCD_EINVAL;
-    if ((int64_t)c->tokens * c->Hq > 0x7FFFFFFF) return CCD_EINVAL;
+    if ((int64_t)c->tokens * c->Hq > 0x7FFFFFFF || (int64_t)c->B * c->Hkv > 0x7FFFFFFF) return CCD_EINVAL;
     if (c->window < 0 || (c->behind != 0 && c->behind != 1) || c->max_new < 0 || c->max_len < 0) return CCD_EINVAL;
     if (!(c->scale >= 0.f) || isinf(c->scale)) return CCD_EINVAL;
     strides[n++] = {c->q_stride_b, 0}; strides[n++] = {c->q_stride_t, c->d}; strides[n++] = {c->q_stride_h, c->d};

@@ -309,8 +309,14 @@ def _here(*tensors):
 
 
 def _int32(*tensors):
-    for t in tensors:
+    """Pairs of an index tensor and the entries that the descriptor says it has."""
+    for t, entries in tensors:
         assert t.dtype is torch.int32 and t.is_contiguous(), "contiguous int32 needed"
+        assert t.numel() >= entries, f"{t.numel()} entries, {entries} needed"
+
+
+def _turns(turns, rope):
+    assert turns.dtype is torch.int64 and turns.is_contiguous() and turns.numel() >= rope.rot // 2, "turns as rope_turns gives them"
 
 
 def make_plan(block_table, *, tokens, page, n_pages) -> ccd_paged_t:
@@ -391,7 +397,9 @@ def ccd_paged_plan(paged, len_before, len_after, block_table, block_table_next, 
                    stream=None) -> int:
     """len_before, len_after [B], block_table and block_table_next [B, table_width] (may be one), free_pages [n_pages], cursor and
     cursor_next [4] (may be one), q_start [B + 1], slots and positions [tokens]: int32."""
-    _int32(len_before, len_after, block_table, block_table_next, free_pages, cursor, cursor_next, q_start, slots, positions)
+    B, entries = paged.B, paged.B * paged.table_width
+    _int32((len_before, B), (len_after, B), (block_table, entries), (block_table_next, entries), (free_pages, paged.n_pages), (cursor, 4), (cursor_next, 4),
+           (q_start, B + 1), (slots, paged.tokens), (positions, paged.tokens))
     _here(block_table)
     return _check(lib().ccd_paged_plan(ctypes.byref(paged), _ptr(len_before), _ptr(len_after), _ptr(block_table), _ptr(block_table_next),
                                        _ptr(free_pages), _ptr(cursor), _ptr(cursor_next), _ptr(q_start), _ptr(slots), _ptr(positions),
@@ -400,26 +408,31 @@ def ccd_paged_plan(paged, len_before, len_after, block_table, block_table_next, 
 
 def ccd_rope(rope, X, positions, turns, Y, stream=None) -> int:
     """positions int32 [tokens]; turns as rope_turns gives them; Y may be X."""
-    _int32(positions)
+    _int32((positions, rope.tokens))
+    _turns(turns, rope)
     _here(X, positions)
     return _check(lib().ccd_rope(ctypes.byref(rope), _ptr(X), _ptr(positions), _ptr(turns), _ptr(Y), _stream(stream)))
 
 
 def ccd_paged_append(paged, K_new, V_new, slots, K_pages, V_pages, rope=None, positions=None, turns=None, stream=None) -> int:
     """K_new and V_new have the same strides, as have K_pages and V_pages; with a rope descriptor the keys are embedded at `positions`."""
-    _int32(slots)
+    _int32((slots, paged.tokens))
+    assert K_new.stride() == V_new.stride() and K_new.shape == V_new.shape and K_new.dtype == V_new.dtype == K_pages.dtype
+    assert K_pages.stride() == V_pages.stride() and K_pages.shape == V_pages.shape and K_pages.dtype == V_pages.dtype
+    if rope is not None:
+        _int32((positions, paged.tokens))
+        _turns(turns, rope)
     _here(K_pages, slots)
-    assert K_new.stride() == V_new.stride() and K_pages.stride() == V_pages.stride()
-    assert rope is None or (positions is not None and turns is not None)
     return _check(lib().ccd_paged_append(ctypes.byref(paged), None if rope is None else ctypes.byref(rope), _ptr(K_new), _ptr(V_new), _ptr(slots),
                                          _ptr(positions), _ptr(turns), _ptr(K_pages), _ptr(V_pages), _stream(stream)))
 
 
 def ccd_paged_attend(paged, Q, K_pages, V_pages, block_table, q_start, kv_len, out, lse, workspace, stream=None) -> int:
     """block_table [B, table_width], q_start [B + 1], kv_len [B]: int32; lse fp32 or None."""
-    _int32(block_table, q_start, kv_len)
+    _int32((block_table, paged.B * paged.table_width), (q_start, paged.B + 1), (kv_len, paged.B))
+    assert K_pages.stride() == V_pages.stride() and K_pages.shape == V_pages.shape
+    assert Q.dtype == out.dtype == K_pages.dtype == V_pages.dtype and (lse is None or lse.dtype == torch.float32)
     _here(Q, K_pages, block_table)
-    assert K_pages.stride() == V_pages.stride()
     return _check(lib().ccd_paged_attend(ctypes.byref(paged), _ptr(Q), _ptr(K_pages), _ptr(V_pages), _ptr(block_table), _ptr(q_start), _ptr(kv_len),
                                          _ptr(out), _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel(),
                                          _stream(stream)))

@@ -18,6 +18,16 @@ import torch
 from . import infinipot as ip
 
 
+def _workspace(held, paged, device):
+    """(the workspace to keep, the workspace of this call): the one held, if it is large enough.  A graph that is being captured has one of its own,
+    which nobody frees or uses between its replays."""
+    if torch.cuda.is_current_stream_capturing():
+        return held, ip.alloc_paged_workspace(paged, device)
+    if held is None or held.numel() < ip.ccd_paged_workspace_bytes(paged):
+        held = ip.alloc_paged_workspace(paged, device)
+    return held, held
+
+
 class MemoryPot:
     def __init__(self, B, L, Hkv, d, n_cap, k, T, *, dtype=torch.bfloat16, pool_w=7, pool_mode=ip.CCD_POOL_MAX,
                  device="cuda"):
@@ -59,24 +69,30 @@ class MemoryPot:
         q = Q if one else Q.reshape(-1, *Q.shape[2:])
         out = torch.empty_like(Q, memory_format=torch.contiguous_format) if out is None else out
         lse = torch.empty(Q.shape[:-1], dtype=torch.float32, device=Q.device) if lse is None else lse
+        table, q_start, kv_len = self._attn_index(pages, m, Q.device)
+        o, s = (out, lse) if one else (out.view(-1, *out.shape[2:]), lse.view(-1, *lse.shape[2:]))
+        paged = ip.make_paged(keys, tokens=pages * m, block_table=table, Q=q, out=o, lse=s, window=window, behind=behind, max_new=m, max_len=max(1, self.n_valid))
+        self._attn_ws, ws = _workspace(self._attn_ws, paged, Q.device)
+        rc = ip.ccd_paged_attend(paged, q, keys, values, table, q_start, kv_len, o, s, ws)
+        assert rc == ip.CCD_OK, rc
+        return out, lse
+
+    def _attn_index(self, pages, m, device):
+        """Block table, q_start and kv_len of `pages` pots of m query tokens each."""
+        def rows():
+            return (torch.arange(pages, dtype=torch.int32, device=device)[:, None].contiguous(),
+                    torch.arange(pages + 1, dtype=torch.int32, device=device) * m)
+        if torch.cuda.is_current_stream_capturing():        # a graph keeps its own: nothing is written before it is replayed
+            return *rows(), torch.full((pages,), self.n_valid, dtype=torch.int32, device=device)
         if (pages, m) not in self._attn_rows:
-            self._attn_rows[pages, m] = (torch.arange(pages, dtype=torch.int32, device=Q.device)[:, None].contiguous(),
-                                         torch.arange(pages + 1, dtype=torch.int32, device=Q.device) * m)
-        table, q_start = self._attn_rows[pages, m]
+            self._attn_rows[pages, m] = rows()
         kv_len, held = self._attn_len
         if kv_len is None:
-            kv_len = torch.empty(self.B * self.L, dtype=torch.int32, device=Q.device)
+            kv_len = torch.empty(self.B * self.L, dtype=torch.int32, device=device)
         if held != self.n_valid:
             kv_len.fill_(self.n_valid)
             self._attn_len = (kv_len, self.n_valid)
-        o, s = (out, lse) if one else (out.view(-1, *out.shape[2:]), lse.view(-1, *lse.shape[2:]))
-        paged = ip.make_paged(keys, tokens=pages * m, block_table=table, Q=q, out=o, lse=s, window=window, behind=behind, max_new=m, max_len=max(1, self.n_valid))
-        need = ip.ccd_paged_workspace_bytes(paged)
-        if self._attn_ws is None or self._attn_ws.numel() < need:
-            self._attn_ws = ip.alloc_paged_workspace(paged, Q.device)
-        rc = ip.ccd_paged_attend(paged, q, keys, values, table, q_start, kv_len[:pages], o, s, self._attn_ws)
-        assert rc == ip.CCD_OK, rc
-        return out, lse
+        return *self._attn_rows[pages, m], kv_len[:pages]
 
     def distill(self, Q_cat, scores=None, lse=None) -> int:
         """One CCD compression if the pot is full; returns the library's code (CCD_OK or CCD_NOOP).  lse: the catalyst rows' log-sum-exps, as
@@ -125,7 +141,8 @@ class PagedPots:
         return -(-length // self.page)
 
     def step(self, lengths) -> int:
-        """Plans the step that leaves sequence b with lengths[b] tokens; returns the number of new ones."""
+        """Plans the step that leaves sequence b with lengths[b] tokens; returns the number of new ones.  The lengths come from the host: a step is
+        not captured into a graph, its `append` and `attend` may be (for steps of the same number of rows)."""
         lengths = [int(n) for n in lengths]
         new = [max(0, n - o) for o, n in zip(self.lengths, lengths)]
         if len(lengths) != len(self.lengths) or min(lengths) < 0 or self.pages(max(lengths)) > self.table.shape[1] or sum(new) > self.step_tokens:
@@ -157,16 +174,15 @@ class PagedPots:
         out = torch.empty_like(Q, memory_format=torch.contiguous_format) if out is None else out
         lse = torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device) if lse is None else lse
         paged = self._paged(layer, Q.shape[0], Q=Q, out=out, lse=lse)
-        need = ip.ccd_paged_workspace_bytes(paged)
-        if self._ws is None or self._ws.numel() < need:
-            self._ws = ip.alloc_paged_workspace(paged, Q.device)
-        rc = ip.ccd_paged_attend(paged, Q, self.K[:, layer], self.V[:, layer], self.table, self.q_start, self.after, out, lse, self._ws)
+        self._ws, ws = _workspace(self._ws, paged, Q.device)
+        rc = ip.ccd_paged_attend(paged, Q, self.K[:, layer], self.V[:, layer], self.table, self.q_start, self.after, out, lse, ws)
         assert rc == ip.CCD_OK, rc
         return out, lse
 
     def distill(self, b, page_id, Q_cat, novelty, keep_idx, workspace, *, k, T, pool_w=7, pool_mode=ip.CCD_POOL_MAX, lse=None) -> int:
         """Compresses the pot of sequence b, the page page_id that it holds (one page per sequence), if it is full: Q_cat [1, L, Hq, P, d], novelty
-        [1, page] or [1, L, Hkv, page], keep_idx [1, L, Hkv, k].  Returns the library's code; after CCD_OK the sequence has k tokens."""
+        [1, page] or [1, L, Hkv, page], keep_idx [1, L, Hkv, k].  Returns the library's code; after CCD_OK the sequence has k tokens, as of the
+        next step."""
         assert self.table.shape[1] == 1, "distillation needs pages that are whole pots"
         K, V = self.K[page_id: page_id + 1], self.V[page_id: page_id + 1]
         shape = ip.make_shape(Q_cat, K, novelty, k=k, T=T, pool_w=pool_w, pool_mode=pool_mode, n_valid=max(1, self.lengths[b]))

@@ -167,3 +167,84 @@ def test_streaming_recipe_runs():
         out, lse = pot.attend(torch.randn((1, 1, cfg.Hq, 128, cfg.d), generator=g, device="cuda").bfloat16())
         assert torch.isfinite(out.float()).all() and torch.isfinite(lse).all()
     assert pot.calls == 1
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_captured_attention_of_pots_stands_for_itself(dtype):
+    """A graph captured before anything ran eagerly, replayed among eager calls over other lengths, other numbers of tokens and larger workspaces."""
+    pot = MemoryPot(2, 2, 2, 64, 3000, 100, 50, dtype=DT[dtype])
+    _fill(pot, 217, 1)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    Q = torch.randn((2, 2, 6, 3, 64), generator=g, device="cuda").to(DT[dtype])
+    big = torch.randn((2, 2, 6, 500, 64), generator=g, device="cuda").to(DT[dtype])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        out, lse = pot.attend(Q)
+    before = pot.attend(Q)                                   # eager, before the first replay
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, before[0]) and torch.equal(lse, before[1])
+    for n in (1, 1500):
+        _fill(pot, n, 3)
+        pot.attend(Q)
+        _, large = pot.attend(big, behind=True)
+        out.zero_()
+        lse.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, before[0]) and torch.equal(lse, before[1])
+        assert torch.isfinite(large).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_captured_attention_over_a_pool(dtype):
+    """append and attend of a decoding step in a graph: replayed for later steps of the same number of rows, between eager calls of others."""
+    lens, L, Hq, Hkv, d = [40, 700, 1], 2, 4, 2, 64
+    pools = [PagedPots(3, 80, 16, 1100, 64, L, Hq, Hkv, d, dtype=DT[dtype]) for _ in range(2)]
+    g = torch.Generator(device="cuda").manual_seed(4)
+    make = lambda rows, heads: torch.randn((rows, heads, d), generator=g, device="cuda").to(DT[dtype])            # noqa: E731
+    for start in range(0, 700, 20):                          # fill both alike
+        now = [min(n, start + 20) for n in lens]
+        rows = [p.step(now) for p in pools][0]
+        K, V = make(64, Hkv), make(64, Hkv)
+        for p in pools:
+            for layer in range(L):
+                p.append(layer, K, V)
+    K, V, Q = make(3, Hkv), make(3, Hkv), make(3, Hq)
+    now = [n + 1 for n in lens]
+    for p in pools:
+        assert p.step(now) == 3
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        for layer in range(L):
+            pools[0].append(layer, K, V)
+        outs = [pools[0].attend(layer, Q) for layer in range(L)]
+    for step in range(4):
+        if step:
+            now = [n + 1 for n in now]
+            for p in pools:
+                assert p.step(now) == 3
+            for t, heads in ((K, Hkv), (V, Hkv), (Q, Hq)):
+                t.copy_(make(3, heads))
+        graph.replay()
+        for layer in range(L):
+            pools[1].append(layer, K, V)
+        want = [pools[1].attend(layer, Q) for layer in range(L)]
+        torch.cuda.synchronize()
+        for (o, s), (wo, ws) in zip(outs, want):
+            # (the cut may differ: the graph keeps the lengths that the host knew at its capture)
+            slack = 2.0 ** -7 if dtype == "bf16" else 2.0 ** -18
+            A = pools[1].V.abs().max().double()
+            assert ((o.double() - wo.double()).abs() <= slack * A).all() and ((s - ws).abs() <= 1e-4).all()
+        if step == 1:                                        # a chunk in between, on both
+            now = [now[0] + 50, now[1], now[2] + 3]
+            k, v, q = make(64, Hkv), make(64, Hkv), make(64, Hq)
+            for p in pools:
+                assert p.step(now) == 53
+                for layer in range(L):
+                    p.append(layer, k, v)
+                    p.attend(layer, q)

@@ -190,3 +190,39 @@ def test_reference_rope_pins():
     y = O.rope(x, [12345], O.frequencies(6, 10000.0), half=False)
     np.testing.assert_allclose(np.linalg.norm(y), np.linalg.norm(x))
     np.testing.assert_allclose(O.rope(y, [12345], O.frequencies(6, 10000.0), half=False, inverse=True), x)
+
+
+def test_more_units_than_can_be_counted_are_refused():
+    assert _attend(_paged(B=1 << 20, table_width=1, Hkv=1 << 12, Hq=1 << 12, tokens=6)) == ip.CCD_EINVAL
+    assert ip.ccd_paged_workspace_bytes(_paged(B=1 << 20, table_width=1, Hkv=1 << 12, Hq=1 << 12, tokens=6)) == 0
+
+
+def test_the_binding_refuses_index_tensors_that_are_too_short():
+    i = lambda n: torch.zeros(n, dtype=torch.int32)                            # noqa: E731
+    c = _paged()
+    good = dict(len_before=i(2), len_after=i(2), block_table=i(8), block_table_next=i(8), free_pages=i(10), cursor=i(4), cursor_next=i(4), q_start=i(3),
+                slots=i(6), positions=i(6))
+    for name, t in good.items():
+        with pytest.raises(AssertionError, match="needed"):
+            ip.ccd_paged_plan(c, **{**good, name: t[:-1]})
+        with pytest.raises(AssertionError, match="int32"):
+            ip.ccd_paged_plan(c, **{**good, name: t.float()})
+    K = torch.zeros((10, 2, 16, 128), dtype=torch.bfloat16)
+    Q, K_new = torch.zeros((6, 8, 128), dtype=torch.bfloat16), torch.zeros((6, 2, 128), dtype=torch.bfloat16)
+    attend = dict(block_table=i(8), q_start=i(3), kv_len=i(2))
+    for name, t in attend.items():
+        with pytest.raises(AssertionError, match="needed"):
+            ip.ccd_paged_attend(c, Q, K, K.clone(), out=Q.clone(), lse=None, workspace=None, **{**attend, name: t[:-1]})
+    with pytest.raises(AssertionError):
+        ip.ccd_paged_attend(c, Q.float(), K, K.clone(), out=Q.clone(), lse=None, workspace=None, **attend)
+    rope = ip.make_rope(K_new, rot=64)
+    with pytest.raises(AssertionError, match="needed"):
+        ip.ccd_paged_append(c, K_new, K_new.clone(), i(5), K, K.clone())
+    with pytest.raises(AssertionError, match="needed"):
+        ip.ccd_paged_append(c, K_new, K_new.clone(), i(6), K, K.clone(), rope=rope, positions=i(5), turns=torch.zeros(32, dtype=torch.int64))
+    with pytest.raises(AssertionError, match="turns"):
+        ip.ccd_paged_append(c, K_new, K_new.clone(), i(6), K, K.clone(), rope=rope, positions=i(6), turns=torch.zeros(31, dtype=torch.int64))
+    with pytest.raises(AssertionError):
+        ip.ccd_paged_append(c, K_new, K_new.float(), i(6), K, K.clone())
+    with pytest.raises(AssertionError, match="turns"):
+        ip.ccd_rope(rope, K_new, i(6), torch.zeros(32, dtype=torch.int32), K_new)
