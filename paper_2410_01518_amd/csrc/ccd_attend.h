@@ -179,7 +179,7 @@ inline unsigned grid_size(const Paged& P, const AttendPlan& pl) {
   return (unsigned)((int64_t)P.Hkv * pl.parts * (pl.blocks > 0 ? pl.blocks : (int64_t)P.B * pl.row_blocks));
 }
 
-// rows kernel (bf16): a workgroup per (unit, block of 128 rows, stretch), its waves share the tiles
-void launch_attend_rows(const Paged& P, const AttendPlan& pl, const AttendArgs& A, hipStream_t s);
+// rows kernel (bf16): a workgroup per (unit, block of 128 rows, stretch), its waves share the tiles; with it the even cut, if there is one
+void launch_attend_rows(const Paged& P, const AttendPlan& pl, const AttendArgs& A, const AttendPlan& even, const Partials& even_part, hipStream_t s);
 
 }  // namespace ccd

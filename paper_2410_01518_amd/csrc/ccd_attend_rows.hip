@@ -11,7 +11,7 @@
 // where a product of 8192^3 reaches 1.2 - 1.3.  The matrix cores are busy 52 % of the cycles and the clock is at 1.9 - 2.0 GHz: what is left is bound by power
 // (removing all bank conflicts and a tenth of the instructions took 20 % of the cycles and 4 % of the time).  Waves of 64 rows, one per SIMD,
 // read LDS half as often and keep 2.4 GHz, but a wave alone cannot cover its own waits: 1010 - 1040 us, and coarser blocks for short calls.
-#include "ccd_attend.h"
+#include "ccd_attend_few.h"
 
 #include <type_traits>
 
@@ -48,15 +48,19 @@ __device__ __forceinline__ float largest(const v16f& x) {
 }
 
 // BANDED: pages of whole runs of 16 rows, so that a wave's 16 rows of a tile lie in one page
+template <int D>
+struct RowsLds {
+  __align__(1024) char tile[2][2][kTile * D * 2];                                  // [tile][keys, values]
+  uint32_t here[2][kRowWaves];                                                     // [tile]: which of 16 tokens have a page
+};
 template <int D, bool BANDED>
-__global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_kernel(Paged P, AttendPlan pl, AttendArgs A) {
+__device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl, const AttendArgs& A, RowsLds<D>& L, int idx) {
   constexpr int kRows = 32 * kRowWaves, kRowB = D * 2, kPieces = D / 8;            // 16-byte pieces of a row
   constexpr int kPerLoad = 64 / kPieces, kLoads = 16 / kPerLoad;                   // rows per load instruction, loads of a wave's 16 rows
   constexpr int kTileB = kTile * kRowB, kSteps = D / 16, kBlocks = D / 32;
-  __shared__ __align__(1024) char lds[2][2][kTileB];                               // [tile][keys, values]
-  __shared__ uint32_t here[2][kRowWaves];                                          // [tile]: which of 16 tokens have a page
+  auto& lds = L.tile;
+  auto& here = L.here;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5;
-  int idx = blockIdx.x;
   const int hkv = idx % P.Hkv;
   idx /= P.Hkv;
   int b = idx % P.B;
@@ -371,18 +375,41 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_kernel(Paged P,
   }
 }
 
-template <int D>
-static void rows_launch(const Paged& P, const AttendPlan& pl, const AttendArgs& A, hipStream_t s) {
-  const dim3 grid(grid_size(P, pl)), block(64 * kRowWaves);
-  // (a lane's offset within the 16 rows of a run is 32 bits)
-  const bool banded = P.div.page % 16 == 0 && P.row_stride * 2 * 16 < (int64_t)1 << 31;
-  if (banded) launch(attend_rows_kernel<D, true>, grid, block, s, P, pl, A);
-  else        launch(attend_rows_kernel<D, false>, grid, block, s, P, pl, A);
+template <int D, bool BANDED>
+__global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_kernel(Paged P, AttendPlan pl, AttendArgs A) {
+  __shared__ RowsLds<D> L;
+  attend_rows<D, BANDED>(P, pl, A, L, blockIdx.x);
 }
 
-void launch_attend_rows(const Paged& P, const AttendPlan& pl, const AttendArgs& A, hipStream_t s) {
-  if (P.d == 64) rows_launch<64>(P, pl, A, s);
-  else           rows_launch<128>(P, pl, A, s);
+// Chunks, and the sequences of few rows among them: their workgroups come last and fill what the others leave idle.  (17 sequences of 1 to 969 new tokens over
+// 519 to 8192, 32 heads of 8 groups: 238 us, 266 one after the other.)
+template <int D, bool BANDED, int NQ>
+__global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_mixed_kernel(Paged P, AttendPlan grid, AttendPlan even, AttendArgs A, Partials even_part, int grid_wgs) {
+  using Few = EvenLds<uint16_t, D, NQ>;
+  __shared__ __align__(1024) char lds[sizeof(RowsLds<D>) > sizeof(Few) ? sizeof(RowsLds<D>) : sizeof(Few)];
+  if ((int)blockIdx.x < grid_wgs) {
+    attend_rows<D, BANDED>(P, grid, A, reinterpret_cast<RowsLds<D>&>(lds), blockIdx.x);
+  } else {
+    A.part = even_part;
+    attend_evenly<uint16_t, D, NQ>(P, even, A, reinterpret_cast<Few&>(lds), blockIdx.x - grid_wgs, even.parts);
+  }
+}
+
+template <int D, bool BANDED>
+static void rows_launch(const Paged& P, const AttendPlan& pl, const AttendArgs& A, const AttendPlan& even, const Partials& even_part, hipStream_t s) {
+  static_assert(kRowWaves == kWaves);
+  const int wgs = (int)grid_size(P, pl);
+  const dim3 all((unsigned)(wgs + even.parts)), block(64 * kRowWaves);
+  if (even.rows == 0)       launch(attend_rows_kernel<D, BANDED>, all, block, s, P, pl, A);
+  else if (even.rows == 16) launch(attend_rows_mixed_kernel<D, BANDED, 1>, all, block, s, P, pl, even, A, even_part, wgs);
+  else                      launch(attend_rows_mixed_kernel<D, BANDED, 2>, all, block, s, P, pl, even, A, even_part, wgs);
+}
+
+void launch_attend_rows(const Paged& P, const AttendPlan& pl, const AttendArgs& A, const AttendPlan& even, const Partials& even_part, hipStream_t s) {
+  // (a lane's offset within the 16 rows of a run is 32 bits)
+  const bool banded = P.div.page % 16 == 0 && P.row_stride * 2 * 16 < (int64_t)1 << 31;
+  if (P.d == 64) banded ? rows_launch<64, true>(P, pl, A, even, even_part, s) : rows_launch<64, false>(P, pl, A, even, even_part, s);
+  else           banded ? rows_launch<128, true>(P, pl, A, even, even_part, s) : rows_launch<128, false>(P, pl, A, even, even_part, s);
 }
 
 }  // namespace ccd
