@@ -26,9 +26,10 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 // are left to the even cut.  Evenly: `parts` workgroups, at most `rows` rows per unit; only_few: sequences of more than `few` rows are left to the grid.
 // join: rows of a unit, as far as the host knows.
 // turn: blocks of rows of the first half of one round (rows kernel), 0: the call is more than one round.
+// wide: workgroups of eight waves, not four.
 // blocks: 0: the grid has row_blocks blocks of rows for every sequence; else it has these for all (find_block).
 struct AttendPlan {
-  int by_rows, rows, row_blocks, blocks, parts, chunk, few, only_few, turn, join;
+  int by_rows, rows, row_blocks, blocks, parts, chunk, few, only_few, turn, join, wide;
 };
 
 // what a workgroup knows of its sequence

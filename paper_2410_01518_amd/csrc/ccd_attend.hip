@@ -3,10 +3,10 @@
 
 namespace ccd {
 
-template <class T, int D, int NQ>
-__global__ __launch_bounds__(64 * kWaves, (split_waves<T, D, NQ>())) void attend_split_kernel(Paged P, AttendPlan pl, AttendArgs A) {
-  __shared__ SplitLds<T, D, NQ> L;
-  attend_on_grid<T, D, NQ, false>(P, pl, A, L, blockIdx.x);
+template <class T, int D, int NQ, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, (WAVES == 8 ? 2 : split_waves<T, D, NQ>())) void attend_split_kernel(Paged P, AttendPlan pl, AttendArgs A) {
+  __shared__ SplitLds<T, D, NQ, WAVES> L;
+  attend_on_grid<T, D, NQ, WAVES, false>(P, pl, A, L, blockIdx.x);
 }
 
 template <class T, int D, int NQ>
@@ -21,7 +21,7 @@ template <class T, int D, int NQ, bool LISTED>
 __global__ __launch_bounds__(64 * kWaves, 2) void attend_mixed_kernel(Paged P, AttendPlan grid, AttendPlan even, AttendArgs A, Partials even_part, int grid_wgs) {
   __shared__ __align__(16) char lds[sizeof(SplitLds<T, D, 2>) > sizeof(EvenLds<T, D, NQ>) ? sizeof(SplitLds<T, D, 2>) : sizeof(EvenLds<T, D, NQ>)];
   if ((int)blockIdx.x < grid_wgs) {
-    attend_on_grid<T, D, 2, LISTED>(P, grid, A, reinterpret_cast<SplitLds<T, D, 2>&>(lds), blockIdx.x);
+    attend_on_grid<T, D, 2, kWaves, LISTED>(P, grid, A, reinterpret_cast<SplitLds<T, D, 2>&>(lds), blockIdx.x);
   } else {
     A.part = even_part;
     attend_evenly<T, D, NQ>(P, even, A, reinterpret_cast<EvenLds<T, D, NQ>&>(lds), blockIdx.x - grid_wgs, even.parts);
@@ -171,13 +171,15 @@ static AttendCuts plan_attend(const Paged& P, int dtype, int max_new, int max_le
     int64_t wgs = (units * len + kEvenLeast - 1) / kEvenLeast;
     if (wgs > cus * waves) wgs = cus * waves;
     e.parts = (int)(wgs < 1 ? 1 : wgs);
-    // Short caches: workgroups that stay with one unit.  Not cut at all, which saves the second kernel, where one workgroup reads its unit, at 50 bytes/ns
-    // (d 64 32, fp32 35), in the time that the second kernel costs and half of all units take at 5100 (half: lengths differ, and the host knows the
-    // longest alone).  Else cut as finely as there are compute units to spare.  32 query heads of 8 groups, d 128, us uncut / by 128 / by 256 /
-    // evenly: one sequence of 400 tokens 10.9 / 12.1 / 13.2 / 17.9, of 1000 16.1 / 12.8 / 13.6 / 14.6, of 4000 30.6 / 13.6 / 14.0 / 18.3;
-    // 16 of 1000 17.8 / 23.8 / 20.8 / 25.6; 32 of 2000 51 / 78 / 63 / 62; 256 of 100 .. 512 60 / 107 / 81 / 80.
-    const int64_t row = 2 * (int64_t)P.d * (dtype == 0 ? 4 : 2);
-    const bool uncut = len <= 2048 && len * row / (dtype == 0 ? 35 : P.d == 64 ? 32 : 50) <= 6000 + units * len * row / 10200;
+    // Short caches: workgroups that stay with one unit.  Not cut at all, which saves the second kernel, where one workgroup reads its unit in the time that
+    // the second kernel costs and half of all units take at 5100 bytes/ns (half: lengths differ, and the host knows the longest alone).  A
+    // workgroup reads 50 bytes/ns (d 64 32, fp32 35); of eight waves, where there is one per compute unit, 65 (60, 40).  Else cut as finely as there are
+    // compute units to spare.  32 query heads of 8 groups, d 128, us uncut / uncut by eight waves / by 128 / by 256 / evenly: one sequence of 400 tokens
+    // 10.4 / 9.7 / 12.0 / 12.3 / 17.9, of 1000 15.4 / 13.0 / 12.5 / 12.4 / 14.6, of 4000 29.7 / 24.3 / 13.7 / 13.3 / 18.3; 16 of 1000 17.3 /
+    // 16.3 / 20.1 / 20.2 / 25.6; 32 of 2000 51.4 / 51.1 / 63 / 63 / 62; 256 of 100 .. 512 60 / - / 107 / 81 / 80.
+    const bool wide = units <= cus && len > 256;
+    const int64_t row = 2 * (int64_t)P.d * (dtype == 0 ? 4 : 2), rate = wide ? (dtype == 0 ? 40 : P.d == 64 ? 60 : 65) : (dtype == 0 ? 35 : P.d == 64 ? 32 : 50);
+    const bool uncut = len <= 2048 && len * row / rate <= 6000 + units * len * row / 10200;
     for (int chunk = uncut ? 2048 : 128; !many && chunk <= 2048; chunk *= 2) {
       const int64_t chunks = (len + chunk - 1) / chunk;
       if (!uncut && (chunks > 64 || units * chunks > (chunk <= 256 ? cus : cus * waves) || chunk > 512)) continue;
@@ -186,6 +188,7 @@ static AttendCuts plan_attend(const Paged& P, int dtype, int max_new, int max_le
       c.grid.row_blocks = (int)((rows + e.rows - 1) / e.rows);
       c.grid.chunk = chunk;
       c.grid.parts = (int)(chunks < 1 ? 1 : chunks);
+      c.grid.wide = uncut && wide;
       c.even.rows = c.even.parts = 0;
       break;
     }
@@ -279,8 +282,11 @@ static void attend_launch(const Paged& P, const AttendCuts& c, const AttendArgs&
       else                   mixed_launch<T, D, 1>(P, c, grid, even.part, s);
     }
   } else if (c.grid.rows > 0) {
-    if (c.grid.rows == 16) launch(attend_split_kernel<T, D, 1>, dim3(grid_size(P, c.grid)), block, s, P, c.grid, grid);
-    else                   launch(attend_split_kernel<T, D, 2>, dim3(grid_size(P, c.grid)), block, s, P, c.grid, grid);
+    const dim3 wgs(grid_size(P, c.grid));
+    if (c.grid.wide && c.grid.rows == 16) launch(attend_split_kernel<T, D, 1, 8>, wgs, dim3(512), s, P, c.grid, grid);
+    else if (c.grid.wide)                 launch(attend_split_kernel<T, D, 2, 8>, wgs, dim3(512), s, P, c.grid, grid);
+    else if (c.grid.rows == 16)           launch(attend_split_kernel<T, D, 1, kWaves>, wgs, block, s, P, c.grid, grid);
+    else                                  launch(attend_split_kernel<T, D, 2, kWaves>, wgs, block, s, P, c.grid, grid);
   } else if (c.even.rows == 16) {
     launch(attend_even_kernel<T, D, 1>, dim3((unsigned)c.even.parts), block, s, P, c.even, even);
   } else {

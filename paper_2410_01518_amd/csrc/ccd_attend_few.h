@@ -203,6 +203,8 @@ struct Tile<float, D> {
   __device__ static int element(int c, int lane, int i) { return 64 * (c >> 2) + 4 * (4 * (lane >> 4) + i) + (c & 3); }
 };
 
+__device__ __forceinline__ void store_piece(float* to, const float (&x)[2]) { *reinterpret_cast<float2*>(to) = make_float2(x[0], x[1]); }
+__device__ __forceinline__ void store_piece(uint16_t* to, const float (&x)[2]) { *reinterpret_cast<uint32_t*>(to) = pack_bf16(x[0], x[1]); }
 __device__ __forceinline__ void store_piece(float* to, const float (&x)[4]) { *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]); }
 __device__ __forceinline__ void store_piece(float* to, const float (&x)[8]) {
   *reinterpret_cast<float4*>(to) = make_float4(x[0], x[1], x[2], x[3]);
@@ -229,22 +231,22 @@ __device__ __forceinline__ float row_sum(float x) {
 template <class T, int D, int NQ>
 constexpr int split_waves() { return NQ == 2 || D == 128 ? 2 : 3; }
 
-template <class T, int D, int NQ>
+template <class T, int D, int NQ, int WAVES = kWaves>
 struct SplitLds {
   static constexpr int kRows = 16 * NQ, kPitch = D + 4;
   static constexpr int kWaveBytes = Tile<T, D>::kLdsBytes > 16 * kPitch * 4 ? Tile<T, D>::kLdsBytes : 16 * kPitch * 4;
-  __align__(16) char wave[kWaves][kWaveBytes];
-  float m[kWaves][kRows], l[kWaves][kRows];
+  __align__(16) char wave[WAVES][kWaveBytes];
+  float m[WAVES][kRows], l[WAVES][kRows];
 };
 
 // Rows r0 .. r1 - 1 of unit (b, hkv) over the tokens t_begin .. t_end - 1, by the workgroup.  whole_row: these are all tokens the rows see, the result
 // is written; else (o, m, l) of row r go to entry part0 + (r - r0) of the workspace, or, part0 < 0, to those of part_no by the row's number.
 // Returns whether the rows have to be done again (redo_rows).
-template <class T, int D, int NQ>
-__device__ __forceinline__ bool attend_stretch(const Paged& P, const AttendArgs& A, SplitLds<T, D, NQ>& L, const Sequence& sq, int b, int hkv, int r0, int r1,
+template <class T, int D, int NQ, int WAVES>
+__device__ __forceinline__ bool attend_stretch(const Paged& P, const AttendArgs& A, SplitLds<T, D, NQ, WAVES>& L, const Sequence& sq, int b, int hkv, int r0, int r1,
                                                int t_begin, int t_end, bool whole_row, int64_t part0, int part_no) {
   using Tl = Tile<T, D>;
-  constexpr int kPitch = SplitLds<T, D, NQ>::kPitch, kStride = kWaves * Tl::kTokens;
+  constexpr int kPitch = SplitLds<T, D, NQ, WAVES>::kPitch, kStride = WAVES * Tl::kTokens;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t* pages = A.table + (int64_t)b * P.table_width;
   const T* Kh = static_cast<const T*>(A.K) + hkv * P.head_stride;
@@ -374,7 +376,7 @@ __device__ __forceinline__ bool attend_stretch(const Paged& P, const AttendArgs&
   for (int j = 0; j < NQ; ++j) {
     float all = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) all = fmaxf(all, L.m[w][16 * j + (lane & 15)]);
+    for (int w = 0; w < WAVES; ++w) all = fmaxf(all, L.m[w][16 * j + (lane & 15)]);
     const float keep = m[j] == -INFINITY ? (l[j] == l[j] ? 0.f : l[j]) : fast_exp2(m[j] - all);
     float* mine = reinterpret_cast<float*>(L.wave[wave]) + (lane & 15) * kPitch;
     if (j > 0) __syncthreads();
@@ -383,19 +385,19 @@ __device__ __forceinline__ bool attend_stretch(const Paged& P, const AttendArgs&
 #pragma unroll
       for (int i = 0; i < 4; ++i) mine[Tl::element(c, lane, i)] = o[j][c][i] * keep;
     __syncthreads();
-    // 16 rows of D elements by 256 threads
-    constexpr int kPer = 16 * D / (64 * kWaves);           // 4 or 8 elements a thread
+    // 16 rows of D elements by all threads
+    constexpr int kPer = 16 * D / (64 * WAVES);           // 2, 4 or 8 elements a thread
     const int q_row = tid / (D / kPer), e0 = tid % (D / kPer) * kPer, r = r0 + 16 * j + q_row;
     float acc[kPer] = {}, top = -INFINITY, sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       const float* from = reinterpret_cast<const float*>(L.wave[w]) + q_row * kPitch + e0;
 #pragma unroll
       for (int e = 0; e < kPer; ++e) acc[e] += from[e];
       top = fmaxf(top, L.m[w][16 * j + q_row]);
     }
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
       const float mw = L.m[w][16 * j + q_row], lw = L.l[w][16 * j + q_row];
       sum += mw == -INFINITY ? (lw == lw ? 0.f : lw) : lw * fast_exp2(mw - top);
     }
@@ -425,8 +427,8 @@ __device__ __forceinline__ bool attend_stretch(const Paged& P, const AttendArgs&
 
 // the call cut on a grid: (head, sequence, stretch, block of rows), or (head, stretch, block of the call)
 // LISTED: the latter (not in the other kernels: the search costs 0.9 of 13 us).  By workgroup idx.
-template <class T, int D, int NQ, bool LISTED>
-__device__ __forceinline__ void attend_on_grid(const Paged& P, const AttendPlan& pl, const AttendArgs& A, SplitLds<T, D, NQ>& L, int idx) {
+template <class T, int D, int NQ, int WAVES, bool LISTED>
+__device__ __forceinline__ void attend_on_grid(const Paged& P, const AttendPlan& pl, const AttendArgs& A, SplitLds<T, D, NQ, WAVES>& L, int idx) {
   constexpr int kRows = 16 * NQ;
   const int hkv = idx % P.Hkv;
   idx /= P.Hkv;
@@ -444,8 +446,8 @@ __device__ __forceinline__ void attend_on_grid(const Paged& P, const AttendPlan&
       const Stretch st = cut_rows(P, sq, r0, r1, pl.parts, pl.chunk);
       const int t_begin = st.begin + part_no * st.chunk, t_end = t_begin + st.chunk < st.end ? t_begin + st.chunk : st.end;
       if (part_no >= st.parts) {}
-      else if (pass == 0) again = attend_stretch<T, D, NQ>(P, A, L, sq, b, hkv, r0, r1, t_begin, t_end, st.parts == 1, -1, part_no) || again;
-      else                redo_rows<T, D>(P, A, sq, b, hkv, r0 + (int)(threadIdx.x >> 6), r1, kWaves, t_begin, t_end, st.parts == 1, part_no);
+      else if (pass == 0) again = attend_stretch<T, D, NQ, WAVES>(P, A, L, sq, b, hkv, r0, r1, t_begin, t_end, st.parts == 1, -1, part_no) || again;
+      else                redo_rows<T, D>(P, A, sq, b, hkv, r0 + (int)(threadIdx.x >> 6), r1, WAVES, t_begin, t_end, st.parts == 1, part_no);
       r0 += pl.row_blocks * kRows;                         // (more rows than the host expected)
       k += pl.blocks;
     }
@@ -555,7 +557,7 @@ __device__ __forceinline__ void attend_evenly(const Paged& P, const AttendPlan& 
       const int t_begin = sp.begin + (int)(at - unit_at), t_stop = sp.begin + (int)(until - unit_at);
       if (!alone || first == me)
         for (int r0 = 0; r0 < rows_all; r0 += kRows) {
-          const bool again = attend_stretch<T, D, NQ>(P, A, L, sq, b, h, r0, r0 + kRows < rows_all ? r0 + kRows : rows_all, alone ? sp.begin : t_begin,
+          const bool again = attend_stretch<T, D, NQ, kWaves>(P, A, L, sq, b, h, r0, r0 + kRows < rows_all ? r0 + kRows : rows_all, alone ? sp.begin : t_begin,
                                                       alone || t_stop > sp.end ? sp.end : t_stop, alone || first == last, (int64_t)(2 * me + (first == me)) * kRows, 0);
           // (the kernel that joins does them again, those of several stretches without being told)
           if (again && (alone || first == last) && tid == 0) meta[b * P.Hkv + h].y = kAgain;
