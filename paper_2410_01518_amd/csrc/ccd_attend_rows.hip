@@ -7,7 +7,7 @@
 // lanes on, and the weights are already the operand of D[d][row] = V^T W^T if that product counts its tokens in the same order; values
 // are transposed by the LDS read (ds_read_b64_tr_b16).
 //
-// Measured, a chunk of 2048 tokens over 32768 cached ones, 32 query heads on 8 KV heads of 128 elements: 970 - 1020 us by the machine, 1.04 - 1.10 PFLOP/s,
+// Measured, a chunk of 2048 tokens over 32768 cached ones, 32 query heads on 8 KV heads of 128 elements: 966 - 1049 us by the machine, 1.02 - 1.10 PFLOP/s,
 // where a product of 8192^3 reaches 1.2 - 1.3.  The matrix cores are busy 52 % of the cycles and the clock is at 1.9 - 2.0 GHz: what is left is bound by power
 // (removing all bank conflicts and a tenth of the instructions took 20 % of the cycles and 4 % of the time).  Waves of 64 rows, one per SIMD,
 // read LDS half as often and keep 2.4 GHz, but a wave alone cannot cover its own waits: 1010 - 1040 us, and coarser blocks for short calls.

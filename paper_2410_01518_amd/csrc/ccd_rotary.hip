@@ -1,6 +1,8 @@
 // ccd_rope: rotary embedding of the queries and keys of a step, and ccd_paged_append, which embeds keys on their way into the
 // pages.  Both move their rows once in and once out and are bound by memory; what could be in the way is the arithmetic of
-// cosine and sine (about 35 instructions a pair), so a wave works them out once for a token and takes all its heads.
+// cosine and sine (about 35 instructions a pair), so a wave works them out once for a token and takes all its heads, four pieces of heads read before
+// they are written.  Measured, bf16: 8192 tokens of 40 heads of 128 35.4 us (4.75 TB/s moved, a copy reaches 5.12), 16384 tokens of 8 heads appended with
+// their keys embedded 29.5 us (4.55); 16 tokens 3.6 us and the launch.
 #include "ccd_paged.h"
 #include "ccd_rotary.h"
 
