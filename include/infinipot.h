@@ -224,8 +224,8 @@ typedef struct {
   int32_t B;                  /* sequences (rows of the block table)                                               */
   int32_t tokens;             /* rows of Q, out, lse, K_new, V_new, slots, positions: the step's new tokens and any  */
                               /* padding behind the last sequence's, which is left as it is                         */
-  int32_t Hq, Hkv, d;         /* query heads, KV heads (Hq % Hkv == 0; tokens * Hq and B * Hkv < 2^31), head       */
-                              /* dimension 64 or 128                                                                */
+  int32_t Hq, Hkv, d;         /* query heads, KV heads (Hq % Hkv == 0; attention: tokens * Hq <= 2^28 and      */
+                              /* B * Hkv <= 2^21, else CCD_EUNSUPPORTED), head dimension 64 or 128                  */
   int32_t dtype;              /* CCD_FP32 or CCD_BF16, for Q, out, K, V                                             */
   int32_t page, n_pages;      /* tokens per page, pages of the cache; page * n_pages < 2^31                         */
   int32_t table_width;        /* entries per row of the block table; page * table_width < 2^31                      */
@@ -282,7 +282,7 @@ CCD_API int ccd_paged_plan(const ccd_paged_t* paged, const int32_t* len_before, 
 enum { CCD_ROPE_HALF = 0, CCD_ROPE_PAIRS = 1 };
 enum { CCD_ROPE_PLAIN = 0, CCD_ROPE_LINEAR = 1, CCD_ROPE_NTK = 2, CCD_ROPE_PARTS = 3 };
 typedef struct {
-  int32_t tokens, heads, d;   /* X, Y [tokens, heads, d]; d a multiple of 16 bytes, at most 1024                    */
+  int32_t tokens, heads, d;   /* X, Y [tokens, heads, d]; tokens <= 2^25; d a multiple of 16 bytes, at most 1024    */
   int32_t rot;                /* elements of a head that are turned: even, 2 .. d                                   */
   int32_t dtype;              /* CCD_FP32 or CCD_BF16                                                               */
   int32_t layout, inverse;    /* CCD_ROPE_HALF or CCD_ROPE_PAIRS; 0 or 1                                            */
@@ -306,7 +306,7 @@ CCD_API int ccd_rope(const ccd_rope_t* rope, const void* X, const int32_t* posit
 /* Key and value of new token t (K_new, V_new [tokens, Hkv, d]) go to row slots[t] % page of page slots[t] / page; a slot
  * outside 0 .. page * n_pages - 1 (the plan's -1) is not written.  Two tokens must not have the same slot.  rope (nullable):
  * the keys are embedded on the way at positions[t], with turns as in ccd_rope (rot, layout, inverse and amplitude of rope are
- * read; a token with a negative position is not written); without it positions and turns are not read. */
+ * read; a token with a negative position is not written); without it positions and turns are not read.  tokens <= 2^25. */
 CCD_API int ccd_paged_append(const ccd_paged_t* paged, const ccd_rope_t* rope, const void* K_new, const void* V_new,
                      const int32_t* slots, const int32_t* positions, const uint64_t* turns, void* K_pages, void* V_pages,
                      void* hip_stream);

@@ -36,7 +36,6 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Paged P, AttendPlan pl
   constexpr int kPer = D / 64;
   __shared__ float sums[WAVES > 1 ? WAVES : 1][D];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t at0 = WAVES > 1 ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * 4 + wave;
   // entry of the first stretch, of the second less a step, distance of the others
   auto join = [&](const Sequence& sq, int b, int hkv, int r, int parts, int64_t part_first, int64_t part_0, int64_t part_step) __attribute__((always_inline)) {
     auto entry = [&](int p) { return p == 0 ? part_first : part_0 + p * part_step; };
@@ -97,30 +96,38 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Paged P, AttendPlan pl
     if (A.lse != nullptr && lane == 0) A.lse[b * P.l_b + row * P.l_t + head * P.l_h] = to_natural_lse(top, sum);
   };
 
-  if constexpr (EVEN) {
-    const int unit = (int)(at0 / pl.join), hkv = unit % P.Hkv, b = unit / P.Hkv;
-    if (b >= P.B) return;
-    const Sequence sq = load_sequence(P, b, A.q_start, A.kv_len);
-    const int rows_all = sq.m * P.G;
-    if (rows_all < 1 || (pl.only_few && rows_all > pl.few)) return;
-    const int2 cut = A.part.meta[unit];
-    if (cut.y == 1 || (cut.y == kAgain && WAVES > 1 && wave != 0)) return;
-    for (int r = (int)(at0 % pl.join); r < rows_all; r += pl.join) {
-      if (cut.y == kAgain) { redo_row<T, D>(P, A, sq, b, hkv, r, 0, sq.n, true, 0); continue; }
-      join(sq, b, hkv, r, cut.y, (int64_t)(2 * cut.x + 1) * pl.rows + r, (int64_t)(2 * cut.x) * pl.rows + r, 2 * pl.rows);
+  auto one = [&](int64_t at0) __attribute__((always_inline)) {
+    if constexpr (EVEN) {
+      const int unit = (int)(at0 / pl.join), hkv = unit % P.Hkv, b = unit / P.Hkv;
+      if (b >= P.B) return;
+      const Sequence sq = load_sequence(P, b, A.q_start, A.kv_len);
+      const int rows_all = sq.m * P.G;
+      if (rows_all < 1 || (pl.only_few && rows_all > pl.few)) return;
+      const int2 cut = A.part.meta[unit];
+      if (cut.y == 1 || (cut.y == kAgain && WAVES > 1 && wave != 0)) return;
+      for (int r = (int)(at0 % pl.join); r < rows_all; r += pl.join) {
+        if (cut.y == kAgain) { redo_row<T, D>(P, A, sq, b, hkv, r, 0, sq.n, true, 0); continue; }
+        join(sq, b, hkv, r, cut.y, (int64_t)(2 * cut.x + 1) * pl.rows + r, (int64_t)(2 * cut.x) * pl.rows + r, 2 * pl.rows);
+      }
+    } else {
+      const int row = (int)(at0 / P.Hq), head = (int)(at0 % P.Hq);
+      if (row >= P.tokens) return;
+      int b = 0;                                                          // sequences that end at or before the row: counted, no chain of loads
+      for (int b0 = 1; b0 <= P.B; b0 += 64) b += __popcll(__ballot(b0 + lane <= P.B && A.q_start[b0 + lane <= P.B ? b0 + lane : P.B] <= row));
+      if (b >= P.B || row < A.q_start[0]) return;
+      const Sequence sq = load_sequence(P, b, A.q_start, A.kv_len);
+      const int r = (row - sq.first) * P.G + head % P.G, rows_all = sq.m * P.G;
+      if (r < 0 || r >= rows_all || rows_all <= pl.few) return;
+      const int r0 = r / pl.rows * pl.rows;
+      const int parts = cut_rows(P, sq, r0, r0 + pl.rows < rows_all ? r0 + pl.rows : rows_all, pl.parts, pl.chunk).parts;
+      if (parts > 1) join(sq, b, head / P.G, r, parts, at0, at0, (int64_t)P.tokens * P.Hq);
     }
+  };
+  if constexpr (WAVES > 1) {
+    one(blockIdx.x);
   } else {
-    const int row = (int)(at0 / P.Hq), head = (int)(at0 % P.Hq);
-    if (row >= P.tokens) return;
-    int b = 0;                                                          // sequences that end at or before the row: counted, no chain of loads
-    for (int b0 = 1; b0 <= P.B; b0 += 64) b += __popcll(__ballot(b0 + lane <= P.B && A.q_start[b0 + lane <= P.B ? b0 + lane : P.B] <= row));
-    if (b >= P.B || row < A.q_start[0]) return;
-    const Sequence sq = load_sequence(P, b, A.q_start, A.kv_len);
-    const int r = (row - sq.first) * P.G + head % P.G, rows_all = sq.m * P.G;
-    if (r < 0 || r >= rows_all || rows_all <= pl.few) return;
-    const int r0 = r / pl.rows * pl.rows;
-    const int parts = cut_rows(P, sq, r0, r0 + pl.rows < rows_all ? r0 + pl.rows : rows_all, pl.parts, pl.chunk).parts;
-    if (parts > 1) join(sq, b, head / P.G, r, parts, at0, at0, (int64_t)P.tokens * P.Hq);
+    const int64_t all = EVEN ? (int64_t)P.B * P.Hkv * pl.join : (int64_t)P.tokens * P.Hq;
+    for (int64_t at0 = (int64_t)blockIdx.x * 4 + wave; at0 < all; at0 += (int64_t)gridDim.x * 4) one(at0);
   }
 }
 
@@ -256,12 +263,14 @@ size_t attend_workspace_bytes(const Paged& P, int dtype, int max_new, int max_le
   return lay_out(P, plan_attend(P, dtype, max_new, max_len)).total;
 }
 
+constexpr int64_t kJoinMost = 1 << 22;      // workgroups
+
 template <class T, int D, bool EVEN>
 static void join_launch(const Paged& P, const AttendPlan& pl, const AttendArgs& A, hipStream_t s) {
   const int64_t rows = EVEN ? (int64_t)P.B * P.Hkv * pl.join : (int64_t)P.tokens * P.Hq;
   // (few rows, or many stretches: four waves each)
   if (rows <= 1024) launch(attend_join_kernel<T, D, 4, EVEN>, dim3((unsigned)rows), dim3(256), s, P, pl, A);
-  else              launch(attend_join_kernel<T, D, 1, EVEN>, dim3((unsigned)((rows + 3) / 4)), dim3(256), s, P, pl, A);
+  else              launch(attend_join_kernel<T, D, 1, EVEN>, dim3((unsigned)(rows < kJoinMost * 4 ? (rows + 3) / 4 : kJoinMost)), dim3(256), s, P, pl, A);
 }
 
 template <class T, int D, int NQ>

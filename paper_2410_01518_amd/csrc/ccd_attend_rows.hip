@@ -30,11 +30,11 @@ __device__ __forceinline__ void load_to_lds(uint32_t lds_addr, const void* p) {
 template <int N>
 __device__ __forceinline__ void load_run_to_lds(uint32_t lds_addr, const uint32_t (&offset)[N], const void* base) {
   if constexpr (N == 4)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:1024\n\t"
-                 "global_load_lds_dwordx4 %3, %5 offset:2048\n\tglobal_load_lds_dwordx4 %4, %5 offset:3072"
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\tglobal_load_lds_dwordx4 %2, %5 offset:0x400\n\t"
+                 "global_load_lds_dwordx4 %3, %5 offset:0x800\n\tglobal_load_lds_dwordx4 %4, %5 offset:0xC00"
                  ::"s"(lds_addr), "v"(offset[0]), "v"(offset[1]), "v"(offset[2]), "v"(offset[3]), "s"(base) : "memory");
   else
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:1024"
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\tglobal_load_lds_dwordx4 %2, %3 offset:0x400"
                  ::"s"(lds_addr), "v"(offset[0]), "v"(offset[1]), "s"(base) : "memory");
 }
 constexpr int kRunBack = 4096;

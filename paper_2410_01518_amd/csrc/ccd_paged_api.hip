@@ -12,6 +12,7 @@ namespace ccd {
 static bool on_16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 static int paged_status() { return hipGetLastError() == hipSuccess ? CCD_OK : CCD_ELAUNCH; }
 
+constexpr int32_t kMostTokens = 1 << 25;               // of a launch of a wave each
 enum PagedNeed { kPlan = 1, kCache = 2, kNew = 4, kAttend = 8 };
 
 static int check_stride(int64_t stride, int64_t least, int64_t esz) {
@@ -37,10 +38,12 @@ static int check_paged(const ccd_paged_t* c, int need) {
   Stride strides[10];
   int n = 0;
   strides[n++] = {c->page_stride, c->d}; strides[n++] = {c->head_stride, c->d}; strides[n++] = {c->row_stride, c->d};
+  if ((need & kNew) && c->tokens > kMostTokens) return CCD_EUNSUPPORTED;
   if (need & kNew) { strides[n++] = {c->new_stride_t, c->d}; strides[n++] = {c->new_stride_h, c->d}; }
   if (need & kAttend) {
     if (c->Hq < 1 || c->Hq % c->Hkv != 0) return CCD_EINVAL;
-    if ((int64_t)c->tokens * c->Hq > 0x7FFFFFFF || (int64_t)c->B * c->Hkv > 0x7FFFFFFF) return CCD_EINVAL;
+    // (a launch has less than 2^32 threads)
+    if ((int64_t)c->tokens * c->Hq > 1 << 28 || (int64_t)c->B * c->Hkv > 1 << 21) return CCD_EUNSUPPORTED;
     if (c->window < 0 || (c->behind != 0 && c->behind != 1) || c->max_new < 0 || c->max_len < 0) return CCD_EINVAL;
     if (!(c->scale >= 0.f) || isinf(c->scale)) return CCD_EINVAL;
     strides[n++] = {c->q_stride_b, 0}; strides[n++] = {c->q_stride_t, c->d}; strides[n++] = {c->q_stride_h, c->d};
@@ -140,7 +143,7 @@ int ccd_rope_turns(const ccd_rope_t* rope, uint64_t* turns) {
 int ccd_rope(const ccd_rope_t* rope, const void* X, const int32_t* positions, const uint64_t* turns, void* Y, void* hip_stream) {
   if (rope == nullptr) return CCD_EINVAL;
   if (rope->tokens < 0 || rope->heads < 1 || rope->heads > 65535 || rope->d < 1) return CCD_EINVAL;
-  if (rope->dtype != CCD_FP32 && rope->dtype != CCD_BF16) return CCD_EUNSUPPORTED;
+  if ((rope->dtype != CCD_FP32 && rope->dtype != CCD_BF16) || rope->tokens > kMostTokens) return CCD_EUNSUPPORTED;
   const int64_t esz = rope->dtype == CCD_FP32 ? 4 : 2;
   if (rope->d > 1024 || (rope->d * esz) % 16 != 0) return CCD_EUNSUPPORTED;
   int rc = check_rotation(rope, rope->d);

@@ -666,3 +666,24 @@ def test_decoding_of_many_sequences_cut_evenly(dtype):
     p = _attend_problem(17, dtype, lens, news, 4, 2, 64, 16, pad=2)
     out, lse = _run_attend(p)
     _check_attend(p, out, lse, dtype)
+
+
+def test_rows_at_the_end_of_more_than_one_launch_of_joins():
+    """16.8 million rows of padding before a sequence's one new token: its stretches are joined, the padding is left alone."""
+    p = _attend_problem(18, "bf16", [1500], [1], 4, 1, 64, 16)
+    T = (1 << 22) + 8
+    Q = torch.zeros((T, 4, 64), dtype=torch.bfloat16, device="cuda")
+    Q[-1] = p["Q"][0]
+    out = torch.full_like(Q, 5.0)
+    lse = torch.full((T, 4), 5.0, device="cuda")
+    table, lens = _dev(p["table"]), _dev(p["lens"])
+    q_start = torch.tensor([T - 1, T], dtype=torch.int32, device="cuda")
+    paged = ip.make_paged(p["K"], tokens=T, block_table=table, Q=Q, out=out, lse=lse, max_new=1, max_len=1500)
+    ws = ip.alloc_paged_workspace(paged)
+    assert ws.numel() > T * 4 * 64 * 4                                # several stretches
+    assert ip.ccd_paged_attend(paged, Q, p["K"], p["V"], table, q_start, lens, out, lse, ws) == ip.CCD_OK
+    torch.cuda.synchronize()
+    _check_attend(p, out[-1:].clone(), lse[-1:].clone(), "bf16")
+    assert bool((out[:-1] == 5.0).all()) and bool((lse[:-1] == 5.0).all())
+    del ws, Q, out, lse
+    torch.cuda.empty_cache()

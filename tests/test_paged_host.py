@@ -192,9 +192,13 @@ def test_reference_rope_pins():
     np.testing.assert_allclose(O.rope(y, [12345], O.frequencies(6, 10000.0), half=False, inverse=True), x)
 
 
-def test_more_units_than_can_be_counted_are_refused():
-    assert _attend(_paged(B=1 << 20, table_width=1, Hkv=1 << 12, Hq=1 << 12, tokens=6)) == ip.CCD_EINVAL
-    assert ip.ccd_paged_workspace_bytes(_paged(B=1 << 20, table_width=1, Hkv=1 << 12, Hq=1 << 12, tokens=6)) == 0
+def test_calls_of_more_threads_than_a_launch_has_are_refused():
+    for kw in (dict(B=1 << 20, table_width=1, Hkv=4, Hq=4), dict(B=1 << 20, table_width=1, Hkv=1 << 12, Hq=1 << 12), dict(tokens=(1 << 25) + 1)):
+        assert _attend(_paged(**kw)) == ip.CCD_EUNSUPPORTED
+        assert ip.ccd_paged_workspace_bytes(_paged(**kw)) == 0
+    assert ip.ccd_paged_workspace_bytes(_paged(B=1 << 20, table_width=1)) > 0 and ip.ccd_paged_workspace_bytes(_paged(tokens=1 << 25)) > 0
+    assert _append(_paged(tokens=(1 << 25) + 1)) == ip.CCD_EUNSUPPORTED
+    assert ip.lib().ccd_rope(ctypes.byref(_rope(tokens=(1 << 25) + 1)), P, P, P, P2, None) == ip.CCD_EUNSUPPORTED
 
 
 def test_the_binding_refuses_index_tensors_that_are_too_short():
