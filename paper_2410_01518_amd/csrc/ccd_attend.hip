@@ -185,10 +185,12 @@ static AttendCuts plan_attend(const Paged& P, int dtype, int max_new, int max_le
     // 10.4 / 9.7 / 12.0 / 12.3 / 17.9, of 1000 15.4 / 13.0 / 12.5 / 12.4 / 14.6, of 4000 29.7 / 24.3 / 13.7 / 13.3 / 18.3; 16 of 1000 17.3 /
     // 16.3 / 20.1 / 20.2 / 25.6; 32 of 2000 51.4 / 51.1 / 63 / 63 / 62; 256 of 100 .. 512 60 / - / 107 / 81 / 80.  By 1024, or 2048, and evenly: 16 of
     // 500 .. 4096 36.8, 36.8, d 64 19.9, 23.8; 8 of 16384 101, 104; but 32 of 500 .. 4096, two stretches each, 62, 57; fp32, 8 of 2000 .. 8192 76, 66.
+    // Many rounds of units are dealt out as they end: 512 of 500 .. 4096, us whole and evenly, 616, 644, of 1 .. 16384 712, 801; but 256 of 500 .. 8192
+    // 520, 513, and fp32, 512 of 100 .. 4000, 479, 426.
     const bool wide = units <= cus && len > 256;
     const int64_t row = 2 * (int64_t)P.d * (dtype == 0 ? 4 : 2), rate = wide ? (dtype == 0 ? 40 : P.d == 64 ? 60 : 65) : (dtype == 0 ? 35 : P.d == 64 ? 32 : 50);
-    const bool uncut = len <= 2048 && len * row / rate <= 6000 + units * len * row / 10200;
-    for (int chunk = uncut ? 2048 : 128; !many && chunk <= 2048; chunk *= 2) {
+    const bool uncut = (len <= 2048 && len * row / rate <= 6000 + units * len * row / 10200) || (dtype != 0 && units >= 16 * cus);
+    for (int chunk = uncut ? (int)len : 128; !many && (uncut || chunk <= 2048); chunk *= 2) {
       const int64_t chunks = (len + chunk - 1) / chunk;
       if (!uncut && (chunks > 64 || units * chunks > (chunk <= 256 ? cus : cus * waves) || (chunk > 512 && (dtype == 0 || chunks < 4)))) continue;
       c.grid = e;

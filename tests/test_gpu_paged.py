@@ -687,3 +687,16 @@ def test_rows_at_the_end_of_more_than_one_launch_of_joins():
     assert bool((out[:-1] == 5.0).all()) and bool((lse[:-1] == 5.0).all())
     del ws, Q, out, lse
     torch.cuda.empty_cache()
+
+
+def test_decoding_of_thousands_of_sequences():
+    """More units than several rounds of the chip: whole, whatever their lengths."""
+    rng = np.random.default_rng(19)
+    lens = [int(x) for x in rng.integers(0, 20, 2100)]
+    for b, n in ((0, 2300), (1024, 700), (2099, 4100)):
+        lens[b] = n
+    news = [min(1, n) if b % 5 else 0 for b, n in enumerate(lens)]
+    news[2099] = 3
+    p = _attend_problem(20, "bf16", lens, news, 4, 2, 64, 16, pad=1)
+    out, lse = _run_attend(p)
+    _check_attend(p, out, lse, "bf16")
