@@ -26,7 +26,7 @@ static int check_paged(const ccd_paged_t* c, int need) {
   if ((int64_t)c->page * c->n_pages > 0x7FFFFFFF) return CCD_EINVAL;
   if (need & (kPlan | kAttend)) {
     if (c->B < 1 || c->table_width < 1 || (int64_t)c->B * c->table_width > 0x7FFFFFFF) return CCD_EINVAL;
-    if ((int64_t)c->page * c->table_width > 0x7FFFFFFF) return CCD_EINVAL;
+    if ((int64_t)c->page * c->table_width > 1 << 30) return CCD_EINVAL;                // positions, and a tile past them, are counted in int32
   }
   if ((need & kPlan) && c->B > kPlanMaxSequences) return CCD_EUNSUPPORTED;
   if (!(need & kCache)) return CCD_OK;

@@ -60,8 +60,8 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(Paged P, PlanA
   const int head = A.cursor[0], count = A.cursor[1];
   auto pages = [&](int len) { return len > 0 ? page_of(P.div, len - 1) + 1 : 0; };
   // the thread's sequences are neighbours
-  int take = 0, give = 0, short_of = 0;
-  int64_t fresh = 0;
+  int take = 0, give = 0;
+  int64_t fresh = 0, short_of = 0;
   int takes[kPer], gives[kPer], news[kPer];
 #pragma unroll
   for (int j = 0; j < kPer; ++j) {
@@ -158,18 +158,18 @@ __global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(Paged P, PlanA
       __syncthreads();
     }
     // the pages short: of the ring, and those a row of the table has no room for
-    const int over = wave_inclusive(short_of, lane);
-    if (lane == 63) wave_take[wave] = over;
+    const int64_t over = wave_inclusive(short_of, lane);
+    if (lane == 63) wave_new[wave] = over;
     __syncthreads();
     if (tid == 0) {
-      int missing = all_taken - taken;
-      for (int w = 0; w < kPlanWaves; ++w) missing += wave_take[w];
+      int64_t missing = all_taken - taken;
+      for (int w = 0; w < kPlanWaves; ++w) missing += wave_new[w];
       if (A.cursor_next != A.cursor) {
         A.cursor_next[0] = ring_at(taken);
         A.cursor_next[1] = free_now - taken + given;
         A.cursor_next[3] = 0;
       }
-      A.cursor_next[2] = missing;
+      A.cursor_next[2] = missing < 0x7FFFFFFF ? (int)missing : 0x7FFFFFFF;
     }
   }
 

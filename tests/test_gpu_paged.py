@@ -700,3 +700,18 @@ def test_decoding_of_thousands_of_sequences():
     p = _attend_problem(20, "bf16", lens, news, 4, 2, 64, 16, pad=1)
     out, lse = _run_attend(p)
     _check_attend(p, out, lse, "bf16")
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_plan_counts_that_pass_31_bits_stop_there(in_place):
+    top = (1 << 31) - 1
+    before, after = np.array([0, 1, 0], np.int32), np.array([top, top, top], np.int32)
+    table = np.array([[-1] * 4, [8, -1, -1, -1], [-1] * 4], np.int32)
+    ring, cursor = np.arange(9, dtype=np.int32), np.array([0, 8, 0, 0], np.int32)
+    t, r, c, q, slots, pos = _run_plan(before, after, table, ring, cursor, page=1, n_pages=9, tokens=9, in_place=in_place)
+    np.testing.assert_array_equal(t, [[0, 1, 2, 3], [8, 4, 5, 6], [7, -1, -1, -1]])
+    np.testing.assert_array_equal(r, ring)
+    np.testing.assert_array_equal(c, [8, 0, top, 0])
+    np.testing.assert_array_equal(q, [0, top, top, top])
+    np.testing.assert_array_equal(slots, [0, 1, 2, 3] + [-1] * 5)
+    np.testing.assert_array_equal(pos, np.arange(9))

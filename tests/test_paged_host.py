@@ -230,3 +230,11 @@ def test_the_binding_refuses_index_tensors_that_are_too_short():
         ip.ccd_paged_append(c, K_new, K_new.float(), i(6), K, K.clone())
     with pytest.raises(AssertionError, match="turns"):
         ip.ccd_rope(rope, K_new, i(6), torch.zeros(32, dtype=torch.int32), K_new)
+
+
+def test_positions_that_int32_could_not_count_are_refused():
+    """Repeated pages make a table of 2^30 tokens small; beyond that a tile would be counted past 2^31."""
+    big = dict(page=1 << 20, n_pages=1, page_stride=1 << 28, head_stride=1 << 27)
+    assert ip.ccd_paged_workspace_bytes(_paged(table_width=1 << 10, **big)) > 0
+    c = _paged(table_width=(1 << 10) + 1, **big)
+    assert _attend(c) == _plan(c) == ip.CCD_EINVAL and ip.ccd_paged_workspace_bytes(c) == 0
