@@ -229,13 +229,14 @@ static AttendCuts plan_attend(const Paged& P, int dtype, int max_new, int max_le
   return c;
 }
 
+// (the answer of the first device serves all: one GPU model per node)
 int attend_compute_units() {
-  static int cus = 0;             // (the answer of the first device serves all: one GPU model per node)
-  if (cus == 0) {
+  static const int cus = [] {
     int dev = 0, n = 0;
-    if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) n = 256;
-    cus = n;
-  }
+    if (hipGetDevice(&dev) == hipSuccess && hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) == hipSuccess && n > 0) return n;
+    (void)hipGetLastError();                                 // none: sizes may be asked for where there is no device
+    return 256;
+  }();
   return cus;
 }
 
