@@ -25,12 +25,18 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 // that gives more than `parts` (so the host's idea of the lengths only decides how well the work is spread); sequences of `few` rows or less
 // are left to the even cut.  Evenly: `parts` workgroups, at most `rows` rows per unit; only_few: sequences of more than `few` rows are left to the grid.
 // join: rows of a unit, as far as the host knows.
-// turn: blocks of rows of the first half of one round (rows kernel), 0: the call is more than one round.
+// turn: blocks of rows of the first half of one round (in_turn), 0: the call is more than one round.
 // wide: workgroups of eight waves, not four.
 // blocks: 0: the grid has row_blocks blocks of rows for every sequence; else it has these for all (find_block).
 struct AttendPlan {
   int by_rows, rows, row_blocks, blocks, parts, chunk, few, only_few, turn, join, wide;
 };
+
+// The last rows see most and come first.  Where the call is one round of two workgroups per compute unit, its second half runs the other way, so that
+// a compute unit has a long one and a short one.
+__device__ __forceinline__ int in_turn(const AttendPlan& pl, int turn_no) {
+  return pl.turn > 0 && turn_no >= pl.turn ? pl.row_blocks - 1 - (turn_no - pl.turn) : turn_no;
+}
 
 // what a workgroup knows of its sequence
 struct Sequence {

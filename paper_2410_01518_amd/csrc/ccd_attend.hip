@@ -224,7 +224,7 @@ static AttendCuts plan_attend(const Paged& P, int dtype, int max_new, int max_le
     g.chunk = (int)(((len + parts - 1) / parts + 127) / 128 * 128);
     g.parts = (int)((len + g.chunk - 1) / g.chunk);
     if (g.parts < 1) g.parts = 1;
-    if (g.by_rows && g.blocks == 0 && units * g.parts <= 2 * cus) g.turn = (g.row_blocks + 1) / 2;
+    if (g.blocks == 0 && units * g.parts <= 2 * cus) g.turn = (g.row_blocks + 1) / 2;
   }
   return c;
 }

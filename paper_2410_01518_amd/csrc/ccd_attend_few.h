@@ -10,7 +10,7 @@
 //
 // Measured, 32 query heads on 8 KV heads of 128 elements, bf16: one sequence of 131072 tokens 94 us (5.7 TB/s; the card reads 5.9), the join 6; 64
 // sequences of 500 to 8192, cut evenly, 133 us (5.3 TB/s), the join 5; 4 of 200 to 500, whole, 9.4 with the launch.  fp32 chunks are bound by
-// the fp32 matrix instructions, which are busy two thirds of the time: 1024 tokens over 4096, 16 heads of 128, 302 us (195 at the full rate).
+// the fp32 matrix instructions, which are busy two thirds of the time: 1024 tokens over 4096, 16 heads of 128, 293 us (195 at the full rate).
 #pragma once
 #include "ccd_attend.h"
 
@@ -438,7 +438,7 @@ __device__ __forceinline__ void attend_on_grid(const Paged& P, const AttendPlan&
   idx /= P.Hkv;
   const int own_b = idx % P.B;
   if (!LISTED) idx /= P.B;
-  const int part_no = idx % pl.parts, turn_no = idx / pl.parts;
+  const int part_no = idx % pl.parts, turn_no = LISTED ? idx / pl.parts : in_turn(pl, idx / pl.parts);
   bool again = false;
   for (int pass = 0; pass < 2; ++pass) {                   // (once more over all of it, row by row, if need be)
     int b = own_b, r0 = (pl.row_blocks - 1 - turn_no) * kRows, k = turn_no;              // the last rows see most: first

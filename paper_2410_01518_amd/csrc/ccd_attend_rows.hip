@@ -66,10 +66,7 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
   int b = idx % P.B;
   if (pl.blocks == 0) idx /= P.B;
   const int part_no = idx % pl.parts;
-  // The last rows see most and come first.  Where the call is one round of two workgroups per compute unit, its second half runs the other way, so that
-  // a compute unit has a long one and a short one.
-  int turn_no = idx / pl.parts;
-  if (pl.turn > 0 && turn_no >= pl.turn) turn_no = pl.row_blocks - 1 - (turn_no - pl.turn);
+  int turn_no = in_turn(pl, idx / pl.parts);
   const uint16_t* Kh = static_cast<const uint16_t*>(A.K) + hkv * P.head_stride;
   const uint16_t* Vh = static_cast<const uint16_t*>(A.V) + hkv * P.head_stride;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)&lds[0][0][0];
