@@ -26,10 +26,10 @@ typedef float v16f __attribute__((ext_vector_type(16)));
 // are left to the even cut.  Evenly: `parts` workgroups, at most `rows` rows per unit; only_few: sequences of more than `few` rows are left to the grid.
 // join: rows of a unit, as far as the host knows.
 // turn: blocks of rows of the first half of one round (in_turn), 0: the call is more than one round.
-// wide: workgroups of eight waves, not four.
+// wide: workgroups of eight waves, not four.  sums: of the rounded weights, too (rows kernel).
 // blocks: 0: the grid has row_blocks blocks of rows for every sequence; else it has these for all (find_block).
 struct AttendPlan {
-  int by_rows, rows, row_blocks, blocks, parts, chunk, few, only_few, turn, join, wide;
+  int by_rows, rows, row_blocks, blocks, parts, chunk, few, only_few, turn, join, wide, sums;
 };
 
 // The last rows see most and come first.  Where the call is one round of two workgroups per compute unit, its second half runs the other way, so that

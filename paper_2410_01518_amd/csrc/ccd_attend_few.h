@@ -63,8 +63,7 @@ __device__ __forceinline__ void load_rows(v4u* r, const char* p, int first, int 
 
 // sum + two weights as they are rounded to bf16.  The weights of the product with the values are rounded, their sum is not; a row that one token rules
 // would be off by that token's rounding.  So the product is taken times l / lr in the end, lr being the sum of the rounded weights.
-// (One query of 8 heads over 438 tokens: 3.0e-3 off in the norm where the output's own rounding is 1.8e-3; 1.9e-3 so.  Not in the rows kernel: over the rows of a chunk it
-// hardly shows, and costs 5 percent of the time.)
+// (One query of 8 heads over 438 tokens: 3.0e-3 off in the norm where the output's own rounding is 1.8e-3; 1.9e-3 so.)
 __device__ __forceinline__ float add_rounded(v8bf w, int pair, float sum) {
   typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
   return __builtin_amdgcn_fdot2_f32_bf16(v2bf{w[2 * pair], w[2 * pair + 1]}, v2bf{(__bf16)1.f, (__bf16)1.f}, sum, false);

@@ -48,12 +48,13 @@ __device__ __forceinline__ float largest(const v16f& x) {
 }
 
 // BANDED: pages of whole runs of 16 rows, so that a wave's 16 rows of a tile lie in one page
+// SUMS: those of the rounded weights, too (add_rounded), for rows that see few tokens: over many, roundings cancel
 template <int D>
 struct RowsLds {
   __align__(1024) char tile[2][2][kTile * D * 2];                                  // [tile][keys, values]
   uint32_t here[2][kRowWaves];                                                     // [tile]: which of 16 tokens have a page
 };
-template <int D, bool BANDED>
+template <int D, bool BANDED, bool SUMS>
 __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl, const AttendArgs& A, RowsLds<D>& L, int idx) {
   constexpr int kRows = 32 * kRowWaves, kRowB = D * 2, kPieces = D / 8;            // 16-byte pieces of a row
   constexpr int kPerLoad = 64 / kPieces, kLoads = 16 / kPerLoad;                   // rows per load instruction, loads of a wave's 16 rows
@@ -117,7 +118,7 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
         q[s] = __builtin_bit_cast(v8bf, w);
       }
     }
-    float m = 0.f, l = 0.f;                                    // reference (0 until the row has one), sum of weights
+    float m = 0.f, l = 0.f, lr = 0.f;                          // reference (0 until the row has one), sums of weights (add_rounded)
     bool seen = r >= r1;                                       // has the row a reference?
     v16f o[kBlocks];
 #pragma unroll
@@ -211,6 +212,7 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
         if (to != -INFINITY) {
           const float keep = seen ? fast_exp2(m - to) : 0.f;
           l *= keep;
+          if (SUMS) lr *= keep;
 #pragma unroll
           for (int c = 0; c < kBlocks; ++c) o[c] *= keep;
           m = to;
@@ -243,6 +245,8 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
     };
     auto add_values = [&](const v8bf (&w)[2], const char* vt, int sub) __attribute__((always_inline)) {
 #pragma unroll
+      for (int p = 0; SUMS && p < 8; ++p) lr = add_rounded(w[p / 4], p % 4, lr);
+#pragma unroll
       for (int s = 0; s < 2; ++s)
 #pragma unroll
         for (int c = 0; c < kBlocks; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(value_of(vt, sub, s, c), w[s], o[c], 0, 0, 0);
@@ -270,7 +274,12 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
         const v8bf a = f[i % (kAhead + 1)];
         if (i < kSteps) y = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[i], y, 0, 0, 0);
         else o[(i - kSteps) % kBlocks] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, w[(i - kSteps) / kBlocks], o[(i - kSteps) % kBlocks], 0, 0, 0);
-        // the product's share of block j's 16 logits (as in weigh)
+        // the product's share of block j - 1's weights, and of block j's 16 logits (as in weigh)
+#pragma unroll
+        for (int p = i * 8 / kProducts; SUMS && p < (i + 1) * 8 / kProducts; ++p) {
+          lr = add_rounded(w[p / 4], p % 4, lr);
+          asm volatile("" ::"v"(lr));
+        }
 #pragma unroll
         for (int e = i * 16 / kProducts; e < (i + 1) * 16 / kProducts; ++e) {
           v[e & 1] = fast_exp2(fmaf(x[e], P.scale_log2, -m));
@@ -338,6 +347,7 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
     }
 
     l += __shfl_xor(l, 32);
+    const float whole = SUMS ? unrounded(l, lr + __shfl_xor(lr, 32)) : 1.f;
     bool none = false;                                                         // (also from tokens of its tiles that no row sees)
 #pragma unroll
     for (int c = 0; c < kBlocks; ++c)
@@ -348,7 +358,7 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
     } else if (r < r1) {
       const int64_t row = sq.first + i_row;
       if (st.parts == 1) {
-        const float inv = inverse_sum(l);
+        const float inv = inverse_sum(l) * whole;
         uint16_t* to = static_cast<uint16_t*>(A.out) + b * P.o_b + row * P.o_t + (int64_t)head * P.o_h + 4 * half;
 #pragma unroll
         for (int c = 0; c < kBlocks; ++c)
@@ -364,7 +374,7 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
         for (int c = 0; c < kBlocks; ++c)
 #pragma unroll
           for (int e = 0; e < 4; ++e)
-            *reinterpret_cast<float4*>(to + 32 * c + 8 * e) = make_float4(o[c][4 * e], o[c][4 * e + 1], o[c][4 * e + 2], o[c][4 * e + 3]);
+            *reinterpret_cast<float4*>(to + 32 * c + 8 * e) = make_float4(o[c][4 * e] * whole, o[c][4 * e + 1] * whole, o[c][4 * e + 2] * whole, o[c][4 * e + 3] * whole);
         if (half == 0) A.part.ml[at] = make_float2(seen ? m : -INFINITY, l);
       }
     }
@@ -372,41 +382,46 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
   }
 }
 
-template <int D, bool BANDED>
+template <int D, bool BANDED, bool SUMS>
 __global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_kernel(Paged P, AttendPlan pl, AttendArgs A) {
   __shared__ RowsLds<D> L;
-  attend_rows<D, BANDED>(P, pl, A, L, blockIdx.x);
+  attend_rows<D, BANDED, SUMS>(P, pl, A, L, blockIdx.x);
 }
 
 // Chunks, and the sequences of few rows among them: their workgroups come last and fill what the others leave idle.  (17 sequences of 1 to 969 new tokens over
 // 519 to 8192, 32 heads of 8 groups: 238 us, 266 one after the other.)
-template <int D, bool BANDED, int NQ>
+template <int D, bool BANDED, bool SUMS, int NQ>
 __global__ __launch_bounds__(64 * kRowWaves, 2) void attend_rows_mixed_kernel(Paged P, AttendPlan grid, AttendPlan even, AttendArgs A, Partials even_part, int grid_wgs) {
   using Few = EvenLds<uint16_t, D, NQ>;
   __shared__ __align__(1024) char lds[sizeof(RowsLds<D>) > sizeof(Few) ? sizeof(RowsLds<D>) : sizeof(Few)];
   if ((int)blockIdx.x < grid_wgs) {
-    attend_rows<D, BANDED>(P, grid, A, reinterpret_cast<RowsLds<D>&>(lds), blockIdx.x);
+    attend_rows<D, BANDED, SUMS>(P, grid, A, reinterpret_cast<RowsLds<D>&>(lds), blockIdx.x);
   } else {
     A.part = even_part;
     attend_evenly<uint16_t, D, NQ>(P, even, A, reinterpret_cast<Few&>(lds), blockIdx.x - grid_wgs, even.parts);
   }
 }
 
-template <int D, bool BANDED>
+template <int D, bool BANDED, bool SUMS>
 static void rows_launch(const Paged& P, const AttendPlan& pl, const AttendArgs& A, const AttendPlan& even, const Partials& even_part, hipStream_t s) {
   static_assert(kRowWaves == kWaves);
   const int wgs = (int)grid_size(P, pl);
   const dim3 all((unsigned)(wgs + even.parts)), block(64 * kRowWaves);
-  if (even.rows == 0)       launch(attend_rows_kernel<D, BANDED>, all, block, s, P, pl, A);
-  else if (even.rows == 16) launch(attend_rows_mixed_kernel<D, BANDED, 1>, all, block, s, P, pl, even, A, even_part, wgs);
-  else                      launch(attend_rows_mixed_kernel<D, BANDED, 2>, all, block, s, P, pl, even, A, even_part, wgs);
+  if (even.rows == 0)       launch(attend_rows_kernel<D, BANDED, SUMS>, all, block, s, P, pl, A);
+  else if (even.rows == 16) launch(attend_rows_mixed_kernel<D, BANDED, SUMS, 1>, all, block, s, P, pl, even, A, even_part, wgs);
+  else                      launch(attend_rows_mixed_kernel<D, BANDED, SUMS, 2>, all, block, s, P, pl, even, A, even_part, wgs);
+}
+template <int D, bool BANDED>
+static void rows_launch_of(const Paged& P, const AttendPlan& pl, const AttendArgs& A, const AttendPlan& even, const Partials& even_part, hipStream_t s) {
+  if (pl.sums) rows_launch<D, BANDED, true>(P, pl, A, even, even_part, s);
+  else         rows_launch<D, BANDED, false>(P, pl, A, even, even_part, s);
 }
 
 void launch_attend_rows(const Paged& P, const AttendPlan& pl, const AttendArgs& A, const AttendPlan& even, const Partials& even_part, hipStream_t s) {
   // (a lane's offset within the 16 rows of a run is 32 bits)
   const bool banded = P.div.page % 16 == 0 && P.row_stride * 2 * 16 < (int64_t)1 << 31;
-  if (P.d == 64) banded ? rows_launch<64, true>(P, pl, A, even, even_part, s) : rows_launch<64, false>(P, pl, A, even, even_part, s);
-  else           banded ? rows_launch<128, true>(P, pl, A, even, even_part, s) : rows_launch<128, false>(P, pl, A, even, even_part, s);
+  if (P.d == 64) banded ? rows_launch_of<64, true>(P, pl, A, even, even_part, s) : rows_launch_of<64, false>(P, pl, A, even, even_part, s);
+  else           banded ? rows_launch_of<128, true>(P, pl, A, even, even_part, s) : rows_launch_of<128, false>(P, pl, A, even, even_part, s);
 }
 
 }  // namespace ccd
