@@ -18,14 +18,23 @@ import torch
 from . import infinipot as ip
 
 
-def _workspace(held, paged, device):
-    """(the workspace to keep, the workspace of this call): the one held, if it is large enough.  A graph that is being captured has one of its own,
-    which nobody frees or uses between its replays."""
-    if torch.cuda.is_current_stream_capturing():
-        return held, ip.alloc_paged_workspace(paged, device)
-    if held is None or held.numel() < ip.ccd_paged_workspace_bytes(paged):
-        held = ip.alloc_paged_workspace(paged, device)
-    return held, held
+class _Kept:
+    """What calls of one stream keep for the next ones: nothing says that another stream's are done with it, or have written it."""
+
+    def __init__(self):
+        self.ws, self.rows, self.kv_len, self.held = None, {}, None, None      # rows: (pages, tokens) -> block table, q_start; held: the number in kv_len
+
+    def workspace(self, paged, device):
+        """A graph that is being captured has one of its own, which nobody frees or uses between its replays."""
+        if torch.cuda.is_current_stream_capturing():
+            return ip.alloc_paged_workspace(paged, device)
+        if self.ws is None or self.ws.numel() < ip.ccd_paged_workspace_bytes(paged):
+            self.ws = ip.alloc_paged_workspace(paged, device)
+        return self.ws
+
+
+def _kept(by_stream):
+    return by_stream.setdefault(torch.cuda.current_stream().cuda_stream, _Kept())
 
 
 class MemoryPot:
@@ -40,9 +49,7 @@ class MemoryPot:
         self.n_valid = 0
         self.calls = 0
         self._ws = None
-        self._attn_ws = None
-        self._attn_len = (None, None)           # kv_len as last written, and the number it holds
-        self._attn_rows = {}                    # (pages, tokens) -> block table, q_start
+        self._attn = {}                         # stream -> _Kept
 
     @property
     def room(self) -> int:
@@ -72,7 +79,7 @@ class MemoryPot:
         table, q_start, kv_len = self._attn_index(pages, m, Q.device)
         o, s = (out, lse) if one else (out.view(-1, *out.shape[2:]), lse.view(-1, *lse.shape[2:]))
         paged = ip.make_paged(keys, tokens=pages * m, block_table=table, Q=q, out=o, lse=s, window=window, behind=behind, max_new=m, max_len=max(1, self.n_valid))
-        self._attn_ws, ws = _workspace(self._attn_ws, paged, Q.device)
+        ws = _kept(self._attn).workspace(paged, Q.device)
         rc = ip.ccd_paged_attend(paged, q, keys, values, table, q_start, kv_len, o, s, ws)
         assert rc == ip.CCD_OK, rc
         return out, lse
@@ -84,15 +91,15 @@ class MemoryPot:
                     torch.arange(pages + 1, dtype=torch.int32, device=device) * m)
         if torch.cuda.is_current_stream_capturing():        # a graph keeps its own: nothing is written before it is replayed
             return *rows(), torch.full((pages,), self.n_valid, dtype=torch.int32, device=device)
-        if (pages, m) not in self._attn_rows:
-            self._attn_rows[pages, m] = rows()
-        kv_len, held = self._attn_len
-        if kv_len is None:
-            kv_len = torch.empty(self.B * self.L, dtype=torch.int32, device=device)
-        if held != self.n_valid:
-            kv_len.fill_(self.n_valid)
-            self._attn_len = (kv_len, self.n_valid)
-        return *self._attn_rows[pages, m], kv_len[:pages]
+        kept = _kept(self._attn)
+        if (pages, m) not in kept.rows:
+            kept.rows[pages, m] = rows()
+        if kept.kv_len is None:
+            kept.kv_len = torch.empty(self.B * self.L, dtype=torch.int32, device=device)
+        if kept.held != self.n_valid:
+            kept.kv_len.fill_(self.n_valid)
+            kept.held = self.n_valid
+        return *kept.rows[pages, m], kept.kv_len[:pages]
 
     def distill(self, Q_cat, scores=None, lse=None) -> int:
         """One CCD compression if the pot is full; returns the library's code (CCD_OK or CCD_NOOP).  lse: the catalyst rows' log-sum-exps, as
@@ -135,7 +142,7 @@ class PagedPots:
         self.lengths = [0] * sequences                  # on the host, as of the last step
         self.new = [0] * sequences
         self._plan = ip.make_plan(self.table, tokens=step_tokens, page=page, n_pages=n_pages)
-        self._ws = None
+        self._attn = {}                                 # stream -> _Kept
 
     def pages(self, length) -> int:
         return -(-length // self.page)
@@ -174,7 +181,7 @@ class PagedPots:
         out = torch.empty_like(Q, memory_format=torch.contiguous_format) if out is None else out
         lse = torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device) if lse is None else lse
         paged = self._paged(layer, Q.shape[0], Q=Q, out=out, lse=lse)
-        self._ws, ws = _workspace(self._ws, paged, Q.device)
+        ws = _kept(self._attn).workspace(paged, Q.device)
         rc = ip.ccd_paged_attend(paged, Q, self.K[:, layer], self.V[:, layer], self.table, self.q_start, self.after, out, lse, ws)
         assert rc == ip.CCD_OK, rc
         return out, lse

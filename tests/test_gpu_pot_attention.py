@@ -248,3 +248,24 @@ def test_captured_attention_over_a_pool(dtype):
                 for layer in range(L):
                     p.append(layer, k, v)
                     p.attend(layer, q)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_a_pots_attention_on_two_streams_at_once(dtype):
+    """Calls that nothing orders share no workspace and no index tensor."""
+    pot = MemoryPot(2, 2, 2, 64, 3000, 100, 50, dtype=DT[dtype])
+    _fill(pot, 2900, 5)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    Qs = [torch.randn((2, 2, 6, m, 64), generator=g, device="cuda").to(DT[dtype]) for m in (1, 40)]
+    want = [pot.attend(Q, behind=True) for Q in Qs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in Qs]
+    outs = [[], []]
+    for _ in range(20):
+        for i, (Q, stream) in enumerate(zip(Qs, streams)):
+            with torch.cuda.stream(stream):
+                outs[i].append(pot.attend(Q, behind=True))
+    torch.cuda.synchronize()
+    for (w, wl), got in zip(want, outs):
+        for o, lse in got:
+            assert torch.equal(o, w) and torch.equal(lse, wl)
