@@ -300,23 +300,38 @@ def ccd_compress_kcat(shape, Q_cat, K, V, K_cap, novelty, keep_idx, workspace, s
 
 # ---- paged caches
 
-def _here(*tensors):
-    """The call runs on the current device's stream: its tensors must be there."""
-    device = torch.cuda.current_device()
+# The checks below stand in the way of calls whose kernels take 4 us: attributes of a tensor are read once each, and the device is asked for once.
+_I32 = torch.int32
+_get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _stream_here(stream, t, u):
+    """The stream to launch on; t and u must be on the current device."""
+    device = _get_device()
+    if t.get_device() != device or u.get_device() != device:
+        raise ValueError(f"tensors on {t.device} and {u.device}, and the current device is cuda:{device}")
+    if stream is not None:
+        return stream.cuda_stream
+    return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(device)
+
+
+def _int32(entries, *tensors):
+    """Index tensors, and the entries that the descriptor says they have."""
     for t in tensors:
-        if t.device.index != device:
-            raise ValueError(f"a tensor on {t.device}, and the current device is cuda:{device}")
-
-
-def _int32(*tensors):
-    """Pairs of an index tensor and the entries that the descriptor says it has."""
-    for t, entries in tensors:
-        assert t.dtype is torch.int32 and t.is_contiguous(), "contiguous int32 needed"
-        assert t.numel() >= entries, f"{t.numel()} entries, {entries} needed"
+        if t.dtype is not _I32 or not t.is_contiguous():
+            raise AssertionError("contiguous int32 needed")
+        if t.numel() < entries:
+            raise AssertionError(f"{t.numel()} entries, {entries} needed")
 
 
 def _turns(turns, rope):
-    assert turns.dtype is torch.int64 and turns.is_contiguous() and turns.numel() >= rope.rot // 2, "turns as rope_turns gives them"
+    if turns.dtype is not torch.int64 or turns.numel() < rope.rot // 2 or not turns.is_contiguous():
+        raise AssertionError("turns as rope_turns gives them needed")
+
+
+def _alike(a, b):
+    if a.stride() != b.stride() or a.dtype is not b.dtype or a.numel() != b.numel():
+        raise AssertionError("keys and values differ in shape, strides or type")
 
 
 def make_plan(block_table, *, tokens, page, n_pages) -> ccd_paged_t:
@@ -397,45 +412,57 @@ def ccd_paged_plan(paged, len_before, len_after, block_table, block_table_next, 
                    stream=None) -> int:
     """len_before, len_after [B], block_table and block_table_next [B, table_width] (may be one), free_pages [n_pages], cursor and
     cursor_next [4] (may be one), q_start [B + 1], slots and positions [tokens]: int32."""
-    B, entries = paged.B, paged.B * paged.table_width
-    _int32((len_before, B), (len_after, B), (block_table, entries), (block_table_next, entries), (free_pages, paged.n_pages), (cursor, 4), (cursor_next, 4),
-           (q_start, B + 1), (slots, paged.tokens), (positions, paged.tokens))
-    _here(block_table)
-    return _check(lib().ccd_paged_plan(ctypes.byref(paged), _ptr(len_before), _ptr(len_after), _ptr(block_table), _ptr(block_table_next),
-                                       _ptr(free_pages), _ptr(cursor), _ptr(cursor_next), _ptr(q_start), _ptr(slots), _ptr(positions),
-                                       _stream(stream)))
+    B, tokens = paged.B, paged.tokens
+    _int32(B, len_before, len_after)
+    _int32(B * paged.table_width, block_table, block_table_next)
+    _int32(paged.n_pages, free_pages)
+    _int32(4, cursor, cursor_next)
+    _int32(B + 1, q_start)
+    _int32(tokens, slots, positions)
+    stream = _stream_here(stream, block_table, slots)
+    return _check(lib().ccd_paged_plan(ctypes.byref(paged), len_before.data_ptr(), len_after.data_ptr(), block_table.data_ptr(), block_table_next.data_ptr(),
+                                       free_pages.data_ptr(), cursor.data_ptr(), cursor_next.data_ptr(), q_start.data_ptr(), slots.data_ptr(),
+                                       positions.data_ptr(), stream))
 
 
 def ccd_rope(rope, X, positions, turns, Y, stream=None) -> int:
     """positions int32 [tokens]; turns as rope_turns gives them; Y may be X."""
-    _int32((positions, rope.tokens))
+    _int32(rope.tokens, positions)
     _turns(turns, rope)
-    _here(X, positions)
-    return _check(lib().ccd_rope(ctypes.byref(rope), _ptr(X), _ptr(positions), _ptr(turns), _ptr(Y), _stream(stream)))
+    stream = _stream_here(stream, X, positions)
+    return _check(lib().ccd_rope(ctypes.byref(rope), X.data_ptr(), positions.data_ptr(), turns.data_ptr(), Y.data_ptr(), stream))
 
 
 def ccd_paged_append(paged, K_new, V_new, slots, K_pages, V_pages, rope=None, positions=None, turns=None, stream=None) -> int:
     """K_new and V_new have the same strides, as have K_pages and V_pages; with a rope descriptor the keys are embedded at `positions`."""
-    _int32((slots, paged.tokens))
-    assert K_new.stride() == V_new.stride() and K_new.shape == V_new.shape and K_new.dtype == V_new.dtype == K_pages.dtype
-    assert K_pages.stride() == V_pages.stride() and K_pages.shape == V_pages.shape and K_pages.dtype == V_pages.dtype
-    if rope is not None:
-        _int32((positions, paged.tokens))
-        _turns(turns, rope)
-    _here(K_pages, slots)
-    return _check(lib().ccd_paged_append(ctypes.byref(paged), None if rope is None else ctypes.byref(rope), _ptr(K_new), _ptr(V_new), _ptr(slots),
-                                         _ptr(positions), _ptr(turns), _ptr(K_pages), _ptr(V_pages), _stream(stream)))
+    tokens = paged.tokens
+    _alike(K_new, V_new)
+    _alike(K_pages, V_pages)
+    if K_new.dtype is not K_pages.dtype:
+        raise AssertionError("new keys and the cache differ in type")
+    if rope is None:
+        _int32(tokens, slots)
+        return _check(lib().ccd_paged_append(ctypes.byref(paged), None, K_new.data_ptr(), V_new.data_ptr(), slots.data_ptr(), None, None, K_pages.data_ptr(),
+                                             V_pages.data_ptr(), _stream_here(stream, K_pages, slots)))
+    _int32(tokens, slots, positions)
+    _turns(turns, rope)
+    return _check(lib().ccd_paged_append(ctypes.byref(paged), ctypes.byref(rope), K_new.data_ptr(), V_new.data_ptr(), slots.data_ptr(), positions.data_ptr(),
+                                         turns.data_ptr(), K_pages.data_ptr(), V_pages.data_ptr(), _stream_here(stream, K_pages, slots)))
 
 
 def ccd_paged_attend(paged, Q, K_pages, V_pages, block_table, q_start, kv_len, out, lse, workspace, stream=None) -> int:
     """block_table [B, table_width], q_start [B + 1], kv_len [B]: int32; lse fp32 or None."""
-    _int32((block_table, paged.B * paged.table_width), (q_start, paged.B + 1), (kv_len, paged.B))
-    assert K_pages.stride() == V_pages.stride() and K_pages.shape == V_pages.shape
-    assert Q.dtype == out.dtype == K_pages.dtype == V_pages.dtype and (lse is None or lse.dtype == torch.float32)
-    _here(Q, K_pages, block_table)
-    return _check(lib().ccd_paged_attend(ctypes.byref(paged), _ptr(Q), _ptr(K_pages), _ptr(V_pages), _ptr(block_table), _ptr(q_start), _ptr(kv_len),
-                                         _ptr(out), _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel(),
-                                         _stream(stream)))
+    B, dtype = paged.B, K_pages.dtype
+    _int32(B * paged.table_width, block_table)
+    _int32(B + 1, q_start)
+    _int32(B, kv_len)
+    _alike(K_pages, V_pages)
+    if Q.dtype is not dtype or out.dtype is not dtype or (lse is not None and lse.dtype is not torch.float32):
+        raise AssertionError("Q, out and the cache differ in type, or lse is not fp32")
+    stream = _stream_here(stream, Q, K_pages)
+    return _check(lib().ccd_paged_attend(ctypes.byref(paged), Q.data_ptr(), K_pages.data_ptr(), V_pages.data_ptr(), block_table.data_ptr(), q_start.data_ptr(),
+                                         kv_len.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
+                                         *((None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())), stream))
 
 
 def ccd_profile_enable(on: bool) -> int:
