@@ -154,6 +154,9 @@ ROPE = [  # dtype, tokens, heads, d, rot, layout
     ("bf16", 9, 7, 128, 90, "half"), ("bf16", 9, 7, 128, 90, "pairs"), ("bf16", 300, 12, 80, 80, "half"), ("bf16", 2, 5, 1024, 512, "half"), ("bf16", 2, 5, 1024, 1024, "pairs"),
     ("bf16", 2, 2, 8, 2, "half"), ("fp32", 37, 5, 128, 128, "half"), ("fp32", 37, 5, 64, 64, "pairs"), ("fp32", 11, 33, 128, 64, "half"), ("fp32", 3, 2, 4, 4, "pairs"),
     ("fp32", 3, 2, 1024, 1000, "half"), ("fp32", 4, 9, 128, 66, "pairs"), ("fp32", 1100, 2, 64, 24, "half"),
+    # turned parts of no whole pieces, through more heads than one batch
+    ("bf16", 1050, 72, 64, 60, "half"), ("bf16", 1050, 72, 64, 58, "pairs"), ("fp32", 1030, 40, 128, 118, "half"), ("fp32", 7, 40, 128, 126, "pairs"), ("bf16", 6, 131, 64, 2, "pairs"),
+    ("bf16", 3, 20, 512, 300, "pairs"),
 ]
 
 
