@@ -270,7 +270,8 @@ CCD_API int ccd_paged_plan(const ccd_paged_t* paged, const int32_t* len_before, 
 /* Rotary positions.  Pair i of the first `rot` elements of a head is turned by the angle position * f_i:
  *   y_1 = a * (x_1 cos - x_2 sin),  y_2 = a * (x_2 cos + x_1 sin)
  * (x_1, x_2) being elements (i, i + rot/2) with CCD_ROPE_HALF and (2 i, 2 i + 1) with CCD_ROPE_PAIRS, a = amplitude; elements
- * from rot on are copied.  `inverse` turns the other way: the embedding taken off again, and the gradient of the embedding.
+ * from rot on are copied.  `inverse` turns the other way: the gradient of the embedding and, with a = 1, the embedding taken off
+ * again.
  * Frequencies, in radians per position: f_i = base^(-2 i / rot), and for contexts longer than the trained one
  *   CCD_ROPE_LINEAR  f_i / factor
  *   CCD_ROPE_NTK     with base * factor^(rot / (rot - 2)) as the base (rot = 2: unchanged)
@@ -320,7 +321,8 @@ CCD_API size_t ccd_paged_workspace_bytes(const ccd_paged_t* paged);
  * position p = n - m + i (behind: n + i) and
  *   out = sum_t w_t v_t / sum_t w_t,  w_t = exp(scale * <q, k_t>),  lse = log sum_t w_t
  * over the positions t < n with t <= p, t > p - window if there is one, and a page in the table.  A row that sees nothing has
- * out = 0 and lse = -inf.  out must not overlap Q; lse (fp32) may be NULL.  Rows of no sequence are left as they are.
+ * out = 0 and lse = -inf; keys and values that a row does not see do not reach it, infinite or NaN as they may be.  out must not
+ * overlap Q; lse (fp32) may be NULL.  Rows of no sequence are left as they are.
  * Logits, softmax and sums are fp32; with a bf16 cache the weights of a tile of tokens are rounded to bf16 for their product
  * with the values. */
 CCD_API int ccd_paged_attend(const ccd_paged_t* paged, const void* Q, const void* K_pages, const void* V_pages,
