@@ -579,8 +579,10 @@ __device__ __forceinline__ void attend_evenly(const Paged& P, const AttendPlan& 
       const int t_begin = sp.begin + (int)(at - unit_at), t_stop = sp.begin + (int)(until - unit_at);
       if (!alone || first == me)
         for (int r0 = 0; r0 < rows_all; r0 += kRows) {
-          const bool again = attend_stretch<T, D, NQ, kWaves>(P, A, L, sq, b, h, r0, r0 + kRows < rows_all ? r0 + kRows : rows_all, alone ? sp.begin : t_begin,
-                                                      alone || t_stop > sp.end ? sp.end : t_stop, alone || first == last, (int64_t)(2 * me + (first == me)) * kRows, 0);
+          const int r1 = r0 + kRows < rows_all ? r0 + kRows : rows_all;
+          Stretch st{t_begin, t_stop < sp.end ? t_stop : sp.end, 1, 0};
+          if (alone) st = cut_rows(P, sq, r0, r1, 1, 1 << 30);               // what the block sees, which is not what the unit does
+          const bool again = attend_stretch<T, D, NQ, kWaves>(P, A, L, sq, b, h, r0, r1, st.begin, st.end, alone || first == last, (int64_t)(2 * me + (first == me)) * kRows, 0);
           // (the kernel that joins does them again, those of several stretches without being told)
           if (again && (alone || first == last) && tid == 0) meta[b * P.Hkv + h].y = kAgain;
         }
