@@ -321,7 +321,9 @@ CCD_API size_t ccd_paged_workspace_bytes(const ccd_paged_t* paged);
  * position p = n - m + i (behind: n + i) and
  *   out = sum_t w_t v_t / sum_t w_t,  w_t = exp(scale * <q, k_t>),  lse = log sum_t w_t
  * over the positions t < n with t <= p, t > p - window if there is one, and a page in the table.  A row that sees nothing has
- * out = 0 and lse = -inf; keys and values that a row does not see do not reach it, infinite or NaN as they may be.  out must not
+ * out = 0 and lse = -inf; keys and values that a row does not see do not reach it, infinite or NaN as they may be (rows that stand beside
+ * such a value are worked out once more, one by one: some milliseconds each over long caches).  An infinite value that a row does see makes its element
+ * infinite, or NaN where its weight is 0 in fp32.  out must not
  * overlap Q; lse (fp32) may be NULL.  Rows of no sequence are left as they are.
  * Logits, softmax and sums are fp32; with a bf16 cache the weights of a tile of tokens are rounded to bf16 for their product
  * with the values. */

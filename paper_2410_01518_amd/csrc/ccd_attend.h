@@ -131,38 +131,93 @@ __device__ __forceinline__ bool find_block(const Paged& P, const AttendPlan& pl,
 }
 
 // A weight of 0 takes a token out of a product only if its value is a number.  Where some rows see a token and others do not, and its value is infinite
-// or NaN, the products carry NaN into rows that do not see it.  Sums that come out as NaN where the rows are of several new tokens are therefore
-// taken once more, by a wave a row, over those of the tokens t_begin .. t_end - 1 alone that it sees.  They are the result (whole_row) or
-// the stretch's `entry` of the workspace.
+// or NaN, the products carry NaN into rows that do not see it.  A row is therefore taken once more, over those tokens alone that it sees, if its sums come out
+// as NaN and that can be why: its sum of weights is a number (weights of unseen tokens are 0 before they are summed up: where it is none, the row
+// sees a key, or has a query, that is none), and an unseen value that went into the products is none.  Both are looked at because rows that see a NaN
+// stay NaN, and a row by itself is slow, 5 ms over 32768 tokens of a bf16 cache: 2048 new tokens over 32768, with a NaN that all of them see,
+// 1150 ms if every row is taken again, 1.1 so; 158 where the NaN is in the last token's value, for the rows of its block (a wave has 32 of them) before it.
+
+// Of the tokens t_first .. t_end - 1: is a value that some of the rows r0 .. r1 - 1 do not see (nobody those before t_begin) infinite or NaN?  By the wave.
+template <class T, int D>
+__device__ __forceinline__ bool bad_unseen(const Paged& P, const AttendArgs& A, const Sequence& sq, int b, int hkv, int r0, int r1, int t_first, int t_begin, int t_end) {
+  const int low = first_seen(P, sq.base + (r1 - 1) / P.G), next = sq.base + r0 / P.G + 1, all_from = low > t_begin ? low : t_begin;
+  const int32_t* pages = A.table + (int64_t)b * P.table_width;
+  const T* V = static_cast<const T*>(A.V) + hkv * P.head_stride + (threadIdx.x & 63);
+  bool bad = false;
+  for (int t = t_first; t < t_end; ++t) {
+    if (t >= all_from && t < next) t = next;                    // (all rows see those)
+    if (t >= t_end) break;
+    const int c = page_of(P.div, t), id = pages[c];
+    if (id < 0 || id >= P.n_pages) continue;
+    const T* v = V + id * P.page_stride + (int64_t)(t - c * P.div.page) * P.row_stride;
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) bad = bad || !(fabsf(load_elem(v + j * 64)) < INFINITY);
+  }
+  return __any(bad);
+}
+
+// Row r over the tokens of t_begin .. t_end - 1 that it sees, by a wave, 64 tokens at a time: a lane has the logit of one of them, and then d / 64 elements of the sums.
+// That is the result (whole_row), or the stretch's `entry` of the workspace.
 template <class T, int D>
 __device__ __forceinline__ void redo_row(const Paged& P, const AttendArgs& A, const Sequence& sq, int b, int hkv, int r, int t_begin, int t_end,
                                          bool whole_row, int64_t entry) {
-  constexpr int kPer = D / 64;
+  constexpr int kPer = D / 64, kEPL = 16 / sizeof(T), kSide = 8;
   const int lane = threadIdx.x & 63;
   const int32_t* pages = A.table + (int64_t)b * P.table_width;
   const T* K = static_cast<const T*>(A.K) + hkv * P.head_stride;
   const T* V = static_cast<const T*>(A.V) + hkv * P.head_stride;
+  const T* zero = reinterpret_cast<const T*>(g_zero_row);
   const int i = r / P.G, head = hkv * P.G + r - i * P.G, pos = sq.base + i, low = first_seen(P, pos);
   const int64_t row = sq.first + i;
-  const T* q = static_cast<const T*>(A.Q) + b * P.q_b + row * P.q_t + head * P.q_h;
+  const T* from = static_cast<const T*>(A.Q) + b * P.q_b + row * P.q_t + head * P.q_h;
   const int begin = low > t_begin ? low : t_begin, end = pos + 1 < t_end ? pos + 1 : t_end;
-  float m = -INFINITY, l = 0.f, o[kPer] = {};
-  for (int t = begin; t < end; ++t) {
-    const int c = page_of(P.div, t), id = pages[c];
-    if (id < 0 || id >= P.n_pages) continue;
-    const int64_t at = id * P.page_stride + (int64_t)(t - c * P.div.page) * P.row_stride;
+  auto of_lane = [](float x, int u) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), u)); };
+  float q[kPer], m = -INFINITY, l = 0.f, o[kPer] = {};
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) q[j] = load_elem(from + j * 64 + lane);
+  for (int t0 = begin; t0 < end; t0 += 64) {
+    int64_t off = -1;                                           // of token t0 + lane
+    if (t0 + lane < end) {
+      const int t = t0 + lane, c = page_of(P.div, t), id = pages[c];
+      if (id >= 0 && id < P.n_pages) off = id * P.page_stride + (int64_t)(t - c * P.div.page) * P.row_stride;
+    }
+    const T* k = off >= 0 ? K + off : zero;
     float x = 0.f;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) x = fmaf(load_elem(q + j * 64 + lane), load_elem(K + at + j * 64 + lane), x);
+    for (int j = 0; j < kPer; ++j)
+#pragma unroll 2
+      for (int p = 0; p < 64; p += kEPL) {
+        float y[kEPL];
+        load_f32(*reinterpret_cast<const v4u*>(k + j * 64 + p), y, static_cast<const T*>(nullptr));
 #pragma unroll
-    for (int s = 32; s; s >>= 1) x += __shfl_xor(x, s);
-    x *= P.scale_log2;
-    const float next = fmaxf(m, x), keep = next == -INFINITY ? 1.f : fast_exp2(m - next), w = next == -INFINITY && x == x ? 0.f : fast_exp2(x - next);
+        for (int e = 0; e < kEPL; ++e) x = fmaf(of_lane(q[j], p + e), y[e], x);
+      }
+    x = off >= 0 ? x * P.scale_log2 : -INFINITY;
+    float next = fmaxf(m, x);
+#pragma unroll
+    for (int s = 32; s; s >>= 1) next = fmaxf(next, __shfl_xor(next, s));
+    const float keep = next == -INFINITY ? 1.f : fast_exp2(m - next), w = fast_exp2(x - (next == -INFINITY ? 0.f : next));
     m = next;
     l = l * keep + w;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) o[j] = o[j] * keep + (w != 0.f ? w * load_elem(V + at + j * 64 + lane) : 0.f);
+    for (int j = 0; j < kPer; ++j) o[j] *= keep;
+    for (int u0 = 0; u0 < 64 && t0 + u0 < end; u0 += kSide) {
+      float v[kSide][kPer];
+#pragma unroll
+      for (int u = 0; u < kSide; ++u) {
+        const int64_t at = (int64_t)__builtin_amdgcn_readlane((int)(off >> 32), u0 + u) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)off, u0 + u);
+        const T* from_v = at >= 0 ? V + at : zero;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) v[u][j] = load_elem(from_v + j * 64 + lane);
+      }
+#pragma unroll
+      for (int u = 0; u < kSide; ++u)
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) o[j] = fmaf(of_lane(w, u0 + u), v[u][j], o[j]);
+    }
   }
+#pragma unroll
+  for (int s = 32; s; s >>= 1) l += __shfl_xor(l, s);
   if (whole_row) {
     const float inv = inverse_sum(l);
 #pragma unroll
@@ -174,12 +229,10 @@ __device__ __forceinline__ void redo_row(const Paged& P, const AttendArgs& A, co
     if (lane == 0) A.part.ml[entry] = make_float2(m, l);
   }
 }
-// rows r0, r0 + step .. of those before r1, in a grid's stretch part_no, by the wave
+// the same for a grid's stretch part_no
 template <class T, int D>
-__device__ __forceinline__ void redo_rows(const Paged& P, const AttendArgs& A, const Sequence& sq, int b, int hkv, int r0, int r1, int step, int t_begin, int t_end,
-                                          bool whole_row, int part_no) {
-  for (int r = r0; r < r1; r += step)
-    redo_row<T, D>(P, A, sq, b, hkv, r, t_begin, t_end, whole_row, ((int64_t)part_no * P.tokens + sq.first + r / P.G) * P.Hq + hkv * P.G + r % P.G);
+__device__ __forceinline__ void redo_row_of(const Paged& P, const AttendArgs& A, const Sequence& sq, int b, int hkv, int r, int t_begin, int t_end, bool whole_row, int part_no) {
+  redo_row<T, D>(P, A, sq, b, hkv, r, t_begin, t_end, whole_row, ((int64_t)part_no * P.tokens + sq.first + r / P.G) * P.Hq + hkv * P.G + r % P.G);
 }
 
 inline unsigned grid_size(const Paged& P, const AttendPlan& pl) {

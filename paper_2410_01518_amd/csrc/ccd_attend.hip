@@ -36,6 +36,13 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Paged P, AttendPlan pl
   constexpr int kPer = D / 64;
   __shared__ float sums[WAVES > 1 ? WAVES : 1][D];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  // row r of a unit of the even cut, whose products took in what the unit sees (those of a block of more rows than expected, less)
+  auto again = [&](const Sequence& sq, int b, int hkv, int r) __attribute__((always_inline)) {
+    const Span sp = span_of(P, pl, sq);
+    const bool bad = bad_unseen<T, D>(P, A, sq, b, hkv, r, r + 1, sp.begin, sp.begin, sp.end);
+    if (bad) redo_row<T, D>(P, A, sq, b, hkv, r, 0, sq.n, true, 0);
+    return bad;
+  };
   // entry of the first stretch, of the second less a step, distance of the others
   auto join = [&](const Sequence& sq, int b, int hkv, int r, int parts, int64_t part_first, int64_t part_0, int64_t part_step) __attribute__((always_inline)) {
     auto entry = [&](int p) { return p == 0 ? part_first : part_0 + p * part_step; };
@@ -84,11 +91,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Paged P, AttendPlan pl
     }
     bool none = false;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) none = none || acc[j] != acc[j];
-    if (EVEN && sq.m > 1 && __builtin_expect(__any(none), 0)) {
-      redo_row<T, D>(P, A, sq, b, hkv, r, 0, sq.n, true, 0);
-      return;
-    }
+    for (int j = 0; j < kPer; ++j) none = none || (acc[j] != acc[j] && sum == sum);
+    if (EVEN && sq.m > 1 && __builtin_expect(__any(none), 0) && again(sq, b, hkv, r)) return;
     const int row = sq.first + r / P.G, head = hkv * P.G + r % P.G;
     const float inv = inverse_sum(sum);
 #pragma unroll
@@ -106,7 +110,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(Paged P, AttendPlan pl
       const int2 cut = A.part.meta[unit];
       if (cut.y == 1 || (cut.y == kAgain && WAVES > 1 && wave != 0)) return;
       for (int r = (int)(at0 % pl.join); r < rows_all; r += pl.join) {
-        if (cut.y == kAgain) { redo_row<T, D>(P, A, sq, b, hkv, r, 0, sq.n, true, 0); continue; }
+        if (cut.y == kAgain) { again(sq, b, hkv, r); continue; }
         join(sq, b, hkv, r, cut.y, (int64_t)(2 * cut.x + 1) * pl.rows + r, (int64_t)(2 * cut.x) * pl.rows + r, 2 * pl.rows);
       }
     } else {

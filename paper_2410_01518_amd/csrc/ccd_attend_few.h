@@ -260,7 +260,7 @@ struct SplitLds {
 
 // Rows r0 .. r1 - 1 of unit (b, hkv) over the tokens t_begin .. t_end - 1, by the workgroup.  whole_row: these are all tokens the rows see, the result
 // is written; else (o, m, l) of row r go to entry part0 + (r - r0) of the workspace, or, part0 < 0, to those of part_no by the row's number.
-// Returns whether the rows have to be done again (redo_rows).
+// Returns whether the rows may have to be done again (bad_unseen says).
 template <class T, int D, int NQ, int WAVES>
 __device__ __forceinline__ bool attend_stretch(const Paged& P, const AttendArgs& A, SplitLds<T, D, NQ, WAVES>& L, const Sequence& sq, int b, int hkv, int r0, int r1,
                                                int t_begin, int t_end, bool whole_row, int64_t part0, int part_no) {
@@ -393,7 +393,7 @@ __device__ __forceinline__ bool attend_stretch(const Paged& P, const AttendArgs&
     if (lane < 16) { L.m[wave][16 * j + lane] = m[j]; L.l[wave][16 * j + lane] = l[j]; }
   }
   __syncthreads();
-  bool none = false;                                        // sums that are no numbers
+  bool none = false;                                        // sums that are no numbers, of weights that are
 #pragma unroll
   for (int j = 0; j < NQ; ++j) {
     float all = -INFINITY;
@@ -425,7 +425,7 @@ __device__ __forceinline__ bool attend_stretch(const Paged& P, const AttendArgs&
     }
     if (r < r1) {
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) none = none || acc[e] != acc[e];
+      for (int e = 0; e < kPer; ++e) none = none || (acc[e] != acc[e] && sum == sum);
       const int i = r / P.G, head = hkv * P.G + r - i * P.G;
       const int64_t row = sq.first + i;
       if (whole_row) {
@@ -457,9 +457,8 @@ __device__ __forceinline__ void attend_on_grid(const Paged& P, const AttendPlan&
   const int own_b = idx % P.B;
   if (!LISTED) idx /= P.B;
   const int part_no = idx % pl.parts, turn_no = LISTED ? idx / pl.parts : in_turn(pl, idx / pl.parts);
-  bool again = false;
-  for (int pass = 0; pass < 2; ++pass) {                   // (once more over all of it, row by row, if need be)
-    int b = own_b, r0 = (pl.row_blocks - 1 - turn_no) * kRows, k = turn_no;              // the last rows see most: first
+  auto blocks = [&](auto&& block) __attribute__((always_inline)) {
+    int b = own_b, r0 = (pl.row_blocks - 1 - turn_no) * kRows, k = turn_no;                // the last rows see most: first
     while (!LISTED || find_block(P, pl, A, k, b, r0)) {
       const Sequence sq = load_sequence(P, b, A.q_start, A.kv_len);
       const int rows_all = sq.m * P.G;
@@ -467,17 +466,23 @@ __device__ __forceinline__ void attend_on_grid(const Paged& P, const AttendPlan&
       const int r1 = r0 + kRows < rows_all ? r0 + kRows : rows_all;
       const Stretch st = cut_rows(P, sq, r0, r1, pl.parts, pl.chunk);
       const int t_begin = st.begin + part_no * st.chunk, t_end = t_begin + st.chunk < st.end ? t_begin + st.chunk : st.end;
-      if (part_no >= st.parts) {}
-      else if (pass == 0) again = attend_stretch<T, D, NQ, WAVES>(P, A, L, sq, b, hkv, r0, r1, t_begin, t_end, st.parts == 1, -1, part_no) || again;
-      else                redo_rows<T, D>(P, A, sq, b, hkv, r0 + (int)(threadIdx.x >> 6), r1, WAVES, t_begin, t_end, st.parts == 1, part_no);
+      if (part_no < st.parts) block(sq, b, r0, r1, t_begin, t_end, st.parts == 1);
       r0 += pl.row_blocks * kRows;                         // (more rows than the host expected)
       k += pl.blocks;
     }
-    if (__builtin_expect(!again, 1)) break;
-  }
+  };
+  bool again = false;
+  blocks([&](const Sequence& sq, int b, int r0, int r1, int t_begin, int t_end, bool whole) __attribute__((always_inline)) {
+    again = attend_stretch<T, D, NQ, WAVES>(P, A, L, sq, b, hkv, r0, r1, t_begin, t_end, whole, -1, part_no) || again;
+  });
+  if (__builtin_expect(!again, 1)) return;
+  blocks([&](const Sequence& sq, int b, int r0, int r1, int t_begin, int t_end, bool whole) __attribute__((always_inline)) {
+    if (!bad_unseen<T, D>(P, A, sq, b, hkv, r0, r1, t_begin, t_begin, t_end)) return;
+    for (int r = r0 + (int)(threadIdx.x >> 6); r < r1; r += WAVES) redo_row_of<T, D>(P, A, sq, b, hkv, r, t_begin, t_end, whole, part_no);
+  });
 }
 
-constexpr int kAgain = -1;                                  // for a unit's number of stretches: its rows have to be done again
+constexpr int kAgain = -1;                                  // for a unit's number of stretches: its rows may have to be done again
 
 // What all lanes have alike, into scalar registers (what comes from LDS the compiler takes to differ by lane).
 __device__ __forceinline__ int64_t uniform(int64_t x) {
@@ -583,7 +588,7 @@ __device__ __forceinline__ void attend_evenly(const Paged& P, const AttendPlan& 
           Stretch st{t_begin, t_stop < sp.end ? t_stop : sp.end, 1, 0};
           if (alone) st = cut_rows(P, sq, r0, r1, 1, 1 << 30);               // what the block sees, which is not what the unit does
           const bool again = attend_stretch<T, D, NQ, kWaves>(P, A, L, sq, b, h, r0, r1, st.begin, st.end, alone || first == last, (int64_t)(2 * me + (first == me)) * kRows, 0);
-          // (the kernel that joins does them again, those of several stretches without being told)
+          // (the kernel that joins sees to it, for those of several stretches without being told)
           if (again && (alone || first == last) && tid == 0) meta[b * P.Hkv + h].y = kAgain;
         }
       at = until;

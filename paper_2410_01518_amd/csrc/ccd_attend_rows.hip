@@ -348,14 +348,18 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
 
     l += __shfl_xor(l, 32);
     const float whole = SUMS ? unrounded(l, lr + __shfl_xor(lr, 32)) : 1.f;
-    bool none = false;                                                         // (also from tokens of its tiles that no row sees)
+    bool none = false;
 #pragma unroll
     for (int c = 0; c < kBlocks; ++c)
 #pragma unroll
       for (int e = 0; e < 16; ++e) none = none || o[c][e] != o[c][e];
-    if (__builtin_expect(__any(none && r < r1), 0)) {
-      redo_rows<uint16_t, D>(P, A, sq, b, hkv, w0, w1, 1, t_begin, t_end, st.parts == 1, part_no);
-    } else if (r < r1) {
+    none = none && l == l && r < r1;
+    uint32_t again = 0;                                                        // the wave's rows that are taken once more (the tiles begin before the stretch)
+    if (__builtin_expect(__any(none), 0) && bad_unseen<uint16_t, D>(P, A, sq, b, hkv, w0, w1, tile0, t_begin, t_end)) {
+      const uint64_t lanes = __ballot(none);
+      again = (uint32_t)lanes | (uint32_t)(lanes >> 32);
+    }
+    if (r < r1 && !((again >> (lane & 31)) & 1u)) {
       const int64_t row = sq.first + i_row;
       if (st.parts == 1) {
         const float inv = inverse_sum(l) * whole;
@@ -378,6 +382,7 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
         if (half == 0) A.part.ml[at] = make_float2(seen ? m : -INFINITY, l);
       }
     }
+    for (; again != 0; again &= again - 1) redo_row_of<uint16_t, D>(P, A, sq, b, hkv, w0 + __builtin_ctz(again), t_begin, t_end, st.parts == 1, part_no);
     __syncthreads();
   }
 }
