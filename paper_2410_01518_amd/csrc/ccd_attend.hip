@@ -1,5 +1,6 @@
 // ccd_paged_attend: the kernels of few rows per unit and of fp32 caches (ccd_attend_few.h), the joining of stretches, and how a call is cut.
 #include "ccd_attend_few.h"
+#include "ccd_attend_grid.h"
 
 namespace ccd {
 
@@ -213,12 +214,15 @@ static AttendCuts plan_attend(const Paged& P, int dtype, int max_new, int max_le
     g.rows = g.by_rows ? 128 : 32;
     g.few = c.even.few;
     g.row_blocks = (int)((rows + g.rows - 1) / g.rows);
-    // What the rows of all sequences fill, and one more block for each, is all that there can be.
+    // (as many blocks as there can be, not the most of any sequence for all: 512 slots, 64 of them with a chunk or a token)
     const int64_t filled = ((int64_t)P.tokens * P.G + g.rows - 1) / g.rows, of_all = (int64_t)P.B * g.row_blocks;
-    if (of_all > filled + P.B) g.blocks = (int)(filled + P.B);
+    const int64_t listed = most_blocks(P.B, P.tokens, P.G, g.rows, g.few);
+    if (of_all > listed) g.blocks = (int)listed;
     const int64_t units = P.Hkv * (filled < 1 ? 1 : filled < of_all ? filled : of_all);
     if (P.window > 0 && len > (int64_t)P.window + g.rows / P.G + 1) len = (int64_t)P.window + g.rows / P.G + 1;      // of one block
-    const int64_t most = len < 256 * 64 ? (len + 255) / 256 : 64;
+    const int64_t held = most_parts((of_all < listed ? of_all : listed) * P.Hkv, c.even.parts);
+    int64_t most = len < 256 * 64 ? (len + 255) / 256 : 64;
+    if (most > held) most = held;
     int64_t parts = 1;
     double least = 0;
     for (int64_t p = 1; p <= most; ++p) {
