@@ -47,6 +47,7 @@ class ccd_paged_t(ctypes.Structure):
     _fields_ += [(n, ctypes.c_int64) for n in
                  ("page_stride", "head_stride", "row_stride", "new_stride_t", "new_stride_h", "q_stride_b", "q_stride_t", "q_stride_h",
                   "o_stride_b", "o_stride_t", "o_stride_h", "lse_stride_b", "lse_stride_t", "lse_stride_h")]
+    _appended = _attended = None   # the geometry, descriptor and tensors, of its last calls (below)
 
 
 class ccd_rope_t(ctypes.Structure):
@@ -55,6 +56,7 @@ class ccd_rope_t(ctypes.Structure):
     _fields_ += [(n, ctypes.c_int64) for n in ("x_stride_t", "x_stride_h", "y_stride_t", "y_stride_h")]
     _fields_ += [("scaling", ctypes.c_int32), ("context", ctypes.c_int32)]
     _fields_ += [(n, ctypes.c_double) for n in ("base", "factor", "low", "high")]
+    _turned = None
 
 
 class CCDError(RuntimeError):
@@ -300,16 +302,18 @@ def ccd_compress_kcat(shape, Q_cat, K, V, K_cap, novelty, keep_idx, workspace, s
 
 # ---- paged caches
 
-# The checks below stand in the way of calls whose kernels take 4 us: attributes of a tensor are read once each, and the device is asked for once.
+# The checks below stand in the way of calls whose kernels take 4 us.  So attributes of a tensor are read once each, and a call of the same geometry as the
+# descriptor's last one (its bytes, the tensors' types, shapes and strides) is not held against the rules again.
 _I32 = torch.int32
 _get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _stream_here(stream, t, u):
-    """The stream to launch on; t and u must be on the current device."""
+def _stream_here(stream, *tensors):
+    """The stream to launch on; all tensors must be on the current device: kernels take their addresses as they are."""
     device = _get_device()
-    if t.get_device() != device or u.get_device() != device:
-        raise ValueError(f"tensors on {t.device} and {u.device}, and the current device is cuda:{device}")
+    for t in tensors:
+        if t.get_device() != device:
+            raise ValueError(f"a tensor on {t.device}, and the current device is cuda:{device}")
     if stream is not None:
         return stream.cuda_stream
     return torch.cuda.current_stream().cuda_stream if _raw_stream is None else _raw_stream(device)
@@ -330,8 +334,18 @@ def _turns(turns, rope):
 
 
 def _alike(a, b):
-    if a.stride() != b.stride() or a.dtype is not b.dtype or a.numel() != b.numel():
+    if a.stride() != b.stride() or a.dtype is not b.dtype or a.shape != b.shape:
         raise AssertionError("keys and values differ in shape, strides or type")
+
+
+def _holds(t, shape, strides, more=0):
+    """t has what a descriptor of this geometry reaches: its own (more rows at most), or one that ends behind it.  `more`: elements
+    that a batch of it lies further on."""
+    own = t.shape
+    if t.stride() == strides and own[0] >= shape[0] and own[1:] == shape[1:] and not more:
+        return
+    if min(shape) > 0 and more + sum((n - 1) * s for n, s in zip(shape, strides)) > sum((n - 1) * s for n, s in zip(own, t.stride())):
+        raise AssertionError(f"a tensor of shape {tuple(own)} and strides {t.stride()}, and the descriptor has {shape}, {strides}")
 
 
 def make_plan(block_table, *, tokens, page, n_pages) -> ccd_paged_t:
@@ -419,47 +433,92 @@ def ccd_paged_plan(paged, len_before, len_after, block_table, block_table_next, 
     _int32(4, cursor, cursor_next)
     _int32(B + 1, q_start)
     _int32(tokens, slots, positions)
-    stream = _stream_here(stream, block_table, slots)
+    stream = _stream_here(stream, len_before, len_after, block_table, block_table_next, free_pages, cursor, cursor_next, q_start, slots, positions)
     return _check(lib().ccd_paged_plan(ctypes.byref(paged), len_before.data_ptr(), len_after.data_ptr(), block_table.data_ptr(), block_table_next.data_ptr(),
                                        free_pages.data_ptr(), cursor.data_ptr(), cursor_next.data_ptr(), q_start.data_ptr(), slots.data_ptr(),
                                        positions.data_ptr(), stream))
 
 
+def _check_rope(rope, X, positions, turns, Y):
+    tokens, heads, d = shape = rope.tokens, rope.heads, rope.d
+    _int32(tokens, positions)
+    _turns(turns, rope)
+    _holds(X, shape, (rope.x_stride_t, rope.x_stride_h, 1))
+    _holds(Y, shape, (rope.y_stride_t, rope.y_stride_h, 1))
+    if X.dtype is not Y.dtype or _dtype_code(X) != rope.dtype:
+        raise AssertionError("X, Y and the descriptor differ in type")
+
+
 def ccd_rope(rope, X, positions, turns, Y, stream=None) -> int:
     """positions int32 [tokens]; turns as rope_turns gives them; Y may be X."""
-    _int32(rope.tokens, positions)
-    _turns(turns, rope)
-    stream = _stream_here(stream, X, positions)
+    geometry = (bytes(rope), X.dtype, X.shape, X.stride(), positions.dtype, positions.shape, positions.is_contiguous(), turns.dtype, turns.shape, turns.is_contiguous(),
+                Y.dtype, Y.shape, Y.stride())
+    if geometry != rope._turned:
+        _check_rope(rope, X, positions, turns, Y)
+        rope._turned = geometry
+    stream = _stream_here(stream, X, positions, turns, Y)
     return _check(lib().ccd_rope(ctypes.byref(rope), X.data_ptr(), positions.data_ptr(), turns.data_ptr(), Y.data_ptr(), stream))
+
+
+def _check_append(paged, rope, K_new, V_new, slots, K_pages, V_pages, positions, turns):
+    tokens, Hkv, d = paged.tokens, paged.Hkv, paged.d
+    _alike(K_new, V_new)
+    _alike(K_pages, V_pages)
+    if K_new.dtype is not K_pages.dtype or _dtype_code(K_pages) != paged.dtype:
+        raise AssertionError("new keys, the cache and the descriptor differ in type")
+    _holds(K_new, (tokens, Hkv, d), (paged.new_stride_t, paged.new_stride_h, 1))
+    _holds(K_pages, (paged.n_pages, Hkv, paged.page, d), (paged.page_stride, paged.head_stride, paged.row_stride, 1))
+    _int32(tokens, slots)
+    if rope is not None:
+        _int32(tokens, positions)
+        _turns(turns, rope)
 
 
 def ccd_paged_append(paged, K_new, V_new, slots, K_pages, V_pages, rope=None, positions=None, turns=None, stream=None) -> int:
     """K_new and V_new have the same strides, as have K_pages and V_pages; with a rope descriptor the keys are embedded at `positions`."""
-    tokens = paged.tokens
-    _alike(K_new, V_new)
-    _alike(K_pages, V_pages)
-    if K_new.dtype is not K_pages.dtype:
-        raise AssertionError("new keys and the cache differ in type")
+    geometry = (bytes(paged), K_new.dtype, K_new.shape, K_new.stride(), V_new.dtype, V_new.shape, V_new.stride(), slots.dtype, slots.shape, slots.is_contiguous(),
+                K_pages.dtype, K_pages.shape, K_pages.stride(), V_pages.dtype, V_pages.shape, V_pages.stride())
+    if rope is not None:
+        geometry += (bytes(rope), positions.dtype, positions.shape, positions.is_contiguous(), turns.dtype, turns.shape, turns.is_contiguous())
+    if geometry != paged._appended:
+        _check_append(paged, rope, K_new, V_new, slots, K_pages, V_pages, positions, turns)
+        paged._appended = geometry
     if rope is None:
-        _int32(tokens, slots)
         return _check(lib().ccd_paged_append(ctypes.byref(paged), None, K_new.data_ptr(), V_new.data_ptr(), slots.data_ptr(), None, None, K_pages.data_ptr(),
-                                             V_pages.data_ptr(), _stream_here(stream, K_pages, slots)))
-    _int32(tokens, slots, positions)
-    _turns(turns, rope)
+                                             V_pages.data_ptr(), _stream_here(stream, K_new, V_new, slots, K_pages, V_pages)))
     return _check(lib().ccd_paged_append(ctypes.byref(paged), ctypes.byref(rope), K_new.data_ptr(), V_new.data_ptr(), slots.data_ptr(), positions.data_ptr(),
-                                         turns.data_ptr(), K_pages.data_ptr(), V_pages.data_ptr(), _stream_here(stream, K_pages, slots)))
+                                         turns.data_ptr(), K_pages.data_ptr(), V_pages.data_ptr(),
+                                         _stream_here(stream, K_new, V_new, slots, K_pages, V_pages, positions, turns)))
 
 
-def ccd_paged_attend(paged, Q, K_pages, V_pages, block_table, q_start, kv_len, out, lse, workspace, stream=None) -> int:
-    """block_table [B, table_width], q_start [B + 1], kv_len [B]: int32; lse fp32 or None."""
-    B, dtype = paged.B, K_pages.dtype
+def _check_attend(paged, Q, K_pages, V_pages, block_table, q_start, kv_len, out, lse):
+    B, dtype, shape = paged.B, K_pages.dtype, (paged.tokens, paged.Hq, paged.d)
     _int32(B * paged.table_width, block_table)
     _int32(B + 1, q_start)
     _int32(B, kv_len)
     _alike(K_pages, V_pages)
-    if Q.dtype is not dtype or out.dtype is not dtype or (lse is not None and lse.dtype is not torch.float32):
-        raise AssertionError("Q, out and the cache differ in type, or lse is not fp32")
-    stream = _stream_here(stream, Q, K_pages)
+    if Q.dtype is not dtype or out.dtype is not dtype or (lse is not None and lse.dtype is not torch.float32) or _dtype_code(K_pages) != paged.dtype:
+        raise AssertionError("Q, out, the cache and the descriptor differ in type, or lse is not fp32")
+    _holds(K_pages, (paged.n_pages, paged.Hkv, paged.page, paged.d), (paged.page_stride, paged.head_stride, paged.row_stride, 1))
+    _holds(Q, shape, (paged.q_stride_t, paged.q_stride_h, 1), (B - 1) * paged.q_stride_b)
+    _holds(out, shape, (paged.o_stride_t, paged.o_stride_h, 1), (B - 1) * paged.o_stride_b)
+    if lse is not None:
+        _holds(lse, shape[:2], (paged.lse_stride_t, paged.lse_stride_h), (B - 1) * paged.lse_stride_b)
+
+
+def ccd_paged_attend(paged, Q, K_pages, V_pages, block_table, q_start, kv_len, out, lse, workspace, stream=None) -> int:
+    """block_table [B, table_width], q_start [B + 1], kv_len [B]: int32; lse fp32 or None."""
+    geometry = (bytes(paged), Q.dtype, Q.shape, Q.stride(), K_pages.dtype, K_pages.shape, K_pages.stride(), V_pages.dtype, V_pages.shape, V_pages.stride(),
+                block_table.dtype, block_table.shape, block_table.is_contiguous(), q_start.dtype, q_start.shape, q_start.is_contiguous(),
+                kv_len.dtype, kv_len.shape, kv_len.is_contiguous(), out.dtype, out.shape, out.stride())
+    there = (Q, K_pages, V_pages, block_table, q_start, kv_len, out)
+    if lse is not None:
+        geometry += (lse.dtype, lse.shape, lse.stride())
+        there += (lse,)
+    if geometry != paged._attended:
+        _check_attend(paged, Q, K_pages, V_pages, block_table, q_start, kv_len, out, lse)
+        paged._attended = geometry
+    stream = _stream_here(stream, *there) if workspace is None else _stream_here(stream, *there, workspace)
     return _check(lib().ccd_paged_attend(ctypes.byref(paged), Q.data_ptr(), K_pages.data_ptr(), V_pages.data_ptr(), block_table.data_ptr(), q_start.data_ptr(),
                                          kv_len.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
                                          *((None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())), stream))
