@@ -21,6 +21,8 @@ from . import infinipot as ip
 class _Kept:
     """What calls of one stream keep for the next ones: nothing says that another stream's are done with it, or have written it."""
 
+    MOST = 16               # of rows: the oldest leaves (chunks of ever other lengths)
+
     def __init__(self):
         self.ws, self.rows, self.kv_len, self.held = None, {}, None, None      # rows: (pages, tokens) -> block table, q_start; held: the number in kv_len
 
@@ -93,6 +95,8 @@ class MemoryPot:
             return *rows(), torch.full((pages,), self.n_valid, dtype=torch.int32, device=device)
         kept = _kept(self._attn)
         if (pages, m) not in kept.rows:
+            if len(kept.rows) == _Kept.MOST:
+                del kept.rows[next(iter(kept.rows))]            # (the stream's own memory: what still runs is before what takes it next)
             kept.rows[pages, m] = rows()
         if kept.kv_len is None:
             kept.kv_len = torch.empty(self.B * self.L, dtype=torch.int32, device=device)

@@ -1,0 +1,125 @@
+"""The drivers of pot.py on the paths that a model takes: keys embedded on their way into a pool, a window, other keys than the stored ones,
+a pool's pot distilled with attention's log-sum-exps, chunks of ever other lengths.
+
+Tolerances: embedded keys as in test_gpu_paged.py, attention as there over the keys that are stored; scores from attention's log-sum-exps as in
+test_gpu_pot_attention.py.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged_oracle as O
+from paper_2410_01518_amd import infinipot as ip
+from paper_2410_01518_amd.pot import MemoryPot, PagedPots
+from tests import gpu_util as gu
+from tests.test_gpu_paged import DT, _check_attend, _f64, _rope_bound
+from tests.test_gpu_pot_attention import _fill
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("layout,rot", [(0, 64), (1, 48)])
+@pytest.mark.parametrize("window", [0, 23])
+def test_a_pool_embeds_keys_and_attends_through_a_window(dtype, layout, rot, window):
+    S, L, Hq, Hkv, d, cap, longest = 4, 2, 4, 2, 64, 140, 160
+    pool = PagedPots(S, 50, 16, longest, cap, L, Hq, Hkv, d, dtype=DT[dtype], window=window)
+    rng, g = np.random.default_rng(2), torch.Generator(device="cuda").manual_seed(2)
+    one = torch.empty((cap, Hkv, d), dtype=DT[dtype], device="cuda")
+    rope_k, rope_q = ip.make_rope(one, layout=layout, rot=rot), ip.make_rope(torch.empty((cap, Hq, d), dtype=DT[dtype], device="cuda"), layout=layout, rot=rot)
+    turns, f = ip.rope_turns(rope_k), O.frequencies(rot, 10000.0)
+    for step in range(5):
+        lengths = [min(longest, n + (1 if rng.random() < 0.4 else int(rng.integers(0, 33)))) for n in pool.lengths]
+        if step == 3:
+            lengths[1] = 0
+        total = pool.step(lengths)
+        positions = pool.positions.cpu().numpy()
+        for layer in range(L):
+            K, V = (torch.randn((cap, Hkv, d), generator=g, device="cuda").to(DT[dtype]) for _ in range(2))
+            Q = torch.randn((cap, Hq, d), generator=g, device="cuda").to(DT[dtype])
+            pool.append(layer, K, V, rope=rope_k, turns=turns)
+            ip.ccd_rope(rope_q, Q, pool.positions, turns, Q)
+            out, lse = torch.full_like(Q, 5.0), torch.full((cap, Hq), 5.0, device="cuda")
+            pool.attend(layer, Q, out, lse)
+            torch.cuda.synchronize()
+            slots = pool.slots.cpu().numpy()[:total]
+            stored_k, stored_v = _f64(pool.K[:, layer]), _f64(pool.V[:, layer])
+            want = O.rope(_f64(K)[:total], positions[:total], f, half=layout == 0)
+            got = stored_k[slots // 16, :, slots % 16]
+            assert (np.abs(got - want) <= _rope_bound(_f64(K)[:total], want, rot, layout == 0, dtype, 1.0)).all()
+            assert (stored_v[slots // 16, :, slots % 16] == _f64(V)[:total]).all()
+            p = dict(Q=Q, K=pool.K[:, layer], V=pool.V[:, layer], table=pool.table.cpu().numpy(), q_start=pool.q_start.cpu().numpy(), lens=np.array(lengths), T=total)
+            _check_attend(p, out, lse, dtype, window=window)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("layer", [None, 1])
+def test_a_pot_attends_with_other_keys(dtype, layer):
+    """The embedded keys of CR-RoPE beside the stored ones."""
+    B, L, Hkv, d, n_cap, Hq, m, n = 2, 2, 2, 64, 300, 6, 17, 170
+    pot = MemoryPot(B, L, Hkv, d, n_cap, 100, 50, dtype=DT[dtype])
+    _fill(pot, n, 1)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    other = torch.randn(pot.K.shape, generator=g, device="cuda").to(DT[dtype])
+    Q = torch.randn((B, L, Hq, m, d), generator=g, device="cuda").to(DT[dtype])
+    q, K, V = (Q, other, pot.V) if layer is None else (Q[:, layer], other[:, layer: layer + 1], pot.V[:, layer: layer + 1])
+    out, lse = pot.attend(q, layer=layer, behind=True, K=other)
+    torch.cuda.synchronize()
+    pages = B * (L if layer is None else 1)
+    rows = pages * m
+    flat = q.reshape(pages, Hq, m, d).transpose(1, 2).reshape(rows, Hq, d)
+    p = dict(Q=flat, K=K.flatten(0, 1), V=V.flatten(0, 1), table=np.arange(pages)[:, None], q_start=np.arange(pages + 1) * m, lens=np.full(pages, n), T=rows)
+    _check_attend(p, out.reshape(pages, Hq, m, d).transpose(1, 2).reshape(rows, Hq, d), lse.reshape(pages, Hq, m).transpose(1, 2).reshape(rows, Hq), dtype, behind=True)
+
+
+def test_a_pools_pot_is_distilled_with_attentions_log_sum_exps():
+    L, Hq, Hkv, d, n, k, P = 2, 8, 2, 128, 512, 200, 32
+    g = torch.Generator(device="cuda").manual_seed(4)
+    K, V = (torch.randn((L, n, Hkv, d), generator=g, device="cuda").bfloat16() for _ in range(2))
+    Q_cat, nov = torch.randn((1, L, Hq, P, d), generator=g, device="cuda").bfloat16(), torch.rand((1, n), generator=g, device="cuda")
+    kept, scores = [], torch.empty((1, L, Hkv, n), device="cuda")
+    for given in (True, False):
+        pool = PagedPots(2, 3, n, n, n, L, Hq, Hkv, d)
+        pool.step([0, n])
+        for layer in range(L):
+            pool.append(layer, K[layer], V[layer])
+        page = int(pool.table[1, 0])
+        pot = pool.K[page: page + 1]
+        shape, keep, lse = ip.make_shape(Q_cat, pot, nov, k=k, T=40, pool_w=7), torch.empty((1, L, Hkv, k), dtype=torch.int32, device="cuda"), None
+        ws = ip.alloc_workspace(shape)
+        if given:
+            lse = torch.empty((L, Hq, P), device="cuda")
+            out, q_start = torch.empty_like(Q_cat[0]), torch.arange(L + 1, dtype=torch.int32, device="cuda") * P
+            table, lens = torch.arange(L, dtype=torch.int32, device="cuda")[:, None].contiguous(), torch.full((L,), n, dtype=torch.int32, device="cuda")
+            paged = ip.make_paged(pot[0], tokens=L * P, block_table=table, Q=Q_cat[0], out=out, lse=lse, behind=True, max_new=P, max_len=n)
+            ip.ccd_paged_attend(paged, Q_cat[0], pot[0], pool.V[page], table, q_start, lens, out, lse, ip.alloc_paged_workspace(paged))
+            lse = lse[None]
+        else:
+            ip.ccd_score(shape, Q_cat, pot, nov, scores, ws)
+        assert pool.distill(1, page, Q_cat, nov, keep, ws, k=k, T=40, lse=lse) == ip.CCD_OK
+        assert pool.lengths == [0, k]
+        torch.cuda.synchronize()
+        kept.append(keep)
+        kh = keep.cpu().numpy().astype(np.int64)[0]
+        for layer in range(L):
+            for h in range(Hkv):
+                assert torch.equal(pool.K[page, layer, h, :k], K[layer, torch.from_numpy(kh[layer, h]).cuda(), h])
+                assert torch.equal(pool.V[page, layer, h, :k], V[layer, torch.from_numpy(kh[layer, h]).cuda(), h])
+    gu.assert_keep_matches(gu.to_host(kept[0]), gu.to_host(kept[1]), scores.cpu().numpy(), k)
+
+
+def test_chunks_of_ever_other_lengths_are_not_all_remembered():
+    """What a stream's calls keep for the next ones is bounded, and one whose index tensors are gone makes them anew."""
+    pot = MemoryPot(2, 2, 2, 64, 200, 100, 50)
+    _fill(pot, 150, 1)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    Q = torch.randn((2, 2, 4, 120, 64), generator=g, device="cuda").bfloat16()
+    outs = [pot.attend(Q[..., :m, :].contiguous(), behind=True)[0] for m in range(1, 101)]
+    (kept,) = pot._attn.values()
+    assert len(kept.rows) <= 16
+    again, _ = pot.attend(Q[..., :3, :].contiguous(), behind=True)
+    torch.cuda.synchronize()
+    assert torch.equal(again, outs[2])
+    slack = 2.0 ** -6 * pot.V.abs().max().item()
+    for m, out in enumerate(outs, 1):
+        assert ((out.float() - outs[-1][..., :m, :].float()).abs() <= slack).all()
