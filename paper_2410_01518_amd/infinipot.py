@@ -427,12 +427,12 @@ def ccd_paged_plan(paged, len_before, len_after, block_table, block_table_next, 
     """len_before, len_after [B], block_table and block_table_next [B, table_width] (may be one), free_pages [n_pages], cursor and
     cursor_next [4] (may be one), q_start [B + 1], slots and positions [tokens]: int32."""
     B, tokens = paged.B, paged.tokens
-    _int32(B, len_before, len_after)
-    _int32(B * paged.table_width, block_table, block_table_next)
-    _int32(paged.n_pages, free_pages)
-    _int32(4, cursor, cursor_next)
-    _int32(B + 1, q_start)
-    _int32(tokens, slots, positions)
+    table = B * paged.table_width
+    # (one pass over ten tensors, without ten calls)
+    for t, entries in ((len_before, B), (len_after, B), (block_table, table), (block_table_next, table), (free_pages, paged.n_pages), (cursor, 4), (cursor_next, 4),
+                       (q_start, B + 1), (slots, tokens), (positions, tokens)):
+        if t.dtype is not _I32 or t.numel() < entries or not t.is_contiguous():
+            _int32(entries, t)
     stream = _stream_here(stream, len_before, len_after, block_table, block_table_next, free_pages, cursor, cursor_next, q_start, slots, positions)
     return _check(lib().ccd_paged_plan(ctypes.byref(paged), len_before.data_ptr(), len_after.data_ptr(), block_table.data_ptr(), block_table_next.data_ptr(),
                                        free_pages.data_ptr(), cursor.data_ptr(), cursor_next.data_ptr(), q_start.data_ptr(), slots.data_ptr(),
