@@ -227,7 +227,8 @@ typedef struct {
   int32_t Hq, Hkv, d;         /* query heads, KV heads (Hq % Hkv == 0; attention: tokens * Hq <= 2^28 and      */
                               /* B * Hkv <= 2^21, else CCD_EUNSUPPORTED), head dimension 64 or 128                  */
   int32_t dtype;              /* CCD_FP32 or CCD_BF16, for Q, out, K, V                                             */
-  int32_t page, n_pages;      /* tokens per page, pages of the cache; page * n_pages < 2^31                         */
+  int32_t page, n_pages;      /* tokens per page, pages of the cache; page * n_pages < 2^31 (bf16 chunks: pages of a   */
+                              /* multiple of 16 tokens take half the time of others)                                */
   int32_t table_width;        /* entries per row of the block table; page * table_width <= 2^30                     */
   int32_t window;             /* sliding attention window in tokens, 0 = none: a query at position p sees the       */
                               /* positions p - window + 1 .. p only                                                 */

@@ -229,8 +229,11 @@ static AttendCuts plan_attend(const Paged& P, int dtype, int max_new, int max_le
       const double t = grid_time(P, g.by_rows, units, len, p, cus);
       if (p == 1 || t < least) { least = t; parts = p; }
     }
-    // (208 tokens of 12 heads over 536: 2.5e-3 off in the norm where the output's own rounding is 1.7e-3, 2.1e-3 so.  It costs 5 percent of the time: 29.2 us for
-    // 512 tokens over 1024, 30.5 so; over long caches, where 1000 us would be 1053, roundings cancel.)
+    // Whether the products are put right by the sums of the weights as rounded (add_rounded).  That takes some of the error off at any length, and costs more the longer
+    // the call: error in the norm against 64 bits (the output's own rounding 1.65e-3) and us, without and with, 32 heads on 8 of 128: 512 new tokens
+    // over 512 1.78e-3, 1.76e-3 and 20.0, 20.7; over 1024 2.12e-3, 1.99e-3 and 30.2, 31.4; over 2048 1.75e-3, 1.70e-3 and 49.8, 51.2; over 4096 1.87e-3, 1.73e-3 and
+    // 69, 72; 2048 over 4096 1.97e-3, 1.76e-3 and 118, 130; over 32768 2.08e-3, 1.86e-3 and 973, 1023.  So it is a matter of time: up to 1024 tokens it
+    // is one microsecond, and there rows see the fewest tokens (one that a single token rules is off by all of that token's rounding).
     g.sums = g.by_rows && len <= 1024;
     g.chunk = (int)(((len + parts - 1) / parts + 127) / 128 * 128);
     g.parts = (int)((len + g.chunk - 1) / g.chunk);

@@ -9,8 +9,8 @@
 // product are counted in that order.  The waves join their sums at the end; stretches are joined by a second kernel.
 //
 // Measured, 32 query heads on 8 KV heads of 128 elements, bf16: one sequence of 131072 tokens 94 us (5.7 TB/s; the card reads 5.9), the join 6; 64
-// sequences of 500 to 8192, cut evenly, 133 us (5.3 TB/s), the join 5; 4 of 200 to 500, whole, 9.4 with the launch.  fp32 chunks are bound by
-// the fp32 matrix instructions, which are busy two thirds of the time: 1024 tokens over 4096, 16 heads of 128, 293 us (195 at the full rate).
+// sequences of 500 to 8192, cut evenly, 136 us (5.2 TB/s), the join 6; 4 of 200 to 500, whole, 9.4 a call among others.  fp32 chunks are bound by
+// the fp32 matrix instructions, which are busy two thirds of the time: 1024 tokens over 4096, 16 heads of 128, 278 to 290 us (195 at the full rate).
 #pragma once
 #include "ccd_attend.h"
 

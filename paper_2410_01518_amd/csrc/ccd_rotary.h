@@ -11,7 +11,7 @@
 namespace ccd {
 
 // cosine and sine of a phase: the nearest quarter turn is taken off (exact, the phase is an integer), the rest lies within
-// an eighth of a turn, |x| <= pi/4, where the Taylor sums up to x^10 and x^9 stop 2e-9 (cosine) and 2e-9 (sine) short
+// an eighth of a turn, |x| <= pi/4, where the Taylor sums up to x^10 (cosine) and x^11 (sine) stop 1.2e-10 and 7e-12 short
 __device__ __forceinline__ void cos_sin_of_phase(uint64_t phase, float& c, float& s) {
   const uint32_t ph = (uint32_t)(phase >> 32);
   const uint32_t q = (ph + 0x20000000u) >> 30;
