@@ -152,7 +152,8 @@ int attend_compute_units();
 
 // About the time (ns) of a grid that cuts `units` blocks of rows and heads into `parts` stretches each.  A workgroup takes `token` ns a token where it has a
 // compute unit alone, and 250 tokens' time for itself; two that share one take `shared` times that (in between, while some have one alone:
-// the rows kernel is bound by power).  Sums of stretches are written and read again by one more kernel.  What was measured in us:
+// the rows kernel is bound by power).  Sums of stretches are written and read again by one more kernel.  The 250 tokens, the factors of a shared compute unit and of a
+// round that is not full are fitted to what was measured, in us:
 //   rows kernel, d 128, 32 heads of 8 groups, 8192 tokens, for 1, 2, 3, 4 stretches:  512 new tokens 160, 102, 101, 91;  1024: 162, 160, 168, 167;
 //   1536: 213, 235, 250, 237;  64 new tokens, for 4, 8, 16, 32: 52, 35, 29, 33
 //   fp32, 16 heads of 4 groups, 4096 tokens, for 1, 2, 3, 4, 6, 8:  d 64, 256 new tokens 111, 64, 71, 58, 77, 64;  d 128, 300: 167, 174, 128, 139, 140, 133
