@@ -39,6 +39,19 @@ def _kept(by_stream):
     return by_stream.setdefault(torch.cuda.current_stream().cuda_stream, _Kept())
 
 
+def _described(held, kind, geometry, make):
+    """The descriptor of the last call of this kind, if this one's geometry is the same (a step's layers, a chunk's), or a new one: making and
+    checking one takes longer on the host than a call."""
+    last = held.get(kind)
+    if last is None or last[0] != geometry:
+        last = held[kind] = (geometry, make())
+    return last[1]
+
+
+def _geometry(*tensors):
+    return [(t.shape, t.stride()) for t in tensors]
+
+
 class MemoryPot:
     def __init__(self, B, L, Hkv, d, n_cap, k, T, *, dtype=torch.bfloat16, pool_w=7, pool_mode=ip.CCD_POOL_MAX,
                  device="cuda"):
@@ -52,6 +65,7 @@ class MemoryPot:
         self.calls = 0
         self._ws = None
         self._attn = {}                         # stream -> _Kept
+        self._held = {}                         # descriptors (_described)
 
     @property
     def room(self) -> int:
@@ -80,7 +94,8 @@ class MemoryPot:
         lse = torch.empty(Q.shape[:-1], dtype=torch.float32, device=Q.device) if lse is None else lse
         table, q_start, kv_len = self._attn_index(pages, m, Q.device)
         o, s = (out, lse) if one else (out.view(-1, *out.shape[2:]), lse.view(-1, *lse.shape[2:]))
-        paged = ip.make_paged(keys, tokens=pages * m, block_table=table, Q=q, out=o, lse=s, window=window, behind=behind, max_new=m, max_len=max(1, self.n_valid))
+        paged = _described(self._held, "attend", (window, behind, self.n_valid, _geometry(keys, q, o, s)), lambda: ip.make_paged(
+            keys, tokens=pages * m, block_table=table, Q=q, out=o, lse=s, window=window, behind=behind, max_new=m, max_len=max(1, self.n_valid)))
         ws = _kept(self._attn).workspace(paged, Q.device)
         rc = ip.ccd_paged_attend(paged, q, keys, values, table, q_start, kv_len, o, s, ws)
         assert rc == ip.CCD_OK, rc
@@ -147,6 +162,11 @@ class PagedPots:
         self.new = [0] * sequences
         self._plan = ip.make_plan(self.table, tokens=step_tokens, page=page, n_pages=n_pages)
         self._attn = {}                                 # stream -> _Kept
+        self._held = {}                                 # descriptors (_described)
+        self._hints()
+
+    def _hints(self):
+        self._most = max(1, *self.new), max(1, *self.lengths)
 
     def pages(self, length) -> int:
         return -(-length // self.page)
@@ -168,25 +188,25 @@ class PagedPots:
                                self.slots, self.positions)
         assert rc == ip.CCD_OK, rc
         self.lengths, self.new = lengths, new
+        self._hints()
         return sum(new)
-
-    def _paged(self, layer, tokens, **kw):
-        return ip.make_paged(self.K[:, layer], tokens=tokens, block_table=self.table, window=self.window, max_new=max(1, *self.new), max_len=max(1, *self.lengths), **kw)
 
     def append(self, layer, K_new, V_new, rope=None, turns=None) -> None:
         """Keys and values of the step's new tokens, [rows, Hkv, d]; rope and turns (as of rope_turns): the keys are embedded at their positions."""
-        rows = K_new.shape[0]
-        rc = ip.ccd_paged_append(self._paged(layer, rows, K_new=K_new), K_new, V_new, self.slots[:rows], self.K[:, layer], self.V[:, layer], rope=rope,
-                                 positions=None if rope is None else self.positions[:rows], turns=turns)
+        rows, K, V = K_new.shape[0], self.K[:, layer], self.V[:, layer]
+        paged = _described(self._held, "append", _geometry(K_new), lambda: ip.make_paged(K, tokens=rows, K_new=K_new))
+        rc = ip.ccd_paged_append(paged, K_new, V_new, self.slots[:rows], K, V, rope=rope, positions=None if rope is None else self.positions[:rows], turns=turns)
         assert rc == ip.CCD_OK, rc
 
     def attend(self, layer, Q, out=None, lse=None):
         """Q [rows, Hq, d] of the step's new tokens, their keys and values appended; returns (out, lse)."""
         out = torch.empty_like(Q, memory_format=torch.contiguous_format) if out is None else out
         lse = torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device) if lse is None else lse
-        paged = self._paged(layer, Q.shape[0], Q=Q, out=out, lse=lse)
+        K, V = self.K[:, layer], self.V[:, layer]
+        paged = _described(self._held, "attend", (self.window, self._most, _geometry(Q, out, lse)), lambda: ip.make_paged(
+            K, tokens=Q.shape[0], block_table=self.table, Q=Q, out=out, lse=lse, window=self.window, max_new=self._most[0], max_len=self._most[1]))
         ws = _kept(self._attn).workspace(paged, Q.device)
-        rc = ip.ccd_paged_attend(paged, Q, self.K[:, layer], self.V[:, layer], self.table, self.q_start, self.after, out, lse, ws)
+        rc = ip.ccd_paged_attend(paged, Q, K, V, self.table, self.q_start, self.after, out, lse, ws)
         assert rc == ip.CCD_OK, rc
         return out, lse
 
@@ -203,4 +223,5 @@ class PagedPots:
             rc = ip.ccd_compress(shape, Q_cat, K, V, novelty, keep_idx, workspace)
         if rc == ip.CCD_OK:
             self.lengths[b] = k
+            self._hints()
         return rc

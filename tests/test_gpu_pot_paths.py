@@ -123,3 +123,42 @@ def test_chunks_of_ever_other_lengths_are_not_all_remembered():
     slack = 2.0 ** -6 * pot.V.abs().max().item()
     for m, out in enumerate(outs, 1):
         assert ((out.float() - outs[-1][..., :m, :].float()).abs() <= slack).all()
+
+
+def test_a_descriptor_that_is_kept_is_that_of_the_call():
+    """Calls of changing layouts, windows, lengths and sides on one pot, each against a pot that has seen no other; other types are refused still."""
+    def pot_of(n):
+        pot = MemoryPot(2, 2, 2, 64, 300, 100, 50)
+        _fill(pot, n, 1)
+        return pot
+    g = torch.Generator(device="cuda").manual_seed(6)
+    wide = torch.randn((2, 2, 12, 20, 64), generator=g, device="cuda").bfloat16()
+    pot = pot_of(120)
+    for more, q, kw in ((0, wide[:, :, :4].contiguous(), {}), (0, wide[:, :, 4:8], {}), (0, wide[:, :, 4:8], dict(window=30)), (0, wide[:, :, 4:8], dict(behind=True)), (50, wide[:, :, 4:8], dict(behind=True)),
+                        (0, wide[:, 1, 8:], dict(layer=1)), (0, wide[:, 0, 8:], dict(layer=0)), (0, wide[:, :, :, :7], {}), (0, wide[:, :, 4:8], dict(behind=True))):
+        if more:
+            _fill(pot, more, 2)
+        fresh = pot_of(120)
+        if pot.n_valid > 120:
+            _fill(fresh, pot.n_valid - 120, 2)
+        out, lse = pot.attend(q, **kw)
+        want, want_lse = fresh.attend(q, **kw)
+        assert torch.equal(out, want) and torch.equal(lse, want_lse)
+    with pytest.raises(AssertionError):
+        pot.attend(wide[:, :, 4:8].float(), behind=True)
+    pool = PagedPots(2, 20, 16, 100, 40, 1, 4, 2, 64)
+    x = torch.randn((40, 8, 64), generator=g, device="cuda").bfloat16()
+    for lengths in ([17, 3], [18, 4], [30, 4]):
+        pool.step(lengths)
+        pool.append(0, x[:, 4:6], x[:, 6:8])
+        pool.append(0, x[:, 4:6].contiguous(), x[:, 6:8].contiguous())
+        total, outs = int(pool.q_start[-1]), []
+        for q in (x[:, :4], x[:, :4].contiguous(), x[:, :4][:total]):
+            out = torch.full(q.shape, 5.0, dtype=torch.bfloat16, device="cuda")
+            pool.attend(0, q, out=out)
+            outs.append(out)
+        assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0][:total], outs[2]) and (outs[0][total:] == 5.0).all()
+        with pytest.raises(AssertionError):
+            pool.append(0, x[:, 4:6].float(), x[:, 6:8].float())
+        with pytest.raises(AssertionError):
+            pool.attend(0, x[:, :4].float())
