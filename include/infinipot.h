@@ -332,6 +332,67 @@ CCD_API int ccd_paged_attend(const ccd_paged_t* paged, const void* Q, const void
                      const int32_t* block_table, const int32_t* q_start, const int32_t* kv_len, void* out, float* lse,
                      void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- The same cache in 8 bits ---------------------------------------------------------------------------------------
+ *
+ * K_codes and V_codes [n_pages, Hkv, page, d] hold a byte per element, K_scales and V_scales (fp32) [n_pages, Hkv, page / scale_rows]
+ * what a code of 1 stands for: x = code * scale.  Decoding reads half the bytes of a bf16 cache, and a memory pot takes half of the memory.
+ *   CCD_INT8   scale_rows = 1, a scale for every token and head: scale = max(|x| / 127, 2^-120) over the head's d elements, code = x / scale rounded to
+ *              nearest, halves to even (of the exact quotient).  A token and head that holds an infinite value or a NaN has a scale of NaN, and reads as NaN.
+ *   CCD_E4M3   (four bits of exponent, three of mantissa, the largest number 448, no infinities) a scale for every scale_rows tokens and head: the
+ *              smallest power of two, 2^-120 at least, with |x| <= 448 * scale; code = x / scale rounded to nearest, halves to even.  A floating code
+ *              keeps its precision under a scale that is too large, down to 2^-6 of it, so tokens can share one.  An infinite value or a
+ *              NaN has the code of NaN and no part in the scale.
+ * Tokens that share a scale are a block: rows scale_rows * j .. scale_rows * (j + 1) - 1 of a page.  A call that writes the first row of a block begins it
+ * anew: what the block held is gone.  Otherwise the block's scale is the larger of its own and what the new rows need, and where it grows, the rows before the
+ * first new one are rounded again to the new scale (of a power of two: only what falls below 2^-6 of it changes).
+ *
+ *   ccd_paged_append_codes   quantises new keys and values (embedded on the way, if asked for) and writes them to their rows
+ *   ccd_paged_read_codes     cached tokens back as numbers: for the scores of a distillation, or to hand a sequence on
+ *   ccd_paged_attend_codes   attention over codes
+ *   ccd_paged_compact_codes  keeps some rows of every page, in place: the last step of a distillation
+ *
+ * In these calls the descriptor's dtype is that of Q, out, K_new, V_new, K_out and V_out, page_stride, head_stride and row_stride are those of
+ * the codes (elements, of a byte each: multiples of 16), and what is said of ccd_paged_* above holds unless stated otherwise. */
+enum { CCD_INT8 = 0, CCD_E4M3 = 1 };
+typedef struct {
+  int32_t code;               /* CCD_INT8 or CCD_E4M3                                                               */
+  int32_t scale_rows;         /* tokens that share a scale: CCD_INT8 1; CCD_E4M3 a power of two that divides page  */
+  int64_t scale_page_stride, scale_head_stride;      /* K_scales and V_scales, in elements; a head's scales are dense */
+  int64_t new_rows, new_stride_b;                    /* 0: K_new, V_new are [tokens, Hkv, d].  Else new token t stands at        */
+                              /* (t / new_rows) * new_stride_b + (t % new_rows) * new_stride_t, as in [B, Hkv, new_rows, d] */
+} ccd_codes_t;
+
+/* ccd_paged_append into codes; slots, positions, rope and turns as there.  With scale_rows > 1 the new tokens of one block have to stand side by side
+ * in the call, in any order, as the plan numbers them.  The rotation is fp32 and not rounded before it is quantised. */
+CCD_API int ccd_paged_append_codes(const ccd_paged_t* paged, const ccd_codes_t* codes, const ccd_rope_t* rope, const void* K_new, const void* V_new,
+                           const int32_t* slots, const int32_t* positions, const uint64_t* turns, void* K_codes, void* V_codes,
+                           float* K_scales, float* V_scales, void* hip_stream);
+
+/* The last m = q_start[b + 1] - q_start[b] of the kv_len[b] tokens of sequence b as numbers of dtype, rounded once (bf16: nearest even): that at position
+ * kv_len[b] - m + i, KV head h goes to b * o_stride_b + (q_start[b] + i) * o_stride_t + h * o_stride_h of K_out and V_out; 0 where there is no such position, or
+ * no page in the table.  Rows of no sequence are left as they are.  K_out may be NULL (K_codes and K_scales are not read), or V_out.
+ * Hq, window, behind and the strides of Q and lse are not read; tokens <= 2^25, tokens * Hkv <= 2^28. */
+CCD_API int ccd_paged_read_codes(const ccd_paged_t* paged, const ccd_codes_t* codes, const void* K_codes, const void* V_codes, const float* K_scales,
+                         const float* V_scales, const int32_t* block_table, const int32_t* q_start, const int32_t* kv_len, void* K_out, void* V_out,
+                         void* hip_stream);
+
+/* Bytes of scratch ccd_paged_attend_codes needs (0 if a descriptor is invalid); the rest as of ccd_paged_workspace_bytes. */
+CCD_API size_t ccd_codes_workspace_bytes(const ccd_paged_t* paged, const ccd_codes_t* codes);
+
+/* ccd_paged_attend over codes: k_t and v_t are the numbers that the codes stand for.  Keys and values that a row does not see do not reach it, whatever their
+ * codes and scales.  Products of codes are exact: codes are bf16 numbers.  With bf16 queries the weights of a tile of tokens, times the scales of
+ * the values, are rounded to bf16 for their product with the codes; fp32 queries and weights enter as sums of three bf16 numbers. */
+CCD_API int ccd_paged_attend_codes(const ccd_paged_t* paged, const ccd_codes_t* codes, const void* Q, const void* K_codes, const void* V_codes,
+                           const float* K_scales, const float* V_scales, const int32_t* block_table, const int32_t* q_start, const int32_t* kv_len,
+                           void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* ccd_compact over pots in 8 bits: row j of every page and head becomes row keep_idx[page][head][j], j < k, of codes and scales, in place; rows from k on are
+ * left as they are.  keep_idx: device int32 [n_pages, Hkv, k] dense, strictly ascending per head as ccd_select produces, k <= page (an entry outside the page: the
+ * row is left as it is).  novelty (nullable): fp32 [n_pages, Hkv, page] dense, compacted the same way.  scale_rows has to be 1 (CCD_EUNSUPPORTED): rows that
+ * share a scale cannot be parted.  Reads Hkv, d, page, n_pages and the codes' strides. */
+CCD_API int ccd_paged_compact_codes(const ccd_paged_t* paged, const ccd_codes_t* codes, void* K_codes, void* V_codes, float* K_scales, float* V_scales,
+                            const int32_t* keep_idx, int32_t k, float* novelty, void* hip_stream);
+
 /* Per-kernel timing of ccd_compress for benchmarks: a host-side aid, off by default, and the only state the library
  * keeps between calls (process-wide: enable it from one thread, for calls on one stream).  While enabled, each
  * kernel of ccd_compress is launched with two HIP events attached that take the kernel's own begin and end time

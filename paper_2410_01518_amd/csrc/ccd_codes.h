@@ -1,0 +1,91 @@
+// Caches in 8 bits: what the host hands to the kernels of ccd_paged_*_codes, and what a code stands for.
+//
+// int8: c * scale, a scale per token and head.  e4m3: c * scale, c a float of four bits of exponent and three of mantissa, the scale a
+// power of two for every 2^shift tokens and head.  Both kinds of code are bf16 numbers exactly (8 bits of significand hold -127 .. 127; e4m3 has 4,
+// down to 2^-9), so products of codes on the matrix cores are as exact as those of a bf16 cache.
+#pragma once
+#include "ccd_common.h"
+#include "ccd_paged.h"
+#include "ccd_rotary.h"
+
+namespace ccd {
+
+enum { kInt8 = 0, kE4m3 = 1 };
+constexpr float kLeastScale = 7.52316384526264e-37f;        // 2^-120
+
+struct Codes {
+  int32_t shift;                                  // log2 of the tokens that share a scale
+  int64_t page, head;                             // strides of the scales
+  int64_t new_rows, new_b;                        // 0, or new tokens per batch of K_new and V_new and the batches' distance
+};
+
+// four codes of a word as floats
+template <int CODE>
+__device__ __forceinline__ void numbers(uint32_t w, float (&x)[4]) {
+  if constexpr (CODE == kInt8) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (float)(int8_t)(w >> (8 * i));
+  } else {
+    typedef float v2f __attribute__((ext_vector_type(2)));
+    const v2f lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+    x[0] = lo[0]; x[1] = lo[1]; x[2] = hi[0]; x[3] = hi[1];
+  }
+}
+// one code as a float
+template <int CODE>
+__device__ __forceinline__ float number(uint8_t c) {
+  if constexpr (CODE == kInt8) return (float)(int8_t)c;
+  return __builtin_amdgcn_cvt_f32_fp8((int)c, 0);
+}
+
+// The scale that rows of a largest finite |x| of `top` need.  int8: top / 127 rounded; e4m3: with top = m 2^e, 1 <= m < 2, and 448 = 1.75 * 2^8 the
+// smallest power of two is 2^(e - 8) up to m = 1.75, else 2^(e - 7): worked out on the bits, exact.
+template <int CODE>
+__device__ __forceinline__ float scale_for(float top) {
+  if constexpr (CODE == kInt8) return fmaxf(top / 127.f, kLeastScale);
+  const uint32_t bits = __float_as_uint(top);
+  const int e = (int)(bits >> 23) - 8 + ((bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);          // biased
+  return __uint_as_float((uint32_t)(e < 7 ? 7 : e) << 23);                                  // (7: 2^-120)
+}
+
+// x / scale as a code; inverse = 1 / scale.  int8: the quotient by the rounded inverse is within 2^-16 of the exact one, so the nearest whole number is
+// found or missed by one, close to a half.  What is left over, x - c scale, is exact in fp32 (an integer below 2^24 of scale's last
+// bit), and says which.  e4m3: the quotient by a power of two is exact, and the conversion rounds to nearest even; no number lies above 448.
+__device__ __forceinline__ int int8_code(float x, float scale, float inverse) {
+  float c = rintf(x * inverse);
+  const float left = fmaf(-c, scale, x), half = 0.5f * scale;
+  const bool odd = ((int)c & 1) != 0;
+  if (fabsf(left) > half || (fabsf(left) == half && odd)) c += left > 0.f ? 1.f : -1.f;
+  return fabsf(x) < INFINITY ? (int)c : 0;                                                  // (its row's scale says that it is no number)
+}
+template <int CODE>
+__device__ __forceinline__ uint32_t four_codes(const float (&x)[4], float scale, float inverse) {
+  if constexpr (CODE == kInt8) {
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w |= (uint32_t)(int8_code(x[i], scale, inverse) & 0xFF) << (8 * i);
+    return w;
+  } else {
+    // (an infinite quotient has no e4m3 number: NaN, as for a NaN)
+    const float y[4] = {x[0] * inverse, x[1] * inverse, x[2] * inverse, x[3] * inverse};
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (!(fabsf(x[i]) < INFINITY)) w = (w & ~(0xFF << (8 * i))) | (0x7F << (8 * i));
+    return (uint32_t)w;
+  }
+}
+
+void launch_append_codes(const Paged& P, const Codes& C, int code, int dtype, const Rotary* rope, const void* K_new, const void* V_new, const int32_t* slots,
+                         const int32_t* positions, const uint64_t* turns, void* K, void* V, float* K_scales, float* V_scales, hipStream_t s);
+void launch_read_codes(const Paged& P, const Codes& C, int code, int dtype, const void* K, const void* V, const float* K_scales, const float* V_scales,
+                       const int32_t* table, const int32_t* q_start, const int32_t* kv_len, void* K_out, void* V_out, hipStream_t s);
+void launch_compact_codes(const Paged& P, const Codes& C, void* K, void* V, float* K_scales, float* V_scales, const int32_t* keep, int32_t k, float* novelty,
+                          hipStream_t s);
+size_t attend_codes_workspace_bytes(const Paged& P, const Codes& C, int dtype, int max_new, int max_len);
+void launch_attend_codes(const Paged& P, const Codes& C, int code, int dtype, int max_new, int max_len, const void* Q, const void* K, const void* V,
+                         const float* K_scales, const float* V_scales, const int32_t* table, const int32_t* q_start, const int32_t* kv_len, void* out, float* lse,
+                         void* workspace, hipStream_t s);
+
+}  // namespace ccd

@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include "../../include/infinipot.h"
+#include "ccd_codes.h"
 #include "ccd_launch.h"
 #include "ccd_paged.h"
 
@@ -13,7 +14,7 @@ static bool on_16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u)
 static int paged_status() { return hipGetLastError() == hipSuccess ? CCD_OK : CCD_ELAUNCH; }
 
 constexpr int32_t kMostTokens = 1 << 25;               // of a launch of a wave each
-enum PagedNeed { kPlan = 1, kCache = 2, kNew = 4, kAttend = 8 };
+enum PagedNeed { kPlan = 1, kCache = 2, kNew = 4, kAttend = 8, kRead = 16, kBytes = 32 };      // kBytes: the cache has one per element
 
 static int check_stride(int64_t stride, int64_t least, int64_t esz) {
   if (stride < least) return CCD_EINVAL;
@@ -24,7 +25,7 @@ static int check_paged(const ccd_paged_t* c, int need) {
   if (c == nullptr) return CCD_EINVAL;
   if (c->tokens < 0 || c->page < 1 || c->n_pages < 1) return CCD_EINVAL;
   if ((int64_t)c->page * c->n_pages > 0x7FFFFFFF) return CCD_EINVAL;
-  if (need & (kPlan | kAttend)) {
+  if (need & (kPlan | kAttend | kRead)) {
     if (c->B < 1 || c->table_width < 1 || (int64_t)c->B * c->table_width > 0x7FFFFFFF) return CCD_EINVAL;
     if ((int64_t)c->page * c->table_width > 1 << 30) return CCD_EINVAL;                // positions, and a tile past them, are counted in int32
   }
@@ -34,28 +35,55 @@ static int check_paged(const ccd_paged_t* c, int need) {
   if (c->dtype != CCD_FP32 && c->dtype != CCD_BF16) return CCD_EUNSUPPORTED;
   if (c->d != 64 && c->d != 128) return CCD_EUNSUPPORTED;
   const int64_t esz = c->dtype == CCD_FP32 ? 4 : 2;
-  struct Stride { int64_t value, least; };
+  const int64_t cache_esz = need & kBytes ? 1 : esz;
+  struct Stride { int64_t value, least, esz; };
   Stride strides[10];
   int n = 0;
-  strides[n++] = {c->page_stride, c->d}; strides[n++] = {c->head_stride, c->d}; strides[n++] = {c->row_stride, c->d};
-  if ((need & kNew) && c->tokens > kMostTokens) return CCD_EUNSUPPORTED;
-  if (need & kNew) { strides[n++] = {c->new_stride_t, c->d}; strides[n++] = {c->new_stride_h, c->d}; }
+  strides[n++] = {c->page_stride, c->d, cache_esz}; strides[n++] = {c->head_stride, c->d, cache_esz}; strides[n++] = {c->row_stride, c->d, cache_esz};
+  if ((need & (kNew | kRead)) && c->tokens > kMostTokens) return CCD_EUNSUPPORTED;
+  if (need & kNew) { strides[n++] = {c->new_stride_t, c->d, esz}; strides[n++] = {c->new_stride_h, c->d, esz}; }
+  if (need & kRead) {
+    if ((int64_t)c->tokens * c->Hkv > 1 << 28) return CCD_EUNSUPPORTED;
+    strides[n++] = {c->o_stride_b, 0, esz}; strides[n++] = {c->o_stride_t, c->d, esz}; strides[n++] = {c->o_stride_h, c->d, esz};
+  }
   if (need & kAttend) {
     if (c->Hq < 1 || c->Hq % c->Hkv != 0) return CCD_EINVAL;
     // (a launch has less than 2^32 threads)
     if ((int64_t)c->tokens * c->Hq > 1 << 28 || (int64_t)c->B * c->Hkv > 1 << 21) return CCD_EUNSUPPORTED;
     if (c->window < 0 || (c->behind != 0 && c->behind != 1) || c->max_new < 0 || c->max_len < 0) return CCD_EINVAL;
     if (!(c->scale >= 0.f) || isinf(c->scale)) return CCD_EINVAL;
-    strides[n++] = {c->q_stride_b, 0}; strides[n++] = {c->q_stride_t, c->d}; strides[n++] = {c->q_stride_h, c->d};
-    strides[n++] = {c->o_stride_b, 0}; strides[n++] = {c->o_stride_t, c->d}; strides[n++] = {c->o_stride_h, c->d};
+    strides[n++] = {c->q_stride_b, 0, esz}; strides[n++] = {c->q_stride_t, c->d, esz}; strides[n++] = {c->q_stride_h, c->d, esz};
+    strides[n++] = {c->o_stride_b, 0, esz}; strides[n++] = {c->o_stride_t, c->d, esz}; strides[n++] = {c->o_stride_h, c->d, esz};
     if (c->lse_stride_b < 0 || c->lse_stride_t < 1 || c->lse_stride_h < 1) return CCD_EINVAL;
   }
   for (int pass = 0; pass < 2; ++pass)                   // ranges before alignment, as in the other calls
     for (int i = 0; i < n; ++i) {
-      const int rc = check_stride(strides[i].value, strides[i].least, esz);
+      const int rc = check_stride(strides[i].value, strides[i].least, strides[i].esz);
       if (rc == (pass == 0 ? CCD_EINVAL : CCD_EALIGN)) return rc;
     }
   return CCD_OK;
+}
+
+static bool on_4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+// codes of a checked descriptor
+static int check_codes(const ccd_codes_t* k, const ccd_paged_t* c, bool new_tokens) {
+  if (k == nullptr) return CCD_EINVAL;
+  if (k->code != CCD_INT8 && k->code != CCD_E4M3) return CCD_EUNSUPPORTED;
+  if (k->scale_rows < 1 || (k->scale_rows & (k->scale_rows - 1)) != 0 || c->page % k->scale_rows != 0) return CCD_EINVAL;
+  if (k->code == CCD_INT8 && k->scale_rows != 1) return CCD_EUNSUPPORTED;
+  if (k->scale_page_stride < c->page / k->scale_rows || k->scale_head_stride < c->page / k->scale_rows) return CCD_EINVAL;
+  if (!new_tokens) return CCD_OK;
+  if (k->new_rows < 0 || k->new_rows > 0x7FFFFFFF || (k->new_rows > 0 && k->new_stride_b < c->d)) return CCD_EINVAL;
+  return k->new_rows > 0 && (k->new_stride_b * (c->dtype == CCD_FP32 ? 4 : 2)) % 16 ? CCD_EALIGN : CCD_OK;
+}
+
+static Codes make_codes(const ccd_codes_t* k) {
+  Codes C{};
+  while ((1 << C.shift) < k->scale_rows) ++C.shift;
+  C.page = k->scale_page_stride; C.head = k->scale_head_stride;
+  C.new_rows = k->new_rows; C.new_b = k->new_stride_b;
+  return C;
 }
 
 static Paged make_paged(const ccd_paged_t* c) {
@@ -201,6 +229,85 @@ int ccd_paged_attend(const ccd_paged_t* paged, const void* Q, const void* K_page
     return CCD_EWORKSPACE;
   launch_attend(P, paged->dtype, max_new, max_len, Q, K_pages, V_pages, block_table, q_start, kv_len, out, lse, workspace,
                 static_cast<hipStream_t>(hip_stream));
+  return paged_status();
+}
+
+int ccd_paged_append_codes(const ccd_paged_t* paged, const ccd_codes_t* codes, const ccd_rope_t* rope, const void* K_new, const void* V_new,
+                           const int32_t* slots, const int32_t* positions, const uint64_t* turns, void* K_codes, void* V_codes, float* K_scales,
+                           float* V_scales, void* hip_stream) {
+  int rc = check_paged(paged, kCache | kNew | kBytes);
+  if (rc != CCD_OK || (rc = check_codes(codes, paged, true)) != CCD_OK) return rc;
+  if (rope != nullptr && (rc = check_rotation(rope, paged->d)) != CCD_OK) return rc;
+  if (paged->tokens == 0) return CCD_OK;
+  if (K_new == nullptr || V_new == nullptr || slots == nullptr || K_codes == nullptr || V_codes == nullptr || K_scales == nullptr || V_scales == nullptr) return CCD_EINVAL;
+  if (rope != nullptr && (positions == nullptr || turns == nullptr)) return CCD_EINVAL;
+  if (K_codes == V_codes || K_scales == V_scales || K_new == K_codes || V_new == V_codes) return CCD_EINVAL;
+  if (!on_16(K_new) || !on_16(V_new) || !on_16(K_codes) || !on_16(V_codes) || !on_4(K_scales) || !on_4(V_scales)) return CCD_EALIGN;
+  Rotary R{};
+  if (rope != nullptr) {
+    R = make_rotary(rope);
+    R.d = paged->d;
+  }
+  launch_append_codes(make_paged(paged), make_codes(codes), codes->code, paged->dtype, rope != nullptr ? &R : nullptr, K_new, V_new, slots, positions, turns, K_codes,
+                      V_codes, K_scales, V_scales, static_cast<hipStream_t>(hip_stream));
+  return paged_status();
+}
+
+int ccd_paged_read_codes(const ccd_paged_t* paged, const ccd_codes_t* codes, const void* K_codes, const void* V_codes, const float* K_scales, const float* V_scales,
+                         const int32_t* block_table, const int32_t* q_start, const int32_t* kv_len, void* K_out, void* V_out, void* hip_stream) {
+  int rc = check_paged(paged, kCache | kRead | kBytes);
+  if (rc != CCD_OK || (rc = check_codes(codes, paged, false)) != CCD_OK) return rc;
+  if (paged->tokens == 0) return CCD_OK;
+  if (block_table == nullptr || q_start == nullptr || kv_len == nullptr || (K_out == nullptr && V_out == nullptr)) return CCD_EINVAL;
+  if ((K_out != nullptr && (K_codes == nullptr || K_scales == nullptr)) || (V_out != nullptr && (V_codes == nullptr || V_scales == nullptr))) return CCD_EINVAL;
+  if (K_out == V_out || (K_out != nullptr && K_out == K_codes) || (V_out != nullptr && V_out == V_codes)) return CCD_EINVAL;
+  if (!on_16(K_out) || !on_16(V_out) || (K_out != nullptr && (!on_16(K_codes) || !on_4(K_scales))) || (V_out != nullptr && (!on_16(V_codes) || !on_4(V_scales))))
+    return CCD_EALIGN;
+  launch_read_codes(make_paged(paged), make_codes(codes), codes->code, paged->dtype, K_codes, V_codes, K_scales, V_scales, block_table, q_start, kv_len, K_out, V_out,
+                    static_cast<hipStream_t>(hip_stream));
+  return paged_status();
+}
+
+size_t ccd_codes_workspace_bytes(const ccd_paged_t* paged, const ccd_codes_t* codes) {
+  if (check_paged(paged, kCache | kAttend | kBytes) != CCD_OK || check_codes(codes, paged, false) != CCD_OK) return 0;
+  const Paged P = make_paged(paged);
+  return attend_codes_workspace_bytes(P, make_codes(codes), paged->dtype, hint_new(paged), hint_len(paged, P));
+}
+
+int ccd_paged_attend_codes(const ccd_paged_t* paged, const ccd_codes_t* codes, const void* Q, const void* K_codes, const void* V_codes, const float* K_scales,
+                           const float* V_scales, const int32_t* block_table, const int32_t* q_start, const int32_t* kv_len, void* out, float* lse,
+                           void* workspace, size_t workspace_bytes, void* hip_stream) {
+  int rc = check_paged(paged, kCache | kAttend | kBytes);
+  if (rc != CCD_OK || (rc = check_codes(codes, paged, false)) != CCD_OK) return rc;
+  if (paged->tokens == 0) return CCD_OK;
+  if (Q == nullptr || K_codes == nullptr || V_codes == nullptr || K_scales == nullptr || V_scales == nullptr || block_table == nullptr || q_start == nullptr ||
+      kv_len == nullptr || out == nullptr)
+    return CCD_EINVAL;
+  if (out == Q || out == K_codes || out == V_codes) return CCD_EINVAL;
+  if (!on_16(Q) || !on_16(K_codes) || !on_16(V_codes) || !on_16(out) || !on_4(K_scales) || !on_4(V_scales)) return CCD_EALIGN;
+  const Paged P = make_paged(paged);
+  const Codes C = make_codes(codes);
+  const int max_new = hint_new(paged), max_len = hint_len(paged, P);
+  if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 ||
+      workspace_bytes < attend_codes_workspace_bytes(P, C, paged->dtype, max_new, max_len))
+    return CCD_EWORKSPACE;
+  launch_attend_codes(P, C, codes->code, paged->dtype, max_new, max_len, Q, K_codes, V_codes, K_scales, V_scales, block_table, q_start, kv_len, out, lse, workspace,
+                      static_cast<hipStream_t>(hip_stream));
+  return paged_status();
+}
+
+int ccd_paged_compact_codes(const ccd_paged_t* paged, const ccd_codes_t* codes, void* K_codes, void* V_codes, float* K_scales, float* V_scales, const int32_t* keep_idx,
+                            int32_t k, float* novelty, void* hip_stream) {
+  int rc = check_paged(paged, kCache | kBytes);
+  if (rc != CCD_OK || (rc = check_codes(codes, paged, false)) != CCD_OK) return rc;
+  if (codes->scale_rows != 1) return CCD_EUNSUPPORTED;
+  if (k < 0 || k > paged->page) return CCD_EINVAL;
+  if ((int64_t)paged->n_pages * paged->Hkv > 1 << 21) return CCD_EUNSUPPORTED;
+  if (k == 0) return CCD_OK;
+  if (K_codes == nullptr || V_codes == nullptr || K_scales == nullptr || V_scales == nullptr || keep_idx == nullptr) return CCD_EINVAL;
+  if (K_codes == V_codes || K_scales == V_scales) return CCD_EINVAL;
+  if (!on_16(K_codes) || !on_16(V_codes) || !on_4(K_scales) || !on_4(V_scales)) return CCD_EALIGN;
+  launch_compact_codes(make_paged(paged), make_codes(codes), K_codes, V_codes, K_scales, V_scales, keep_idx, k, novelty, static_cast<hipStream_t>(hip_stream));
   return paged_status();
 }
 

@@ -23,12 +23,14 @@ CCD_POOL_NONE, CCD_POOL_MAX, CCD_POOL_AVG = 0, 1, 2
 CCD_PATH_AUTO, CCD_PATH_VALU, CCD_PATH_MFMA_SLICES, CCD_PATH_MFMA_UNIT = 0, 1, 2, 3
 CCD_ROPE_HALF, CCD_ROPE_PAIRS = 0, 1
 CCD_ROPE_PLAIN, CCD_ROPE_LINEAR, CCD_ROPE_NTK, CCD_ROPE_PARTS = 0, 1, 2, 3
+CCD_INT8, CCD_E4M3 = 0, 1
 
 EXPORTS = ("ccd_workspace_bytes", "ccd_score", "ccd_select", "ccd_compact", "ccd_compress", "ccd_append", "ccd_cr_rope",
            "ccd_compress_rope", "ccd_score_kcat", "ccd_compress_kcat", "ccd_score_lse", "ccd_compress_lse",
            "ccd_nuc_from_logits", "ccd_compress_noalloc", "ccd_profile_enable", "ccd_profile_stages", "ccd_profile_stage_name",
            "ccd_profile_collect", "ccd_strerror", "ccd_paged_plan", "ccd_rope_turns", "ccd_rope", "ccd_paged_append",
-           "ccd_paged_workspace_bytes", "ccd_paged_attend")
+           "ccd_paged_workspace_bytes", "ccd_paged_attend", "ccd_paged_append_codes", "ccd_paged_read_codes", "ccd_codes_workspace_bytes",
+           "ccd_paged_attend_codes", "ccd_paged_compact_codes")
 
 
 class ccd_shape_t(ctypes.Structure):
@@ -47,7 +49,7 @@ class ccd_paged_t(ctypes.Structure):
     _fields_ += [(n, ctypes.c_int64) for n in
                  ("page_stride", "head_stride", "row_stride", "new_stride_t", "new_stride_h", "q_stride_b", "q_stride_t", "q_stride_h",
                   "o_stride_b", "o_stride_t", "o_stride_h", "lse_stride_b", "lse_stride_t", "lse_stride_h")]
-    _appended = _attended = None   # the geometry, descriptor and tensors, of its last calls (below)
+    _appended = _attended = _read = None   # the geometry, descriptor and tensors, of its last calls (below)
 
 
 class ccd_rope_t(ctypes.Structure):
@@ -57,6 +59,11 @@ class ccd_rope_t(ctypes.Structure):
     _fields_ += [("scaling", ctypes.c_int32), ("context", ctypes.c_int32)]
     _fields_ += [(n, ctypes.c_double) for n in ("base", "factor", "low", "high")]
     _turned = None
+
+
+class ccd_codes_t(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("code", "scale_rows")]
+    _fields_ += [(n, ctypes.c_int64) for n in ("scale_page_stride", "scale_head_stride", "new_rows", "new_stride_b")]
 
 
 class CCDError(RuntimeError):
@@ -119,6 +126,17 @@ def lib() -> ctypes.CDLL:
         L.ccd_paged_workspace_bytes.argtypes = [cp]
         L.ccd_paged_attend.restype = ctypes.c_int
         L.ccd_paged_attend.argtypes = [cp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        kp = ctypes.POINTER(ccd_codes_t)
+        L.ccd_paged_append_codes.restype = ctypes.c_int
+        L.ccd_paged_append_codes.argtypes = [cp, kp, rp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.ccd_paged_read_codes.restype = ctypes.c_int
+        L.ccd_paged_read_codes.argtypes = [cp, kp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.ccd_codes_workspace_bytes.restype = ctypes.c_size_t
+        L.ccd_codes_workspace_bytes.argtypes = [cp, kp]
+        L.ccd_paged_attend_codes.restype = ctypes.c_int
+        L.ccd_paged_attend_codes.argtypes = [cp, kp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, ctypes.c_size_t, vp]
+        L.ccd_paged_compact_codes.restype = ctypes.c_int
+        L.ccd_paged_compact_codes.argtypes = [cp, kp, vp, vp, vp, vp, vp, ctypes.c_int32, vp, vp]
         L.ccd_profile_enable.restype = ctypes.c_int
         L.ccd_profile_enable.argtypes = [ctypes.c_int]
         L.ccd_profile_stages.restype = ctypes.c_int
@@ -161,12 +179,16 @@ def _stream(stream):
     return _raw_stream(torch.cuda.current_device())
 
 
-def _dtype_code(t: torch.Tensor) -> int:
-    if t.dtype == torch.float32:
+def _dtype_code_of(dtype) -> int:
+    if dtype == torch.float32:
         return CCD_FP32
-    if t.dtype in (torch.bfloat16, torch.int16, torch.uint16):
+    if dtype in (torch.bfloat16, torch.int16, torch.uint16):
         return CCD_BF16
-    raise TypeError(f"unsupported cache dtype {t.dtype}")
+    raise TypeError(f"unsupported cache dtype {dtype}")
+
+
+def _dtype_code(t: torch.Tensor) -> int:
+    return _dtype_code_of(t.dtype)
 
 
 def make_shape(Q_cat, K, novelty, *, k, T=0, pool_w=1, pool_mode=CCD_POOL_MAX, scale=0.0, n_valid=None,
@@ -356,20 +378,25 @@ def make_plan(block_table, *, tokens, page, n_pages) -> ccd_paged_t:
 
 
 def make_paged(K_pages, *, tokens, block_table=None, Q=None, out=None, lse=None, K_new=None, window=0, behind=False, max_new=0,
-               max_len=0, scale=0.0) -> ccd_paged_t:
+               max_len=0, scale=0.0, dtype=None) -> ccd_paged_t:
     """Descriptor from tensor geometry: K_pages (and V_pages) [n_pages, Hkv, page, d] in any order of the outer three
     dimensions, block_table [B, table_width].  Q and out are [tokens, Hq, d] with lse [tokens, Hq], or, `tokens` = B m,
-    [B, Hq, m, d] with lse [B, Hq, m]; K_new (and V_new) [tokens, Hkv, d]."""
+    [B, Hq, m, d] with lse [B, Hq, m]; K_new (and V_new) [tokens, Hkv, d].  Where K_pages are codes, dtype is that of the others, an `out`
+    without Q has Hkv heads (for reading back), and K_new may be [B, Hkv, m, d] (which make_codes then has to be told, too)."""
     n_pages, Hkv, page, d = K_pages.shape
+    dtype = K_pages.dtype if dtype is None else dtype
     ps, hs, rs, es = K_pages.stride()
     assert es == 1, "rows of the cache must be contiguous"
-    p = ccd_paged_t(B=1, tokens=tokens, Hq=Hkv, Hkv=Hkv, d=d, dtype=_dtype_code(K_pages), page=page, n_pages=n_pages, table_width=1,
+    p = ccd_paged_t(B=1, tokens=tokens, Hq=Hkv, Hkv=Hkv, d=d, dtype=_dtype_code_of(dtype), page=page, n_pages=n_pages, table_width=1,
                     window=window, behind=int(behind), max_new=max_new, max_len=max_len, scale=scale, page_stride=ps, head_stride=hs,
                     row_stride=rs, new_stride_t=Hkv * d, new_stride_h=d)
     if block_table is not None:
         p.B, p.table_width = block_table.shape
-    if K_new is not None:
-        assert tuple(K_new.shape) == (tokens, Hkv, d) and K_new.stride(2) == 1 and K_new.dtype == K_pages.dtype
+    if K_new is not None and K_new.dim() == 4 and K_pages.dtype in CODE_TYPES:
+        assert K_new.shape[0] * K_new.shape[2] == tokens and K_new.shape[1::2] == (Hkv, d) and K_new.stride(3) == 1 and K_new.dtype == dtype
+        p.new_stride_t, p.new_stride_h = K_new.stride(2), K_new.stride(1)
+    elif K_new is not None:
+        assert tuple(K_new.shape) == (tokens, Hkv, d) and K_new.stride(2) == 1 and K_new.dtype == dtype
         p.new_stride_t, p.new_stride_h = K_new.stride(0), K_new.stride(1)
     p.Hq = Hkv if Q is None else Q.shape[1]
     for t, name, batched in ((Q, "q", 4), (out, "o", 4), (lse, "lse", 3)):
@@ -379,7 +406,7 @@ def make_paged(K_pages, *, tokens, block_table=None, Q=None, out=None, lse=None,
             if name == "lse":
                 assert t.dtype == torch.float32
             else:
-                assert t.shape[-1] == d and t.stride(-1) == 1 and t.dtype == K_pages.dtype
+                assert t.shape[-1] == d and t.stride(-1) == 1 and t.dtype == dtype
             assert t.shape[1] == p.Hq
             if t.dim() == batched:
                 m = t.shape[2]
@@ -522,6 +549,160 @@ def ccd_paged_attend(paged, Q, K_pages, V_pages, block_table, q_start, kv_len, o
     return _check(lib().ccd_paged_attend(ctypes.byref(paged), Q.data_ptr(), K_pages.data_ptr(), V_pages.data_ptr(), block_table.data_ptr(), q_start.data_ptr(),
                                          kv_len.data_ptr(), out.data_ptr(), None if lse is None else lse.data_ptr(),
                                          *((None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())), stream))
+
+
+# ---- paged caches in 8 bits
+
+CODE_TYPES = {torch.int8: CCD_INT8, torch.float8_e4m3fn: CCD_E4M3}
+
+
+def make_codes(K_codes, K_scales, K_new=None) -> ccd_codes_t:
+    """Descriptor from tensor geometry: K_codes (and V_codes) [n_pages, Hkv, page, d], int8 or float8_e4m3fn, K_scales (and V_scales)
+    [n_pages, Hkv, page / scale_rows] fp32.  K_new [B, Hkv, m, d] (and V_new): new tokens in that order, where they are not [tokens, Hkv, d]."""
+    n_pages, Hkv, page, d = K_codes.shape
+    if K_codes.dtype not in CODE_TYPES:
+        raise TypeError(f"unsupported code type {K_codes.dtype}")
+    assert K_scales.dtype == torch.float32 and K_scales.shape[:2] == (n_pages, Hkv) and (K_scales.shape[2] == 1 or K_scales.stride(2) == 1)
+    rows = page // max(1, K_scales.shape[2])
+    assert rows * K_scales.shape[2] == page, "a scale for every scale_rows tokens"
+    new_rows = new_b = 0
+    if K_new is not None and K_new.dim() == 4:
+        new_rows, new_b = K_new.shape[2], K_new.stride(0)
+    return ccd_codes_t(CODE_TYPES[K_codes.dtype], rows, K_scales.stride(0), K_scales.stride(1), new_rows, new_b)
+
+
+def ccd_codes_workspace_bytes(paged: ccd_paged_t, codes: ccd_codes_t) -> int:
+    return int(lib().ccd_codes_workspace_bytes(ctypes.byref(paged), ctypes.byref(codes)))
+
+
+def alloc_codes_workspace(paged: ccd_paged_t, codes: ccd_codes_t, device="cuda") -> torch.Tensor:
+    nbytes = ccd_codes_workspace_bytes(paged, codes)
+    if nbytes == 0:
+        raise CCDError(CCD_EINVAL, "invalid descriptor")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _check_cache(paged, codes, K_codes, V_codes, K_scales, V_scales):
+    """What the descriptors say of codes and scales; K or V may be None."""
+    for a, b in ((K_codes, V_codes), (K_scales, V_scales)):
+        if a is not None and b is not None:
+            _alike(a, b)
+    rows = codes.scale_rows
+    for c, s in ((K_codes, K_scales), (V_codes, V_scales)):
+        if c is None and s is None:
+            continue
+        if CODE_TYPES.get(c.dtype) != codes.code or s.dtype is not torch.float32:
+            raise AssertionError("codes, scales and the descriptor differ in type")
+        _holds(c, (paged.n_pages, paged.Hkv, paged.page, paged.d), (paged.page_stride, paged.head_stride, paged.row_stride, 1))
+        _holds(s, (paged.n_pages, paged.Hkv, paged.page // rows if rows > 0 else 0), (codes.scale_page_stride, codes.scale_head_stride, 1))
+
+
+def _geometry_of(paged, codes, *tensors):
+    return (bytes(paged), bytes(codes)) + tuple(None if t is None else (t.dtype, t.shape, t.stride()) for t in tensors)
+
+
+def _check_append_codes(paged, codes, rope, K_new, V_new, slots, K_codes, V_codes, K_scales, V_scales, positions, turns):
+    tokens, Hkv, d = paged.tokens, paged.Hkv, paged.d
+    _alike(K_new, V_new)
+    if _dtype_code(K_new) != paged.dtype:
+        raise AssertionError("new keys and the descriptor differ in type")
+    if codes.new_rows > 0 and K_new.dim() == 4:
+        full = -(-tokens // codes.new_rows)
+        _holds(K_new, (full, Hkv, codes.new_rows, d), (codes.new_stride_b, paged.new_stride_h, paged.new_stride_t, 1))
+    else:
+        if codes.new_rows > 0:
+            raise AssertionError("new keys [B, Hkv, m, d] needed")
+        _holds(K_new, (tokens, Hkv, d), (paged.new_stride_t, paged.new_stride_h, 1))
+    _check_cache(paged, codes, K_codes, V_codes, K_scales, V_scales)
+    _int32(tokens, slots)
+    if rope is not None:
+        _int32(tokens, positions)
+        _turns(turns, rope)
+
+
+def ccd_paged_append_codes(paged, codes, K_new, V_new, slots, K_codes, V_codes, K_scales, V_scales, rope=None, positions=None, turns=None, stream=None) -> int:
+    """K_new and V_new have the same strides, as have codes and scales of keys and values; with a rope descriptor the keys are embedded at `positions`."""
+    there = (K_new, V_new, slots, K_codes, V_codes, K_scales, V_scales)
+    if rope is not None:
+        there += (positions, turns)
+    geometry = _geometry_of(paged, codes, *there) + (None if rope is None else bytes(rope),)
+    if geometry != paged._appended:
+        _check_append_codes(paged, codes, rope, K_new, V_new, slots, K_codes, V_codes, K_scales, V_scales, positions, turns)
+        paged._appended = geometry
+    stream = _stream_here(stream, *there)
+    return _check(lib().ccd_paged_append_codes(ctypes.byref(paged), ctypes.byref(codes), None if rope is None else ctypes.byref(rope), K_new.data_ptr(),
+                                               V_new.data_ptr(), slots.data_ptr(), None if rope is None else positions.data_ptr(), None if rope is None else turns.data_ptr(),
+                                               K_codes.data_ptr(), V_codes.data_ptr(), K_scales.data_ptr(), V_scales.data_ptr(), stream))
+
+
+def _check_read_codes(paged, codes, K_codes, V_codes, K_scales, V_scales, block_table, q_start, kv_len, K_out, V_out):
+    B = paged.B
+    _int32(B * paged.table_width, block_table)
+    _int32(B + 1, q_start)
+    _int32(B, kv_len)
+    if K_out is not None and V_out is not None:
+        _alike(K_out, V_out)
+    _check_cache(paged, codes, K_codes if K_out is not None else None, V_codes if V_out is not None else None, K_scales if K_out is not None else None,
+                 V_scales if V_out is not None else None)
+    for out in (K_out, V_out):
+        if out is not None:
+            if _dtype_code(out) != paged.dtype:
+                raise AssertionError("the numbers read and the descriptor differ in type")
+            _holds(out, (paged.tokens, paged.Hkv, paged.d), (paged.o_stride_t, paged.o_stride_h, 1), (B - 1) * paged.o_stride_b)
+
+
+def ccd_paged_read_codes(paged, codes, K_codes, V_codes, K_scales, V_scales, block_table, q_start, kv_len, K_out, V_out, stream=None) -> int:
+    """block_table [B, table_width], q_start [B + 1], kv_len [B]: int32; K_out or V_out may be None (its codes and scales then, too)."""
+    there = (K_codes, V_codes, K_scales, V_scales, block_table, q_start, kv_len, K_out, V_out)
+    geometry = _geometry_of(paged, codes, *there)
+    if geometry != paged._read:
+        _check_read_codes(paged, codes, *there)
+        paged._read = geometry
+    stream = _stream_here(stream, *(t for t in there if t is not None))
+    return _check(lib().ccd_paged_read_codes(ctypes.byref(paged), ctypes.byref(codes), _ptr(K_codes), _ptr(V_codes), _ptr(K_scales), _ptr(V_scales), block_table.data_ptr(),
+                                             q_start.data_ptr(), kv_len.data_ptr(), _ptr(K_out), _ptr(V_out), stream))
+
+
+def _check_attend_codes(paged, codes, Q, K_codes, V_codes, K_scales, V_scales, block_table, q_start, kv_len, out, lse):
+    B, shape = paged.B, (paged.tokens, paged.Hq, paged.d)
+    _int32(B * paged.table_width, block_table)
+    _int32(B + 1, q_start)
+    _int32(B, kv_len)
+    if Q.dtype is not out.dtype or _dtype_code(Q) != paged.dtype or (lse is not None and lse.dtype is not torch.float32):
+        raise AssertionError("Q, out and the descriptor differ in type, or lse is not fp32")
+    _check_cache(paged, codes, K_codes, V_codes, K_scales, V_scales)
+    _holds(Q, shape, (paged.q_stride_t, paged.q_stride_h, 1), (B - 1) * paged.q_stride_b)
+    _holds(out, shape, (paged.o_stride_t, paged.o_stride_h, 1), (B - 1) * paged.o_stride_b)
+    if lse is not None:
+        _holds(lse, shape[:2], (paged.lse_stride_t, paged.lse_stride_h), (B - 1) * paged.lse_stride_b)
+
+
+def ccd_paged_attend_codes(paged, codes, Q, K_codes, V_codes, K_scales, V_scales, block_table, q_start, kv_len, out, lse, workspace, stream=None) -> int:
+    """block_table [B, table_width], q_start [B + 1], kv_len [B]: int32; lse fp32 or None."""
+    there = (Q, K_codes, V_codes, K_scales, V_scales, block_table, q_start, kv_len, out) + (() if lse is None else (lse,))
+    geometry = _geometry_of(paged, codes, *there)
+    if geometry != paged._attended:
+        _check_attend_codes(paged, codes, Q, K_codes, V_codes, K_scales, V_scales, block_table, q_start, kv_len, out, lse)
+        paged._attended = geometry
+    stream = _stream_here(stream, *there) if workspace is None else _stream_here(stream, *there, workspace)
+    return _check(lib().ccd_paged_attend_codes(ctypes.byref(paged), ctypes.byref(codes), Q.data_ptr(), K_codes.data_ptr(), V_codes.data_ptr(), K_scales.data_ptr(),
+                                               V_scales.data_ptr(), block_table.data_ptr(), q_start.data_ptr(), kv_len.data_ptr(), out.data_ptr(),
+                                               None if lse is None else lse.data_ptr(), *((None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel())),
+                                               stream))
+
+
+def ccd_paged_compact_codes(paged, codes, K_codes, V_codes, K_scales, V_scales, keep_idx, novelty=None, stream=None) -> int:
+    """keep_idx int32 [n_pages, Hkv, k], novelty fp32 [n_pages, Hkv, page] or None, both contiguous; in place."""
+    k = keep_idx.shape[-1]
+    _check_cache(paged, codes, K_codes, V_codes, K_scales, V_scales)
+    _int32(paged.n_pages * paged.Hkv * k, keep_idx)
+    there = (K_codes, V_codes, K_scales, V_scales, keep_idx)
+    if novelty is not None:
+        if novelty.dtype is not torch.float32 or not novelty.is_contiguous() or novelty.numel() < paged.n_pages * paged.Hkv * paged.page:
+            raise AssertionError("novelty [n_pages, Hkv, page] fp32, contiguous, needed")
+        there += (novelty,)
+    return _check(lib().ccd_paged_compact_codes(ctypes.byref(paged), ctypes.byref(codes), K_codes.data_ptr(), V_codes.data_ptr(), K_scales.data_ptr(), V_scales.data_ptr(),
+                                                keep_idx.data_ptr(), k, _ptr(novelty), _stream_here(stream, *there)))
 
 
 def ccd_profile_enable(on: bool) -> int:

@@ -1,0 +1,294 @@
+"""The cache in 8 bits on the host: descriptors, refusals (all decided before any launch), what the binding refuses, and the reference's own pins."""
+import ctypes
+import math
+import os
+import subprocess
+import tempfile
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import codes_oracle as C
+from paper_2410_01518_amd import infinipot as ip
+from tests.test_paged_binding import Elsewhere, launches  # noqa: F401  (a fixture)
+from tests.test_paged_host import _paged, _rope
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+P = 0x1000  # a fake, aligned, non-null device address: never dereferenced because every case below fails on the host
+P2 = 0x100000
+
+
+def test_struct_layout_matches_the_header():
+    fields = ("code", "scale_rows", "scale_page_stride", "scale_head_stride", "new_rows", "new_stride_b")
+    prog = '#include <stdio.h>\n#include <stddef.h>\n#include "infinipot.h"\nint main(void){printf("%zu' + " %zu" * len(fields) + ' %d %d\\n", sizeof(ccd_codes_t), ' + \
+        ", ".join(f"offsetof(ccd_codes_t, {f})" for f in fields) + ", CCD_INT8, CCD_E4M3); return 0; }"
+    with tempfile.TemporaryDirectory() as td:
+        open(os.path.join(td, "t.c"), "w").write(prog)
+        subprocess.run(["gcc", "-std=c99", "-I", os.path.join(ROOT, "include"), os.path.join(td, "t.c"), "-o", os.path.join(td, "t")], check=True)
+        out = [int(v) for v in subprocess.run([os.path.join(td, "t")], capture_output=True, text=True, check=True).stdout.split()]
+    S = ip.ccd_codes_t
+    assert out == [ctypes.sizeof(S)] + [getattr(S, f).offset for f in fields] + [ip.CCD_INT8, ip.CCD_E4M3]
+
+
+def _codes(**kw):
+    base = dict(code=ip.CCD_E4M3, scale_rows=4, scale_page_stride=8, scale_head_stride=4)
+    base.update(kw)
+    return ip.ccd_codes_t(**base)
+
+
+def _append(c, k, rope=None, K_new=P, V_new=P, slots=P, positions=P, turns=P, K=P2, V=2 * P2, Ks=3 * P2, Vs=4 * P2):
+    return ip.lib().ccd_paged_append_codes(ctypes.byref(c), None if k is None else ctypes.byref(k), None if rope is None else ctypes.byref(rope), K_new, V_new, slots, positions,
+                                           turns, K, V, Ks, Vs, None)
+
+
+def _read(c, k, K=P, V=P2, Ks=P, Vs=P, table=P, q_start=P, kv_len=P, K_out=2 * P2, V_out=3 * P2):
+    return ip.lib().ccd_paged_read_codes(ctypes.byref(c), None if k is None else ctypes.byref(k), K, V, Ks, Vs, table, q_start, kv_len, K_out, V_out, None)
+
+
+def _attend(c, k, Q=P, K=P2, V=2 * P2, Ks=P, Vs=P, table=P, q_start=P, kv_len=P, out=3 * P2, lse=P, ws=0x10000, ws_bytes=1 << 40):
+    return ip.lib().ccd_paged_attend_codes(ctypes.byref(c), None if k is None else ctypes.byref(k), Q, K, V, Ks, Vs, table, q_start, kv_len, out, lse, ws, ws_bytes, None)
+
+
+def _compact(c, k, K=P, V=P2, Ks=P, Vs=P2, keep=P, kept=3, nov=None):
+    return ip.lib().ccd_paged_compact_codes(ctypes.byref(c), None if k is None else ctypes.byref(k), K, V, Ks, Vs, keep, kept, nov, None)
+
+
+INT8 = dict(code=ip.CCD_INT8, scale_rows=1, scale_page_stride=32, scale_head_stride=16)
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(code=2), ip.CCD_EUNSUPPORTED), (dict(code=-1), ip.CCD_EUNSUPPORTED), (dict(scale_rows=0), ip.CCD_EINVAL), (dict(scale_rows=3), ip.CCD_EINVAL),
+    (dict(scale_rows=32), ip.CCD_EINVAL), (dict(scale_rows=-4), ip.CCD_EINVAL), (dict(code=ip.CCD_INT8), ip.CCD_EUNSUPPORTED), (dict(scale_page_stride=3), ip.CCD_EINVAL),
+    (dict(scale_head_stride=0), ip.CCD_EINVAL),
+])
+def test_bad_code_descriptors_are_refused(kw, code):
+    c, k = _paged(), _codes(**kw)
+    for call in (_append, _read, _attend, _compact):
+        assert call(c, k) == code
+        assert call(c, None) == ip.CCD_EINVAL
+    assert ip.ccd_codes_workspace_bytes(c, k) == 0
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(page=0), ip.CCD_EINVAL), (dict(n_pages=0), ip.CCD_EINVAL), (dict(tokens=-1), ip.CCD_EINVAL), (dict(Hkv=0), ip.CCD_EINVAL), (dict(d=96), ip.CCD_EUNSUPPORTED),
+    (dict(dtype=2), ip.CCD_EUNSUPPORTED), (dict(row_stride=64), ip.CCD_EINVAL), (dict(page_stride=4), ip.CCD_EINVAL), (dict(head_stride=16 * 128 + 8), ip.CCD_EALIGN),
+])
+def test_bad_cache_descriptors_are_refused(kw, code):
+    for call in (_append, _read, _attend, _compact):
+        assert call(_paged(**kw), _codes(**INT8)) == code
+
+
+def test_strides_of_codes_are_bytes():
+    """8 elements are 16 bytes of a bf16 cache, and 8 of codes."""
+    c = _paged(head_stride=16 * 128 + 8)
+    assert ip.ccd_paged_workspace_bytes(c) > 0 and ip.ccd_codes_workspace_bytes(c, _codes()) == 0
+    assert ip.ccd_codes_workspace_bytes(_paged(head_stride=16 * 128 + 16), _codes()) >= 256
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(B=0), ip.CCD_EINVAL), (dict(table_width=0), ip.CCD_EINVAL), (dict(Hq=7), ip.CCD_EINVAL), (dict(window=-1), ip.CCD_EINVAL), (dict(behind=2), ip.CCD_EINVAL),
+    (dict(scale=float("nan")), ip.CCD_EINVAL), (dict(q_stride_t=1028), ip.CCD_EALIGN), (dict(o_stride_h=130), ip.CCD_EALIGN), (dict(lse_stride_h=0), ip.CCD_EINVAL),
+    (dict(tokens=1 << 26), ip.CCD_EUNSUPPORTED),
+])
+def test_bad_descriptors_of_attention_are_refused(kw, code):
+    assert _attend(_paged(**kw), _codes()) == code
+    assert ip.ccd_codes_workspace_bytes(_paged(**kw), _codes()) == 0
+
+
+def test_bad_pointers_and_workspaces_of_attention_are_refused():
+    c, k = _paged(), _codes()
+    need = ip.ccd_codes_workspace_bytes(c, k)
+    assert need >= 256
+    for name in ("Q", "K", "V", "Ks", "Vs", "table", "q_start", "kv_len", "out"):
+        assert _attend(c, k, **{name: None}) == ip.CCD_EINVAL
+    for name in ("Q", "K", "V", "out"):
+        assert _attend(c, k, **{name: 5 * P2 + 8}) == ip.CCD_EALIGN
+    for name in ("Ks", "Vs"):
+        assert _attend(c, k, **{name: P + 2}) == ip.CCD_EALIGN
+    assert _attend(c, k, out=P) == ip.CCD_EINVAL                  # out over Q
+    assert _attend(c, k, ws=None) == ip.CCD_EWORKSPACE
+    assert _attend(c, k, ws=0x10010) == ip.CCD_EWORKSPACE
+    assert _attend(c, k, ws_bytes=need - 1) == ip.CCD_EWORKSPACE
+    assert _attend(_paged(tokens=0), k, Q=None, out=None, ws=None) == ip.CCD_OK          # an empty step: nothing to do
+
+
+def test_bad_appends_are_refused():
+    c, k = _paged(), _codes()
+    for name in ("K_new", "V_new", "slots", "K", "V", "Ks", "Vs"):
+        assert _append(c, k, **{name: None}) == ip.CCD_EINVAL
+    for name in ("K_new", "V_new", "K", "V"):
+        assert _append(c, k, **{name: 5 * P2 + 8}) == ip.CCD_EALIGN
+    assert _append(c, k, Ks=P + 2) == ip.CCD_EALIGN
+    assert _append(c, k, V=P2) == ip.CCD_EINVAL and _append(c, k, Vs=3 * P2) == ip.CCD_EINVAL
+    assert _append(c, k, rope=_rope(), positions=None) == ip.CCD_EINVAL and _append(c, k, rope=_rope(), turns=None) == ip.CCD_EINVAL
+    assert _append(c, k, rope=_rope(rot=130)) == ip.CCD_EINVAL
+    assert _append(_paged(new_stride_t=64), k) == ip.CCD_EINVAL and _append(_paged(new_stride_h=132), k) == ip.CCD_EALIGN
+    assert _append(_paged(tokens=(1 << 25) + 1), k) == ip.CCD_EUNSUPPORTED
+    for kw, code in ((dict(new_rows=-1), ip.CCD_EINVAL), (dict(new_rows=3, new_stride_b=64), ip.CCD_EINVAL), (dict(new_rows=3, new_stride_b=132), ip.CCD_EALIGN)):
+        assert _append(c, _codes(**kw)) == code
+    assert _append(_paged(tokens=0), k, K_new=None, K=None) == ip.CCD_OK
+
+
+def test_bad_reads_are_refused():
+    c, k = _paged(), _codes()
+    for name in ("K", "V", "Ks", "Vs", "table", "q_start", "kv_len"):
+        assert _read(c, k, **{name: None}) == ip.CCD_EINVAL
+    for name in ("K", "V", "K_out", "V_out"):
+        assert _read(c, k, **{name: 5 * P2 + 8}) == ip.CCD_EALIGN
+    assert _read(c, k, Ks=P + 2) == ip.CCD_EALIGN
+    assert _read(c, k, K_out=None, V_out=None) == ip.CCD_EINVAL
+    assert _read(c, k, V_out=2 * P2) == ip.CCD_EINVAL and _read(c, k, K_out=P) == ip.CCD_EINVAL
+    assert _read(c, k, K_out=None, K=None, Ks=None, V=None) == ip.CCD_EINVAL
+    for kw, code in ((dict(B=0), ip.CCD_EINVAL), (dict(table_width=0), ip.CCD_EINVAL), (dict(o_stride_t=64), ip.CCD_EINVAL), (dict(o_stride_b=4), ip.CCD_EALIGN),
+                     (dict(tokens=(1 << 25) + 1), ip.CCD_EUNSUPPORTED), (dict(tokens=1 << 24, Hkv=32, Hq=32), ip.CCD_EUNSUPPORTED)):
+        assert _read(_paged(**kw), k) == code
+    assert _read(_paged(tokens=0), k, K_out=None, V_out=None) == ip.CCD_OK
+
+
+def test_bad_compactions_are_refused():
+    c, k = _paged(), _codes(**INT8)
+    for name in ("K", "V", "Ks", "Vs", "keep"):
+        assert _compact(c, k, **{name: None}) == ip.CCD_EINVAL
+    assert _compact(c, k, V=P) == ip.CCD_EINVAL and _compact(c, k, Vs=P) == ip.CCD_EINVAL
+    assert _compact(c, k, K=5 * P2 + 8) == ip.CCD_EALIGN and _compact(c, k, Ks=P + 2) == ip.CCD_EALIGN
+    assert _compact(c, k, kept=-1) == ip.CCD_EINVAL and _compact(c, k, kept=17) == ip.CCD_EINVAL
+    assert _compact(c, _codes()) == ip.CCD_EUNSUPPORTED           # rows that share a scale
+    assert _compact(_paged(n_pages=1 << 21, page=16), _codes(**INT8)) == ip.CCD_EUNSUPPORTED
+    assert _compact(c, k, kept=0, K=None) == ip.CCD_OK
+
+
+# ------------------------------------------------------------------------------------------------ binding
+
+B, TOKENS, HQ, HKV, D, PAGE, N_PAGES, W, R = 3, 6, 8, 2, 64, 16, 10, 4, 4
+
+
+def _ints(*shape):
+    return torch.zeros(shape, dtype=torch.int32)
+
+
+def _cache():
+    codes = torch.zeros((N_PAGES, HKV, PAGE, D), dtype=torch.uint8).view(torch.float8_e4m3fn)
+    return dict(K_codes=codes, V_codes=codes.clone(), K_scales=torch.zeros((N_PAGES, HKV, PAGE // R)), V_scales=torch.zeros((N_PAGES, HKV, PAGE // R)))
+
+
+def _bf16(*shape):
+    return torch.zeros(shape, dtype=torch.bfloat16)
+
+
+def _append_call(batched):
+    shape = (B, HKV, TOKENS // B, D) if batched else (TOKENS, HKV, D)
+    t = dict(K_new=_bf16(*shape), V_new=_bf16(*shape), slots=_ints(TOKENS), positions=_ints(TOKENS), turns=torch.zeros(D // 2, dtype=torch.int64), **_cache())
+    paged, codes = ip.make_paged(t["K_codes"], tokens=TOKENS, dtype=torch.bfloat16, K_new=t["K_new"]), ip.make_codes(t["K_codes"], t["K_scales"], K_new=t["K_new"])
+    rope = ip.make_rope(_bf16(TOKENS, HKV, D))
+    return t, lambda t: ip.ccd_paged_append_codes(paged, codes, rope=rope, **t)
+
+
+def _read_call():
+    t = dict(block_table=_ints(B, W), q_start=_ints(B + 1), kv_len=_ints(B), K_out=_bf16(TOKENS, HKV, D), V_out=_bf16(TOKENS, HKV, D), **_cache())
+    paged, codes = ip.make_paged(t["K_codes"], tokens=TOKENS, dtype=torch.bfloat16, block_table=t["block_table"], out=t["K_out"]), ip.make_codes(t["K_codes"], t["K_scales"])
+    return t, lambda t: ip.ccd_paged_read_codes(paged, codes, **t)
+
+
+def _attend_call():
+    Q = _bf16(TOKENS, HQ, D)
+    t = dict(Q=Q, block_table=_ints(B, W), q_start=_ints(B + 1), kv_len=_ints(B), out=Q.clone(), lse=torch.zeros(Q.shape[:-1]), workspace=torch.zeros(1 << 20, dtype=torch.uint8), **_cache())
+    paged = ip.make_paged(t["K_codes"], tokens=TOKENS, dtype=torch.bfloat16, block_table=t["block_table"], Q=Q, out=t["out"], lse=t["lse"])
+    codes = ip.make_codes(t["K_codes"], t["K_scales"])
+    return t, lambda t: ip.ccd_paged_attend_codes(paged, codes, **t)
+
+
+def _compact_call():
+    t = dict(keep_idx=_ints(N_PAGES, HKV, 5), novelty=torch.zeros((N_PAGES, HKV, PAGE)), **_cache())
+    paged, codes = ip.make_paged(t["K_codes"], tokens=0, dtype=torch.bfloat16), ip.make_codes(t["K_codes"], t["K_scales"])
+    return t, lambda t: ip.ccd_paged_compact_codes(paged, codes, **t)
+
+
+CALLS = {"append": lambda: _append_call(False), "append batched": lambda: _append_call(True), "read": _read_call, "attend": _attend_call, "compact": _compact_call}
+PAIRS = {"K_new": "V_new", "K_codes": "V_codes", "K_scales": "V_scales", "K_out": "V_out"}
+PAIRS.update({v: k for k, v in PAIRS.items()})
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_every_tensor_has_to_be_on_the_current_device(launches, name):  # noqa: F811
+    t, call = CALLS[name]()
+    assert call(t) == ip.CCD_OK and launches.calls == 1
+    for x in t:
+        with pytest.raises(ValueError, match="current device"):
+            call({**t, x: t[x].as_subclass(Elsewhere)})
+    assert launches.calls == 1
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_no_tensor_may_end_before_what_the_descriptor_reaches(launches, name):  # noqa: F811
+    t, call = CALLS[name]()
+    for x in t:
+        if x == "workspace":
+            continue
+        for axis in range(t[x].dim()):
+            if x == "keep_idx" and axis == 2:                          # (its last axis says how many rows are kept)
+                continue
+            raw = t[x].view(torch.uint8) if "codes" in x else t[x]
+            short = raw[:-1] if t[x].dtype is torch.int32 and raw.dim() > 1 else raw.narrow(axis, 0, raw.shape[axis] - 1).clone()
+            short = short.view(t[x].dtype)
+            with pytest.raises(AssertionError):
+                call({**t, x: short, **({PAIRS[x]: short.clone()} if x in PAIRS else {})})
+            if x in PAIRS:
+                with pytest.raises(AssertionError, match="differ"):
+                    call({**t, x: short})
+    assert launches.calls == 0
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_types_that_are_not_the_descriptors(launches, name):  # noqa: F811
+    t, call = CALLS[name]()
+    other = {torch.bfloat16: torch.float32, torch.float32: torch.bfloat16, torch.int32: torch.int64, torch.int64: torch.int32, torch.float8_e4m3fn: torch.int8}
+    for x in t:
+        if x == "workspace":
+            continue
+        wrong = t[x].view(torch.int8) if "codes" in x else t[x].to(other[t[x].dtype])
+        with pytest.raises(AssertionError):
+            call({**t, x: wrong, **({PAIRS[x]: wrong.clone()} if x in PAIRS else {})})
+    assert launches.calls == 0
+
+
+def test_descriptors_from_tensors():
+    t = _cache()
+    k = ip.make_codes(t["K_codes"], t["K_scales"])
+    assert (k.code, k.scale_rows, k.scale_page_stride, k.scale_head_stride, k.new_rows) == (ip.CCD_E4M3, R, HKV * PAGE // R, PAGE // R, 0)
+    with pytest.raises(AssertionError):
+        ip.make_codes(t["K_codes"], torch.zeros((N_PAGES, HKV, 5)))
+    with pytest.raises(TypeError):
+        ip.make_codes(t["K_codes"].view(torch.uint8), t["K_scales"])
+    with pytest.raises(TypeError):
+        ip.make_paged(t["K_codes"], tokens=3)                          # the type of the others has to be said
+
+
+# ------------------------------------------------------------------------------------------------ the reference's own pins
+
+def test_what_e4m3_codes_stand_for():
+    bits = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).double().numpy()
+    np.testing.assert_array_equal(np.isnan(C.E4M3), np.isnan(bits))
+    np.testing.assert_array_equal(np.nan_to_num(C.E4M3), np.nan_to_num(bits))
+
+
+def test_codes_of_the_reference():
+    x = np.linspace(-448.0, 448.0, 99991)
+    np.testing.assert_array_equal(C.encode(x, 1.0, "e4m3"), torch.from_numpy(x).float().to(torch.float8_e4m3fn).view(torch.uint8).numpy())
+    small = np.arange(-4096, 4097) * 2.0 ** -14
+    np.testing.assert_array_equal(C.encode(small, 1.0, "e4m3"), torch.from_numpy(small).float().to(torch.float8_e4m3fn).view(torch.uint8).numpy())
+    assert C.encode([0.5, 1.5, 2.5, -0.5, -1.5, 127.0], 1.0, "int8").view(np.int8).tolist() == [0, 2, 2, 0, -2, 127]
+    assert C.scale_for(np.array([448.0]), "e4m3") == 1.0 and C.scale_for(np.array([448.0001]), "e4m3") == 2.0 and C.scale_for(np.array([224.0]), "e4m3") == 0.5
+    assert C.scale_for(np.zeros(3), "int8") == 2.0 ** -120 == C.scale_for(np.zeros(3), "e4m3")
+
+
+def test_a_block_of_the_reference_worked_by_hand():
+    """Blocks of two rows: 448 begins one (scale 1), 900 makes it 4 (900 / 448 > 2), a first row again makes it what it needs."""
+    codes, scales = np.zeros((1, 1, 4, 1), np.uint8), np.full((1, 1, 2), 7.0, np.float32)
+    C.append(np.array([[[448.0]]]), [0], codes, scales, "e4m3", 2)
+    assert scales[0, 0, 0] == 1.0 and codes[0, 0, 0, 0] == 0x7E
+    C.append(np.array([[[900.0]]]), [1], codes, scales, "e4m3", 2)
+    assert scales[0, 0, 0] == 4.0 and C.decode(codes, scales, "e4m3", 2)[0, 0, :2, 0].tolist() == [448.0, 896.0]
+    C.append(np.array([[[0.25]]]), [0], codes, scales, "e4m3", 2)
+    assert scales[0, 0, 0] == 2.0 ** -10 and scales[0, 0, 1] == 7.0
+    assert math.isclose(C.decode(codes, scales, "e4m3", 2)[0, 0, 0, 0], 0.25)
