@@ -8,6 +8,7 @@
 // The rows of a unit (sequence, KV head) are its new tokens times the G query heads that share the head, row r = token r / G, head r % G:
 // heads of one token lie side by side and see the same keys, and a block of rows is a narrow band of positions.
 #pragma once
+#include "ccd_codes.h"
 #include "ccd_common.h"
 #include "ccd_paged.h"
 #include "ccd_rotary.h"
@@ -15,6 +16,24 @@
 namespace ccd {
 
 constexpr float kRaise = 8.f;
+
+// What the kernels' T stands for: uint16_t and float, queries, cache and results of one type; Coded, a cache of codes under queries and results of type Q, read by
+// tiles of TOKENS.
+template <class Q, int CODE, int TOKENS>
+struct Coded {};
+template <class T>
+struct CacheOf {
+  using Out = T;
+  static constexpr bool kCoded = false;
+};
+template <class Q, int CODE_, int TOKENS>
+struct CacheOf<Coded<Q, CODE_, TOKENS>> {
+  using Out = Q;
+  static constexpr bool kCoded = true;
+  static constexpr int kCode = CODE_;
+};
+template <class T>
+using OutOf = typename CacheOf<T>::Out;
 
 typedef short v4s __attribute__((ext_vector_type(4)));
 typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
@@ -103,6 +122,9 @@ struct AttendArgs {
   void* out;
   float* lse;
   Partials part;
+  // caches of codes
+  Codes codes;
+  const float *K_scales, *V_scales;
 };
 
 // Block k of the call's blocks of rows, counted from the last sequence's last: where the sequences' new tokens differ, a grid for the most of any
@@ -139,7 +161,7 @@ __device__ __forceinline__ bool find_block(const Paged& P, const AttendPlan& pl,
 
 // Of the tokens t_first .. t_end - 1: is a value that some of the rows r0 .. r1 - 1 do not see (nobody those before t_begin) infinite or NaN?  By the wave.
 template <class T, int D>
-__device__ __forceinline__ bool bad_unseen(const Paged& P, const AttendArgs& A, const Sequence& sq, int b, int hkv, int r0, int r1, int t_first, int t_begin, int t_end) {
+__device__ __forceinline__ bool bad_unseen_rows(const Paged& P, const AttendArgs& A, const Sequence& sq, int b, int hkv, int r0, int r1, int t_first, int t_begin, int t_end) {
   const int low = first_seen(P, sq.base + (r1 - 1) / P.G), next = sq.base + r0 / P.G + 1, all_from = low > t_begin ? low : t_begin;
   const int32_t* pages = A.table + (int64_t)b * P.table_width;
   const T* V = static_cast<const T*>(A.V) + hkv * P.head_stride + (threadIdx.x & 63);
@@ -159,7 +181,7 @@ __device__ __forceinline__ bool bad_unseen(const Paged& P, const AttendArgs& A, 
 // Row r over the tokens of t_begin .. t_end - 1 that it sees, by a wave, 64 tokens at a time: a lane has the logit of one of them, and then d / 64 elements of the sums.
 // That is the result (whole_row), or the stretch's `entry` of the workspace.
 template <class T, int D>
-__device__ __forceinline__ void redo_row(const Paged& P, const AttendArgs& A, const Sequence& sq, int b, int hkv, int r, int t_begin, int t_end,
+__device__ __forceinline__ void redo_row_rows(const Paged& P, const AttendArgs& A, const Sequence& sq, int b, int hkv, int r, int t_begin, int t_end,
                                          bool whole_row, int64_t entry) {
   constexpr int kPer = D / 64, kEPL = 16 / sizeof(T), kSide = 8;
   const int lane = threadIdx.x & 63;
@@ -228,6 +250,109 @@ __device__ __forceinline__ void redo_row(const Paged& P, const AttendArgs& A, co
     for (int j = 0; j < kPer; ++j) A.part.o[entry * D + j * 64 + lane] = o[j];
     if (lane == 0) A.part.ml[entry] = make_float2(m, l);
   }
+}
+
+// The same over a cache of codes.  int8: a code is a number, and the scale of an unseen token is not looked at, so nothing unseen can reach a row; e4m3 has a code for what is none.
+template <class T, int D>
+__device__ __forceinline__ bool bad_unseen_codes(const Paged& P, const AttendArgs& A, const Sequence& sq, int b, int hkv, int r0, int r1, int t_first, int t_begin, int t_end) {
+  if constexpr (CacheOf<T>::kCode == kInt8) return false;
+  const int low = first_seen(P, sq.base + (r1 - 1) / P.G), next = sq.base + r0 / P.G + 1, all_from = low > t_begin ? low : t_begin;
+  const int32_t* pages = A.table + (int64_t)b * P.table_width;
+  const uint8_t* V = static_cast<const uint8_t*>(A.V) + hkv * P.head_stride + (threadIdx.x & 63);
+  bool bad = false;
+  for (int t = t_first; t < t_end; ++t) {
+    if (t >= all_from && t < next) t = next;                    // (all rows see those)
+    if (t >= t_end) break;
+    const int c = page_of(P.div, t), id = pages[c];
+    if (id < 0 || id >= P.n_pages) continue;
+    const uint8_t* v = V + id * P.page_stride + (int64_t)(t - c * P.div.page) * P.row_stride;
+#pragma unroll
+    for (int j = 0; j < D / 64; ++j) bad = bad || (v[j * 64] & 0x7F) == 0x7F;
+  }
+  return __any(bad);
+}
+
+template <class T, int D>
+__device__ __forceinline__ void redo_row_codes(const Paged& P, const AttendArgs& A, const Sequence& sq, int b, int hkv, int r, int t_begin, int t_end,
+                                               bool whole_row, int64_t entry) {
+  using Q = OutOf<T>;
+  constexpr int kPer = D / 64, kCode = CacheOf<T>::kCode;
+  const int lane = threadIdx.x & 63;
+  const int32_t* pages = A.table + (int64_t)b * P.table_width;
+  const uint8_t* K = static_cast<const uint8_t*>(A.K) + hkv * P.head_stride;
+  const uint8_t* V = static_cast<const uint8_t*>(A.V) + hkv * P.head_stride;
+  const uint8_t* zero = reinterpret_cast<const uint8_t*>(g_zero_row);
+  const int i = r / P.G, head = hkv * P.G + r - i * P.G, pos = sq.base + i, low = first_seen(P, pos);
+  const int64_t row = sq.first + i;
+  const Q* from = static_cast<const Q*>(A.Q) + b * P.q_b + row * P.q_t + head * P.q_h;
+  const int begin = low > t_begin ? low : t_begin, end = pos + 1 < t_end ? pos + 1 : t_end;
+  auto of_lane = [](float x, int u) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), u)); };
+  float q[kPer], m = -INFINITY, l = 0.f, o[kPer] = {};
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) q[j] = load_elem(from + j * 64 + lane);
+  for (int t0 = begin; t0 < end; t0 += 64) {
+    int64_t off = -1;                                           // of token t0 + lane
+    float ks = 0.f, vs = 0.f, x = 0.f;
+    if (t0 + lane < end) {
+      const int t = t0 + lane, c = page_of(P.div, t), id = pages[c], at = t - c * P.div.page;
+      if (id >= 0 && id < P.n_pages) {
+        off = id * P.page_stride + at * P.row_stride;
+        const int64_t s = id * A.codes.page + hkv * A.codes.head + (at >> A.codes.shift);
+        ks = A.K_scales[s];
+        vs = A.V_scales[s];
+      }
+    }
+    const uint8_t* k = off >= 0 ? K + off : zero;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+#pragma unroll 2
+      for (int p = 0; p < 64; p += 4) {
+        float y[4];
+        numbers<kCode>(*reinterpret_cast<const uint32_t*>(k + j * 64 + p), y);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x = fmaf(of_lane(q[j], p + e), y[e], x);
+      }
+    x = off >= 0 ? x * ks * P.scale_log2 : -INFINITY;
+    float next = fmaxf(m, x);
+#pragma unroll
+    for (int s = 32; s; s >>= 1) next = fmaxf(next, __shfl_xor(next, s));
+    const float keep = next == -INFINITY ? 1.f : fast_exp2(m - next), w = fast_exp2(x - (next == -INFINITY ? 0.f : next));
+    m = next;
+    l = l * keep + w;
+    const float weight = off >= 0 ? w * vs : 0.f;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) o[j] *= keep;
+    for (int u = 0; u < 64 && t0 + u < end; ++u) {
+      const int64_t at = (int64_t)__builtin_amdgcn_readlane((int)(off >> 32), u) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)off, u);
+      const uint8_t* v = at >= 0 ? V + at : zero;
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) o[j] = fmaf(of_lane(weight, u), number<kCode>(v[j * 64 + lane]), o[j]);
+    }
+  }
+#pragma unroll
+  for (int s = 32; s; s >>= 1) l += __shfl_xor(l, s);
+  if (whole_row) {
+    const float inv = inverse_sum(l);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) store_elem(static_cast<Q*>(A.out) + b * P.o_b + row * P.o_t + head * P.o_h + j * 64 + lane, o[j] * inv);
+    if (A.lse != nullptr && lane == 0) A.lse[b * P.l_b + row * P.l_t + head * P.l_h] = to_natural_lse(m, l);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) A.part.o[entry * D + j * 64 + lane] = o[j];
+    if (lane == 0) A.part.ml[entry] = make_float2(m, l);
+  }
+}
+
+template <class T, int D>
+__device__ __forceinline__ bool bad_unseen(const Paged& P, const AttendArgs& A, const Sequence& sq, int b, int hkv, int r0, int r1, int t_first, int t_begin, int t_end) {
+  if constexpr (CacheOf<T>::kCoded) return bad_unseen_codes<T, D>(P, A, sq, b, hkv, r0, r1, t_first, t_begin, t_end);
+  else                              return bad_unseen_rows<T, D>(P, A, sq, b, hkv, r0, r1, t_first, t_begin, t_end);
+}
+template <class T, int D>
+__device__ __forceinline__ void redo_row(const Paged& P, const AttendArgs& A, const Sequence& sq, int b, int hkv, int r, int t_begin, int t_end, bool whole_row,
+                                         int64_t entry) {
+  if constexpr (CacheOf<T>::kCoded) redo_row_codes<T, D>(P, A, sq, b, hkv, r, t_begin, t_end, whole_row, entry);
+  else                              redo_row_rows<T, D>(P, A, sq, b, hkv, r, t_begin, t_end, whole_row, entry);
 }
 // the same for a grid's stretch part_no
 template <class T, int D>

@@ -248,7 +248,7 @@ __device__ __forceinline__ float row_sum(float x) {
 
 // workgroups per compute unit, and so waves per SIMD, that the registers are cut for: what the rows of queries and of sums leave room for
 template <class T, int D, int NQ>
-constexpr int split_waves() { return NQ == 2 || D == 128 ? 2 : 3; }
+constexpr int split_waves() { return NQ == 2 || D == 128 || CacheOf<T>::kCoded ? 2 : 3; }
 
 template <class T, int D, int NQ, int WAVES = kWaves>
 struct SplitLds {
@@ -258,14 +258,82 @@ struct SplitLds {
   float m[WAVES][kRows], l[WAVES][kRows];
 };
 
+// The end of a stretch: the waves' sums together, all to the largest reference, 16 rows at a time through LDS.  l: a row's sum of weights; fix: what its product
+// with the values is to be taken times (add_rounded).  Returns whether the rows may have to be done again.
+template <class T, int D, int NQ, int WAVES>
+__device__ __forceinline__ bool join_waves(const Paged& P, const AttendArgs& A, SplitLds<T, D, NQ, WAVES>& L, const Sequence& sq, int b, int hkv, int r0, int r1, bool whole_row,
+                                           int64_t part0, int part_no, const float (&m)[NQ], const float (&l)[NQ], const float (&fix)[NQ],
+                                           const v4f (&o)[NQ][Tile<T, D>::kBlocks]) {
+  using Tl = Tile<T, D>;
+  constexpr int kPitch = SplitLds<T, D, NQ, WAVES>::kPitch;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    if (lane < 16) { L.m[wave][16 * j + lane] = m[j]; L.l[wave][16 * j + lane] = l[j]; }
+  }
+  __syncthreads();
+  bool none = false;                                        // sums that are no numbers, of weights that are
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    float all = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) all = fmaxf(all, L.m[w][16 * j + (lane & 15)]);
+    const float keep = m[j] == -INFINITY ? (l[j] == l[j] ? 0.f : l[j]) : fast_exp2(m[j] - all) * fix[j];
+    float* mine = reinterpret_cast<float*>(L.wave[wave]) + (lane & 15) * kPitch;
+    if (j > 0) __syncthreads();
+#pragma unroll
+    for (int c = 0; c < Tl::kBlocks; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) mine[Tl::element(c, lane, i)] = o[j][c][i] * keep;
+    __syncthreads();
+    // 16 rows of D elements by all threads
+    constexpr int kPer = 16 * D / (64 * WAVES);           // 2, 4 or 8 elements a thread
+    const int q_row = tid / (D / kPer), e0 = tid % (D / kPer) * kPer, r = r0 + 16 * j + q_row;
+    float acc[kPer] = {}, top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const float* from = reinterpret_cast<const float*>(L.wave[w]) + q_row * kPitch + e0;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) acc[e] += from[e];
+      top = fmaxf(top, L.m[w][16 * j + q_row]);
+    }
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const float mw = L.m[w][16 * j + q_row], lw = L.l[w][16 * j + q_row];
+      sum += mw == -INFINITY ? (lw == lw ? 0.f : lw) : lw * fast_exp2(mw - top);
+    }
+    if (r < r1) {
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) none = none || (acc[e] != acc[e] && sum == sum);
+      const int i = r / P.G, head = hkv * P.G + r - i * P.G;
+      const int64_t row = sq.first + i;
+      if (whole_row) {
+        const float inv = inverse_sum(sum);
+        OutOf<T>* to = static_cast<OutOf<T>*>(A.out) + b * P.o_b + row * P.o_t + head * P.o_h + e0;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) acc[e] *= inv;
+        store_piece(to, acc);
+        if (A.lse != nullptr && e0 == 0) A.lse[b * P.l_b + row * P.l_t + head * P.l_h] = to_natural_lse(top, sum);
+      } else {
+        const int64_t at = part0 >= 0 ? part0 + (r - r0) : ((int64_t)part_no * P.tokens + row) * P.Hq + head;
+        float* to = A.part.o + at * D + e0;
+        store_piece(to, acc);
+        if (e0 == 0) A.part.ml[at] = make_float2(top, sum);
+      }
+    }
+  }
+  // one new token alone sees all tokens of the stretch: what it has is its own
+  return __syncthreads_or(none && r0 / P.G != (r1 - 1) / P.G);
+}
+
 // Rows r0 .. r1 - 1 of unit (b, hkv) over the tokens t_begin .. t_end - 1, by the workgroup.  whole_row: these are all tokens the rows see, the result
 // is written; else (o, m, l) of row r go to entry part0 + (r - r0) of the workspace, or, part0 < 0, to those of part_no by the row's number.
 // Returns whether the rows may have to be done again (bad_unseen says).
 template <class T, int D, int NQ, int WAVES>
-__device__ __forceinline__ bool attend_stretch(const Paged& P, const AttendArgs& A, SplitLds<T, D, NQ, WAVES>& L, const Sequence& sq, int b, int hkv, int r0, int r1,
+__device__ __forceinline__ bool attend_stretch_rows(const Paged& P, const AttendArgs& A, SplitLds<T, D, NQ, WAVES>& L, const Sequence& sq, int b, int hkv, int r0, int r1,
                                                int t_begin, int t_end, bool whole_row, int64_t part0, int part_no) {
   using Tl = Tile<T, D>;
-  constexpr int kPitch = SplitLds<T, D, NQ, WAVES>::kPitch, kStride = WAVES * Tl::kTokens;
+  constexpr int kStride = WAVES * Tl::kTokens;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int32_t* pages = A.table + (int64_t)b * P.table_width;
   const T* Kh = static_cast<const T*>(A.K) + hkv * P.head_stride;
@@ -385,66 +453,24 @@ __device__ __forceinline__ bool attend_stretch(const Paged& P, const AttendArgs&
     }
   }
 
-  // the waves' sums together: all to the largest reference, 16 rows at a time through LDS
+  float fix[NQ];
 #pragma unroll
   for (int j = 0; j < NQ; ++j) {
     l[j] = row_sum(l[j]);
-    lr[j] = row_sum(lr[j]);
-    if (lane < 16) { L.m[wave][16 * j + lane] = m[j]; L.l[wave][16 * j + lane] = l[j]; }
+    fix[j] = unrounded(l[j], row_sum(lr[j]));
   }
-  __syncthreads();
-  bool none = false;                                        // sums that are no numbers, of weights that are
-#pragma unroll
-  for (int j = 0; j < NQ; ++j) {
-    float all = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) all = fmaxf(all, L.m[w][16 * j + (lane & 15)]);
-    const float keep = m[j] == -INFINITY ? (l[j] == l[j] ? 0.f : l[j]) : fast_exp2(m[j] - all) * unrounded(l[j], lr[j]);
-    float* mine = reinterpret_cast<float*>(L.wave[wave]) + (lane & 15) * kPitch;
-    if (j > 0) __syncthreads();
-#pragma unroll
-    for (int c = 0; c < Tl::kBlocks; ++c)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) mine[Tl::element(c, lane, i)] = o[j][c][i] * keep;
-    __syncthreads();
-    // 16 rows of D elements by all threads
-    constexpr int kPer = 16 * D / (64 * WAVES);           // 2, 4 or 8 elements a thread
-    const int q_row = tid / (D / kPer), e0 = tid % (D / kPer) * kPer, r = r0 + 16 * j + q_row;
-    float acc[kPer] = {}, top = -INFINITY, sum = 0.f;
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-      const float* from = reinterpret_cast<const float*>(L.wave[w]) + q_row * kPitch + e0;
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) acc[e] += from[e];
-      top = fmaxf(top, L.m[w][16 * j + q_row]);
-    }
-#pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
-      const float mw = L.m[w][16 * j + q_row], lw = L.l[w][16 * j + q_row];
-      sum += mw == -INFINITY ? (lw == lw ? 0.f : lw) : lw * fast_exp2(mw - top);
-    }
-    if (r < r1) {
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) none = none || (acc[e] != acc[e] && sum == sum);
-      const int i = r / P.G, head = hkv * P.G + r - i * P.G;
-      const int64_t row = sq.first + i;
-      if (whole_row) {
-        const float inv = inverse_sum(sum);
-        T* to = static_cast<T*>(A.out) + b * P.o_b + row * P.o_t + head * P.o_h + e0;
-#pragma unroll
-        for (int e = 0; e < kPer; ++e) acc[e] *= inv;
-        store_piece(to, acc);
-        if (A.lse != nullptr && e0 == 0) A.lse[b * P.l_b + row * P.l_t + head * P.l_h] = to_natural_lse(top, sum);
-      } else {
-        const int64_t at = part0 >= 0 ? part0 + (r - r0) : ((int64_t)part_no * P.tokens + row) * P.Hq + head;
-        float* to = A.part.o + at * D + e0;
-        store_piece(to, acc);
-        if (e0 == 0) A.part.ml[at] = make_float2(top, sum);
-      }
-    }
-  }
-  // one new token alone sees all tokens of the stretch: what it has is its own
-  return __syncthreads_or(none && r0 / P.G != (r1 - 1) / P.G);
+  return join_waves<T, D, NQ, WAVES>(P, A, L, sq, b, hkv, r0, r1, whole_row, part0, part_no, m, l, fix, o);
+}
+
+}  // namespace ccd
+#include "ccd_codes_few.h"
+namespace ccd {
+
+template <class T, int D, int NQ, int WAVES>
+__device__ __forceinline__ bool attend_stretch(const Paged& P, const AttendArgs& A, SplitLds<T, D, NQ, WAVES>& L, const Sequence& sq, int b, int hkv, int r0, int r1,
+                                               int t_begin, int t_end, bool whole_row, int64_t part0, int part_no) {
+  if constexpr (CacheOf<T>::kCoded) return attend_stretch_codes<T, D, NQ, WAVES>(P, A, L, sq, b, hkv, r0, r1, t_begin, t_end, whole_row, part0, part_no);
+  else                              return attend_stretch_rows<T, D, NQ, WAVES>(P, A, L, sq, b, hkv, r0, r1, t_begin, t_end, whole_row, part0, part_no);
 }
 
 // the call cut on a grid: (head, sequence, stretch, block of rows), or (head, stretch, block of the call)
@@ -560,7 +586,7 @@ __device__ __forceinline__ void attend_evenly(const Paged& P, const AttendPlan& 
     for (int64_t x = tid; x < (int64_t)sq.m * P.Hq * (D / 4); x += kThreads) {
       const int e = (int)(x % (D / 4)) * 4, head = (int)(x / (D / 4) % P.Hq), i = (int)(x / (D / 4) / P.Hq);
       const float none[4] = {0.f, 0.f, 0.f, 0.f};
-      store_piece(static_cast<T*>(A.out) + b * P.o_b + (int64_t)(sq.first + i) * P.o_t + head * P.o_h + e, none);
+      store_piece(static_cast<OutOf<T>*>(A.out) + b * P.o_b + (int64_t)(sq.first + i) * P.o_t + head * P.o_h + e, none);
       if (A.lse != nullptr && e == 0) A.lse[b * P.l_b + (int64_t)(sq.first + i) * P.l_t + head * P.l_h] = -INFINITY;
     }
   }

@@ -1,0 +1,306 @@
+// Few rows per unit over a cache of codes: the part of ccd_attend_few.h that reads it (included there).
+//
+// As with bf16 caches, waves go their own ways through tiles of the stretch,   Keys and values come from memory into registers
+// as they lie, quads of lanes reading 64 bytes of a row, and go through the wave's piece of LDS as codes: keys come back as rows, values by the
+// transposing read, and codes become bf16 numbers on their way into the matrix instructions, exactly.  A lane looks up one token of the tile, its page and its two
+// scales.  The keys' scale
+// is a factor of the logit, the values' one of the weight.
+#pragma once
+
+namespace ccd {
+
+// eight codes as an operand
+template <int CODE>
+__device__ __forceinline__ v8bf operand(uint32_t lo, uint32_t hi) {
+  typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+  v4u w;
+  if constexpr (CODE == kInt8) {
+    float x[4], y[4];
+    numbers<CODE>(lo, x);
+    numbers<CODE>(hi, y);
+    // (whole numbers of 8 bits: the upper half of a float is all of it)
+    auto upper = [](float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302); };
+    w = v4u{upper(x[0], x[1]), upper(x[2], x[3]), upper(y[0], y[1]), upper(y[2], y[3])};
+  } else {
+    const v2bf a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
+    const v2bf c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
+    w = v4u{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, c), __builtin_bit_cast(uint32_t, d)};
+  }
+  return __builtin_bit_cast(v8bf, w);
+}
+
+// x as a sum of bf16 numbers, the largest first: one (rounded), or three, which are all of an fp32 number
+template <int PARTS>
+__device__ __forceinline__ void cut(const float (&x)[8], v8bf (&f)[PARTS]) {
+  float rest[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) rest[e] = x[e];
+#pragma unroll
+  for (int p = 0; p < PARTS; ++p) {
+    const v4u w = {pack_bf16(rest[0], rest[1]), pack_bf16(rest[2], rest[3]), pack_bf16(rest[4], rest[5]), pack_bf16(rest[6], rest[7])};
+    f[p] = __builtin_bit_cast(v8bf, w);
+#pragma unroll
+    for (int e = 0; e < 4 && p + 1 < PARTS; ++e) {
+      rest[2 * e] -= __uint_as_float(w[e] << 16);
+      rest[2 * e + 1] -= __uint_as_float(w[e] & 0xFFFF0000u);
+    }
+  }
+}
+
+// Tokens of a tile: 2^k of them.  Part h, row r of it (LDS row 16 h + r) is token kHalves * r + h, so that a lane group's scales lie side by side.
+template <class Q, int CODE, int TOKENS, int D>
+struct Tile<Coded<Q, CODE, TOKENS>, D> {
+  static constexpr int kTokens = TOKENS, kHalves = TOKENS / 16, kBlocks = D / 16, kSteps = D / 32;                        // (steps of 32 elements)
+  static constexpr int kQuads = TOKENS / 4, kCopies = 16 / kQuads, kLoads = TOKENS * D / 1024;                      // a quad's four rows are shared out over kCopies quads
+  static constexpr int kParts = sizeof(Q) == 4 ? 3 : 1;                            // bf16 numbers per element of a query, per weight
+  static constexpr int kSide = kTokens * D;                                        // bytes of keys, or values
+  static constexpr int kLdsBytes = 2 * kSide + 2 * kTokens * 4;                    // (and the scales)
+  struct Query { v8bf f[kSteps][kParts]; };
+  struct Rows { v4u r[kLoads]; };
+
+  // step 2 u + v: elements 16 (4 u + g) + 8 v .. of lane group g, as the codes of a piece give them
+  __device__ static void load_query(Query& q, const Q* row, int lane, bool there) {
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const int e0 = 16 * (4 * (s >> 1) + (lane >> 4)) + 8 * (s & 1);
+      float x[8] = {};
+      if (there) {
+        if constexpr (sizeof(Q) == 2) {
+          load_f32(*reinterpret_cast<const v4u*>(row + e0), x, row);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = row[e0 + e];
+        }
+      }
+      cut(x, q.f[s]);
+    }
+  }
+  // the lane's token: row s of its quad is LDS row kQuads s + quad
+  __device__ static int own_token(int lane) {
+    const int row = kQuads * (lane & 3) + (lane >> 2) % kQuads;
+    return kHalves * (row & 15) + (row >> 4);
+  }
+  // a lane that has the token of part h, row r
+  __device__ static int lane_of(int h, int r) {
+    const int row = 16 * h + r;
+    return 4 * (row % kQuads) + row / kQuads;
+  }
+  // the load n of a lane: row s of its quad, 64 bytes from 64 u on
+  __device__ static int row_of(int n, int lane) { return ((lane >> 2) / kQuads * kLoads + n) & 3; }
+  __device__ static int part_of(int n, int lane) { return ((lane >> 2) / kQuads * kLoads + n) >> 2; }
+  template <int N = 0>
+  __device__ static void load_codes(Rows& r, const char* own, int lane) {
+    if constexpr (N < kLoads) {
+      const char* p = of_row<4, N & 3>(own);
+      if constexpr (kCopies > 1 && kLoads < 4) {                                   // (the other copy's row)
+        const char* q = of_row<4, (N + kLoads) & 3>(own);
+        p = (lane >> 2) / kQuads ? q : p;
+      }
+      r.r[N] = *reinterpret_cast<const v4u*>(p + 64 * part_of(N, lane) + 16 * (lane & 3));
+      load_codes<N + 1>(r, own, lane);
+    }
+  }
+  // Places in LDS: a row's pieces of 16 bytes exchanged so that what a read or a write takes together lies in all banks (16 rows, or four, of one
+  // piece; 8 rows 4 g .. of two parts, of two groups)
+  __device__ static int key_swap(int row) { return D == 128 ? ((row >> 1) & 1) << 2 | ((row >> 2) & 3) : (row >> 2) & 3; }
+  __device__ static int value_swap(int row) {
+    return D == 128 ? ((row >> 1) & 1) << 2 | ((row >> 2) & 1) | ((row >> 4) & 1) << 1 : ((row >> 2) & 1) | ((row >> 4) & 1) << 1;
+  }
+  template <bool KEYS>
+  __device__ static void store_codes(const Rows& r, char* lds, int lane) {
+#pragma unroll
+    for (int n = 0; n < kLoads; ++n) {
+      const int row = kQuads * row_of(n, lane) + (lane >> 2) % kQuads, piece = 4 * part_of(n, lane) + (lane & 3);
+      *reinterpret_cast<v4u*>(lds + row * D + ((piece ^ (KEYS ? key_swap(row) : value_swap(row))) << 4)) = r.r[n];
+    }
+  }
+  // x[j][h][i] = <q, code> of token kHalves (4 g + i) + h, row lane & 15 of block j
+  template <int NQ>
+  __device__ static void logits(v4f (&x)[NQ][kHalves], const char* lds, const Query (&q)[NQ], int lane) {
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) {
+      const int row = 16 * h + (lane & 15);
+#pragma unroll
+      for (int j = 0; j < NQ; ++j) x[j][h] = v4f{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int u = 0; u < D / 64; ++u) {
+        const v4u k = *reinterpret_cast<const v4u*>(lds + row * D + (((4 * u + (lane >> 4)) ^ key_swap(row)) << 4));
+#pragma unroll
+        for (int v = 0; v < 2; ++v) {
+          const v8bf a = operand<CODE>(k[2 * v], k[2 * v + 1]);
+#pragma unroll
+          for (int j = 0; j < NQ; ++j)
+#pragma unroll
+            for (int p = kParts - 1; p >= 0; --p) x[j][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, q[j].f[2 * u + v][p], x[j][h], 0, 0, 0);
+        }
+      }
+    }
+  }
+  struct Weights { v8bf w[kHalves / 2][kParts]; };                                 // of parts 0 and 1, 2 and 3
+  // o[j][c][i] += element 16 c + 4 g + i of the values, for row lane & 15
+  template <int NQ>
+  __device__ static void add_values(v4f (&o)[NQ][kBlocks], const Weights (&w)[NQ], const char* lds, int lane) {
+    typedef int v2i __attribute__((ext_vector_type(2)));
+    const int at = (lane & 15) >> 1, row = 16 * (at >> 2) + 4 * (lane >> 4) + (at & 3);
+#pragma unroll
+    for (int c = 0; c < kBlocks; ++c)
+#pragma unroll
+      for (int s = 0; s < kHalves / 2; ++s) {
+        const v2i t = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) v2i*)(lds + (row + 32 * s) * D + ((c ^ value_swap(row)) << 4) + (lane & 1) * 8));
+        const v8bf a = operand<CODE>((uint32_t)t[0], (uint32_t)t[1]);
+#pragma unroll
+        for (int j = 0; j < NQ; ++j)
+#pragma unroll
+          for (int p = kParts - 1; p >= 0; --p) o[j][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[j].w[s][p], o[j][c], 0, 0, 0);
+      }
+  }
+  __device__ static int element(int c, int lane, int i) { return 16 * c + 4 * (lane >> 4) + i; }
+};
+
+// attend_stretch over codes
+template <class T, int D, int NQ, int WAVES>
+__device__ __forceinline__ bool attend_stretch_codes(const Paged& P, const AttendArgs& A, SplitLds<T, D, NQ, WAVES>& L, const Sequence& sq, int b, int hkv, int r0, int r1,
+                                                     int t_begin, int t_end, bool whole_row, int64_t part0, int part_no) {
+  using Tl = Tile<T, D>;
+  using Q = OutOf<T>;
+  constexpr int kStride = WAVES * Tl::kTokens;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, group = lane >> 4;
+  const int32_t* pages = A.table + (int64_t)b * P.table_width;
+  const uint8_t* Kh = static_cast<const uint8_t*>(A.K) + hkv * P.head_stride;
+  const uint8_t* Vh = static_cast<const uint8_t*>(A.V) + hkv * P.head_stride;
+  const float* Ks = A.K_scales + hkv * A.codes.head;
+  const float* Vs = A.V_scales + hkv * A.codes.head;
+  char* keys_lds = L.wave[wave];
+  char* values_lds = keys_lds + Tl::kSide;
+  float* scales_lds = reinterpret_cast<float*>(values_lds + Tl::kSide);
+  // Keys, values and scales of a tile are asked for a tile ahead, the pages they are in two tiles ahead.
+  typename Tl::Rows keys, values;
+  int64_t off = -1;
+  float ks = 0.f, vs = 0.f;
+  int id = -1;
+  const int own = Tl::own_token(lane);
+  auto look_up = [&](int t0) {
+    const int t = t0 + own;
+    id = t < t_end ? pages[page_of(P.div, t)] : -1;
+  };
+  auto ask = [&](int t0) {
+    const int t = t0 + own, at = t - page_of(P.div, t) * P.div.page;
+    const bool there = id >= 0 && id < P.n_pages;
+    off = there ? id * P.page_stride + (int64_t)at * P.row_stride : -1;
+    ks = vs = 0.f;
+    if (there) {
+      const int64_t s = id * A.codes.page + (at >> A.codes.shift);
+      ks = Ks[s];
+      vs = Vs[s];
+    }
+    const uint8_t* zero = reinterpret_cast<const uint8_t*>(g_zero_row);
+    Tl::load_codes(keys, reinterpret_cast<const char*>(there ? Kh + off : zero), lane);
+    Tl::load_codes(values, reinterpret_cast<const char*>(there ? Vh + off : zero), lane);
+  };
+  int t0 = t_begin + wave * Tl::kTokens;
+  if (t0 < t_end) {
+    look_up(t0);
+    ask(t0);
+    look_up(t0 + kStride);
+  }
+  // the lane's rows
+  typename Tl::Query q[NQ];
+  int pos[NQ], low[NQ];                                    // position of the row, first position it sees
+  const int pos_min = sq.base + r0 / P.G, low_max = first_seen(P, sq.base + (r1 - 1) / P.G);
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    const int r = r0 + 16 * j + (lane & 15), i = r / P.G;
+    pos[j] = sq.base + i;
+    low[j] = first_seen(P, pos[j]);
+    Tl::load_query(q[j], static_cast<const Q*>(A.Q) + b * P.q_b + (int64_t)(sq.first + i) * P.q_t + (int64_t)(hkv * P.G + r - i * P.G) * P.q_h, lane, r < r1);
+  }
+  // l: sums of weights; ls, lr: of weights times the values' scales, as they are and as rounded for the product
+  float m[NQ], l[NQ], ls[NQ], lr[NQ];
+  v4f o[NQ][Tl::kBlocks];
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    m[j] = -INFINITY; l[j] = ls[j] = lr[j] = 0.f;
+#pragma unroll
+    for (int c = 0; c < Tl::kBlocks; ++c) o[j][c] = v4f{0.f, 0.f, 0.f, 0.f};
+  }
+  for (; t0 < t_end; t0 += kStride) {
+    // (by lanes, all that have the token)
+    const uint64_t there = __ballot(off >= 0);
+    const bool whole = there == ~(uint64_t)0 && t0 + Tl::kTokens - 1 <= pos_min && t0 >= low_max;
+    Tl::template store_codes<true>(keys, keys_lds, lane);
+    Tl::template store_codes<false>(values, values_lds, lane);
+    scales_lds[own] = ks;
+    scales_lds[Tl::kTokens + own] = vs;
+    if (t0 + kStride < t_end) {
+      ask(t0 + kStride);
+      look_up(t0 + 2 * kStride);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    v4f x[NQ][Tl::kHalves], sk[Tl::kHalves], sv[Tl::kHalves];       // scales of the group's tokens, 4 kHalves g ..
+#pragma unroll
+    for (int n = 0; n < Tl::kHalves; ++n) {
+      sk[n] = *reinterpret_cast<const v4f*>(scales_lds + 4 * Tl::kHalves * group + 4 * n);
+      sv[n] = *reinterpret_cast<const v4f*>(scales_lds + Tl::kTokens + 4 * Tl::kHalves * group + 4 * n);
+    }
+    auto scale_of = [](const v4f (&s)[Tl::kHalves], int h, int i) { return s[(Tl::kHalves * i + h) >> 2][(Tl::kHalves * i + h) & 3]; };
+    Tl::logits(x, keys_lds, q, lane);
+    typename Tl::Weights w[NQ];
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+      float top = -INFINITY;
+#pragma unroll
+      for (int h = 0; h < Tl::kHalves; ++h)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[j][h][i] *= scale_of(sk, h, i);
+          if (!whole) {
+            const int t = t0 + Tl::kHalves * (4 * group + i) + h;
+            if (!((there >> Tl::lane_of(h, 4 * group + i)) & 1u) || t > pos[j] || t < low[j]) x[j][h][i] = -INFINITY;
+          }
+          top = fmaxf(top, x[j][h][i]);
+        }
+      top *= P.scale_log2;
+      if (__any(top > m[j] + kRaise)) {
+        const float next = fmaxf(m[j], row_max(top));
+        const float keep = next == -INFINITY ? 1.f : fast_exp2(m[j] - next);
+        m[j] = next;
+        l[j] *= keep;
+        ls[j] *= keep;
+        lr[j] *= keep;
+#pragma unroll
+        for (int c = 0; c < Tl::kBlocks; ++c) o[j][c] *= keep;
+      }
+      const float ref = m[j] == -INFINITY ? 0.f : m[j];
+#pragma unroll
+      for (int s = 0; s < Tl::kHalves / 2; ++s) {
+        float e[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          const int h = 2 * s + (k >> 2), i = k & 3;
+          const float weight = fast_exp2(fmaf(x[j][h][i], P.scale_log2, -ref));
+          l[j] += weight;
+          e[k] = weight * scale_of(sv, h, i);
+          if (!whole) e[k] = weight == 0.f ? 0.f : e[k];    // (the scale of a token that is not seen may be no number)
+          ls[j] += e[k];
+        }
+        cut(e, w[j].w[s]);
+        if constexpr (Tl::kParts == 1) {
+#pragma unroll
+          for (int p = 0; p < 4; ++p) lr[j] = add_rounded(w[j].w[s][0], p, lr[j]);
+        }
+      }
+    }
+    Tl::add_values(o, w, values_lds, lane);
+    __builtin_amdgcn_wave_barrier();
+  }
+  float fix[NQ];
+#pragma unroll
+  for (int j = 0; j < NQ; ++j) {
+    l[j] = row_sum(l[j]);
+    fix[j] = Tl::kParts == 1 ? unrounded(row_sum(ls[j]), row_sum(lr[j])) : 1.f;
+  }
+  return join_waves<T, D, NQ, WAVES>(P, A, L, sq, b, hkv, r0, r1, whole_row, part0, part_no, m, l, fix, o);
+}
+
+}  // namespace ccd
