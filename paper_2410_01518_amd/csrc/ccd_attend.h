@@ -17,17 +17,16 @@ namespace ccd {
 
 constexpr float kRaise = 8.f;
 
-// What the kernels' T stands for: uint16_t and float, queries, cache and results of one type; Coded, a cache of codes under queries and results of type Q, read by
-// tiles of TOKENS.
-template <class Q, int CODE, int TOKENS>
+// What the kernels' T stands for: uint16_t and float, queries, cache and results of one type; Coded, a cache of codes under queries and results of type Q.
+template <class Q, int CODE>
 struct Coded {};
 template <class T>
 struct CacheOf {
   using Out = T;
   static constexpr bool kCoded = false;
 };
-template <class Q, int CODE_, int TOKENS>
-struct CacheOf<Coded<Q, CODE_, TOKENS>> {
+template <class Q, int CODE_>
+struct CacheOf<Coded<Q, CODE_>> {
   using Out = Q;
   static constexpr bool kCoded = true;
   static constexpr int kCode = CODE_;

@@ -37,7 +37,7 @@ AttendCuts plan_attend(const Paged& P, int dtype, bool codes, int max_new, int m
     e.only_few = many;
     e.few = e.rows;
     e.join = (int)(most < e.rows ? most : e.rows);
-    const int waves = codes ? 2 : dtype == 0 ? (P.d == 64 ? even_waves<float, 64>(e.rows) : even_waves<float, 128>(e.rows))
+    const int waves = codes ? (e.rows == 16 && (P.d == 64 || dtype != 0) ? 3 : 2) : dtype == 0 ? (P.d == 64 ? even_waves<float, 64>(e.rows) : even_waves<float, 128>(e.rows))
                                  : (P.d == 64 ? even_waves<uint16_t, 64>(e.rows) : even_waves<uint16_t, 128>(e.rows));
     const int64_t units = (int64_t)P.B * P.Hkv;
     int64_t wgs = (units * len + kEvenLeast - 1) / kEvenLeast;

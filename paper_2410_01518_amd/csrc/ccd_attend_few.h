@@ -61,6 +61,11 @@ __device__ __forceinline__ void load_rows(v4u* r, const char* p, int first, int 
   }
 }
 
+// 64 lanes x 16 bytes from memory into LDS, at lds_addr + 16 * lane
+__device__ __forceinline__ void load_to_lds(uint32_t lds_addr, const void* p) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_addr), "v"(p) : "memory");
+}
+
 // sum + two weights as they are rounded to bf16.  The weights of the product with the values are rounded, their sum is not; a row that one token rules
 // would be off by that token's rounding.  So the product is taken times l / lr in the end, lr being the sum of the rounded weights.
 // (One query of 8 heads over 438 tokens: 3.0e-3 off in the norm where the output's own rounding is 1.8e-3; 1.9e-3 so.)
@@ -248,7 +253,7 @@ __device__ __forceinline__ float row_sum(float x) {
 
 // workgroups per compute unit, and so waves per SIMD, that the registers are cut for: what the rows of queries and of sums leave room for
 template <class T, int D, int NQ>
-constexpr int split_waves() { return NQ == 2 || D == 128 || CacheOf<T>::kCoded ? 2 : 3; }
+constexpr int split_waves() { return NQ == 1 && (D == 64 || (CacheOf<T>::kCoded && sizeof(OutOf<T>) == 2)) ? 3 : 2; }
 
 template <class T, int D, int NQ, int WAVES = kWaves>
 struct SplitLds {

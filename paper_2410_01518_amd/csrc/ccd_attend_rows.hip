@@ -21,10 +21,6 @@ constexpr int kRowWaves = 4, kTile = 64;
 constexpr float kFar = 256.f;            // sum of a lane's 16 weights above which the reference is raised
 enum { kKeys = 1, kValues = 2 };
 
-// 64 lanes x 16 bytes from memory into LDS, at lds_addr + 16 * lane
-__device__ __forceinline__ void load_to_lds(uint32_t lds_addr, const void* p) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds_addr), "v"(p) : "memory");
-}
 // N such, to lds_addr + 1024 k + 16 * lane.  An instruction's own offset counts for both addresses: offset[k] is meant with it taken off, and what
 // would then be negative is in the base (run_offset).
 template <int N>

@@ -47,14 +47,14 @@ __device__ __forceinline__ void cut(const float (&x)[8], v8bf (&f)[PARTS]) {
   }
 }
 
-// Tokens of a tile: 2^k of them.  Part h, row r of it (LDS row 16 h + r) is token kHalves * r + h, so that a lane group's scales lie side by side.
-template <class Q, int CODE, int TOKENS, int D>
-struct Tile<Coded<Q, CODE, TOKENS>, D> {
-  static constexpr int kTokens = TOKENS, kHalves = TOKENS / 16, kBlocks = D / 16, kSteps = D / 32;                        // (steps of 32 elements)
-  static constexpr int kQuads = TOKENS / 4, kCopies = 16 / kQuads, kLoads = TOKENS * D / 1024;                      // a quad's four rows are shared out over kCopies quads
+// Part h, row r of a tile (LDS row 16 h + r) is its token kHalves * r + h, so that a lane group's scales lie side by side, and a quad of lanes has row r of all parts.
+template <class Q, int CODE, int D>
+struct Tile<Coded<Q, CODE>, D> {
+  static constexpr int kTokens = 32, kHalves = kTokens / 16, kBlocks = D / 16, kSteps = D / 32;                           // (steps of 32 elements)
+  static constexpr int kPlanes = D / 64, kPlane = kTokens * 64, kLoads = kPlanes * kHalves;                        // LDS has planes of 64 bytes of every row
   static constexpr int kParts = sizeof(Q) == 4 ? 3 : 1;                            // bf16 numbers per element of a query, per weight
   static constexpr int kSide = kTokens * D;                                        // bytes of keys, or values
-  static constexpr int kLdsBytes = 2 * kSide + 2 * kTokens * 4;                    // (and the scales)
+  static constexpr int kLdsBytes = 3 * kSide + 2 * kTokens * 4;                    // keys, values twice, scales
   struct Query { v8bf f[kSteps][kParts]; };
   struct Rows { v4u r[kLoads]; };
 
@@ -75,43 +75,36 @@ struct Tile<Coded<Q, CODE, TOKENS>, D> {
       cut(x, q.f[s]);
     }
   }
-  // the lane's token: row s of its quad is LDS row kQuads s + quad
-  __device__ static int own_token(int lane) {
-    const int row = kQuads * (lane & 3) + (lane >> 2) % kQuads;
-    return kHalves * (row & 15) + (row >> 4);
-  }
-  // a lane that has the token of part h, row r
-  __device__ static int lane_of(int h, int r) {
-    const int row = 16 * h + r;
-    return 4 * (row % kQuads) + row / kQuads;
-  }
-  // the load n of a lane: row s of its quad, 64 bytes from 64 u on
-  __device__ static int row_of(int n, int lane) { return ((lane >> 2) / kQuads * kLoads + n) & 3; }
-  __device__ static int part_of(int n, int lane) { return ((lane >> 2) / kQuads * kLoads + n) >> 2; }
-  template <int N = 0>
-  __device__ static void load_codes(Rows& r, const char* own, int lane) {
-    if constexpr (N < kLoads) {
-      const char* p = of_row<4, N & 3>(own);
-      if constexpr (kCopies > 1 && kLoads < 4) {                                   // (the other copy's row)
-        const char* q = of_row<4, (N + kLoads) & 3>(own);
-        p = (lane >> 2) / kQuads ? q : p;
-      }
-      r.r[N] = *reinterpret_cast<const v4u*>(p + 64 * part_of(N, lane) + 16 * (lane & 3));
-      load_codes<N + 1>(r, own, lane);
+  // the lane's token, that of part h, row r, and a lane that has it
+  __device__ static int own_token(int lane) { return kHalves * (lane >> 2) + lane % kHalves; }
+  __device__ static int token_of(int h, int r) { return kHalves * r + h; }
+  __device__ static int lane_of(int h, int r) { return 4 * r + h; }
+  // The pieces of 16 bytes of a row's 64 change places by the row's number, so that what a read takes together lies in all banks: 16 rows of keys, one
+  // piece; 16 rows of values, 4 g .. of two parts and two lane groups, one piece.
+  __device__ static int key_swap(int row) { return (row >> 2) & 3; }
+  __device__ static int value_swap(int row) { return ((row >> 2) & 1) | ((row >> 4) & 1) << 1; }
+  // Load (u, h): 64 bytes, plane u, of row 16 h + quad.  own: the row of the lane's own token.
+  __device__ static void load_keys(Rows& k, const char* own, int lane) {
+    const int at = 16 * (lane & 3);
+#pragma unroll
+    for (int u = 0; u < kPlanes; ++u) {
+      k.r[kHalves * u] = *reinterpret_cast<const v4u*>(of_row<4, 0>(own) + 64 * u + at);
+      k.r[kHalves * u + 1] = *reinterpret_cast<const v4u*>(of_row<4, 1>(own) + 64 * u + at);
     }
   }
-  // Places in LDS: a row's pieces of 16 bytes exchanged so that what a read or a write takes together lies in all banks (16 rows, or four, of one
-  // piece; 8 rows 4 g .. of two parts, of two groups)
-  __device__ static int key_swap(int row) { return D == 128 ? ((row >> 1) & 1) << 2 | ((row >> 2) & 3) : (row >> 2) & 3; }
-  __device__ static int value_swap(int row) {
-    return D == 128 ? ((row >> 1) & 1) << 2 | ((row >> 2) & 1) | ((row >> 4) & 1) << 1 : ((row >> 2) & 1) | ((row >> 4) & 1) << 1;
-  }
-  template <bool KEYS>
-  __device__ static void store_codes(const Rows& r, char* lds, int lane) {
+  __device__ static void store_keys(const Rows& k, char* lds, int lane) {
 #pragma unroll
     for (int n = 0; n < kLoads; ++n) {
-      const int row = kQuads * row_of(n, lane) + (lane >> 2) % kQuads, piece = 4 * part_of(n, lane) + (lane & 3);
-      *reinterpret_cast<v4u*>(lds + row * D + ((piece ^ (KEYS ? key_swap(row) : value_swap(row))) << 4)) = r.r[n];
+      const int row = 16 * (n % kHalves) + (lane >> 2);
+      *reinterpret_cast<v4u*>(lds + n / kHalves * kPlane + row * 64 + (((lane & 3) ^ key_swap(row)) << 4)) = k.r[n];
+    }
+  }
+  // values straight into LDS
+  __device__ static void load_values(uint32_t lds_addr, const char* own, int lane) {
+#pragma unroll
+    for (int u = 0; u < kPlanes; ++u) {
+      load_to_lds(lds_addr + u * kPlane, of_row<4, 0>(own) + 64 * u + (((lane & 3) ^ value_swap(lane >> 2)) << 4));
+      load_to_lds(lds_addr + u * kPlane + 1024, of_row<4, 1>(own) + 64 * u + (((lane & 3) ^ value_swap(16 + (lane >> 2))) << 4));
     }
   }
   // x[j][h][i] = <q, code> of token kHalves (4 g + i) + h, row lane & 15 of block j
@@ -124,7 +117,7 @@ struct Tile<Coded<Q, CODE, TOKENS>, D> {
       for (int j = 0; j < NQ; ++j) x[j][h] = v4f{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int u = 0; u < D / 64; ++u) {
-        const v4u k = *reinterpret_cast<const v4u*>(lds + row * D + (((4 * u + (lane >> 4)) ^ key_swap(row)) << 4));
+        const v4u k = *reinterpret_cast<const v4u*>(lds + u * kPlane + row * 64 + (((lane >> 4) ^ key_swap(row)) << 4));
 #pragma unroll
         for (int v = 0; v < 2; ++v) {
           const v8bf a = operand<CODE>(k[2 * v], k[2 * v + 1]);
@@ -136,22 +129,20 @@ struct Tile<Coded<Q, CODE, TOKENS>, D> {
       }
     }
   }
-  struct Weights { v8bf w[kHalves / 2][kParts]; };                                 // of parts 0 and 1, 2 and 3
+  struct Weights { v8bf w[kParts]; };
   // o[j][c][i] += element 16 c + 4 g + i of the values, for row lane & 15
   template <int NQ>
   __device__ static void add_values(v4f (&o)[NQ][kBlocks], const Weights (&w)[NQ], const char* lds, int lane) {
     typedef int v2i __attribute__((ext_vector_type(2)));
     const int at = (lane & 15) >> 1, row = 16 * (at >> 2) + 4 * (lane >> 4) + (at & 3);
 #pragma unroll
-    for (int c = 0; c < kBlocks; ++c)
-#pragma unroll
-      for (int s = 0; s < kHalves / 2; ++s) {
-        const v2i t = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) v2i*)(lds + (row + 32 * s) * D + ((c ^ value_swap(row)) << 4) + (lane & 1) * 8));
+    for (int c = 0; c < kBlocks; ++c) {
+        const v2i t = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) v2i*)(lds + (c >> 2) * kPlane + row * 64 + (((c & 3) ^ value_swap(row)) << 4) + (lane & 1) * 8));
         const v8bf a = operand<CODE>((uint32_t)t[0], (uint32_t)t[1]);
 #pragma unroll
         for (int j = 0; j < NQ; ++j)
 #pragma unroll
-          for (int p = kParts - 1; p >= 0; --p) o[j][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[j].w[s][p], o[j][c], 0, 0, 0);
+          for (int p = kParts - 1; p >= 0; --p) o[j][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[j].w[p], o[j][c], 0, 0, 0);
       }
   }
   __device__ static int element(int c, int lane, int i) { return 16 * c + 4 * (lane >> 4) + i; }
@@ -164,20 +155,21 @@ __device__ __forceinline__ bool attend_stretch_codes(const Paged& P, const Atten
   using Tl = Tile<T, D>;
   using Q = OutOf<T>;
   constexpr int kStride = WAVES * Tl::kTokens;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, group = lane >> 4;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), group = lane >> 4;
   const int32_t* pages = A.table + (int64_t)b * P.table_width;
   const uint8_t* Kh = static_cast<const uint8_t*>(A.K) + hkv * P.head_stride;
   const uint8_t* Vh = static_cast<const uint8_t*>(A.V) + hkv * P.head_stride;
   const float* Ks = A.K_scales + hkv * A.codes.head;
   const float* Vs = A.V_scales + hkv * A.codes.head;
   char* keys_lds = L.wave[wave];
-  char* values_lds = keys_lds + Tl::kSide;
-  float* scales_lds = reinterpret_cast<float*>(values_lds + Tl::kSide);
-  // Keys, values and scales of a tile are asked for a tile ahead, the pages they are in two tiles ahead.
-  typename Tl::Rows keys, values;
-  int64_t off = -1;
+  float* scales_lds = reinterpret_cast<float*>(keys_lds + 3 * Tl::kSide);
+  const uint32_t values_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)(keys_lds + Tl::kSide));
+  // Keys, values and scales of a tile are asked for a tile ahead, the pages they are in two tiles ahead; values go straight into LDS, to the place that the tile before
+  // the last left.
+  typename Tl::Rows keys;
   float ks = 0.f, vs = 0.f;
-  int id = -1;
+  int id = -1, slot = 0;                                    // slot: of the values being asked for
+  bool own_there = false;
   const int own = Tl::own_token(lane);
   auto look_up = [&](int t0) {
     const int t = t0 + own;
@@ -185,17 +177,18 @@ __device__ __forceinline__ bool attend_stretch_codes(const Paged& P, const Atten
   };
   auto ask = [&](int t0) {
     const int t = t0 + own, at = t - page_of(P.div, t) * P.div.page;
-    const bool there = id >= 0 && id < P.n_pages;
-    off = there ? id * P.page_stride + (int64_t)at * P.row_stride : -1;
+    own_there = id >= 0 && id < P.n_pages;
     ks = vs = 0.f;
-    if (there) {
-      const int64_t s = id * A.codes.page + (at >> A.codes.shift);
+    const char *k = reinterpret_cast<const char*>(g_zero_row), *v = k;
+    if (own_there) {
+      const int64_t s = id * A.codes.page + (at >> A.codes.shift), off = id * P.page_stride + (int64_t)at * P.row_stride;
       ks = Ks[s];
       vs = Vs[s];
+      k = reinterpret_cast<const char*>(Kh + off);
+      v = reinterpret_cast<const char*>(Vh + off);
     }
-    const uint8_t* zero = reinterpret_cast<const uint8_t*>(g_zero_row);
-    Tl::load_codes(keys, reinterpret_cast<const char*>(there ? Kh + off : zero), lane);
-    Tl::load_codes(values, reinterpret_cast<const char*>(there ? Vh + off : zero), lane);
+    Tl::load_values(__builtin_amdgcn_readfirstlane(values_at + slot), v, lane);
+    Tl::load_keys(keys, k, lane);
   };
   int t0 = t_begin + wave * Tl::kTokens;
   if (t0 < t_end) {
@@ -224,14 +217,17 @@ __device__ __forceinline__ bool attend_stretch_codes(const Paged& P, const Atten
     for (int c = 0; c < Tl::kBlocks; ++c) o[j][c] = v4f{0.f, 0.f, 0.f, 0.f};
   }
   for (; t0 < t_end; t0 += kStride) {
+    // what was asked for is there (loads into LDS do not arrive in the order they were asked for)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     // (by lanes, all that have the token)
-    const uint64_t there = __ballot(off >= 0);
+    const uint64_t there = __ballot(own_there);
     const bool whole = there == ~(uint64_t)0 && t0 + Tl::kTokens - 1 <= pos_min && t0 >= low_max;
-    Tl::template store_codes<true>(keys, keys_lds, lane);
-    Tl::template store_codes<false>(values, values_lds, lane);
+    const char* values_lds = keys_lds + Tl::kSide + slot;
+    Tl::store_keys(keys, keys_lds, lane);
     scales_lds[own] = ks;
     scales_lds[Tl::kTokens + own] = vs;
     if (t0 + kStride < t_end) {
+      slot ^= Tl::kSide;
       ask(t0 + kStride);
       look_up(t0 + 2 * kStride);
     }
@@ -255,7 +251,7 @@ __device__ __forceinline__ bool attend_stretch_codes(const Paged& P, const Atten
         for (int i = 0; i < 4; ++i) {
           x[j][h][i] *= scale_of(sk, h, i);
           if (!whole) {
-            const int t = t0 + Tl::kHalves * (4 * group + i) + h;
+            const int t = t0 + Tl::token_of(h, 4 * group + i);
             if (!((there >> Tl::lane_of(h, 4 * group + i)) & 1u) || t > pos[j] || t < low[j]) x[j][h][i] = -INFINITY;
           }
           top = fmaxf(top, x[j][h][i]);
@@ -272,22 +268,21 @@ __device__ __forceinline__ bool attend_stretch_codes(const Paged& P, const Atten
         for (int c = 0; c < Tl::kBlocks; ++c) o[j][c] *= keep;
       }
       const float ref = m[j] == -INFINITY ? 0.f : m[j];
-#pragma unroll
-      for (int s = 0; s < Tl::kHalves / 2; ++s) {
+      {
         float e[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
-          const int h = 2 * s + (k >> 2), i = k & 3;
+          const int h = k >> 2, i = k & 3;
           const float weight = fast_exp2(fmaf(x[j][h][i], P.scale_log2, -ref));
           l[j] += weight;
           e[k] = weight * scale_of(sv, h, i);
           if (!whole) e[k] = weight == 0.f ? 0.f : e[k];    // (the scale of a token that is not seen may be no number)
           ls[j] += e[k];
         }
-        cut(e, w[j].w[s]);
+        cut(e, w[j].w);
         if constexpr (Tl::kParts == 1) {
 #pragma unroll
-          for (int p = 0; p < 4; ++p) lr[j] = add_rounded(w[j].w[s][0], p, lr[j]);
+          for (int p = 0; p < 4; ++p) lr[j] = add_rounded(w[j].w[0], p, lr[j]);
         }
       }
     }
