@@ -251,10 +251,9 @@ __device__ __forceinline__ void redo_row_rows(const Paged& P, const AttendArgs& 
   }
 }
 
-// The same over a cache of codes.  int8: a code is a number, and the scale of an unseen token is not looked at, so nothing unseen can reach a row; e4m3 has a code for what is none.
+// The same over a cache of codes.  int8: a code is a number, and a scale may be none; e4m3 has a code for what is none.
 template <class T, int D>
 __device__ __forceinline__ bool bad_unseen_codes(const Paged& P, const AttendArgs& A, const Sequence& sq, int b, int hkv, int r0, int r1, int t_first, int t_begin, int t_end) {
-  if constexpr (CacheOf<T>::kCode == kInt8) return false;
   const int low = first_seen(P, sq.base + (r1 - 1) / P.G), next = sq.base + r0 / P.G + 1, all_from = low > t_begin ? low : t_begin;
   const int32_t* pages = A.table + (int64_t)b * P.table_width;
   const uint8_t* V = static_cast<const uint8_t*>(A.V) + hkv * P.head_stride + (threadIdx.x & 63);
@@ -264,9 +263,11 @@ __device__ __forceinline__ bool bad_unseen_codes(const Paged& P, const AttendArg
     if (t >= t_end) break;
     const int c = page_of(P.div, t), id = pages[c];
     if (id < 0 || id >= P.n_pages) continue;
-    const uint8_t* v = V + id * P.page_stride + (int64_t)(t - c * P.div.page) * P.row_stride;
+    const int at = t - c * P.div.page;
+    bad = bad || !(fabsf(A.V_scales[id * A.codes.page + hkv * A.codes.head + (at >> A.codes.shift)]) < INFINITY);
+    const uint8_t* v = V + id * P.page_stride + at * P.row_stride;
 #pragma unroll
-    for (int j = 0; j < D / 64; ++j) bad = bad || (v[j * 64] & 0x7F) == 0x7F;
+    for (int j = 0; j < D / 64 && CacheOf<T>::kCode == kE4m3; ++j) bad = bad || (v[j * 64] & 0x7F) == 0x7F;
   }
   return __any(bad);
 }
@@ -363,7 +364,14 @@ inline unsigned grid_size(const Paged& P, const AttendPlan& pl) {
   return (unsigned)((int64_t)P.Hkv * pl.parts * (pl.blocks > 0 ? pl.blocks : (int64_t)P.B * pl.row_blocks));
 }
 
-// rows kernel (bf16): a workgroup per (unit, block of 128 rows, stretch), its waves share the tiles; with it the even cut, if there is one
+// rows kernel (bf16 queries): a workgroup per (unit, block of 128 rows, stretch), its waves share the tiles; with it the even cut, if there is one
+template <class T>
 void launch_attend_rows(const Paged& P, const AttendPlan& pl, const AttendArgs& A, const AttendPlan& even, const Partials& even_part, hipStream_t s);
+template <>
+void launch_attend_rows<uint16_t>(const Paged& P, const AttendPlan& pl, const AttendArgs& A, const AttendPlan& even, const Partials& even_part, hipStream_t s);
+template <>
+void launch_attend_rows<Coded<uint16_t, kInt8>>(const Paged& P, const AttendPlan& pl, const AttendArgs& A, const AttendPlan& even, const Partials& even_part, hipStream_t s);
+template <>
+void launch_attend_rows<Coded<uint16_t, kE4m3>>(const Paged& P, const AttendPlan& pl, const AttendArgs& A, const AttendPlan& even, const Partials& even_part, hipStream_t s);
 
 }  // namespace ccd

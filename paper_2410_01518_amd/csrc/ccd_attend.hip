@@ -37,7 +37,7 @@ AttendCuts plan_attend(const Paged& P, int dtype, bool codes, int max_new, int m
     e.only_few = many;
     e.few = e.rows;
     e.join = (int)(most < e.rows ? most : e.rows);
-    const int waves = codes ? (e.rows == 16 && (P.d == 64 || dtype != 0) ? 3 : 2) : dtype == 0 ? (P.d == 64 ? even_waves<float, 64>(e.rows) : even_waves<float, 128>(e.rows))
+    const int waves = codes ? (!many && e.rows == 16 && (P.d == 64 || dtype != 0) ? 3 : 2) : dtype == 0 ? (P.d == 64 ? even_waves<float, 64>(e.rows) : even_waves<float, 128>(e.rows))
                                  : (P.d == 64 ? even_waves<uint16_t, 64>(e.rows) : even_waves<uint16_t, 128>(e.rows));
     const int64_t units = (int64_t)P.B * P.Hkv;
     int64_t wgs = (units * len + kEvenLeast - 1) / kEvenLeast;
@@ -70,7 +70,7 @@ AttendCuts plan_attend(const Paged& P, int dtype, bool codes, int max_new, int m
   }
   if (many) {
     AttendPlan& g = c.grid;
-    g.by_rows = dtype != 0 && !codes;
+    g.by_rows = dtype != 0;
     g.rows = g.by_rows ? 128 : 32;
     g.few = c.even.few;
     g.row_blocks = (int)((rows + g.rows - 1) / g.rows);

@@ -179,9 +179,9 @@ template <class T, int D>
 static void attend_launch(const Paged& P, const AttendCuts& c, const AttendArgs& even, const AttendArgs& grid, hipStream_t s) {
   const dim3 block(64 * kWaves);
   if (c.grid.rows > 0 && c.grid.by_rows) {
-    if constexpr (!CacheOf<T>::kCoded) launch_attend_rows(P, c.grid, grid, c.even, even.part, s);
+    if constexpr (sizeof(OutOf<T>) == 2) launch_attend_rows<T>(P, c.grid, grid, c.even, even.part, s);
   } else if (c.grid.rows > 0 && (c.grid.blocks > 0 || c.even.rows > 0)) {
-    if constexpr (!std::is_same_v<T, uint16_t>) {
+    if constexpr (sizeof(OutOf<T>) == 4) {
       if (c.even.rows == 32) mixed_launch<T, D, 2>(P, c, grid, even.part, s);
       else                   mixed_launch<T, D, 1>(P, c, grid, even.part, s);
     }
