@@ -44,6 +44,22 @@ __device__ __forceinline__ float largest(const v16f& x) {
   return top;
 }
 
+// x times what lane n of the row of 16 lanes has of s (DPP row_newbcast, part of the multiplication)
+template <int N>
+__device__ __forceinline__ float times_row_of(float x, float s) {
+  return x * __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(s), 0x150 + N, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float times_row_lane(float x, float s, int n) {
+  switch (n) {                                             // (n is known when the loops around are unrolled)
+    case 0: return times_row_of<0>(x, s);   case 1: return times_row_of<1>(x, s);   case 2: return times_row_of<2>(x, s);   case 3: return times_row_of<3>(x, s);
+    case 4: return times_row_of<4>(x, s);   case 5: return times_row_of<5>(x, s);   case 6: return times_row_of<6>(x, s);   case 7: return times_row_of<7>(x, s);
+    case 8: return times_row_of<8>(x, s);   case 9: return times_row_of<9>(x, s);   case 10: return times_row_of<10>(x, s); case 11: return times_row_of<11>(x, s);
+    case 12: return times_row_of<12>(x, s); case 13: return times_row_of<13>(x, s); case 14: return times_row_of<14>(x, s); default: return times_row_of<15>(x, s);
+  }
+}
+template <int... N>
+__device__ __forceinline__ void times_row(v16f& x, float s, std::integer_sequence<int, N...>) { ((x[N] = times_row_of<N>(x[N], s)), ...); }
+
 // BANDED: pages of whole runs of 16 rows, so that a wave's 16 rows of a tile lie in one page, which is looked up 64 tiles ahead.  Else every row's page is looked
 // up in its tile, and waited for: 2048 new tokens over 4096 in pages of 37 or 100 take 264 to 270 us where pages of 64 take 118, over 32768 2160 and 1045.
 // SUMS: those of the rounded weights, too (add_rounded): calls over few tokens, where that costs little
@@ -201,23 +217,22 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
         H.there = (uint32_t)__ballot(there) & 0xFFFFu;
       }
     };
-    // codes as bf16 numbers to the wave's place in a tile
-    auto put_codes = [&](const Held& H, int tile, int slot, bool keys) __attribute__((always_inline)) {
+    // codes as bf16 numbers to the wave's place in a tile: half n & 1 of piece n / 2 of kHeld
+    constexpr int kPuts = 2 * kHeld;
+    auto put_codes = [&](const Held& H, int slot, bool keys, int n) __attribute__((always_inline)) {
       if constexpr (kCoded) {
-        const int row0 = lane / kCodePieces, piece = lane % kCodePieces;
-#pragma unroll
-        for (int k = 0; k < kHeld; ++k) {
-          const int row = 64 / kCodePieces * k + row0, swap = keys ? key_swap(row) : value_swap(row);
-          char* to = lds[slot][keys ? 0 : 1] + (16 * wave + row) * kRowB;
-#pragma unroll
-          for (int n = 0; n < 2; ++n)
-            *reinterpret_cast<v8bf*>(to + (((2 * piece + n) ^ swap) << 4)) = operand<CacheOf<T>::kCode>(H.c[k][2 * n], H.c[k][2 * n + 1]);
-        }
-        if (keys && lane < 16) {
+        const int row = 64 / kCodePieces * (n / 2) + lane / kCodePieces, piece = 2 * (lane % kCodePieces) + (n & 1);
+        *reinterpret_cast<v8bf*>(lds[slot][keys ? 0 : 1] + (16 * wave + row) * kRowB + ((piece ^ (keys ? key_swap(row) : value_swap(row))) << 4)) =
+            operand<CacheOf<T>::kCode>(H.c[n / 2][2 * (n & 1)], H.c[n / 2][2 * (n & 1) + 1]);
+      }
+    };
+    auto put_scales = [&](const Held& H, int tile, int slot) __attribute__((always_inline)) {
+      if constexpr (kCoded) {
+        if (lane < 16) {
           L.key_scale[slot][16 * wave + lane] = H.ks * P.scale_log2;
           L.value_scale[tile & 3][16 * wave + lane] = H.vs;
         }
-        if (keys && lane == 0) here[slot][wave] = H.there;
+        if (lane == 0) here[slot][wave] = H.there;
       }
     };
     // asks for the wave's 16 rows of a tile
@@ -271,21 +286,20 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
         }
       }
     };
-    // the values' scales of tokens 8 g + 4 half .. of block (tile, sub), and the logits of a block times the keys' scales
-    auto value_scales = [&](int tile, int sub, int g) __attribute__((always_inline)) {
-      v4f s = {1.f, 1.f, 1.f, 1.f};
-      if constexpr (kCoded) s = *reinterpret_cast<const v4f*>(&L.value_scale[tile & 3][32 * sub + 8 * g + 4 * half]);
-      return s;
+    // Scales of a block's tokens: lane n of a row of 16 lanes has that of the n-th of the 16 tokens that the row's lanes have logits of.  (Read as four times 16 bytes a lane
+    // they would take LDS as long as half of the keys do.)
+    const int scale_at = 8 * ((lane & 15) >> 2) + 4 * half + (lane & 3);
+    auto value_scales = [&](int tile, int sub) __attribute__((always_inline)) {
+      if constexpr (kCoded) return L.value_scale[tile & 3][32 * sub + scale_at];
+      return 1.f;
     };
-    auto scale_logits = [&](v16f& x, int slot, int sub) __attribute__((always_inline)) {
-      if constexpr (kCoded) {
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const v4f s = *reinterpret_cast<const v4f*>(&L.key_scale[slot][32 * sub + 8 * g + 4 * half]);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x[4 * g + i] *= s[i];
-        }
-      }
+    auto key_scales = [&](int slot, int sub) __attribute__((always_inline)) {
+      if constexpr (kCoded) return L.key_scale[slot][32 * sub + scale_at];
+      return 1.f;
+    };
+    // x[e] times the scale of token e
+    auto scale_logits = [&](v16f& x, float s) __attribute__((always_inline)) {
+      if constexpr (kCoded) times_row(x, s, std::make_integer_sequence<int, 16>{});
     };
     // (over codes logits have their factor already)
     auto weight_of = [&](float x) __attribute__((always_inline)) { return fast_exp2(kCoded ? x - m : fmaf(x, P.scale_log2, -m)); };
@@ -293,12 +307,12 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
       float sum = 0.f;
       v4u now[2];
       scaled = 0.f;
+      const float vs = value_scales(tile, sub);
 #pragma unroll
       for (int p = 0; p < 8; ++p) {
         const float e0 = weight_of(x[2 * p]), e1 = weight_of(x[2 * p + 1]);
         if constexpr (kCoded) {
-          const v4f s = value_scales(tile, sub, p / 2);
-          const float f0 = e0 * s[2 * p % 4], f1 = e1 * s[2 * p % 4 + 1];
+          const float f0 = times_row_lane(e0, vs, 2 * p), f1 = times_row_lane(e1, vs, 2 * p + 1);
           now[p / 4][p % 4] = pack_bf16(f0, f1);
           if (SUMS) scaled += f0 + f1;
         } else {
@@ -369,9 +383,9 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
     static_assert(kProducts % (kAhead + 1) == 0, "a step begins where the one before left the ring of operands");
     v8bf f[kAhead + 1];
     auto step = [&](const v16f& x, const v8bf (&w)[2], v16f& y, v8bf (&now)[2], const char* kt, const char* vt, int sub, int next_at, uint32_t next_there,
-                    bool chained, int tile, int slot) __attribute__((always_inline)) {
+                    bool chained, int tile, int slot, auto&& side) __attribute__((always_inline)) {
       float sum = 0.f, scaled = 0.f, v[2];
-      v4f vs = value_scales(tile, sub ^ 1, 0);                              // (block j, whose weights are worked out, is the other half)
+      const float vs = value_scales(tile, sub ^ 1), ks = key_scales(slot, sub);      // (block j, whose weights are worked out, is the other half)
       v4u packed[2];
 #pragma unroll
       for (int e = 0; e < 16; ++e) y[e] = 0.f;
@@ -398,22 +412,22 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
           if (e & 1) {
             sum += v[0] + v[1];
             if constexpr (kCoded) {
-              v[0] *= vs[(e - 1) & 3];
-              v[1] *= vs[e & 3];
+              v[0] = times_row_lane(v[0], vs, e - 1);
+              v[1] = times_row_lane(v[1], vs, e);
               if (SUMS) scaled += v[0] + v[1];
-              if ((e & 3) == 3 && e < 15) vs = value_scales(tile, sub ^ 1, (e + 1) / 4);
             }
             const uint32_t two = pack_bf16(v[0], v[1]);
             asm volatile("" ::"v"(two), "v"(sum));
             packed[e / 8][e / 2 % 4] = two;
           }
         }
+        side(i);
         __builtin_amdgcn_sched_barrier(0);
       }
       now[0] = __builtin_bit_cast(v8bf, packed[0]);
       now[1] = __builtin_bit_cast(v8bf, packed[1]);
       settle(x, now, sum, tile, sub ^ 1, scaled);
-      scale_logits(y, slot, sub);
+      scale_logits(y, ks);
       mask(y, next_at, next_there);
     };
 
@@ -437,9 +451,14 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
         ask_codes(k1, 1, true, page1);
         ask_codes(values_held, 1, false, page1);
         ask_codes(keys_held, 2, true, page2);
-        put_codes(k0, 0, 0, true);
-        put_codes(v0, 0, 0, false);
-        put_codes(k1, 1, 1, true);
+#pragma unroll
+        for (int n = 0; n < kPuts; ++n) {
+          put_codes(k0, 0, true, n);
+          put_codes(v0, 0, false, n);
+          put_codes(k1, 1, true, n);
+        }
+        put_scales(k0, 0, 0);
+        put_scales(k1, 1, 1);
         arrived();
       } else {
         ask(0, 0, kKeys | kValues, run_of(0));
@@ -448,11 +467,11 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
         ask(1, 1, kKeys, run1);
       }
       logits(x0, lds[0][0], 0);
-      scale_logits(x0, 0, 0);
+      scale_logits(x0, key_scales(0, 0));
       mask(x0, tile0, uniform(there_of(0, 0)));
       weights(x0, wa, 0, 0);
       logits(x0, lds[0][0], 1);
-      scale_logits(x0, 0, 1);
+      scale_logits(x0, key_scales(0, 1));
       mask(x0, tile0 + 32, uniform(there_of(0, 1)));
       auto turn = [&](auto even, int t) __attribute__((always_inline)) {
         constexpr int slot = decltype(even)::value ? 0 : 1, next = slot ^ 1;   // (places that the compiler knows: addresses without arithmetic)
@@ -463,23 +482,34 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
         for (int i = 0; i < kAhead; ++i) f[i] = key_of(lds[next][0], 0, i);
         const uint32_t here0 = there_of(next, 0), here1 = there_of(next, 1);
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (kCoded) {
-          put_codes(keys_held, t + 2, slot, true);
-          put_codes(values_held, t + 1, next, false);
-          const int page3 = look_up(t + 3);
-          ask_codes(values_held, t + 2, false, page2);
-          ask_codes(keys_held, t + 3, true, page3);
-          page2 = page3;
-        } else {
+        // codes: the next tiles' are converted and written between the products of the first step, more asked for between those of the second
+        auto put_next = [&](int i) __attribute__((always_inline)) {
+          if constexpr (kCoded) {
+            constexpr int kEach = kProducts / (2 * kPuts);
+            const int n = i / kEach;
+            if (i % kEach == 0) put_codes(n < kPuts ? keys_held : values_held, n < kPuts ? slot : next, n < kPuts, n % kPuts);
+            if (i == 1) put_scales(keys_held, t + 2, slot);
+          }
+        };
+        auto ask_next = [&](int i) __attribute__((always_inline)) {
+          if constexpr (kCoded) {
+            if (i == 0) ask_codes(values_held, t + 2, false, page2);
+            if (i == kProducts / 4) {
+              page2 = look_up(t + 3);
+              ask_codes(keys_held, t + 3, true, page2);
+            }
+          }
+        };
+        if constexpr (!kCoded) {
           const int64_t run2 = run_of(t + 2);
           ask(t + 1, next, kValues, run1);
           ask(t + 2, slot, kKeys, run2);
           run1 = run2;
         }
         const uint32_t there0 = uniform(here0), there1 = uniform(here1);
-        step(x0, wa, x1, wb, lds[next][0], lds[slot][1], 0, at, there0, true, t, next);
+        step(x0, wa, x1, wb, lds[next][0], lds[slot][1], 0, at, there0, true, t, next, put_next);
         // (its first operands: read at the end of the step before)
-        step(x1, wb, x0, wa, lds[next][0], lds[slot][1], 1, at + 32, there1, false, t + 1, next);
+        step(x1, wb, x0, wa, lds[next][0], lds[slot][1], 1, at + 32, there1, false, t + 1, next, ask_next);
       };
       for (int t = 0; t + 1 < tiles; t += 2) {
         turn(std::true_type{}, t);
