@@ -164,13 +164,14 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
       }
       return __builtin_amdgcn_readlane(ids, tile & 63);
     };
-    // Codes: the wave's 16 rows of a tile, kHeld pieces of 16 codes a lane; with keys the scales of both of row lane & 15.
+    // Codes: the wave's 16 rows of a tile, kHeld pieces of 16 codes a lane; with keys the scales of both, lanes 0 .. 15 those of the keys, the next 16 those of the values.
     constexpr int kCodePieces = D / 16, kHeld = 16 * kCodePieces / 64;
     struct Held {
       v4u c[kHeld];
-      float ks, vs;
+      float scale;
       uint32_t there;
     } keys_held, values_held;
+    const float* scales = lane & 16 ? A.V_scales : A.K_scales;
     // where the wave's 16 rows of a tile begin, if they are all there and in one page (else -1)
     auto run_of = [&](int tile) __attribute__((always_inline)) -> int64_t {
       const int page_id = look_up(tile), tw = tile0 + tile * kTile + 16 * wave;
@@ -181,16 +182,13 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
     auto ask_codes = [&](Held& H, int tile, bool keys, int page) __attribute__((always_inline)) {
       const int tw = tile0 + tile * kTile + 16 * wave, row = lane / kCodePieces, piece = lane % kCodePieces;
       const Row* X = keys ? Kh : Vh;
-      const int64_t scales = hkv * A.codes.head;
       if (BANDED && page >= 0 && page < P.n_pages) {
         const int at = tw - page_of(P.div, tw) * P.div.page;
         const Row* x = X + page * P.page_stride + (int64_t)at * P.row_stride;
 #pragma unroll
         for (int k = 0; k < kHeld; ++k) H.c[k] = *reinterpret_cast<const v4u*>(x + (64 / kCodePieces * k + row) * (uint32_t)P.row_stride + 16 * piece);
         if (keys) {
-          const int64_t s = page * A.codes.page + scales + ((at + (lane & 15)) >> A.codes.shift);
-          H.ks = A.K_scales[s];
-          H.vs = A.V_scales[s];
+          H.scale = scales[page * A.codes.page + hkv * A.codes.head + ((at + (lane & 15)) >> A.codes.shift)];
           H.there = 0xFFFFu;
         }
         return;
@@ -211,27 +209,30 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
       if (keys) {
         // (a token that is not there: a scale that leaves a logit of -inf, and a weight of 0)
         const bool there = place(tw + (lane & 15), id, at);
-        const int64_t s = id * A.codes.page + scales + (at >> A.codes.shift);
-        H.ks = there ? A.K_scales[s] : 1.f;
-        H.vs = there ? A.V_scales[s] : 0.f;
+        H.scale = lane & 16 ? 0.f : 1.f;
+        if (there) H.scale = scales[id * A.codes.page + hkv * A.codes.head + (at >> A.codes.shift)];
         H.there = (uint32_t)__ballot(there) & 0xFFFFu;
       }
     };
-    // codes as bf16 numbers to the wave's place in a tile: half n & 1 of piece n / 2 of kHeld
-    constexpr int kPuts = 2 * kHeld;
+    // Codes as bf16 numbers to the wave's place in a tile: half n & 1 of piece n / 2 of kHeld.  Row and piece change the place's bits by themselves, so one address serves
+    // all (eight of them, kept through the loop, are registers that are not there: the compiler must not see that they do not change).
+    constexpr int kPuts = 2 * kHeld, kRowStep = 64 / kCodePieces;
+    const int put_row = lane / kCodePieces;
+    const int key_put = (16 * wave + put_row) * kRowB + (((2 * (lane % kCodePieces)) ^ key_swap(put_row)) << 4);
+    const int value_put = (16 * wave + put_row) * kRowB + (((2 * (lane % kCodePieces)) ^ value_swap(put_row)) << 4);
     auto put_codes = [&](const Held& H, int slot, bool keys, int n) __attribute__((always_inline)) {
       if constexpr (kCoded) {
-        const int row = 64 / kCodePieces * (n / 2) + lane / kCodePieces, piece = 2 * (lane % kCodePieces) + (n & 1);
-        *reinterpret_cast<v8bf*>(lds[slot][keys ? 0 : 1] + (16 * wave + row) * kRowB + ((piece ^ (keys ? key_swap(row) : value_swap(row))) << 4)) =
+        int at = keys ? key_put : value_put;
+        asm volatile("" : "+v"(at));
+        const int swap = keys ? key_swap(kRowStep * (n / 2)) : value_swap(kRowStep * (n / 2));
+        *reinterpret_cast<v8bf*>(lds[slot][keys ? 0 : 1] + ((at ^ (((n & 1) ^ swap) << 4)) + kRowStep * (n / 2) * kRowB)) =
             operand<CacheOf<T>::kCode>(H.c[n / 2][2 * (n & 1)], H.c[n / 2][2 * (n & 1) + 1]);
       }
     };
     auto put_scales = [&](const Held& H, int tile, int slot) __attribute__((always_inline)) {
       if constexpr (kCoded) {
-        if (lane < 16) {
-          L.key_scale[slot][16 * wave + lane] = H.ks * P.scale_log2;
-          L.value_scale[tile & 3][16 * wave + lane] = H.vs;
-        }
+        float* to = lane & 16 ? L.value_scale[tile & 3] : L.key_scale[slot];
+        if (lane < 32) to[16 * wave + (lane & 15)] = lane & 16 ? H.scale : H.scale * P.scale_log2;
         if (lane == 0) here[slot][wave] = H.there;
       }
     };
