@@ -50,7 +50,8 @@ __device__ __forceinline__ float scale_for(float top) {
 
 // x / scale as a code; inverse = 1 / scale.  int8: the quotient by the rounded inverse is within 2^-16 of the exact one, so the nearest whole number is
 // found or missed by one, close to a half.  What is left over, x - c scale, is exact in fp32 (an integer below 2^24 of scale's last
-// bit), and says which.  e4m3: the quotient by a power of two is exact, and the conversion rounds to nearest even; no number lies above 448.
+// bit), and says which: no more than half a scale is right, but for the half itself.  e4m3: the quotient by a power of two is exact, and the conversion rounds to
+// nearest even; no number lies above 448.
 __device__ __forceinline__ int int8_code(float x, float scale, float inverse) {
   float c = rintf(x * inverse);
   const float left = fmaf(-c, scale, x), half = 0.5f * scale;
@@ -58,22 +59,38 @@ __device__ __forceinline__ int int8_code(float x, float scale, float inverse) {
   if (fabsf(left) > half || (fabsf(left) == half && odd)) c += left > 0.f ? 1.f : -1.f;
   return fabsf(x) < INFINITY ? (int)c : 0;                                                  // (its row's scale says that it is no number)
 }
+__device__ __forceinline__ uint32_t four_bytes(int a, int b, int c, int d) {
+  return __builtin_amdgcn_perm((uint32_t)__builtin_amdgcn_perm((uint32_t)d, (uint32_t)c, 0x0c0c0400), (uint32_t)__builtin_amdgcn_perm((uint32_t)b, (uint32_t)a, 0x0c0c0400), 0x05040100);
+}
+// eight numbers as codes; fine: all are finite
 template <int CODE>
-__device__ __forceinline__ uint32_t four_codes(const float (&x)[4], float scale, float inverse) {
+__device__ __forceinline__ uint2 eight_codes(const float (&x)[8], float scale, float inverse, bool fine) {
   if constexpr (CODE == kInt8) {
-    uint32_t w = 0;
+    float c[8], left = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w |= (uint32_t)(int8_code(x[i], scale, inverse) & 0xFF) << (8 * i);
-    return w;
+    for (int i = 0; i < 8; ++i) {
+      c[i] = rintf(x[i] * inverse);
+      left = fmaxf(left, fabsf(fmaf(-c[i], scale, x[i])));
+    }
+    if (__builtin_expect(fine && left < 0.5f * scale, 1))
+      return make_uint2(four_bytes((int)c[0], (int)c[1], (int)c[2], (int)c[3]), four_bytes((int)c[4], (int)c[5], (int)c[6], (int)c[7]));
+    int k[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) k[i] = int8_code(x[i], scale, inverse);
+    return make_uint2(four_bytes(k[0], k[1], k[2], k[3]), four_bytes(k[4], k[5], k[6], k[7]));
   } else {
-    // (an infinite quotient has no e4m3 number: NaN, as for a NaN)
-    const float y[4] = {x[0] * inverse, x[1] * inverse, x[2] * inverse, x[3] * inverse};
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+    int w[2] = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (!(fabsf(x[i]) < INFINITY)) w = (w & ~(0xFF << (8 * i))) | (0x7F << (8 * i));
-    return (uint32_t)w;
+    for (int i = 0; i < 2; ++i) {
+      w[i] = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i] * inverse, x[4 * i + 1] * inverse, 0, false);
+      w[i] = __builtin_amdgcn_cvt_pk_fp8_f32(x[4 * i + 2] * inverse, x[4 * i + 3] * inverse, w[i], true);
+    }
+    if (!fine) {                                             // (an infinite quotient has no e4m3 number: NaN, as for a NaN)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (!(fabsf(x[i]) < INFINITY)) w[i >> 2] = (w[i >> 2] & ~(0xFF << (8 * (i & 3)))) | (0x7F << (8 * (i & 3)));
+    }
+    return make_uint2((uint32_t)w[0], (uint32_t)w[1]);
   }
 }
 

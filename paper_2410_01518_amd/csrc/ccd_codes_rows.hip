@@ -18,11 +18,6 @@ __device__ __forceinline__ void store_eight(float* p, const float (&x)[kPer]) {
 __device__ __forceinline__ void store_eight(uint16_t* p, const float (&x)[kPer]) { *reinterpret_cast<v4u*>(p) = store_bits(x, p); }
 
 template <int CODE>
-__device__ __forceinline__ uint2 eight_codes(const float (&x)[kPer], float scale, float inverse) {
-  const float a[4] = {x[0], x[1], x[2], x[3]}, b[4] = {x[4], x[5], x[6], x[7]};
-  return make_uint2(four_codes<CODE>(a, scale, inverse), four_codes<CODE>(b, scale, inverse));
-}
-template <int CODE>
 __device__ __forceinline__ void eight_numbers(uint2 w, float scale, float (&x)[kPer]) {
   float a[4], b[4];
   numbers<CODE>(w.x, a);
@@ -31,124 +26,261 @@ __device__ __forceinline__ void eight_numbers(uint2 w, float scale, float (&x)[k
   for (int i = 0; i < 4; ++i) { x[i] = a[i] * scale; x[4 + i] = b[i] * scale; }
 }
 
-// The rotation of a lane's eight elements of a token: y = c x + s z, z being each one's partner in its pair.
-template <class T>
+// Rotation: y = c x + t z, z being an element's partner in its pair.  Cosines and sines of a token's pairs are worked out once, a pair to a lane, and lie in LDS for all its
+// heads; a lane takes those of its eight elements.
+struct Angle { float c, s; };
+__device__ __forceinline__ Angle angle_of(const Rotary& R, int pair, int position, const uint64_t* __restrict__ turns) {
+  Angle a;
+  cos_sin_of_phase((uint64_t)(uint32_t)position * turns[pair], a.c, a.s);
+  a.c *= R.amplitude;
+  a.s *= R.inverse ? -R.amplitude : R.amplitude;
+  return a;
+}
 struct TurnEight {
-  float c[kPer], s[kPer];
-  __device__ __forceinline__ void angles(const Rotary& R, int e0, int position, const uint64_t* __restrict__ turns) {
+  float c[kPer], t[kPer];
+  __device__ __forceinline__ void take(const Rotary& R, const Angle* lds, int e0) {
     const int pairs = R.rot / 2;
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
       const int e = e0 + j;
-      c[j] = 1.f;
-      s[j] = 0.f;
-      if (e >= R.rot) continue;
-      const bool first = R.half ? e < pairs : (e & 1) == 0;
-      cos_sin_of_phase((uint64_t)(uint32_t)position * turns[R.half ? (first ? e : e - pairs) : e >> 1], c[j], s[j]);
-      c[j] *= R.amplitude;
-      s[j] *= first == (R.inverse == 0) ? -R.amplitude : R.amplitude;
+      const bool turned = e < R.rot, first = R.half ? e < pairs : (e & 1) == 0;
+      const Angle a = lds[!turned ? 0 : R.half ? (first ? e : e - pairs) : e >> 1];
+      c[j] = turned ? a.c : 1.f;
+      t[j] = turned ? (first ? -a.s : a.s) : 0.f;
     }
-  }
-  // row: the head's first element
-  __device__ __forceinline__ void turn(const Rotary& R, const T* row, int e0, float (&x)[kPer]) const {
-    if (e0 >= R.rot) return;
-    float z[kPer];
-    const int pairs = R.rot / 2;
-    if (!R.half) {
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) z[j] = x[j ^ 1];
-    } else if (pairs % kPer == 0) {
-      load_eight(row + (e0 < pairs ? e0 + pairs : e0 - pairs), z);
-    } else {
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) z[j] = e0 + j < R.rot ? load_elem(row + (e0 + j < pairs ? e0 + j + pairs : e0 + j - pairs)) : 0.f;
-    }
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) x[j] = fmaf(z[j], s[j], x[j] * c[j]);
   }
 };
-
-// the largest finite |x|, and whether all are finite
-__device__ __forceinline__ void measure(const float (&x)[kPer], float& top, bool& fine) {
+// the partners of a lane's eight elements: x's neighbours, or (HALF) from the row, by pieces where these are whole
+template <class T>
+__device__ __forceinline__ void load_partners(const Rotary& R, const T* row, int e0, const float (&x)[kPer], float (&z)[kPer]) {
+  const int pairs = R.rot / 2;
+  if (!R.half) {
 #pragma unroll
-  for (int j = 0; j < kPer; ++j) {
-    const float a = fabsf(x[j]);
-    const bool ok = a < INFINITY;
-    top = fmaxf(top, ok ? a : 0.f);
-    fine = fine && ok;
+    for (int j = 0; j < kPer; ++j) z[j] = x[j ^ 1];
+  } else if (pairs % kPer == 0) {
+    load_eight(row + (e0 >= R.rot ? e0 : e0 < pairs ? e0 + pairs : e0 - pairs), z);
+  } else {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) z[j] = load_elem(row + (e0 + j >= R.rot ? e0 + j : e0 + j < pairs ? e0 + j + pairs : e0 + j - pairs));
   }
 }
 
-// A wave per token that begins a block's new rows (scale_rows = 1: per token), keys or values: for four or eight heads at a time the largest element of the
-// rows, then their codes.
-template <class T, int CODE, int D>
-__global__ __launch_bounds__(256) void append_codes_kernel(Paged P, Codes C, Rotary R, bool rope, const T* __restrict__ K_new, const T* __restrict__ V_new,
-                                                           const int32_t* __restrict__ slots, const int32_t* __restrict__ positions,
-                                                           const uint64_t* __restrict__ turns, uint8_t* K, uint8_t* V, float* K_scales, float* V_scales) {
-  constexpr int kLanes = D / kPer, kHeads = 64 / kLanes;
-  const int t = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, e0 = lane % kLanes * kPer;
-  if (t >= P.tokens) return;
-  const bool keys = blockIdx.y == 0, turned = keys && rope;
-  const int rows = 1 << C.shift;
-  const int64_t slots_all = (int64_t)P.div.page * P.n_pages;
-  auto slot_of = [&](int i) { return i < 0 || i >= P.tokens || (rope && positions[i] < 0) || slots[i] >= slots_all ? -1 : slots[i]; };
-  const int slot = slot_of(t);
-  if (slot < 0) return;
-  const int block = slot >> C.shift;
-  int last = t + 1, first = slot;                     // the block's new tokens t .. last - 1, and the lowest of their rows
-  if (rows > 1) {
-    const int before = slot_of(t - 1);
-    if (before >= 0 && before >> C.shift == block) return;
-    for (int next = slot_of(last); next >= 0 && next >> C.shift == block; next = slot_of(++last)) first = next < first ? next : first;
+// the largest |x|, as bits: an infinite value or a NaN is larger than all numbers
+__device__ __forceinline__ uint32_t largest_bits(const float (&x)[kPer], uint32_t top) {
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const uint32_t b = __float_as_uint(x[j]) & 0x7FFFFFFFu;
+    top = top > b ? top : b;
   }
-  const int page = page_of(P.div, slot), at0 = (block << C.shift) - page * P.div.page;       // the block's first row in the page
-  const bool anew = first == block << C.shift;
-  const T* from = keys ? K_new : V_new;
-  uint8_t* to = (keys ? K : V) + page * P.page_stride;
-  float* scales = (keys ? K_scales : V_scales) + page * C.page + (at0 >> C.shift);
-  auto row_of = [&](int i, int h) {
-    const int64_t b = C.new_rows > 0 ? i / C.new_rows : 0, r = C.new_rows > 0 ? i - b * C.new_rows : i;
-    return from + b * C.new_b + r * P.new_t + h * P.new_h;
+  return top;
+}
+constexpr uint32_t kInfiniteBits = 0x7F800000u;
+// ... of those that are finite
+__device__ __forceinline__ uint32_t largest_finite_bits(const float (&x)[kPer], uint32_t top) {
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const uint32_t b = __float_as_uint(x[j]) & 0x7FFFFFFFu;
+    top = b < kInfiniteBits && b > top ? b : top;
+  }
+  return top;
+}
+// over the lanes of a row, which are eight or sixteen side by side
+template <int LANES>
+__device__ __forceinline__ uint32_t row_largest(uint32_t x) {
+  auto with = [&](uint32_t y) { x = x > y ? x : y; };
+  with((uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0xB1, 0xF, 0xF, true));                   // quad_perm 1 0 3 2, 2 3 0 1, row_half_mirror, row_mirror
+  with((uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x4E, 0xF, 0xF, true));
+  with((uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x141, 0xF, 0xF, true));
+  if constexpr (LANES == 16) with((uint32_t)__builtin_amdgcn_mov_dpp((int)x, 0x140, 0xF, 0xF, true));
+  return x;
+}
+
+// the new rows, and where they go
+template <class T>
+struct Append {
+  const T *K_new, *V_new;
+  const int32_t *slots, *positions;
+  const uint64_t* turns;
+  uint8_t *K, *V;
+  float *K_scales, *V_scales;
+};
+template <class T>
+__device__ __forceinline__ int slot_of(const Paged& P, const Append<T>& N, bool rope, int t) {
+  if (t < 0 || t >= P.tokens) return -1;
+  const int s = N.slots[t];
+  return (rope && N.positions[t] < 0) || s >= (int64_t)P.div.page * P.n_pages ? -1 : s;
+}
+template <class T>
+__device__ __forceinline__ const T* new_row(const Paged& P, const Codes& C, const T* X, int t, int h) {
+  const int64_t b = C.new_rows > 0 ? t / C.new_rows : 0, r = C.new_rows > 0 ? t - b * C.new_rows : t;
+  return X + b * C.new_b + r * P.new_t + h * P.new_h;
+}
+
+// A scale per token: a wave per token, four or eight heads side by side, two such sets of keys and of values read before the first is written.
+template <class T, int CODE, int D>
+__global__ __launch_bounds__(256) void append_tokens_kernel(Paged P, Codes C, Rotary R, bool rope, Append<T> N) {
+  constexpr int kLanes = D / kPer, kHeads = 64 / kLanes, kBatch = 2;
+  __shared__ Angle angles[4][64];
+  const int wave = threadIdx.x >> 6, t = blockIdx.x * 4 + wave, lane = threadIdx.x & 63, e0 = lane % kLanes * kPer;
+  if (t >= P.tokens) return;
+  const int slot = slot_of(P, N, rope, t);
+  if (slot < 0) return;
+  const int page = page_of(P.div, slot), at = slot - page * P.div.page;
+  const int64_t to = page * P.page_stride + at * P.row_stride + e0, scale_to = page * C.page + at;
+  const T *K_row = new_row(P, C, N.K_new, t, 0), *V_row = new_row(P, C, N.V_new, t, 0);
+  TurnEight turn;
+  auto put = [&](const float (&x)[kPer], uint8_t* row, float* to_scale) __attribute__((always_inline)) {
+    uint32_t top = row_largest<kLanes>(largest_bits(x, 0));
+    const bool fine = top < kInfiniteBits;
+    if (!fine) top = row_largest<kLanes>(largest_finite_bits(x, 0));
+    const float scale = scale_for<CODE>(__uint_as_float(top));
+    *reinterpret_cast<uint2*>(row) = eight_codes<CODE>(x, scale, 1.f / scale, fine);
+    if (e0 == 0) *to_scale = CODE == kInt8 && !fine ? __uint_as_float(0x7FC00000u) : scale;
   };
-  for (int h0 = 0; h0 < P.Hkv; h0 += kHeads) {
-    const int h = h0 + lane / kLanes;
-    const bool there = h < P.Hkv;
-    float top = 0.f, x[kPer];
-    bool fine = true;
-    TurnEight<T> turn;
-    auto load = [&](int i) {
-      if (!there) return;
-      if (turned) turn.angles(R, e0, positions[i], turns);
-      load_eight(row_of(i, h) + e0, x);
-      if (turned) turn.turn(R, row_of(i, h), e0, x);
-    };
-    for (int i = t; i < last; ++i) {
-      load(i);
-      if (there) measure(x, top, fine);
+  const int own = lane / kLanes;
+  for (int h0 = 0; h0 < P.Hkv; h0 += kBatch * kHeads) {
+    float x[kBatch][kPer], z[kBatch][kPer], y[kBatch][kPer];
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int64_t h = (h0 + u * kHeads + own < P.Hkv ? h0 + u * kHeads + own : 0) * P.new_h;
+      load_eight(K_row + h + e0, x[u]);
+      if (rope) load_partners(R, K_row + h, e0, x[u], z[u]);
+      load_eight(V_row + h + e0, y[u]);
+    }
+    if (rope && h0 == 0) {                                  // (while the rows are on their way)
+      if (lane < R.rot / 2) angles[wave][lane] = angle_of(R, lane, N.positions[t], N.turns);
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      turn.take(R, angles[wave], e0);
     }
 #pragma unroll
-    for (int s = 1; s < kLanes; s <<= 1) {
-      top = fmaxf(top, __shfl_xor(top, s));
-      if (CODE == kInt8) fine = __shfl_xor((int)fine, s) && fine;
-    }
-    if (!there) continue;
-    float scale = scale_for<CODE>(top);
-    const float old = anew ? 0.f : scales[h * C.head];
-    if (!anew) scale = fmaxf(old, scale);
-    const float inverse = 1.f / scale;
-    uint8_t* head = to + h * P.head_stride + e0;
-    if (!anew && scale > old)
-      for (int r = block << C.shift; r < first; ++r) {
-        uint2* p = reinterpret_cast<uint2*>(head + (int64_t)(r - page * P.div.page) * P.row_stride);
-        float y[kPer];
-        eight_numbers<CODE>(*p, old, y);
-        *p = eight_codes<CODE>(y, scale, inverse);
+    for (int u = 0; u < kBatch; ++u) {
+      const int h = h0 + u * kHeads + own;
+      if (h >= P.Hkv) continue;
+      if (rope) {
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) x[u][j] = fmaf(z[u][j], turn.t[j], x[u][j] * turn.c[j]);
       }
-    for (int i = t; i < last; ++i) {
-      if (rows > 1) load(i);
-      *reinterpret_cast<uint2*>(head + (int64_t)(slots[i] - page * P.div.page) * P.row_stride) = eight_codes<CODE>(x, scale, inverse);
+      put(x[u], N.K + to + h * P.head_stride, N.K_scales + scale_to + h * C.head);
+      put(y[u], N.V + to + h * P.head_stride, N.V_scales + scale_to + h * C.head);
     }
-    if (e0 == 0) scales[h * C.head] = CODE == kInt8 && !fine ? __uint_as_float(0x7FC00000u) : scale;
+  }
+}
+
+// A scale per block of 2^shift tokens: a workgroup per `each` tokens, at most 64, takes those that begin a run, tokens of one block side by side, and the run with them.  A
+// wave per head; lanes side by side have a token's row, kKeep times four or eight tokens at a time.  First the run's largest element, then the codes; a run of that many tokens
+// stays in registers in between, longer ones are read twice.
+template <class T, int D>
+__global__ __launch_bounds__(512) void append_blocks_kernel(Paged P, Codes C, Rotary R, bool rope, Append<T> N, int each) {
+  constexpr int kLanes = D / kPer, kTokens = 64 / kLanes, kKeep = 4, kPart = kKeep * kTokens;
+  __shared__ Angle angles[kPart][D / 2];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, e0 = lane % kLanes * kPer, own = lane / kLanes;
+  const bool keys = blockIdx.y == 0, turned = keys && rope;
+  const T* from = keys ? N.K_new : N.V_new;
+  const int t0 = blockIdx.x * each;
+  uint64_t begins;
+  {
+    const int s = lane < each ? slot_of(P, N, rope, t0 + lane) : -1, before = lane < each ? slot_of(P, N, rope, t0 + lane - 1) : -1;
+    begins = __ballot(s >= 0 && (before < 0 || before >> C.shift != s >> C.shift));
+  }
+  for (; begins != 0; begins &= begins - 1) {
+    const int t = t0 + __builtin_ctzll(begins);
+    // the run: tokens t .. t + n - 1, and the lowest of their rows
+    const int slot = N.slots[t], block = slot >> C.shift;
+    int n = 0, first = slot;
+    for (bool more = true; more;) {
+      const int s = slot_of(P, N, rope, t + n + lane);
+      const uint64_t others = ~__ballot(s >= 0 && s >> C.shift == block);
+      const int here = others == 0 ? 64 : __builtin_ctzll(others);
+      int low = lane < here ? s : first;
+#pragma unroll
+      for (int k = 32; k; k >>= 1) { const int y = __shfl_xor(low, k); low = y < low ? y : low; }
+      first = low < first ? low : first;
+      n += here;
+      more = here == 64;
+    }
+    const int page = page_of(P.div, slot), page0 = page * P.div.page, rounds = (P.Hkv + waves - 1) / waves;
+    const bool anew = first == block << C.shift;
+    for (int h0 = 0; h0 < rounds; ++h0) {
+      const bool there = h0 * waves + wave < P.Hkv;
+      const int h = there ? h0 * waves + wave : 0;
+      uint8_t* to = (keys ? N.K : N.V) + page * P.page_stride + h * P.head_stride + e0;
+      float* to_scale = (keys ? N.K_scales : N.V_scales) + page * C.page + h * C.head + (((block << C.shift) - page0) >> C.shift);
+      const float old = anew ? 0.f : *to_scale;
+      float x[kKeep][kPer];
+      int at[kKeep];                                        // row in the page, negative where there is no token
+      // tokens t + part .. of the run
+      auto load = [&](int part) __attribute__((always_inline)) {
+        float z[kKeep][kPer];
+#pragma unroll
+        for (int g = 0; g < kKeep; ++g) {
+          const int i = part + g * kTokens + own;
+          if (g > 0 && part + g * kTokens >= n) break;
+          const T* row = new_row(P, C, from, t + (i < n ? i : 0), h);
+          at[g] = i < n ? N.slots[t + i] - page0 : -1;
+          load_eight(row + e0, x[g]);
+          if (turned) load_partners(R, row, e0, x[g], z[g]);
+        }
+        if (turned) {
+          const int pairs = R.rot / 2, tokens = n - part < kPart ? n - part : kPart;
+          __syncthreads();
+          for (int k = threadIdx.x; k < tokens * pairs; k += blockDim.x)
+            angles[k / pairs][k % pairs] = angle_of(R, k % pairs, N.positions[t + part + k / pairs], N.turns);
+          __syncthreads();
+        }
+#pragma unroll
+        for (int g = 0; g < kKeep; ++g) {
+          if (part + g * kTokens >= n) break;
+          if (turned && at[g] >= 0) {
+            TurnEight turn;
+            turn.take(R, angles[g * kTokens + own], e0);
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) x[g][j] = fmaf(z[g][j], turn.t[j], x[g][j] * turn.c[j]);
+          }
+        }
+      };
+      uint32_t top = 0;
+      bool fine = true;
+      for (int part = 0; part < n; part += kPart) {
+        load(part);
+#pragma unroll
+        for (int g = 0; g < kKeep; ++g) {
+          if (part + g * kTokens >= n) break;
+          if (at[g] < 0) continue;
+          const uint32_t all = largest_bits(x[g], 0);
+          fine = fine && all < kInfiniteBits;
+          top = all < kInfiniteBits ? (all > top ? all : top) : largest_finite_bits(x[g], top);
+        }
+      }
+#pragma unroll
+      for (int k = 32; k; k >>= 1) { const uint32_t y = __shfl_xor(top, k); top = y > top ? y : top; }
+      const float scale = fmaxf(old, scale_for<kE4m3>(__uint_as_float(top))), inverse = 1.f / scale;
+      if (there && !anew && scale > old)
+        for (int r0 = block << C.shift; r0 < first; r0 += kPart) {
+          uint2 w[kKeep];
+#pragma unroll
+          for (int g = 0; g < kKeep; ++g) {
+            const int r = r0 + g * kTokens + own;
+            w[g] = *reinterpret_cast<const uint2*>(to + (int64_t)((r < first ? r : r0) - page0) * P.row_stride);
+          }
+#pragma unroll
+          for (int g = 0; g < kKeep; ++g) {
+            const int r = r0 + g * kTokens + own;
+            float y[kPer];
+            eight_numbers<kE4m3>(w[g], old, y);
+            if (r < first) *reinterpret_cast<uint2*>(to + (int64_t)(r - page0) * P.row_stride) = eight_codes<kE4m3>(y, scale, inverse, false);
+          }
+        }
+      for (int part = 0; part < n; part += kPart) {
+        if (n > kPart) load(part);
+#pragma unroll
+        for (int g = 0; g < kKeep; ++g) {
+          if (part + g * kTokens >= n) break;
+          if (there && at[g] >= 0) *reinterpret_cast<uint2*>(to + at[g] * P.row_stride) = eight_codes<kE4m3>(x[g], scale, inverse, fine);
+        }
+      }
+      if (there && lane == 0) *to_scale = scale;
+    }
   }
 }
 
@@ -186,56 +318,96 @@ __global__ __launch_bounds__(256) void read_codes_kernel(Paged P, Codes C, const
   if (V_out != nullptr) side(V, V_scales, V_out);
 }
 
-// A workgroup per (page, head).  Rows move towards the front: row j comes from keep[j] >= j, so a piece of rows may be written once it has been read, and what later pieces
-// read lies behind it.
-template <int D>
-__global__ __launch_bounds__(256) void compact_codes_kernel(Paged P, Codes C, uint8_t* K, uint8_t* V, float* K_scales, float* V_scales, const int32_t* __restrict__ keep_all,
-                                                            int k, float* novelty) {
-  constexpr int kLanes = D / 16, kRows = 256 / kLanes;
-  const int page = blockIdx.x / P.Hkv, h = blockIdx.x % P.Hkv;
+// A workgroup per (page, head), keys or values, and all of a row or 64 bytes of it.  Rows move towards the front: row j comes from keep[j] >= j, so a piece of rows may be
+// written once all of it has been read, and what later pieces read lies behind it: a piece is read while the one before is written, its indices a piece earlier.
+constexpr int kCompactThreads = 512;
+template <int BYTES>
+__global__ __launch_bounds__(kCompactThreads) void compact_codes_kernel(Paged P, Codes C, uint8_t* K, uint8_t* V, float* K_scales, float* V_scales,
+                                                                        const int32_t* __restrict__ keep_all, int k, float* novelty) {
+  constexpr int kLanes = BYTES / 16, kRows = kCompactThreads / kLanes, kSide = 2, kPiece = kSide * kRows;
+  const int page = blockIdx.x / P.Hkv, h = blockIdx.x % P.Hkv, tid = threadIdx.x, lane = tid % kLanes, row = tid / kLanes, column = blockIdx.y >> 1;
+  const bool keys = (blockIdx.y & 1) == 0, scaled = column == 0 && lane == 0;
   const int32_t* keep = keep_all + (int64_t)blockIdx.x * k;
-  uint8_t* Kh = K + page * P.page_stride + h * P.head_stride;
-  uint8_t* Vh = V + page * P.page_stride + h * P.head_stride;
-  float* ks = K_scales + page * C.page + h * C.head;
-  float* vs = V_scales + page * C.page + h * C.head;
-  float* nov = novelty != nullptr ? novelty + (int64_t)blockIdx.x * P.div.page : nullptr;
-  const int tid = threadIdx.x, e0 = tid % kLanes * 16;
-  for (int j0 = 0; j0 < k; j0 += kRows) {
-    const int j = j0 + tid / kLanes, i = j < k ? keep[j] : -1;
-    const bool moves = i >= 0 && i < P.div.page && i != j;
-    v4u a = {}, b = {};
-    float x = 0.f, y = 0.f, z = 0.f;
-    if (moves) {
-      a = *reinterpret_cast<const v4u*>(Kh + i * P.row_stride + e0);
-      b = *reinterpret_cast<const v4u*>(Vh + i * P.row_stride + e0);
-      if (e0 == 0) { x = ks[i]; y = vs[i]; z = nov != nullptr ? nov[i] : 0.f; }
+  uint8_t* X = (keys ? K : V) + page * P.page_stride + h * P.head_stride + column * BYTES + lane * 16;
+  float* scales = (keys ? K_scales : V_scales) + page * C.page + h * C.head;
+  float* carried = keys && novelty != nullptr ? novelty + (int64_t)blockIdx.x * P.div.page : scales;
+  struct Piece {
+    v4u x[kSide];
+    float s[kSide], n[kSide];
+  } pieces[2];
+  int from[2][kSide];
+  auto index = [&](int (&i)[kSide], int j0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < kSide; ++u) {
+      const int j = j0 + u * kRows + row, found = keep[j < k ? j : k - 1];
+      i[u] = j < k && found >= 0 && found < P.div.page ? found : -1;
     }
-    asm volatile("" ::"v"(a), "v"(b), "v"(x), "v"(y), "v"(z));          // (read, not just asked for)
+  };
+  // (loads are made whether a row moves or not: how many are under way is known then)
+  auto read = [&](Piece& p, const int (&i)[kSide]) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < kSide; ++u) {
+      const int64_t r = i[u] < 0 ? 0 : i[u];
+      p.x[u] = *reinterpret_cast<const v4u*>(X + r * P.row_stride);
+      p.s[u] = scales[r];
+      p.n[u] = carried[r];
+    }
+  };
+  auto write = [&](const Piece& p, const int (&i)[kSide], int j0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < kSide; ++u) asm volatile("" ::"v"(p.x[u]), "v"(p.s[u]), "v"(p.n[u]));          // (read, not just asked for)
     __syncthreads();
-    if (moves) {
-      *reinterpret_cast<v4u*>(Kh + j * P.row_stride + e0) = a;
-      *reinterpret_cast<v4u*>(Vh + j * P.row_stride + e0) = b;
-      if (e0 == 0) {
-        ks[j] = x;
-        vs[j] = y;
-        if (nov != nullptr) nov[j] = z;
+#pragma unroll
+    for (int u = 0; u < kSide; ++u) {
+      const int j = j0 + u * kRows + row;
+      if (i[u] < 0 || i[u] == j) continue;
+      *reinterpret_cast<v4u*>(X + j * P.row_stride) = p.x[u];
+      if (scaled) {
+        scales[j] = p.s[u];
+        if (carried != scales) carried[j] = p.n[u];
       }
     }
+  };
+  index(from[0], 0);
+  read(pieces[0], from[0]);
+  index(from[1], kPiece);
+  for (int j0 = 0; j0 < k; j0 += 2 * kPiece) {
+    read(pieces[1], from[1]);
+    write(pieces[0], from[0], j0);
+    index(from[0], j0 + 2 * kPiece);
+    if (j0 + kPiece >= k) break;
+    read(pieces[0], from[0]);
+    write(pieces[1], from[1], j0 + kPiece);
+    index(from[1], j0 + 3 * kPiece);
   }
 }
 
-template <class T, int CODE>
-static void append_of(const Paged& P, const Codes& C, const Rotary* rope, const void* K_new, const void* V_new, const int32_t* slots, const int32_t* positions,
-                      const uint64_t* turns, void* K, void* V, float* K_scales, float* V_scales, hipStream_t s) {
-  const dim3 wgs((P.tokens + 3) / 4, 2);
-  launch(P.d == 64 ? append_codes_kernel<T, CODE, 64> : append_codes_kernel<T, CODE, 128>, wgs, dim3(256), s, P, C, rope ? *rope : Rotary{}, rope != nullptr,
-         static_cast<const T*>(K_new), static_cast<const T*>(V_new), slots, positions, turns, static_cast<uint8_t*>(K), static_cast<uint8_t*>(V), K_scales, V_scales);
+template <class T>
+static void append_of(const Paged& P, const Codes& C, int code, const Rotary& R, bool rope, const Append<T>& N, hipStream_t s) {
+  if (C.shift == 0) {
+    const dim3 wgs((P.tokens + 3) / 4);
+    if (code == kInt8) launch(P.d == 64 ? append_tokens_kernel<T, kInt8, 64> : append_tokens_kernel<T, kInt8, 128>, wgs, dim3(256), s, P, C, R, rope, N);
+    else               launch(P.d == 64 ? append_tokens_kernel<T, kE4m3, 64> : append_tokens_kernel<T, kE4m3, 128>, wgs, dim3(256), s, P, C, R, rope, N);
+    return;
+  }
+  // (single tokens side by side: a workgroup each; long runs: few that find nothing)
+  int each = P.tokens / 2048;
+  if (each > 1 << C.shift) each = 1 << C.shift;
+  if (each > 64) each = 64;
+  if (each < 1) each = 1;
+  const dim3 wgs((P.tokens + each - 1) / each, 2), block(64 * (P.Hkv < 8 ? P.Hkv : 8));
+  launch(P.d == 64 ? append_blocks_kernel<T, 64> : append_blocks_kernel<T, 128>, wgs, block, s, P, C, R, rope, N, each);
 }
 
 void launch_append_codes(const Paged& P, const Codes& C, int code, int dtype, const Rotary* rope, const void* K_new, const void* V_new, const int32_t* slots,
                          const int32_t* positions, const uint64_t* turns, void* K, void* V, float* K_scales, float* V_scales, hipStream_t s) {
-  auto of = dtype == 0 ? (code == kInt8 ? append_of<float, kInt8> : append_of<float, kE4m3>) : (code == kInt8 ? append_of<uint16_t, kInt8> : append_of<uint16_t, kE4m3>);
-  of(P, C, rope, K_new, V_new, slots, positions, turns, K, V, K_scales, V_scales, s);
+  const Rotary R = rope ? *rope : Rotary{};
+  uint8_t *k = static_cast<uint8_t*>(K), *v = static_cast<uint8_t*>(V);
+  if (dtype == 0)
+    append_of<float>(P, C, code, R, rope != nullptr, {static_cast<const float*>(K_new), static_cast<const float*>(V_new), slots, positions, turns, k, v, K_scales, V_scales}, s);
+  else
+    append_of<uint16_t>(P, C, code, R, rope != nullptr, {static_cast<const uint16_t*>(K_new), static_cast<const uint16_t*>(V_new), slots, positions, turns, k, v, K_scales, V_scales},
+                        s);
 }
 
 template <class T, int CODE>
@@ -251,10 +423,17 @@ void launch_read_codes(const Paged& P, const Codes& C, int code, int dtype, cons
   of(P, C, K, V, K_scales, V_scales, table, q_start, kv_len, K_out, V_out, s);
 }
 
+int attend_compute_units();
+
 void launch_compact_codes(const Paged& P, const Codes& C, void* K, void* V, float* K_scales, float* V_scales, const int32_t* keep, int32_t k, float* novelty,
                           hipStream_t s) {
-  launch(P.d == 64 ? compact_codes_kernel<64> : compact_codes_kernel<128>, dim3((unsigned)(P.n_pages * P.Hkv)), dim3(256), s, P, C, static_cast<uint8_t*>(K),
-         static_cast<uint8_t*>(V), K_scales, V_scales, keep, k, novelty);
+  uint8_t *x = static_cast<uint8_t*>(K), *y = static_cast<uint8_t*>(V);
+  const unsigned units = (unsigned)(P.n_pages * P.Hkv);
+  // (few pots: halves of rows, so that twice as many workgroups share them)
+  if (P.d == 64 || (int64_t)units * 2 < attend_compute_units())
+    launch(compact_codes_kernel<64>, dim3(units, 2 * P.d / 64), dim3(kCompactThreads), s, P, C, x, y, K_scales, V_scales, keep, k, novelty);
+  else
+    launch(compact_codes_kernel<128>, dim3(units, 2), dim3(kCompactThreads), s, P, C, x, y, K_scales, V_scales, keep, k, novelty);
 }
 
 }  // namespace ccd
