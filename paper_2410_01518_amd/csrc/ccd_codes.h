@@ -42,13 +42,23 @@ __device__ __forceinline__ float number(uint8_t c) {
 // smallest power of two is 2^(e - 8) up to m = 1.75, else 2^(e - 7): worked out on the bits, exact.
 template <int CODE>
 __device__ __forceinline__ float scale_for(float top) {
-  if constexpr (CODE == kInt8) return fmaxf(top / 127.f, kLeastScale);
+  if constexpr (CODE == kInt8) {
+    // (a product by the rounded 1 / 127 and one correction: the rounded quotient, for every fp32 number that is not clamped)
+    const float q = top * (1.f / 127.f);
+    return fmaxf(fmaf(fmaf(-q, 127.f, top), 1.f / 127.f, q), kLeastScale);
+  }
   const uint32_t bits = __float_as_uint(top);
   const int e = (int)(bits >> 23) - 8 + ((bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);          // biased
   return __uint_as_float((uint32_t)(e < 7 ? 7 : e) << 23);                                  // (7: 2^-120)
 }
+// 1 / scale: exact for a power of two, 2^-22 of it off at most otherwise
+template <int CODE>
+__device__ __forceinline__ float inverse_scale(float scale) {
+  if constexpr (CODE == kInt8) return __builtin_amdgcn_rcpf(scale);
+  return __uint_as_float(0x7F000000u - __float_as_uint(scale));
+}
 
-// x / scale as a code; inverse = 1 / scale.  int8: the quotient by the rounded inverse is within 2^-16 of the exact one, so the nearest whole number is
+// x / scale as a code; inverse: of inverse_scale.  int8: the quotient by the inverse is within 2^-14 of the exact one, so the nearest whole number is
 // found or missed by one, close to a half.  What is left over, x - c scale, is exact in fp32 (an integer below 2^24 of scale's last
 // bit), and says which: no more than half a scale is right, but for the half itself.  e4m3: the quotient by a power of two is exact, and the conversion rounds to
 // nearest even; no number lies above 448.
@@ -66,14 +76,17 @@ __device__ __forceinline__ uint32_t four_bytes(int a, int b, int c, int d) {
 template <int CODE>
 __device__ __forceinline__ uint2 eight_codes(const float (&x)[8], float scale, float inverse, bool fine) {
   if constexpr (CODE == kInt8) {
+    // (added to 3 2^22 a quotient is rounded to a whole number, whose byte is the sum's last one)
     float c[8], left = 0.f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      c[i] = rintf(x[i] * inverse);
-      left = fmaxf(left, fabsf(fmaf(-c[i], scale, x[i])));
+      c[i] = fmaf(x[i], inverse, 12582912.f);
+      left = fmaxf(left, fabsf(fmaf(12582912.f - c[i], scale, x[i])));
     }
-    if (__builtin_expect(fine && left < 0.5f * scale, 1))
-      return make_uint2(four_bytes((int)c[0], (int)c[1], (int)c[2], (int)c[3]), four_bytes((int)c[4], (int)c[5], (int)c[6], (int)c[7]));
+    if (__builtin_expect(fine && left < 0.5f * scale, 1)) {
+      auto byte = [&](int i) { return (int)__float_as_uint(c[i]); };
+      return make_uint2(four_bytes(byte(0), byte(1), byte(2), byte(3)), four_bytes(byte(4), byte(5), byte(6), byte(7)));
+    }
     int k[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) k[i] = int8_code(x[i], scale, inverse);

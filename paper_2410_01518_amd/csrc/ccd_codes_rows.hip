@@ -118,7 +118,7 @@ __device__ __forceinline__ const T* new_row(const Paged& P, const Codes& C, cons
 
 // A scale per token: a wave per token, four or eight heads side by side, two such sets of keys and of values read before the first is written.
 template <class T, int CODE, int D>
-__global__ __launch_bounds__(256) void append_tokens_kernel(Paged P, Codes C, Rotary R, bool rope, Append<T> N) {
+__global__ __launch_bounds__(256, 4) void append_tokens_kernel(Paged P, Codes C, Rotary R, bool rope, Append<T> N) {
   constexpr int kLanes = D / kPer, kHeads = 64 / kLanes, kBatch = 2;
   __shared__ Angle angles[4][64];
   const int wave = threadIdx.x >> 6, t = blockIdx.x * 4 + wave, lane = threadIdx.x & 63, e0 = lane % kLanes * kPer;
@@ -134,7 +134,7 @@ __global__ __launch_bounds__(256) void append_tokens_kernel(Paged P, Codes C, Ro
     const bool fine = top < kInfiniteBits;
     if (!fine) top = row_largest<kLanes>(largest_finite_bits(x, 0));
     const float scale = scale_for<CODE>(__uint_as_float(top));
-    *reinterpret_cast<uint2*>(row) = eight_codes<CODE>(x, scale, 1.f / scale, fine);
+    *reinterpret_cast<uint2*>(row) = eight_codes<CODE>(x, scale, inverse_scale<CODE>(scale), fine);
     if (e0 == 0) *to_scale = CODE == kInt8 && !fine ? __uint_as_float(0x7FC00000u) : scale;
   };
   const int own = lane / kLanes;
@@ -171,7 +171,7 @@ __global__ __launch_bounds__(256) void append_tokens_kernel(Paged P, Codes C, Ro
 // wave per head; lanes side by side have a token's row, kKeep times four or eight tokens at a time.  First the run's largest element, then the codes; a run of that many tokens
 // stays in registers in between, longer ones are read twice.
 template <class T, int D>
-__global__ __launch_bounds__(512) void append_blocks_kernel(Paged P, Codes C, Rotary R, bool rope, Append<T> N, int each) {
+__global__ __launch_bounds__(512, 4) void append_blocks_kernel(Paged P, Codes C, Rotary R, bool rope, Append<T> N, int each) {
   constexpr int kLanes = D / kPer, kTokens = 64 / kLanes, kKeep = 4, kPart = kKeep * kTokens;
   __shared__ Angle angles[kPart][D / 2];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, e0 = lane % kLanes * kPer, own = lane / kLanes;
@@ -214,10 +214,11 @@ __global__ __launch_bounds__(512) void append_blocks_kernel(Paged P, Codes C, Ro
         float z[kKeep][kPer];
 #pragma unroll
         for (int g = 0; g < kKeep; ++g) {
-          const int i = part + g * kTokens + own;
-          if (g > 0 && part + g * kTokens >= n) break;
-          const T* row = new_row(P, C, from, t + (i < n ? i : 0), h);
-          at[g] = i < n ? N.slots[t + i] - page0 : -1;
+          // (all are read, the last token's row in the place of those behind it: how many loads are under way is known then)
+          const int i = part + g * kTokens + own, ti = t + (i < n ? i : n - 1);
+          const T* row = new_row(P, C, from, ti, h);
+          at[g] = N.slots[ti] - page0;
+          if (i >= n) at[g] = -1;
           load_eight(row + e0, x[g]);
           if (turned) load_partners(R, row, e0, x[g], z[g]);
         }
@@ -230,7 +231,6 @@ __global__ __launch_bounds__(512) void append_blocks_kernel(Paged P, Codes C, Ro
         }
 #pragma unroll
         for (int g = 0; g < kKeep; ++g) {
-          if (part + g * kTokens >= n) break;
           if (turned && at[g] >= 0) {
             TurnEight turn;
             turn.take(R, angles[g * kTokens + own], e0);
@@ -245,7 +245,6 @@ __global__ __launch_bounds__(512) void append_blocks_kernel(Paged P, Codes C, Ro
         load(part);
 #pragma unroll
         for (int g = 0; g < kKeep; ++g) {
-          if (part + g * kTokens >= n) break;
           if (at[g] < 0) continue;
           const uint32_t all = largest_bits(x[g], 0);
           fine = fine && all < kInfiniteBits;
@@ -254,7 +253,7 @@ __global__ __launch_bounds__(512) void append_blocks_kernel(Paged P, Codes C, Ro
       }
 #pragma unroll
       for (int k = 32; k; k >>= 1) { const uint32_t y = __shfl_xor(top, k); top = y > top ? y : top; }
-      const float scale = fmaxf(old, scale_for<kE4m3>(__uint_as_float(top))), inverse = 1.f / scale;
+      const float scale = fmaxf(old, scale_for<kE4m3>(__uint_as_float(top))), inverse = inverse_scale<kE4m3>(scale);
       if (there && !anew && scale > old)
         for (int r0 = block << C.shift; r0 < first; r0 += kPart) {
           uint2 w[kKeep];
@@ -275,7 +274,6 @@ __global__ __launch_bounds__(512) void append_blocks_kernel(Paged P, Codes C, Ro
         if (n > kPart) load(part);
 #pragma unroll
         for (int g = 0; g < kKeep; ++g) {
-          if (part + g * kTokens >= n) break;
           if (there && at[g] >= 0) *reinterpret_cast<uint2*>(to + at[g] * P.row_stride) = eight_codes<kE4m3>(x[g], scale, inverse, fine);
         }
       }
