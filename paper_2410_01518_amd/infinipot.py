@@ -49,7 +49,7 @@ class ccd_paged_t(ctypes.Structure):
     _fields_ += [(n, ctypes.c_int64) for n in
                  ("page_stride", "head_stride", "row_stride", "new_stride_t", "new_stride_h", "q_stride_b", "q_stride_t", "q_stride_h",
                   "o_stride_b", "o_stride_t", "o_stride_h", "lse_stride_b", "lse_stride_t", "lse_stride_h")]
-    _appended = _attended = _read = None   # the geometry, descriptor and tensors, of its last calls (below)
+    _appended = _attended = _read = _compacted = None   # the geometry, descriptor and tensors, of its last calls (below)
 
 
 class ccd_rope_t(ctypes.Structure):
@@ -597,10 +597,6 @@ def _check_cache(paged, codes, K_codes, V_codes, K_scales, V_scales):
         _holds(s, (paged.n_pages, paged.Hkv, paged.page // rows if rows > 0 else 0), (codes.scale_page_stride, codes.scale_head_stride, 1))
 
 
-def _geometry_of(paged, codes, *tensors):
-    return (bytes(paged), bytes(codes)) + tuple(None if t is None else (t.dtype, t.shape, t.stride()) for t in tensors)
-
-
 def _check_append_codes(paged, codes, rope, K_new, V_new, slots, K_codes, V_codes, K_scales, V_scales, positions, turns):
     tokens, Hkv, d = paged.tokens, paged.Hkv, paged.d
     _alike(K_new, V_new)
@@ -622,17 +618,21 @@ def _check_append_codes(paged, codes, rope, K_new, V_new, slots, K_codes, V_code
 
 def ccd_paged_append_codes(paged, codes, K_new, V_new, slots, K_codes, V_codes, K_scales, V_scales, rope=None, positions=None, turns=None, stream=None) -> int:
     """K_new and V_new have the same strides, as have codes and scales of keys and values; with a rope descriptor the keys are embedded at `positions`."""
-    there = (K_new, V_new, slots, K_codes, V_codes, K_scales, V_scales)
+    geometry = (bytes(paged), bytes(codes), K_new.dtype, K_new.shape, K_new.stride(), V_new.dtype, V_new.shape, V_new.stride(), slots.dtype, slots.shape, slots.stride(),
+                K_codes.dtype, K_codes.shape, K_codes.stride(), V_codes.dtype, V_codes.shape, V_codes.stride(), K_scales.dtype, K_scales.shape, K_scales.stride(),
+                V_scales.dtype, V_scales.shape, V_scales.stride())
     if rope is not None:
-        there += (positions, turns)
-    geometry = _geometry_of(paged, codes, *there) + (None if rope is None else bytes(rope),)
+        geometry += (bytes(rope), positions.dtype, positions.shape, positions.stride(), turns.dtype, turns.shape, turns.stride())
     if geometry != paged._appended:
         _check_append_codes(paged, codes, rope, K_new, V_new, slots, K_codes, V_codes, K_scales, V_scales, positions, turns)
         paged._appended = geometry
-    stream = _stream_here(stream, *there)
-    return _check(lib().ccd_paged_append_codes(ctypes.byref(paged), ctypes.byref(codes), None if rope is None else ctypes.byref(rope), K_new.data_ptr(),
-                                               V_new.data_ptr(), slots.data_ptr(), None if rope is None else positions.data_ptr(), None if rope is None else turns.data_ptr(),
-                                               K_codes.data_ptr(), V_codes.data_ptr(), K_scales.data_ptr(), V_scales.data_ptr(), stream))
+    if rope is None:
+        return _check(lib().ccd_paged_append_codes(ctypes.byref(paged), ctypes.byref(codes), None, K_new.data_ptr(), V_new.data_ptr(), slots.data_ptr(), None, None,
+                                                   K_codes.data_ptr(), V_codes.data_ptr(), K_scales.data_ptr(), V_scales.data_ptr(),
+                                                   _stream_here(stream, K_new, V_new, slots, K_codes, V_codes, K_scales, V_scales)))
+    return _check(lib().ccd_paged_append_codes(ctypes.byref(paged), ctypes.byref(codes), ctypes.byref(rope), K_new.data_ptr(), V_new.data_ptr(), slots.data_ptr(),
+                                               positions.data_ptr(), turns.data_ptr(), K_codes.data_ptr(), V_codes.data_ptr(), K_scales.data_ptr(), V_scales.data_ptr(),
+                                               _stream_here(stream, K_new, V_new, slots, K_codes, V_codes, K_scales, V_scales, positions, turns)))
 
 
 def _check_read_codes(paged, codes, K_codes, V_codes, K_scales, V_scales, block_table, q_start, kv_len, K_out, V_out):
@@ -653,14 +653,20 @@ def _check_read_codes(paged, codes, K_codes, V_codes, K_scales, V_scales, block_
 
 def ccd_paged_read_codes(paged, codes, K_codes, V_codes, K_scales, V_scales, block_table, q_start, kv_len, K_out, V_out, stream=None) -> int:
     """block_table [B, table_width], q_start [B + 1], kv_len [B]: int32; K_out or V_out may be None (its codes and scales then, too)."""
-    there = (K_codes, V_codes, K_scales, V_scales, block_table, q_start, kv_len, K_out, V_out)
-    geometry = _geometry_of(paged, codes, *there)
+    geometry = (bytes(paged), bytes(codes), block_table.dtype, block_table.shape, block_table.stride(), q_start.dtype, q_start.shape, q_start.stride(), kv_len.dtype,
+                kv_len.shape, kv_len.stride())
+    there = (block_table, q_start, kv_len)
+    if K_out is not None:
+        geometry += (K_codes.dtype, K_codes.shape, K_codes.stride(), K_scales.dtype, K_scales.shape, K_scales.stride(), K_out.dtype, K_out.shape, K_out.stride())
+        there += (K_codes, K_scales, K_out)
+    if V_out is not None:
+        geometry += (V_codes.dtype, V_codes.shape, V_codes.stride(), V_scales.dtype, V_scales.shape, V_scales.stride(), V_out.dtype, V_out.shape, V_out.stride(), K_out is None)
+        there += (V_codes, V_scales, V_out)
     if geometry != paged._read:
-        _check_read_codes(paged, codes, *there)
+        _check_read_codes(paged, codes, K_codes, V_codes, K_scales, V_scales, block_table, q_start, kv_len, K_out, V_out)
         paged._read = geometry
-    stream = _stream_here(stream, *(t for t in there if t is not None))
     return _check(lib().ccd_paged_read_codes(ctypes.byref(paged), ctypes.byref(codes), _ptr(K_codes), _ptr(V_codes), _ptr(K_scales), _ptr(V_scales), block_table.data_ptr(),
-                                             q_start.data_ptr(), kv_len.data_ptr(), _ptr(K_out), _ptr(V_out), stream))
+                                             q_start.data_ptr(), kv_len.data_ptr(), _ptr(K_out), _ptr(V_out), _stream_here(stream, *there)))
 
 
 def _check_attend_codes(paged, codes, Q, K_codes, V_codes, K_scales, V_scales, block_table, q_start, kv_len, out, lse):
@@ -679,8 +685,13 @@ def _check_attend_codes(paged, codes, Q, K_codes, V_codes, K_scales, V_scales, b
 
 def ccd_paged_attend_codes(paged, codes, Q, K_codes, V_codes, K_scales, V_scales, block_table, q_start, kv_len, out, lse, workspace, stream=None) -> int:
     """block_table [B, table_width], q_start [B + 1], kv_len [B]: int32; lse fp32 or None."""
-    there = (Q, K_codes, V_codes, K_scales, V_scales, block_table, q_start, kv_len, out) + (() if lse is None else (lse,))
-    geometry = _geometry_of(paged, codes, *there)
+    geometry = (bytes(paged), bytes(codes), Q.dtype, Q.shape, Q.stride(), K_codes.dtype, K_codes.shape, K_codes.stride(), V_codes.dtype, V_codes.shape, V_codes.stride(),
+                K_scales.dtype, K_scales.shape, K_scales.stride(), V_scales.dtype, V_scales.shape, V_scales.stride(), block_table.dtype, block_table.shape, block_table.stride(),
+                q_start.dtype, q_start.shape, q_start.stride(), kv_len.dtype, kv_len.shape, kv_len.stride(), out.dtype, out.shape, out.stride())
+    there = (Q, K_codes, V_codes, K_scales, V_scales, block_table, q_start, kv_len, out)
+    if lse is not None:
+        geometry += (lse.dtype, lse.shape, lse.stride())
+        there += (lse,)
     if geometry != paged._attended:
         _check_attend_codes(paged, codes, Q, K_codes, V_codes, K_scales, V_scales, block_table, q_start, kv_len, out, lse)
         paged._attended = geometry
@@ -691,18 +702,26 @@ def ccd_paged_attend_codes(paged, codes, Q, K_codes, V_codes, K_scales, V_scales
                                                stream))
 
 
+def _check_compact_codes(paged, codes, K_codes, V_codes, K_scales, V_scales, keep_idx, novelty):
+    _check_cache(paged, codes, K_codes, V_codes, K_scales, V_scales)
+    _int32(paged.n_pages * paged.Hkv * keep_idx.shape[-1], keep_idx)
+    if novelty is not None and (novelty.dtype is not torch.float32 or not novelty.is_contiguous() or novelty.numel() < paged.n_pages * paged.Hkv * paged.page):
+        raise AssertionError("novelty [n_pages, Hkv, page] fp32, contiguous, needed")
+
+
 def ccd_paged_compact_codes(paged, codes, K_codes, V_codes, K_scales, V_scales, keep_idx, novelty=None, stream=None) -> int:
     """keep_idx int32 [n_pages, Hkv, k], novelty fp32 [n_pages, Hkv, page] or None, both contiguous; in place."""
-    k = keep_idx.shape[-1]
-    _check_cache(paged, codes, K_codes, V_codes, K_scales, V_scales)
-    _int32(paged.n_pages * paged.Hkv * k, keep_idx)
+    geometry = (bytes(paged), bytes(codes), K_codes.dtype, K_codes.shape, K_codes.stride(), V_codes.dtype, V_codes.shape, V_codes.stride(), K_scales.dtype, K_scales.shape,
+                K_scales.stride(), V_scales.dtype, V_scales.shape, V_scales.stride(), keep_idx.dtype, keep_idx.shape, keep_idx.stride())
     there = (K_codes, V_codes, K_scales, V_scales, keep_idx)
     if novelty is not None:
-        if novelty.dtype is not torch.float32 or not novelty.is_contiguous() or novelty.numel() < paged.n_pages * paged.Hkv * paged.page:
-            raise AssertionError("novelty [n_pages, Hkv, page] fp32, contiguous, needed")
+        geometry += (novelty.dtype, novelty.shape, novelty.stride())
         there += (novelty,)
+    if geometry != paged._compacted:
+        _check_compact_codes(paged, codes, K_codes, V_codes, K_scales, V_scales, keep_idx, novelty)
+        paged._compacted = geometry
     return _check(lib().ccd_paged_compact_codes(ctypes.byref(paged), ctypes.byref(codes), K_codes.data_ptr(), V_codes.data_ptr(), K_scales.data_ptr(), V_scales.data_ptr(),
-                                                keep_idx.data_ptr(), k, _ptr(novelty), _stream_here(stream, *there)))
+                                                keep_idx.data_ptr(), keep_idx.shape[-1], _ptr(novelty), _stream_here(stream, *there)))
 
 
 def ccd_profile_enable(on: bool) -> int:

@@ -10,6 +10,10 @@ Only buffer bookkeeping happens here; appending, attention, scoring, selection a
 
 `MemoryPot` is one pot per sequence, all filled alike.  `PagedPots` serves sequences of different lengths from one pool of pages; where a
 page is a whole pot, a sequence's pot is distilled as soon as it is full, whatever the others hold.
+
+Either holds its cache in 8 bits if it is given a type of code (`codes`: torch.int8 or torch.float8_e4m3fn): half of a bf16 pot's memory and of the bytes that
+decoding reads.  Keys and values are quantised as they are appended, attention reads the codes; a distillation reads the keys back into a buffer of its own for their
+scores, and moves codes and scales of what it keeps.
 """
 from __future__ import annotations
 
@@ -26,13 +30,17 @@ class _Kept:
     def __init__(self):
         self.ws, self.rows, self.kv_len, self.held = None, {}, None, None      # rows: (pages, tokens) -> block table, q_start; held: the number in kv_len
 
-    def workspace(self, paged, device):
+    def workspace(self, paged, device, codes=None):
         """A graph that is being captured has one of its own, which nobody frees or uses between its replays."""
         if torch.cuda.is_current_stream_capturing():
-            return ip.alloc_paged_workspace(paged, device)
-        if self.ws is None or self.ws.numel() < ip.ccd_paged_workspace_bytes(paged):
-            self.ws = ip.alloc_paged_workspace(paged, device)
+            return self._new(paged, device, codes)
+        if self.ws is None or self.ws.numel() < (ip.ccd_paged_workspace_bytes(paged) if codes is None else ip.ccd_codes_workspace_bytes(paged, codes)):
+            self.ws = self._new(paged, device, codes)
         return self.ws
+
+    @staticmethod
+    def _new(paged, device, codes):
+        return ip.alloc_paged_workspace(paged, device) if codes is None else ip.alloc_codes_workspace(paged, codes, device)
 
 
 def _kept(by_stream):
@@ -52,13 +60,49 @@ def _geometry(*tensors):
     return [(t.shape, t.stride()) for t in tensors]
 
 
+def _pool(shape, dtype, codes, scale_rows, device):
+    """Keys, values, and over codes their scales (else None): shape [..., tokens, d]."""
+    if codes is None:
+        K = torch.zeros(shape, dtype=dtype, device=device)
+        return K, torch.zeros_like(K), None, None
+    if codes not in ip.CODE_TYPES:
+        raise TypeError(f"unsupported code type {codes}")
+    K = torch.zeros(shape, dtype=torch.uint8, device=device).view(codes)
+    scales = torch.zeros((*shape[:-2], shape[-2] // scale_rows), dtype=torch.float32, device=device)
+    return K, torch.zeros_like(K.view(torch.uint8)).view(codes), scales, torch.zeros_like(scales)
+
+
+def _distil_codes(K, V, K_scales, V_scales, Q_cat, novelty, keep_idx, workspace, *, dtype, n_valid, k, T, pool_w, pool_mode, scores=None, lse=None) -> int:
+    """ccd_compress (ccd_compress_lse with lse) over codes K, V [B, L, Hkv, n_cap, d]: the keys are read back for their scores.  workspace: of ccd_score, or None."""
+    B, L, Hkv, n_cap, d = K.shape
+    if n_valid < n_cap or n_valid <= k:
+        return ip.CCD_NOOP
+    pages, device = B * L, K.device
+    numbers = torch.empty(K.shape, dtype=dtype, device=device)
+    table = torch.arange(pages, dtype=torch.int32, device=device)[:, None]
+    q_start, kv_len = torch.arange(pages + 1, dtype=torch.int32, device=device) * n_cap, torch.full((pages,), n_cap, dtype=torch.int32, device=device)
+    flat = [x.flatten(0, 1) for x in (K, V, K_scales, V_scales)]
+    codes = ip.make_codes(flat[0], flat[2])
+    paged = ip.make_paged(flat[0], tokens=pages * n_cap, dtype=dtype, block_table=table, out=numbers.flatten(0, 1))
+    ip.ccd_paged_read_codes(paged, codes, flat[0], None, flat[2], None, table, q_start, kv_len, numbers.flatten(0, 1), None)
+    shape = ip.make_shape(Q_cat, numbers, novelty, k=k, T=T, pool_w=pool_w, pool_mode=pool_mode, n_valid=n_valid)
+    scores = torch.empty((B, L, Hkv, n_valid), dtype=torch.float32, device=device) if scores is None else scores
+    workspace = ip.alloc_workspace(shape, device) if workspace is None else workspace
+    if lse is None:
+        ip.ccd_score(shape, Q_cat, numbers, novelty, scores, workspace)
+    else:
+        ip.ccd_score_lse(shape, Q_cat, numbers, lse, novelty, scores, workspace)
+    ip.ccd_select(shape, scores, keep_idx)
+    return ip.ccd_paged_compact_codes(paged, codes, *flat, keep_idx, novelty=novelty if novelty is not None and novelty.dim() == 4 else None)
+
+
 class MemoryPot:
     def __init__(self, B, L, Hkv, d, n_cap, k, T, *, dtype=torch.bfloat16, pool_w=7, pool_mode=ip.CCD_POOL_MAX,
-                 device="cuda"):
+                 device="cuda", codes=None):
         self.B, self.L, self.Hkv, self.d, self.n_cap, self.k, self.T = B, L, Hkv, d, n_cap, k, T
         self.pool_w, self.pool_mode = pool_w, pool_mode
-        self.K = torch.zeros((B, L, Hkv, n_cap, d), dtype=dtype, device=device)
-        self.V = torch.zeros_like(self.K)
+        self.dtype, self.codes = dtype, codes
+        self.K, self.V, self.K_scales, self.V_scales = _pool((B, L, Hkv, n_cap, d), dtype, codes, 1, device)
         self.novelty = torch.zeros((B, L, Hkv, n_cap), dtype=torch.float32, device=device)
         self.keep_idx = torch.empty((B, L, Hkv, k), dtype=torch.int32, device=device)
         self.n_valid = 0
@@ -75,18 +119,33 @@ class MemoryPot:
         """K_new, V_new [B, L, Hkv, m, d]; novelty_new [B, m] (one value per token, copied to every head)."""
         m = K_new.shape[3]
         assert m <= self.room, "pot overflow: distill first"
+        if self.codes is not None:
+            return self._append_codes(K_new, V_new, novelty_new, m)
         shape = ip.make_shape(None, self.K, self.novelty, k=1, n_valid=self.n_valid)
         rc = ip.ccd_append(shape, self.K, self.V, self.novelty, K_new, V_new, novelty_new)
         assert rc == ip.CCD_OK, rc
         self.n_valid += m
 
+    def _append_codes(self, K_new, V_new, novelty_new, m):
+        pages = self.B * self.L
+        K, V, Ks, Vs = (x.flatten(0, 1) for x in (self.K, self.V, self.K_scales, self.V_scales))
+        new, values = K_new.reshape(pages, self.Hkv, m, self.d), V_new.reshape(pages, self.Hkv, m, self.d)
+        paged, codes = _described(self._held, "append", _geometry(new), lambda: (
+            ip.make_paged(K, tokens=pages * m, dtype=self.dtype, K_new=new), ip.make_codes(K, Ks, K_new=new)))
+        rows = torch.arange(self.n_valid, self.n_valid + m, dtype=torch.int32, device=K.device)
+        slots = (torch.arange(pages, dtype=torch.int32, device=K.device)[:, None] * self.n_cap + rows).reshape(-1)
+        rc = ip.ccd_paged_append_codes(paged, codes, new, values, slots, K, V, Ks, Vs)
+        assert rc == ip.CCD_OK, rc
+        self.novelty[..., self.n_valid: self.n_valid + m] = novelty_new[:, None, None]
+        self.n_valid += m
+
     def attend(self, Q, *, layer=None, behind=False, window=0, K=None, out=None, lse=None):
         """Attention of m query tokens over the pot: Q [B, L, Hq, m, d], or [B, Hq, m, d] of one layer.  The tokens are the pot's last m (already
         appended: each sees what stands before it and itself) or, with `behind`, stand behind it and see all of it (the catalyst prompt).
-        K: other keys than the stored ones (the embedded ones of CR-RoPE).  Returns (out, lse) like Q and Q without its last axis; the
+        K: other keys than the stored ones (the embedded ones of CR-RoPE; over codes a pair of codes and scales).  Returns (out, lse) like Q and Q without its last axis; the
         catalyst prompt's lse is what `distill` can take."""
-        K = self.K if K is None else K
-        one = layer is not None
+        coded, one = self.codes is not None, layer is not None
+        K, K_scales = (self.K, self.K_scales) if K is None else K if coded else (K, None)
         keys, values = (K[:, layer], self.V[:, layer]) if one else (K.view(-1, *K.shape[2:]), self.V.view(-1, *K.shape[2:]))
         pages, (Hq, m) = keys.shape[0], Q.shape[-3:-1]
         q = Q if one else Q.reshape(-1, *Q.shape[2:])
@@ -95,9 +154,15 @@ class MemoryPot:
         table, q_start, kv_len = self._attn_index(pages, m, Q.device)
         o, s = (out, lse) if one else (out.view(-1, *out.shape[2:]), lse.view(-1, *lse.shape[2:]))
         paged = _described(self._held, "attend", (window, behind, self.n_valid, _geometry(keys, q, o, s)), lambda: ip.make_paged(
-            keys, tokens=pages * m, block_table=table, Q=q, out=o, lse=s, window=window, behind=behind, max_new=m, max_len=max(1, self.n_valid)))
-        ws = _kept(self._attn).workspace(paged, Q.device)
-        rc = ip.ccd_paged_attend(paged, q, keys, values, table, q_start, kv_len, o, s, ws)
+            keys, tokens=pages * m, dtype=self.dtype, block_table=table, Q=q, out=o, lse=s, window=window, behind=behind, max_new=m, max_len=max(1, self.n_valid)))
+        if coded:
+            ks, vs = (K_scales[:, layer], self.V_scales[:, layer]) if one else (K_scales.view(-1, *K_scales.shape[2:]), self.V_scales.view(-1, *K_scales.shape[2:]))
+            codes = _described(self._held, "codes", _geometry(keys, ks), lambda: ip.make_codes(keys, ks))
+            ws = _kept(self._attn).workspace(paged, Q.device, codes)
+            rc = ip.ccd_paged_attend_codes(paged, codes, q, keys, values, ks, vs, table, q_start, kv_len, o, s, ws)
+        else:
+            ws = _kept(self._attn).workspace(paged, Q.device)
+            rc = ip.ccd_paged_attend(paged, q, keys, values, table, q_start, kv_len, o, s, ws)
         assert rc == ip.CCD_OK, rc
         return out, lse
 
@@ -123,6 +188,13 @@ class MemoryPot:
     def distill(self, Q_cat, scores=None, lse=None) -> int:
         """One CCD compression if the pot is full; returns the library's code (CCD_OK or CCD_NOOP).  lse: the catalyst rows' log-sum-exps, as
         `attend` returns them (one pass over the keys instead of two)."""
+        if self.codes is not None:
+            rc = _distil_codes(self.K, self.V, self.K_scales, self.V_scales, Q_cat, self.novelty, self.keep_idx, None, dtype=self.dtype, n_valid=self.n_valid, k=self.k, T=self.T,
+                               pool_w=self.pool_w, pool_mode=self.pool_mode, scores=scores, lse=lse)
+            if rc == ip.CCD_OK:
+                self.n_valid = self.k
+                self.calls += 1
+            return rc
         shape = ip.make_shape(Q_cat, self.K, self.novelty, k=self.k, T=self.T, pool_w=self.pool_w,
                               pool_mode=self.pool_mode, n_valid=self.n_valid)
         if self._ws is None:
@@ -146,12 +218,13 @@ class PagedPots:
     and plans where the new ones go; then, in every layer, `append` writes their keys and values and `attend` lets them attend.  The new
     tokens are numbered sequence after sequence; tensors may have more rows than that, which are left alone.  A pool whose pages
     are as long as the longest sequence is a pool of memory pots: `distill` compresses the pot of one sequence.
+    scale_rows: tokens that share a scale, with codes of torch.float8_e4m3fn (pots to be distilled have a scale per token).
     """
 
-    def __init__(self, sequences, n_pages, page, max_len, step_tokens, L, Hq, Hkv, d, *, dtype=torch.bfloat16, window=0, device="cuda"):
+    def __init__(self, sequences, n_pages, page, max_len, step_tokens, L, Hq, Hkv, d, *, dtype=torch.bfloat16, window=0, device="cuda", codes=None, scale_rows=1):
         self.page, self.L, self.Hq, self.window, self.step_tokens = page, L, Hq, window, step_tokens
-        self.K = torch.zeros((n_pages, L, Hkv, page, d), dtype=dtype, device=device)
-        self.V = torch.zeros_like(self.K)
+        self.dtype, self.codes = dtype, codes
+        self.K, self.V, self.K_scales, self.V_scales = _pool((n_pages, L, Hkv, page, d), dtype, codes, scale_rows, device)
         ints = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=device)            # noqa: E731
         self.table = torch.full((sequences, -(-max_len // page)), -1, dtype=torch.int32, device=device)
         self.free_pages = torch.arange(n_pages, dtype=torch.int32, device=device)
@@ -194,6 +267,13 @@ class PagedPots:
     def append(self, layer, K_new, V_new, rope=None, turns=None) -> None:
         """Keys and values of the step's new tokens, [rows, Hkv, d]; rope and turns (as of rope_turns): the keys are embedded at their positions."""
         rows, K, V = K_new.shape[0], self.K[:, layer], self.V[:, layer]
+        if self.codes is not None:
+            Ks, Vs = self.K_scales[:, layer], self.V_scales[:, layer]
+            paged, codes = _described(self._held, "append", _geometry(K_new), lambda: (ip.make_paged(K, tokens=rows, dtype=self.dtype, K_new=K_new), ip.make_codes(K, Ks)))
+            rc = ip.ccd_paged_append_codes(paged, codes, K_new, V_new, self.slots[:rows], K, V, Ks, Vs, rope=rope, positions=None if rope is None else self.positions[:rows],
+                                           turns=turns)
+            assert rc == ip.CCD_OK, rc
+            return
         paged = _described(self._held, "append", _geometry(K_new), lambda: ip.make_paged(K, tokens=rows, K_new=K_new))
         rc = ip.ccd_paged_append(paged, K_new, V_new, self.slots[:rows], K, V, rope=rope, positions=None if rope is None else self.positions[:rows], turns=turns)
         assert rc == ip.CCD_OK, rc
@@ -204,9 +284,15 @@ class PagedPots:
         lse = torch.empty(Q.shape[:2], dtype=torch.float32, device=Q.device) if lse is None else lse
         K, V = self.K[:, layer], self.V[:, layer]
         paged = _described(self._held, "attend", (self.window, self._most, _geometry(Q, out, lse)), lambda: ip.make_paged(
-            K, tokens=Q.shape[0], block_table=self.table, Q=Q, out=out, lse=lse, window=self.window, max_new=self._most[0], max_len=self._most[1]))
-        ws = _kept(self._attn).workspace(paged, Q.device)
-        rc = ip.ccd_paged_attend(paged, Q, K, V, self.table, self.q_start, self.after, out, lse, ws)
+            K, tokens=Q.shape[0], dtype=self.dtype, block_table=self.table, Q=Q, out=out, lse=lse, window=self.window, max_new=self._most[0], max_len=self._most[1]))
+        if self.codes is not None:
+            Ks, Vs = self.K_scales[:, layer], self.V_scales[:, layer]
+            codes = _described(self._held, "codes", None, lambda: ip.make_codes(K, Ks))
+            ws = _kept(self._attn).workspace(paged, Q.device, codes)
+            rc = ip.ccd_paged_attend_codes(paged, codes, Q, K, V, Ks, Vs, self.table, self.q_start, self.after, out, lse, ws)
+        else:
+            ws = _kept(self._attn).workspace(paged, Q.device)
+            rc = ip.ccd_paged_attend(paged, Q, K, V, self.table, self.q_start, self.after, out, lse, ws)
         assert rc == ip.CCD_OK, rc
         return out, lse
 
@@ -216,11 +302,15 @@ class PagedPots:
         next step."""
         assert self.table.shape[1] == 1, "distillation needs pages that are whole pots"
         K, V = self.K[page_id: page_id + 1], self.V[page_id: page_id + 1]
-        shape = ip.make_shape(Q_cat, K, novelty, k=k, T=T, pool_w=pool_w, pool_mode=pool_mode, n_valid=max(1, self.lengths[b]))
-        if lse is not None:
-            rc = ip.ccd_compress_lse(shape, Q_cat, K, V, lse, novelty, keep_idx, workspace)
+        if self.codes is not None:
+            rc = _distil_codes(K, V, self.K_scales[page_id: page_id + 1], self.V_scales[page_id: page_id + 1], Q_cat, novelty, keep_idx, workspace, dtype=self.dtype,
+                               n_valid=self.lengths[b], k=k, T=T, pool_w=pool_w, pool_mode=pool_mode, lse=lse)
         else:
-            rc = ip.ccd_compress(shape, Q_cat, K, V, novelty, keep_idx, workspace)
+            shape = ip.make_shape(Q_cat, K, novelty, k=k, T=T, pool_w=pool_w, pool_mode=pool_mode, n_valid=max(1, self.lengths[b]))
+            if lse is not None:
+                rc = ip.ccd_compress_lse(shape, Q_cat, K, V, lse, novelty, keep_idx, workspace)
+            else:
+                rc = ip.ccd_compress(shape, Q_cat, K, V, novelty, keep_idx, workspace)
         if rc == ip.CCD_OK:
             self.lengths[b] = k
             self._hints()
