@@ -52,8 +52,10 @@ AttendCuts plan_attend(const Paged& P, int dtype, bool codes, int max_new, int m
     // 500 .. 4096 36.8, 36.8, d 64 19.9, 23.8; 8 of 16384 101, 104; but 32 of 500 .. 4096, two stretches each, 62, 57; fp32, 8 of 2000 .. 8192 76, 66.
     // Many rounds of units are dealt out as they end: 512 of 500 .. 4096, us whole and evenly, 616, 644, of 1 .. 16384 712, 801; but 256 of 500 .. 8192
     // 520, 513, and fp32, 512 of 100 .. 4000, 479, 426.
+    // Codes have half the bytes, and are read at half the rate by a workgroup alone: its tiles take as long.  One sequence of 1000 and of 1500, 32 query heads, d 128: whole 13.6,
+    // 17.3, cut 11.3, 11.4; 16 of 1000 14.8, 32 of 2000 27.6, 256 of 100 .. 512 40 (whole).
     const bool wide = units <= cus && len > 256;
-    const int64_t row = 2 * (int64_t)P.d * (codes ? 1 : dtype == 0 ? 4 : 2), rate = wide ? (dtype == 0 ? 40 : P.d == 64 ? 60 : 65) : (dtype == 0 ? 35 : P.d == 64 ? 32 : 50);
+    const int64_t row = 2 * (int64_t)P.d * (codes ? 1 : dtype == 0 ? 4 : 2), rate = codes ? (wide ? 33 : 25) : wide ? (dtype == 0 ? 40 : P.d == 64 ? 60 : 65) : (dtype == 0 ? 35 : P.d == 64 ? 32 : 50);
     const bool uncut = (len <= 2048 && len * row / rate <= 6000 + units * len * row / 10200) || (dtype != 0 && units >= 16 * cus);
     for (int chunk = uncut ? (int)len : 128; !many && (uncut || chunk <= 2048); chunk *= 2) {
       const int64_t chunks = (len + chunk - 1) / chunk;
