@@ -335,7 +335,7 @@ CCD_API int ccd_paged_attend(const ccd_paged_t* paged, const void* Q, const void
 /* ---- The same cache in 8 bits ---------------------------------------------------------------------------------------
  *
  * K_codes and V_codes [n_pages, Hkv, page, d] hold a byte per element, K_scales and V_scales (fp32) [n_pages, Hkv, page / scale_rows]
- * what a code of 1 stands for: x = code * scale.  Decoding reads half the bytes of a bf16 cache, and a memory pot takes half of the memory.
+ * what a code of 1 stands for, not negative: x = code * scale.  Decoding reads half the bytes of a bf16 cache, and a memory pot takes half of the memory.
  *   CCD_INT8   scale_rows = 1, a scale for every token and head: scale = max(|x| / 127, 2^-120) over the head's d elements, code = x / scale rounded to
  *              nearest, halves to even (of the exact quotient).  A token and head that holds an infinite value or a NaN has a scale of NaN, and reads as NaN.
  *   CCD_E4M3   (four bits of exponent, three of mantissa, the largest number 448, no infinities) a scale for every scale_rows tokens and head: the
@@ -363,7 +363,7 @@ typedef struct {
 } ccd_codes_t;
 
 /* ccd_paged_append into codes; slots, positions, rope and turns as there.  With scale_rows > 1 the new tokens of one block have to stand side by side
- * in the call, in any order, as the plan numbers them.  The rotation is fp32 and not rounded before it is quantised. */
+ * in the call, in any order (the plan numbers them so), and no two calls at once may write to one block.  The rotation is fp32 and not rounded before it is quantised. */
 CCD_API int ccd_paged_append_codes(const ccd_paged_t* paged, const ccd_codes_t* codes, const ccd_rope_t* rope, const void* K_new, const void* V_new,
                            const int32_t* slots, const int32_t* positions, const uint64_t* turns, void* K_codes, void* V_codes,
                            float* K_scales, float* V_scales, void* hip_stream);

@@ -394,6 +394,7 @@ static void append_of(const Paged& P, const Codes& C, int code, const Rotary& R,
   if (each > 1 << C.shift) each = 1 << C.shift;
   if (each > 64) each = 64;
   if (each < 1) each = 1;
+  while ((P.tokens + each - 1) / each > 1 << 21) each *= 2;            // (a launch has less than 2^32 threads; 2^25 tokens at most: each stays below 64)
   const dim3 wgs((P.tokens + each - 1) / each, 2), block(64 * (P.Hkv < 8 ? P.Hkv : 8));
   launch(P.d == 64 ? append_blocks_kernel<T, 64> : append_blocks_kernel<T, 128>, wgs, block, s, P, C, R, rope, N, each);
 }

@@ -202,6 +202,49 @@ def test_blocks_that_grow_token_by_token(rows):
             np.testing.assert_array_equal(_bytes(X), bits)
 
 
+@pytest.mark.parametrize("kind,rows", [("int8", 1), ("e4m3", 8)])
+@pytest.mark.parametrize("layout", [0, 1])
+def test_append_turned_the_other_way_and_longer(kind, rows, layout):
+    """inverse and amplitude of the descriptor; a token without a position is not written."""
+    T, Hkv, d, page, rot = 24, 3, 128, 8, 96
+    new = torch.randn((T, Hkv, d), generator=torch.Generator(device="cuda").manual_seed(3), device="cuda")
+    positions = np.arange(T, dtype=np.int32) * 1000
+    positions[-1] = -1
+    K, V, Ks, Vs = _empty_cache(kind, 3, Hkv, page, d, rows, byte=0)
+    rope = ip.make_rope(new, rot=rot, layout=layout, amplitude=1.5, inverse=True)
+    paged, codes = ip.make_paged(K, tokens=T, dtype=torch.float32, K_new=new), ip.make_codes(K, Ks)
+    ip.ccd_paged_append_codes(paged, codes, new, new, torch.arange(T, dtype=torch.int32, device="cuda"), K, V, Ks, Vs, rope=rope, positions=_dev(positions), turns=ip.rope_turns(rope))
+    torch.cuda.synchronize()
+    x = _f64(new)
+    y = O.rope(x, positions, O.frequencies(rot, 10000.0), half=layout == 0, inverse=True, amplitude=1.5)
+    scales = Ks.cpu().numpy().astype(np.float64)
+    got = C.decode(_bytes(K), scales, kind, rows).transpose(0, 2, 1, 3).reshape(T, Hkv, d)
+    step = np.repeat(scales, rows, axis=2).transpose(0, 2, 1).reshape(T, Hkv, 1)
+    half = step / 2 if kind == "int8" else np.maximum(2.0 ** -4 * np.abs(y), 2.0 ** -10 * step)
+    assert (np.abs(got - y) <= half * (1 + 2.0 ** -20) + 2.0 ** -20 * 1.5 * np.abs(x).max())[:-1].all()
+    assert (_bytes(K)[-1, :, -1] == 0).all() and (_bytes(V)[-1, :, -1] == 0).all()
+
+
+def test_append_of_more_tokens_than_a_workgroup_each():
+    """2^24 tokens in blocks of two (rows of the new tensors overlap): the first, last and some in between."""
+    T, Hkv, d, page = (1 << 24) + 6, 8, 64, 1 << 12
+    n_pages = -(-T // page)
+    flat = torch.randn(((T + Hkv) * d,), generator=torch.Generator(device="cuda").manual_seed(4), device="cuda", dtype=torch.float32).bfloat16()
+    new = flat.as_strided((T, Hkv, d), (d, d, 1))
+    K, V = (torch.zeros((n_pages, Hkv, page, d), dtype=torch.uint8, device="cuda").view(CODE["e4m3"]) for _ in range(2))
+    Ks, Vs = (torch.zeros((n_pages, Hkv, page // 2), device="cuda") for _ in range(2))
+    paged, codes = ip.make_paged(K, tokens=T, dtype=torch.bfloat16, K_new=new), ip.make_codes(K, Ks)
+    assert ip.ccd_paged_append_codes(paged, codes, new, new, torch.arange(T, dtype=torch.int32, device="cuda"), K, V, Ks, Vs) == ip.CCD_OK
+    torch.cuda.synchronize()
+    for t in (0, 2, 12346, (1 << 23) + 4, T - 2):
+        bits, scales = np.zeros((1, Hkv, 2, d), np.uint8), np.zeros((1, Hkv, 1), np.float32)
+        C.append(_f64(new[t: t + 2]), np.arange(2), bits, scales, "e4m3", 2)
+        p, r = t // page, t % page
+        for x, s in ((K, Ks), (V, Vs)):
+            np.testing.assert_array_equal(x.view(torch.uint8)[p, :, r: r + 2].cpu().numpy(), bits[0])
+            np.testing.assert_array_equal(s[p, :, r // 2].cpu().numpy(), scales[0, :, 0])
+
+
 @pytest.mark.parametrize("kind,rows", [("int8", 1), ("e4m3", 4)])
 def test_append_of_a_batch_with_heads_before_tokens(kind, rows):
     """K_new [B, Hkv, m, d] as a memory pot is given its chunks."""
@@ -290,6 +333,7 @@ KINDS = [("int8", 1, 1), ("e4m3", 1, 1), ("e4m3", 4, 4), ("e4m3", 16, 16)]      
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("lens,news,Hkv,d,page,pad", [
     ([1], [1], 1, 64, 16, 0), ([40, 0, 7], [40, 0, 3], 3, 128, 16, 2), ([100, 5, 33], [20, 9, 33], 5, 64, 48, 1), ([700], [650], 8, 128, 64, 0), ([3] * 130, [2] * 130, 2, 64, 16, 3),
+    ([3, 0, 50], [7, 2, 20], 2, 128, 16, 1),                                       # more rows than tokens: 0 in front
 ])
 def test_read(kind, rows, unit, dtype, lens, news, Hkv, d, page, pad):
     p = _paged_problem(len(lens) + d, kind, rows, dtype, lens, news, Hkv, Hkv, d, page, rows_first=d == 64, holes=0.2 if len(lens) == 130 else 0.0)
