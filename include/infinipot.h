@@ -344,7 +344,8 @@ CCD_API int ccd_paged_attend(const ccd_paged_t* paged, const void* Q, const void
  *              NaN has the code of NaN and no part in the scale.
  * Tokens that share a scale are a block: rows scale_rows * j .. scale_rows * (j + 1) - 1 of a page.  A call that writes the first row of a block begins it
  * anew: what the block held is gone.  Otherwise the block's scale is the larger of its own and what the new rows need, and where it grows, the rows before the
- * first new one are rounded again to the new scale (of a power of two: only what falls below 2^-6 of it changes).
+ * first new one are rounded again to the new scale (of a power of two: only what falls below 2^-6 of it changes).  Rows of the block that lie behind the
+ * first new one and are not written by the call count as not yet written.
  *
  *   ccd_paged_append_codes   quantises new keys and values (embedded on the way, if asked for) and writes them to their rows
  *   ccd_paged_read_codes     cached tokens back as numbers: for the scores of a distillation, or to hand a sequence on
@@ -363,7 +364,8 @@ typedef struct {
 } ccd_codes_t;
 
 /* ccd_paged_append into codes; slots, positions, rope and turns as there.  With scale_rows > 1 the new tokens of one block have to stand side by side
- * in the call, in any order (the plan numbers them so), and no two calls at once may write to one block.  The rotation is fp32 and not rounded before it is quantised. */
+ * in the call, in any order (the plan numbers them so), and no two calls at once may write to one block.  The rotation is fp32 and not rounded before it is
+ * quantised. */
 CCD_API int ccd_paged_append_codes(const ccd_paged_t* paged, const ccd_codes_t* codes, const ccd_rope_t* rope, const void* K_new, const void* V_new,
                            const int32_t* slots, const int32_t* positions, const uint64_t* turns, void* K_codes, void* V_codes,
                            float* K_scales, float* V_scales, void* hip_stream);

@@ -11,6 +11,12 @@
 // where a product of 8192^3 reaches 1.2 - 1.3.  The matrix cores are busy 52 % of the cycles and the clock is at 1.9 - 2.0 GHz: what is left is bound by power
 // (removing all bank conflicts and a tenth of the instructions took 20 % of the cycles and 4 % of the time).  Waves of 64 rows, one per SIMD,
 // read LDS half as often and keep 2.4 GHz, but a wave alone cannot cover its own waits: 1010 - 1040 us, and coarser blocks for short calls.
+//
+// Codes are read into registers a tile and a half ahead, become bf16 numbers there, once for the 128 rows, and are written to LDS as bf16 tiles would lie; what follows
+// is the same but for the scales, one multiplication per logit and one per weight, by a lane's of the row (DPP), so that they take no LDS reads: read as
+// 16 bytes a lane they cost 164 us where this is 135.  That makes 2.1 times the vector instructions of a bf16 cache (2048 new tokens in a pot of 4096 ones, 8 KV heads: 38 million, 18), the vector ALUs are
+// busy 49 % of the cycles and the matrix cores 30 %: 135 us, where bf16 takes 108.  The chunk of 2048 over 32768: int8 1151 - 1179 us, e4m3 1079 - 1110, bf16 957 - 985 in
+// the same runs; pages of 100 tokens (no runs of rows to load) 197, bf16 276.
 #pragma once
 #include "ccd_attend_few.h"
 
@@ -238,35 +244,33 @@ __device__ __forceinline__ void attend_rows(const Paged& P, const AttendPlan& pl
     };
     // asks for the wave's 16 rows of a tile
     auto ask = [&](int tile, int slot, int what, int64_t run) __attribute__((always_inline)) {
-      if constexpr (kCoded) {
-        return;
-      } else {
-      if (tile >= tiles) return;
-      const int tw = tile0 + tile * kTile + 16 * wave;
-      const uint32_t kd = lds0 + (slot * 2) * kTileB + 16 * wave * kRowB, vd = kd + kTileB;
-      if (BANDED && run >= 0) {
-        if (what & kKeys) load_run_to_lds<kLoads>(kd, key_run, reinterpret_cast<const char*>(Kh + run) - kRunBack);
-        if (what & kValues) load_run_to_lds<kLoads>(vd, value_run, reinterpret_cast<const char*>(Vh + run) - kRunBack);
-        if ((what & kKeys) && lane == 0) here[slot][wave] = 0xFFFFu;
-        return;
-      }
-      auto row_at = [&](int t) __attribute__((always_inline)) -> int64_t {
-        if (t >= t_end) return -1;
-        const int c = page_of(P.div, t), id = pages[c];
-        return id >= 0 && id < P.n_pages ? id * P.page_stride + (int64_t)(t - c * P.div.page) * P.row_stride : -1;
-      };
-      const uint16_t* zero = reinterpret_cast<const uint16_t*>(g_zero_row);
+      if constexpr (!kCoded) {
+        if (tile >= tiles) return;
+        const int tw = tile0 + tile * kTile + 16 * wave;
+        const uint32_t kd = lds0 + (slot * 2) * kTileB + 16 * wave * kRowB, vd = kd + kTileB;
+        if (BANDED && run >= 0) {
+          if (what & kKeys) load_run_to_lds<kLoads>(kd, key_run, reinterpret_cast<const char*>(Kh + run) - kRunBack);
+          if (what & kValues) load_run_to_lds<kLoads>(vd, value_run, reinterpret_cast<const char*>(Vh + run) - kRunBack);
+          if ((what & kKeys) && lane == 0) here[slot][wave] = 0xFFFFu;
+          return;
+        }
+        auto row_at = [&](int t) __attribute__((always_inline)) -> int64_t {
+          if (t >= t_end) return -1;
+          const int c = page_of(P.div, t), id = pages[c];
+          return id >= 0 && id < P.n_pages ? id * P.page_stride + (int64_t)(t - c * P.div.page) * P.row_stride : -1;
+        };
+        const uint16_t* zero = reinterpret_cast<const uint16_t*>(g_zero_row);
 #pragma unroll
-      for (int k = 0; k < kLoads; ++k) {
-        const int row = kPerLoad * k + load_row;
-        const int64_t at = row_at(tw + row);
-        if (what & kKeys) load_to_lds(kd + k * 1024, (at >= 0 ? Kh + at : zero) + ((place ^ key_swap(row)) << 3));
-        if (what & kValues) load_to_lds(vd + k * 1024, (at >= 0 ? Vh + at : zero) + ((place ^ value_swap(row)) << 3));
-      }
-      if (what & kKeys) {
-        const uint32_t mine = (uint32_t)__ballot(row_at(tw + (lane & 15)) >= 0) & 0xFFFFu;
-        if (lane == 0) here[slot][wave] = mine;
-      }
+        for (int k = 0; k < kLoads; ++k) {
+          const int row = kPerLoad * k + load_row;
+          const int64_t at = row_at(tw + row);
+          if (what & kKeys) load_to_lds(kd + k * 1024, (at >= 0 ? Kh + at : zero) + ((place ^ key_swap(row)) << 3));
+          if (what & kValues) load_to_lds(vd + k * 1024, (at >= 0 ? Vh + at : zero) + ((place ^ value_swap(row)) << 3));
+        }
+        if (what & kKeys) {
+          const uint32_t mine = (uint32_t)__ballot(row_at(tw + (lane & 15)) >= 0) & 0xFFFFu;
+          if (lane == 0) here[slot][wave] = mine;
+        }
       }
     };
 

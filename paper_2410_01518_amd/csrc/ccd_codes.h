@@ -60,15 +60,9 @@ __device__ __forceinline__ float inverse_scale(float scale) {
 
 // x / scale as a code; inverse: of inverse_scale.  int8: the quotient by the inverse is within 2^-14 of the exact one, so the nearest whole number is
 // found or missed by one, close to a half.  What is left over, x - c scale, is exact in fp32 (an integer below 2^24 of scale's last
-// bit), and says which: no more than half a scale is right, but for the half itself.  e4m3: the quotient by a power of two is exact, and the conversion rounds to
+// bit), and says which: less than half a scale is right.  Otherwise (eight_codes) the quotients are taken in 64 bits: 2^-43 off, rounded to 2^-40, so that a half is exactly one,
+// where quotients that are no half are 2^-26 from one (x and scale have 24 bits).  e4m3: the quotient by a power of two is exact, and the conversion rounds to
 // nearest even; no number lies above 448.
-__device__ __forceinline__ int int8_code(float x, float scale, float inverse) {
-  float c = rintf(x * inverse);
-  const float left = fmaf(-c, scale, x), half = 0.5f * scale;
-  const bool odd = ((int)c & 1) != 0;
-  if (fabsf(left) > half || (fabsf(left) == half && odd)) c += left > 0.f ? 1.f : -1.f;
-  return fabsf(x) < INFINITY ? (int)c : 0;                                                  // (its row's scale says that it is no number)
-}
 __device__ __forceinline__ uint32_t four_bytes(int a, int b, int c, int d) {
   return __builtin_amdgcn_perm((uint32_t)__builtin_amdgcn_perm((uint32_t)d, (uint32_t)c, 0x0c0c0400), (uint32_t)__builtin_amdgcn_perm((uint32_t)b, (uint32_t)a, 0x0c0c0400), 0x05040100);
 }
@@ -87,9 +81,17 @@ __device__ __forceinline__ uint2 eight_codes(const float (&x)[8], float scale, f
       auto byte = [&](int i) { return (int)__float_as_uint(c[i]); };
       return make_uint2(four_bytes(byte(0), byte(1), byte(2), byte(3)), four_bytes(byte(4), byte(5), byte(6), byte(7)));
     }
+    // (infinite values and NaN end as 0: their row's scale says that they are no numbers)
+    const double wide = (double)scale;
+    double by = __builtin_amdgcn_rcp(wide);
+    by = fma(fma(-wide, by, 1.0), by, by);
+    by = fma(fma(-wide, by, 1.0), by, by);
     int k[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) k[i] = int8_code(x[i], scale, inverse);
+    for (int i = 0; i < 8; ++i) {
+      const double q = fma((double)x[i], by, 6144.0) - 6144.0;                        // (1.5 2^12, 1.5 2^52: the sum's last bits)
+      k[i] = (int)(uint32_t)__builtin_bit_cast(uint64_t, q + 6755399441055744.0);
+    }
     return make_uint2(four_bytes(k[0], k[1], k[2], k[3]), four_bytes(k[4], k[5], k[6], k[7]));
   } else {
     int w[2] = {0, 0};

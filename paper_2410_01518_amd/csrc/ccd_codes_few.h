@@ -1,10 +1,15 @@
 // Few rows per unit over a cache of codes: the part of ccd_attend_few.h that reads it (included there).
 //
-// As with bf16 caches, waves go their own ways through tiles of the stretch,   Keys and values come from memory into registers
-// as they lie, quads of lanes reading 64 bytes of a row, and go through the wave's piece of LDS as codes: keys come back as rows, values by the
-// transposing read, and codes become bf16 numbers on their way into the matrix instructions, exactly.  A lane looks up one token of the tile, its page and its two
-// scales.  The keys' scale
-// is a factor of the logit, the values' one of the weight.
+// As with bf16 caches a workgroup's waves go their own ways through the tiles of a stretch, each with the heads that share a KV head as the rows of its products, and put
+// their sums together in the end.  A tile is 32 tokens: quads of lanes read 64 bytes of a row, keys into registers and from there into the wave's piece of LDS, values
+// straight into it, the next tile's while this one is worked on.  Keys come back as rows, values by the transposing read (ds_read_b64_tr_b8), and
+// codes become bf16 numbers on their way into the matrix instructions, exactly.  A lane looks up one token of the tile, its page and its two scales.  The keys' scale is a
+// factor of the logit, the values' one of the weight.  fp32 queries and weights are the sum of three bf16 numbers each: three products, and nothing rounded.
+//
+// Bound by the reading of the cache, d bytes and four of scale per token, head and side, and by the waves that are there to wait for it: a tile is half the bytes
+// of a bf16 one.  So values take no registers on their way, and three waves share a SIMD.  Measured, bf16 queries, 32 heads on 8 of 128, int8: one sequence of 131072 tokens
+// 59 - 61 us (4.5 - 4.7 TB/s), 64 of 500 .. 8192 101 us (4.35 TB/s; 115 with values through registers and two waves), 256 of them 323 us (4.8 TB/s; 357 so).  Tiles of 64 tokens spill: 135 us for the 64;
+// tiles asked for two ahead change nothing.
 #pragma once
 
 namespace ccd {
@@ -47,11 +52,11 @@ __device__ __forceinline__ void cut(const float (&x)[8], v8bf (&f)[PARTS]) {
   }
 }
 
-// Part h, row r of a tile (LDS row 16 h + r) is its token kHalves * r + h, so that a lane group's scales lie side by side, and a quad of lanes has row r of all parts.
+// Part h, row r of a tile (LDS row 16 h + r) is its token kHalves r + h, so that a lane group's scales lie side by side, and a quad of lanes has row r of all parts.
 template <class Q, int CODE, int D>
 struct Tile<Coded<Q, CODE>, D> {
   static constexpr int kTokens = 32, kHalves = kTokens / 16, kBlocks = D / 16, kSteps = D / 32;                           // (steps of 32 elements)
-  static constexpr int kPlanes = D / 64, kPlane = kTokens * 64, kLoads = kPlanes * kHalves;                        // LDS has planes of 64 bytes of every row
+  static constexpr int kPlanes = D / 64, kPlane = kTokens * 64, kLoads = kPlanes * kHalves;                               // LDS has planes of 64 bytes of every row
   static constexpr int kParts = sizeof(Q) == 4 ? 3 : 1;                            // bf16 numbers per element of a query, per weight
   static constexpr int kSide = kTokens * D;                                        // bytes of keys, or values
   static constexpr int kLdsBytes = 3 * kSide + 2 * kTokens * 4;                    // keys, values twice, scales
@@ -137,13 +142,14 @@ struct Tile<Coded<Q, CODE>, D> {
     const int at = (lane & 15) >> 1, row = 16 * (at >> 2) + 4 * (lane >> 4) + (at & 3);
 #pragma unroll
     for (int c = 0; c < kBlocks; ++c) {
-        const v2i t = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) v2i*)(lds + (c >> 2) * kPlane + row * 64 + (((c & 3) ^ value_swap(row)) << 4) + (lane & 1) * 8));
-        const v8bf a = operand<CODE>((uint32_t)t[0], (uint32_t)t[1]);
+      const char* piece = lds + (c >> 2) * kPlane + row * 64 + (((c & 3) ^ value_swap(row)) << 4) + (lane & 1) * 8;
+      const v2i t = __builtin_amdgcn_ds_read_tr8_b64_v2i32((__attribute__((address_space(3))) v2i*)piece);
+      const v8bf a = operand<CODE>((uint32_t)t[0], (uint32_t)t[1]);
 #pragma unroll
-        for (int j = 0; j < NQ; ++j)
+      for (int j = 0; j < NQ; ++j)
 #pragma unroll
-          for (int p = kParts - 1; p >= 0; --p) o[j][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[j].w[p], o[j][c], 0, 0, 0);
-      }
+        for (int p = kParts - 1; p >= 0; --p) o[j][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, w[j].w[p], o[j][c], 0, 0, 0);
+    }
   }
   __device__ static int element(int c, int lane, int i) { return 16 * c + 4 * (lane >> 4) + i; }
 };
@@ -217,8 +223,8 @@ __device__ __forceinline__ bool attend_stretch_codes(const Paged& P, const Atten
     for (int c = 0; c < Tl::kBlocks; ++c) o[j][c] = v4f{0.f, 0.f, 0.f, 0.f};
   }
   for (; t0 < t_end; t0 += kStride) {
-    // what was asked for is there (loads into LDS do not arrive in the order they were asked for)
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // what was asked for is there (loads into LDS do not arrive in the order they were asked for), and what the tile before read of LDS has been read
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     // (by lanes, all that have the token)
     const uint64_t there = __ballot(own_there);
     const bool whole = there == ~(uint64_t)0 && t0 + Tl::kTokens - 1 <= pos_min && t0 >= low_max;
@@ -268,22 +274,20 @@ __device__ __forceinline__ bool attend_stretch_codes(const Paged& P, const Atten
         for (int c = 0; c < Tl::kBlocks; ++c) o[j][c] *= keep;
       }
       const float ref = m[j] == -INFINITY ? 0.f : m[j];
-      {
-        float e[8];
+      float e[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const int h = k >> 2, i = k & 3;
-          const float weight = fast_exp2(fmaf(x[j][h][i], P.scale_log2, -ref));
-          l[j] += weight;
-          e[k] = weight * scale_of(sv, h, i);
-          if (!whole) e[k] = weight == 0.f ? 0.f : e[k];    // (the scale of a token that is not seen may be no number)
-          ls[j] += e[k];
-        }
-        cut(e, w[j].w);
-        if constexpr (Tl::kParts == 1) {
+      for (int k = 0; k < 8; ++k) {
+        const int h = k >> 2, i = k & 3;
+        const float weight = fast_exp2(fmaf(x[j][h][i], P.scale_log2, -ref));
+        l[j] += weight;
+        e[k] = weight * scale_of(sv, h, i);
+        if (!whole) e[k] = weight == 0.f ? 0.f : e[k];      // (the scale of a token that is not seen may be no number)
+        ls[j] += e[k];
+      }
+      cut(e, w[j].w);
+      if constexpr (Tl::kParts == 1) {
 #pragma unroll
-          for (int p = 0; p < 4; ++p) lr[j] = add_rounded(w[j].w[0], p, lr[j]);
-        }
+        for (int p = 0; p < 4; ++p) lr[j] = add_rounded(w[j].w[0], p, lr[j]);
       }
     }
     Tl::add_values(o, w, values_lds, lane);

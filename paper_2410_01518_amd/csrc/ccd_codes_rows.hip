@@ -36,33 +36,48 @@ __device__ __forceinline__ Angle angle_of(const Rotary& R, int pair, int positio
   a.s *= R.inverse ? -R.amplitude : R.amplitude;
   return a;
 }
+enum Turned { kNot, kPieces, kAnyhow };
+static Turned turned_how(const Rotary& R, bool rope) { return !rope ? kNot : R.half && R.rot / 2 % kPer == 0 ? kPieces : kAnyhow; }
 struct TurnEight {
   float c[kPer], t[kPer];
+  // kPieces: the pairs are whole pieces of eight, so that all of a lane's elements are first ones, second ones, or not turned, and their angles lie side by side
+  template <Turned MODE>
   __device__ __forceinline__ void take(const Rotary& R, const Angle* lds, int e0) {
     const int pairs = R.rot / 2;
+    if constexpr (MODE == kPieces) {
+      const bool turned = e0 < R.rot, first = e0 < pairs;
+      const float4* from = reinterpret_cast<const float4*>(lds + (!turned ? 0 : first ? e0 : e0 - pairs));
+      const float other = first ? -1.f : 1.f;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int e = e0 + j;
-      const bool turned = e < R.rot, first = R.half ? e < pairs : (e & 1) == 0;
-      const Angle a = lds[!turned ? 0 : R.half ? (first ? e : e - pairs) : e >> 1];
-      c[j] = turned ? a.c : 1.f;
-      t[j] = turned ? (first ? -a.s : a.s) : 0.f;
+      for (int j = 0; j < kPer / 2; ++j) {
+        const float4 a = from[j];
+        c[2 * j] = a.x; c[2 * j + 1] = a.z;
+        t[2 * j] = other * a.y; t[2 * j + 1] = other * a.w;
+      }
+      if (!turned) {
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) { c[j] = 1.f; t[j] = 0.f; }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) {
+        const int e = e0 + j;
+        const bool turned = e < R.rot, first = R.half ? e < pairs : (e & 1) == 0;
+        const Angle a = lds[!turned ? 0 : R.half ? (first ? e : e - pairs) : e >> 1];
+        c[j] = turned ? a.c : 1.f;
+        t[j] = turned ? (first ? -a.s : a.s) : 0.f;
+      }
     }
   }
 };
-// the partners of a lane's eight elements: x's neighbours, or (HALF) from the row, by pieces where these are whole
+// where the partners of a lane's eight elements begin (kPieces)
+__device__ __forceinline__ int partners_at(const Rotary& R, int e0) { return e0 >= R.rot ? e0 : e0 < R.rot / 2 ? e0 + R.rot / 2 : e0 - R.rot / 2; }
+// ... and otherwise, one by one: x's neighbours, or from the row
 template <class T>
 __device__ __forceinline__ void load_partners(const Rotary& R, const T* row, int e0, const float (&x)[kPer], float (&z)[kPer]) {
   const int pairs = R.rot / 2;
-  if (!R.half) {
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) z[j] = x[j ^ 1];
-  } else if (pairs % kPer == 0) {
-    load_eight(row + (e0 >= R.rot ? e0 : e0 < pairs ? e0 + pairs : e0 - pairs), z);
-  } else {
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) z[j] = load_elem(row + (e0 + j >= R.rot ? e0 + j : e0 + j < pairs ? e0 + j + pairs : e0 + j - pairs));
-  }
+  for (int j = 0; j < kPer; ++j) z[j] = R.half ? load_elem(row + (e0 + j >= R.rot ? e0 + j : e0 + j < pairs ? e0 + j + pairs : e0 + j - pairs)) : x[j ^ 1];
 }
 
 // the largest |x|, as bits: an infinite value or a NaN is larger than all numbers
@@ -112,23 +127,56 @@ __device__ __forceinline__ int slot_of(const Paged& P, const Append<T>& N, bool 
 }
 template <class T>
 __device__ __forceinline__ const T* new_row(const Paged& P, const Codes& C, const T* X, int t, int h) {
-  const int64_t b = C.new_rows > 0 ? t / C.new_rows : 0, r = C.new_rows > 0 ? t - b * C.new_rows : t;
+  const int rows = (int)C.new_rows, b = rows > 0 ? t / rows : 0, r = t - b * rows;
   return X + b * C.new_b + r * P.new_t + h * P.new_h;
 }
 
-// A scale per token: a wave per token, four or eight heads side by side, two such sets of keys and of values read before the first is written.
-template <class T, int CODE, int D>
-__global__ __launch_bounds__(256, 4) void append_tokens_kernel(Paged P, Codes C, Rotary R, bool rope, Append<T> N) {
-  constexpr int kLanes = D / kPer, kHeads = 64 / kLanes, kBatch = 2;
-  __shared__ Angle angles[4][64];
-  const int wave = threadIdx.x >> 6, t = blockIdx.x * 4 + wave, lane = threadIdx.x & 63, e0 = lane % kLanes * kPer;
+// A scale per token: a wave per token, four or eight heads at once, and those of the next time are asked for before these are worked on.  Keys and values come as they are
+// and become floats one row after the other: what is alive at once decides how many waves there are to wait for memory (80 registers; with two sets of rows worked on at once,
+// and both ways of finding partners in one kernel, 128).  Measured, 16384 tokens of 8 heads of 128, bf16 to int8: embedded 22.7 us, 20.1 without (4.5 and 5.0 TB/s of the 101 MB
+// read and written, as much as a copy; 30 and 27 before).
+template <class T>
+struct Raw { v4u w[sizeof(T) / 2]; };
+template <class T>
+__device__ __forceinline__ void ask_eight(Raw<T>& r, const T* p) {
+#pragma unroll
+  for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = reinterpret_cast<const v4u*>(p)[i];
+}
+__device__ __forceinline__ void eight_of(const Raw<uint16_t>& r, float (&x)[kPer]) { load_f32(r.w[0], x, static_cast<const uint16_t*>(nullptr)); }
+__device__ __forceinline__ void eight_of(const Raw<float>& r, float (&x)[kPer]) {
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) x[j] = __uint_as_float(r.w[j >> 2][j & 3]);
+}
+
+template <class T, int CODE, int D, Turned MODE>
+__global__ __launch_bounds__(256, 4) void append_tokens_kernel(Paged P, Codes C, Rotary R, Append<T> N) {
+  constexpr int kLanes = D / kPer, kHeads = 64 / kLanes;
+  __shared__ __align__(16) Angle angles[4][64];
+  // (uniform: all that belongs to the token is worked out once a wave)
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), t = blockIdx.x * 4 + wave, lane = threadIdx.x & 63, e0 = lane % kLanes * kPer, own = lane / kLanes;
   if (t >= P.tokens) return;
-  const int slot = slot_of(P, N, rope, t);
+  const T *K_row = new_row(P, C, N.K_new, t, 0), *V_row = new_row(P, C, N.V_new, t, 0);
+  struct Set { Raw<T> k, z, v; };
+  auto ask = [&](Set& s, int h0) __attribute__((always_inline)) {
+    const int64_t h = (h0 + own < P.Hkv ? h0 + own : 0) * P.new_h;
+    ask_eight(s.k, K_row + h + e0);
+    if (MODE == kPieces) ask_eight(s.z, K_row + h + partners_at(R, e0));
+    ask_eight(s.v, V_row + h + e0);
+  };
+  Set a, b;
+  ask(a, 0);
+  if (kHeads < P.Hkv) ask(b, kHeads);
+  const int slot = slot_of(P, N, MODE != kNot, t);
   if (slot < 0) return;
   const int page = page_of(P.div, slot), at = slot - page * P.div.page;
-  const int64_t to = page * P.page_stride + at * P.row_stride + e0, scale_to = page * C.page + at;
-  const T *K_row = new_row(P, C, N.K_new, t, 0), *V_row = new_row(P, C, N.V_new, t, 0);
+  const int64_t to = page * P.page_stride + at * P.row_stride, scale_to = page * C.page + at;
   TurnEight turn;
+  if (MODE != kNot) {
+    if (lane < R.rot / 2) angles[wave][lane] = angle_of(R, lane, N.positions[t], N.turns);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    turn.take<MODE>(R, angles[wave], e0);
+  }
   auto put = [&](const float (&x)[kPer], uint8_t* row, float* to_scale) __attribute__((always_inline)) {
     uint32_t top = row_largest<kLanes>(largest_bits(x, 0));
     const bool fine = top < kInfiniteBits;
@@ -137,50 +185,49 @@ __global__ __launch_bounds__(256, 4) void append_tokens_kernel(Paged P, Codes C,
     *reinterpret_cast<uint2*>(row) = eight_codes<CODE>(x, scale, inverse_scale<CODE>(scale), fine);
     if (e0 == 0) *to_scale = CODE == kInt8 && !fine ? __uint_as_float(0x7FC00000u) : scale;
   };
-  const int own = lane / kLanes;
-  for (int h0 = 0; h0 < P.Hkv; h0 += kBatch * kHeads) {
-    float x[kBatch][kPer], z[kBatch][kPer], y[kBatch][kPer];
+  auto work = [&](const Set& s, int h0) __attribute__((always_inline)) {
+    const int h = h0 + own;
+    if (h >= P.Hkv) return;
+    float x[kPer];
+    eight_of(s.k, x);
+    if (MODE != kNot) {
+      float z[kPer];
+      if (MODE == kPieces) eight_of(s.z, z);
+      else load_partners(R, K_row + h * P.new_h, e0, x, z);
 #pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
-      const int64_t h = (h0 + u * kHeads + own < P.Hkv ? h0 + u * kHeads + own : 0) * P.new_h;
-      load_eight(K_row + h + e0, x[u]);
-      if (rope) load_partners(R, K_row + h, e0, x[u], z[u]);
-      load_eight(V_row + h + e0, y[u]);
+      for (int j = 0; j < kPer; ++j) x[j] = fmaf(z[j], turn.t[j], x[j] * turn.c[j]);
     }
-    if (rope && h0 == 0) {                                  // (while the rows are on their way)
-      if (lane < R.rot / 2) angles[wave][lane] = angle_of(R, lane, N.positions[t], N.turns);
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      turn.take(R, angles[wave], e0);
-    }
-#pragma unroll
-    for (int u = 0; u < kBatch; ++u) {
-      const int h = h0 + u * kHeads + own;
-      if (h >= P.Hkv) continue;
-      if (rope) {
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) x[u][j] = fmaf(z[u][j], turn.t[j], x[u][j] * turn.c[j]);
-      }
-      put(x[u], N.K + to + h * P.head_stride, N.K_scales + scale_to + h * C.head);
-      put(y[u], N.V + to + h * P.head_stride, N.V_scales + scale_to + h * C.head);
-    }
+    put(x, N.K + to + h * P.head_stride + e0, N.K_scales + scale_to + h * C.head);
+    __builtin_amdgcn_sched_barrier(0);
+    eight_of(s.v, x);
+    put(x, N.V + to + h * P.head_stride + e0, N.V_scales + scale_to + h * C.head);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  for (int h0 = 0;;) {
+    work(a, h0);
+    if (h0 + kHeads >= P.Hkv) break;
+    if (h0 + 2 * kHeads < P.Hkv) ask(a, h0 + 2 * kHeads);
+    work(b, h0 + kHeads);
+    h0 += 2 * kHeads;
+    if (h0 >= P.Hkv) break;
+    if (h0 + kHeads < P.Hkv) ask(b, h0 + kHeads);
   }
 }
 
 // A scale per block of 2^shift tokens: a workgroup per `each` tokens, at most 64, takes those that begin a run, tokens of one block side by side, and the run with them.  A
 // wave per head; lanes side by side have a token's row, kKeep times four or eight tokens at a time.  First the run's largest element, then the codes; a run of that many tokens
-// stays in registers in between, longer ones are read twice.
-template <class T, int D>
-__global__ __launch_bounds__(512, 4) void append_blocks_kernel(Paged P, Codes C, Rotary R, bool rope, Append<T> N, int each) {
+// stays in registers in between, longer ones are read twice.  Measured, 16384 tokens of 8 heads of 128, bf16: blocks of 16 25 us (4.0 TB/s), embedded 35; of 64, read twice, 36.
+template <class T, int D, Turned MODE>
+__global__ __launch_bounds__(512, 4) void append_blocks_kernel(Paged P, Codes C, Rotary R, Append<T> N, int each) {
   constexpr int kLanes = D / kPer, kTokens = 64 / kLanes, kKeep = 4, kPart = kKeep * kTokens;
-  __shared__ Angle angles[kPart][D / 2];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, e0 = lane % kLanes * kPer, own = lane / kLanes;
-  const bool keys = blockIdx.y == 0, turned = keys && rope;
+  __shared__ __align__(16) Angle angles[kPart][D / 2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6, e0 = lane % kLanes * kPer, own = lane / kLanes;
+  const bool keys = blockIdx.y == 0, turned = MODE != kNot && keys;
   const T* from = keys ? N.K_new : N.V_new;
   const int t0 = blockIdx.x * each;
   uint64_t begins;
   {
-    const int s = lane < each ? slot_of(P, N, rope, t0 + lane) : -1, before = lane < each ? slot_of(P, N, rope, t0 + lane - 1) : -1;
+    const int s = lane < each ? slot_of(P, N, MODE != kNot, t0 + lane) : -1, before = lane < each ? slot_of(P, N, MODE != kNot, t0 + lane - 1) : -1;
     begins = __ballot(s >= 0 && (before < 0 || before >> C.shift != s >> C.shift));
   }
   for (; begins != 0; begins &= begins - 1) {
@@ -189,7 +236,7 @@ __global__ __launch_bounds__(512, 4) void append_blocks_kernel(Paged P, Codes C,
     const int slot = N.slots[t], block = slot >> C.shift;
     int n = 0, first = slot;
     for (bool more = true; more;) {
-      const int s = slot_of(P, N, rope, t + n + lane);
+      const int s = slot_of(P, N, MODE != kNot, t + n + lane);
       const uint64_t others = ~__ballot(s >= 0 && s >> C.shift == block);
       const int here = others == 0 ? 64 : __builtin_ctzll(others);
       int low = lane < here ? s : first;
@@ -220,7 +267,8 @@ __global__ __launch_bounds__(512, 4) void append_blocks_kernel(Paged P, Codes C,
           at[g] = N.slots[ti] - page0;
           if (i >= n) at[g] = -1;
           load_eight(row + e0, x[g]);
-          if (turned) load_partners(R, row, e0, x[g], z[g]);
+          if (turned && MODE == kPieces) load_eight(row + partners_at(R, e0), z[g]);
+          else if (turned) load_partners(R, row, e0, x[g], z[g]);
         }
         if (turned) {
           const int pairs = R.rot / 2, tokens = n - part < kPart ? n - part : kPart;
@@ -233,7 +281,7 @@ __global__ __launch_bounds__(512, 4) void append_blocks_kernel(Paged P, Codes C,
         for (int g = 0; g < kKeep; ++g) {
           if (turned && at[g] >= 0) {
             TurnEight turn;
-            turn.take(R, angles[g * kTokens + own], e0);
+            turn.take<MODE>(R, angles[g * kTokens + own], e0);
 #pragma unroll
             for (int j = 0; j < kPer; ++j) x[g][j] = fmaf(z[g][j], turn.t[j], x[g][j] * turn.c[j]);
           }
@@ -282,13 +330,14 @@ __global__ __launch_bounds__(512, 4) void append_blocks_kernel(Paged P, Codes C,
   }
 }
 
-// a wave per row of K_out and V_out
+// A wave per row of K_out and V_out.  The row's sequence, page and place are uniform: scalar loads, one chain a wave.  Bound by memory: 131072 tokens of 8 heads of 128 to bf16, keys alone, 76 us
+// (406 MB, 5.3 TB/s; 83 with the chain in vector registers).
 template <class T, int CODE, int D>
 __global__ __launch_bounds__(256) void read_codes_kernel(Paged P, Codes C, const uint8_t* __restrict__ K, const uint8_t* __restrict__ V, const float* __restrict__ K_scales,
                                                          const float* __restrict__ V_scales, const int32_t* __restrict__ table, const int32_t* __restrict__ q_start,
                                                          const int32_t* __restrict__ kv_len, T* K_out, T* V_out) {
   constexpr int kLanes = D / kPer, kHeads = 64 / kLanes;
-  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63, e0 = lane % kLanes * kPer;
+  const int row = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63, e0 = lane % kLanes * kPer;
   if (row >= P.tokens) return;
   int b = 0;                                                                // sequences that end at or before the row: counted, no chain of loads
   for (int b0 = 1; b0 <= P.B; b0 += 64) b += __popcll(__ballot(b0 + lane <= P.B && q_start[b0 + lane <= P.B ? b0 + lane : P.B] <= row));
@@ -318,6 +367,7 @@ __global__ __launch_bounds__(256) void read_codes_kernel(Paged P, Codes C, const
 
 // A workgroup per (page, head), keys or values, and all of a row or 64 bytes of it.  Rows move towards the front: row j comes from keep[j] >= j, so a piece of rows may be
 // written once all of it has been read, and what later pieces read lies behind it: a piece is read while the one before is written, its indices a piece earlier.
+// Bound by memory: 32 pots of 8 heads, 4096 -> 2048 rows of 128 and novelty, 57 - 61 us for 283 MB, 4.6 - 5.0 TB/s (107 with a piece at a time); one such pot 5.
 constexpr int kCompactThreads = 512;
 template <int BYTES>
 __global__ __launch_bounds__(kCompactThreads) void compact_codes_kernel(Paged P, Codes C, uint8_t* K, uint8_t* V, float* K_scales, float* V_scales,
@@ -380,23 +430,27 @@ __global__ __launch_bounds__(kCompactThreads) void compact_codes_kernel(Paged P,
   }
 }
 
-template <class T>
-static void append_of(const Paged& P, const Codes& C, int code, const Rotary& R, bool rope, const Append<T>& N, hipStream_t s) {
+template <class T, int D, Turned MODE>
+static void append_turned(const Paged& P, const Codes& C, int code, const Rotary& R, const Append<T>& N, hipStream_t s) {
   if (C.shift == 0) {
-    const dim3 wgs((P.tokens + 3) / 4);
-    if (code == kInt8) launch(P.d == 64 ? append_tokens_kernel<T, kInt8, 64> : append_tokens_kernel<T, kInt8, 128>, wgs, dim3(256), s, P, C, R, rope, N);
-    else               launch(P.d == 64 ? append_tokens_kernel<T, kE4m3, 64> : append_tokens_kernel<T, kE4m3, 128>, wgs, dim3(256), s, P, C, R, rope, N);
+    launch(code == kInt8 ? append_tokens_kernel<T, kInt8, D, MODE> : append_tokens_kernel<T, kE4m3, D, MODE>, dim3((P.tokens + 3) / 4), dim3(256), s, P, C, R, N);
     return;
   }
   // Single tokens side by side: a workgroup each; long runs: none that finds nothing to begin.  (16384 tokens of 8 heads without rotation, blocks of 16 and 64, for 2048, 1024, 512, 256
-  // workgroups: 61, 46, 46, 46 us and 126, 75, 49, 50; of four waves instead of eight 54, 42, 42, 42 and 120, 79, 57, 69.)
+  // workgroups: 33, 25, 25, 25 us and 84, 50, 36, 36.  Four waves instead of eight 24 and 33, but a decoding step of 64 sequences 8.3, 6.4 with eight.)
   int each = P.tokens / 512;
   if (each > 1 << C.shift) each = 1 << C.shift;
   if (each > 64) each = 64;
   if (each < 1) each = 1;
   while ((P.tokens + each - 1) / each > 1 << 21) each *= 2;            // (a launch has less than 2^32 threads; 2^25 tokens at most: each stays below 64)
-  const dim3 wgs((P.tokens + each - 1) / each, 2), block(64 * (P.Hkv < 8 ? P.Hkv : 8));
-  launch(P.d == 64 ? append_blocks_kernel<T, 64> : append_blocks_kernel<T, 128>, wgs, block, s, P, C, R, rope, N, each);
+  launch(append_blocks_kernel<T, D, MODE>, dim3((P.tokens + each - 1) / each, 2), dim3(64 * (P.Hkv < 8 ? P.Hkv : 8)), s, P, C, R, N, each);
+}
+template <class T>
+static void append_of(const Paged& P, const Codes& C, int code, const Rotary& R, bool rope, const Append<T>& N, hipStream_t s) {
+  const Turned how = turned_how(R, rope);
+  auto of = P.d == 64 ? (how == kNot ? append_turned<T, 64, kNot> : how == kPieces ? append_turned<T, 64, kPieces> : append_turned<T, 64, kAnyhow>)
+                      : (how == kNot ? append_turned<T, 128, kNot> : how == kPieces ? append_turned<T, 128, kPieces> : append_turned<T, 128, kAnyhow>);
+  of(P, C, code, R, N, s);
 }
 
 void launch_append_codes(const Paged& P, const Codes& C, int code, int dtype, const Rotary* rope, const void* K_new, const void* V_new, const int32_t* slots,
