@@ -157,6 +157,58 @@ def test_append_of_ties_and_borders():
             np.testing.assert_array_equal(_bytes(X), bits)
 
 
+def test_append_of_many_quotients_next_to_halves():
+    """fp32 rows of which every element is (k + 1/2) times the scale, rounded, or next to that: a half is one only where the quotient is one exactly."""
+    rng, T, d = np.random.default_rng(5), 3000, 128
+    top = (rng.random((T, 1)) + 1) * 2.0 ** rng.integers(-60, 60, (T, 1))
+    top = top.astype(np.float32)
+    top[::3] = np.float32(127.0) * np.float32(2.0) ** rng.integers(-30, 30, top[::3].shape).astype(np.float32)       # scales with few bits: halves that are exact
+    scale = (top.astype(np.float64) / 127.0).astype(np.float32).astype(np.float64)
+    x = ((rng.integers(-126, 126, (T, d)) + 0.5) * scale).astype(np.float32)
+    for _ in range(2):
+        move = rng.integers(-1, 2, x.shape)
+        x = np.where(move < 0, np.nextafter(x, np.float32(-np.inf)), np.where(move > 0, np.nextafter(x, np.float32(np.inf)), x))
+    x[:, :1] = top
+    new = _dev(x.reshape(T, 1, d))
+    K, V, Ks, Vs = _empty_cache("int8", T, 1, 1, d, 1)
+    paged, codes = ip.make_paged(K, tokens=T, dtype=torch.float32, K_new=new), ip.make_codes(K, Ks)
+    assert ip.ccd_paged_append_codes(paged, codes, new, -new, torch.arange(T, dtype=torch.int32, device="cuda"), K, V, Ks, Vs) == ip.CCD_OK
+    torch.cuda.synchronize()
+    for sign, X, S in ((1, K, Ks), (-1, V, Vs)):
+        bits, scales = np.zeros((T, 1, 1, d), np.uint8), np.zeros((T, 1, 1), np.float32)
+        C.append(sign * x.reshape(T, 1, d).astype(np.float64), np.arange(T), bits, scales, "int8", 1)
+        np.testing.assert_array_equal(S.cpu().numpy(), scales)
+        np.testing.assert_array_equal(_bytes(X), bits)
+
+
+@pytest.mark.parametrize("kind,rows", [("int8", 1), ("e4m3", 1), ("e4m3", 4)])
+@pytest.mark.parametrize("Hkv,d", [(4, 128), (5, 128), (12, 128), (13, 128), (17, 64), (33, 64)])
+@pytest.mark.parametrize("rot,layout", [(0, 0), (16, 0), (48, 0), (60, 0), (64, 0), (64, 1), (2, 1)])
+def test_append_of_many_heads(kind, rows, Hkv, d, rot, layout):
+    """Every head of a token comes out as it does alone: sets of heads, partners in pieces and one by one."""
+    T, page = 11, 4
+    new = torch.randn((T, 2, Hkv, d), generator=torch.Generator(device="cuda").manual_seed(rot + Hkv), device="cuda").bfloat16()
+    positions, slots = torch.arange(T, dtype=torch.int32, device="cuda") * 777, torch.arange(T, dtype=torch.int32, device="cuda")
+
+    def append(x):
+        cache = _empty_cache(kind, 3, x.shape[2], page, d, rows, byte=0)
+        paged, codes = ip.make_paged(cache[0], tokens=T, dtype=torch.bfloat16, K_new=x[:, 0]), ip.make_codes(cache[0], cache[2])
+        kw = {}
+        if rot:
+            rope = ip.make_rope(x[:, 0], rot=rot, layout=layout)
+            kw = dict(rope=rope, positions=positions, turns=ip.rope_turns(rope))
+        assert ip.ccd_paged_append_codes(paged, codes, x[:, 0], x[:, 1], slots, *cache, **kw) == ip.CCD_OK
+        return cache
+    all_of_them = append(new)
+    for h in range(Hkv):
+        for a, b in zip(all_of_them, append(new[:, :, h: h + 1])):
+            assert torch.equal(a.view(torch.uint8)[:, h], b.view(torch.uint8)[:, 0])
+    x = C.decode(_bytes(all_of_them[1]), all_of_them[3].cpu().numpy().astype(np.float64), kind, rows).transpose(0, 2, 1, 3).reshape(-1, Hkv, d)[:T]
+    step = np.repeat(all_of_them[3].cpu().numpy(), rows, axis=2).transpose(0, 2, 1).reshape(-1, Hkv, 1)[:T].astype(np.float64)
+    y = _f64(new[:, 1])
+    assert (np.abs(x - y) <= (step / 2 if kind == "int8" else np.maximum(2.0 ** -4 * np.abs(y), 2.0 ** -10 * step)) * (1 + 2.0 ** -20)).all()
+
+
 @pytest.mark.parametrize("kind,rows", [("int8", 1), ("e4m3", 1), ("e4m3", 8)])
 def test_append_of_what_is_no_number(kind, rows):
     """Infinities and NaN: int8, the row's scale is NaN; e4m3, the element's code is, and its neighbours and their scale are as without it."""
@@ -660,3 +712,69 @@ def test_compact_leaves_rows_whose_entry_is_outside_the_page():
     ip.ccd_paged_compact_codes(ip.make_paged(K, tokens=0, dtype=torch.bfloat16), ip.make_codes(K, Ks), K, V, Ks, Vs, _dev(keep))
     torch.cuda.synchronize()
     np.testing.assert_array_equal(_bytes(K), want)
+
+
+@pytest.mark.parametrize("kind,rows", [("int8", 1), ("e4m3", 1), ("e4m3", 8)])
+def test_a_captured_step_on_another_stream(kind, rows):
+    """Append, attention, reading back and (where rows have their own scales) compaction in one graph, replayed with other tokens at other places, eager work and synchronisations
+    in between: the same bits as the calls by themselves."""
+    B, Hq, Hkv, d, page, m = 3, 8, 2, 64, 32, 5
+    g0 = torch.Generator(device="cuda").manual_seed(17)
+    rand = lambda *shape: torch.randn(shape, generator=g0, device="cuda").bfloat16()           # noqa: E731
+    table = torch.tensor([[4, 1], [0, 5], [2, 3]], dtype=torch.int32, device="cuda")
+    q_start = torch.arange(B + 1, dtype=torch.int32, device="cuda") * m
+    keep = torch.sort(torch.rand((6, Hkv, page), generator=g0, device="cuda").argsort(-1)[..., :16])[0].int().contiguous()
+    buffers = dict(new=rand(B * m, 2, Hkv, d), Q=rand(B * m, Hq, d), slots=torch.zeros(B * m, dtype=torch.int32, device="cuda"),
+                   positions=torch.zeros(B * m, dtype=torch.int32, device="cuda"), lens=torch.zeros(B, dtype=torch.int32, device="cuda"))
+
+    def state():
+        return _empty_cache(kind, 6, Hkv, page, d, rows, byte=0x11, scale=2.0 ** -6), torch.empty((B * m, Hq, d), dtype=torch.bfloat16, device="cuda"), \
+            torch.empty((B * m, Hq), device="cuda"), torch.empty((B * m, Hkv, d), dtype=torch.bfloat16, device="cuda"), torch.ones((6, Hkv, page), device="cuda")
+
+    def step(b, s, ws, turns, rope):
+        cache, out, lse, back, novelty = s
+        K_new, V_new = b["new"][:, 0], b["new"][:, 1]
+        codes = ip.make_codes(cache[0], cache[2])
+        ip.ccd_paged_append_codes(ip.make_paged(cache[0], tokens=B * m, dtype=torch.bfloat16, K_new=K_new), codes, K_new, V_new, b["slots"], *cache, rope=rope,
+                                  positions=b["positions"], turns=turns)
+        paged = ip.make_paged(cache[0], tokens=B * m, dtype=torch.bfloat16, block_table=table, Q=b["Q"], out=out, lse=lse)
+        ws = ip.alloc_codes_workspace(paged, codes) if ws is None else ws
+        ip.ccd_paged_attend_codes(paged, codes, b["Q"], *cache, table, q_start, b["lens"], out, lse, ws)
+        ip.ccd_paged_read_codes(ip.make_paged(cache[0], tokens=B * m, dtype=torch.bfloat16, block_table=table, out=back), codes, *cache, table, q_start, b["lens"], back, None)
+        if rows == 1:
+            ip.ccd_paged_compact_codes(ip.make_paged(cache[0], tokens=0, dtype=torch.bfloat16), codes, *cache, keep, novelty=novelty)
+        return ws
+
+    def fill(round_no):
+        held = [3 + 5 * round_no, 20 + round_no, 31 + 2 * round_no]
+        tokens = [(b, t) for b in range(B) for t in range(held[b], held[b] + m)]
+        places = table.cpu().numpy()
+        buffers["slots"].copy_(torch.tensor([int(places[b, t // page]) * page + t % page for b, t in tokens], dtype=torch.int32))
+        buffers["positions"].copy_(torch.tensor([t for _, t in tokens], dtype=torch.int32))
+        buffers["lens"].copy_(torch.tensor([n + m for n in held], dtype=torch.int32))
+        buffers["new"].copy_(rand(B * m, 2, Hkv, d) * 2.0 ** round_no)
+        buffers["Q"].copy_(rand(B * m, Hq, d))
+
+    rope = ip.make_rope(buffers["new"][:, 0], rot=32)
+    turns = ip.rope_turns(rope)
+    fill(0)
+    captured, eager = state(), state()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        ws = step(buffers, state(), None, turns, rope)                   # (once outside: allocations and lazy loading)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step(buffers, captured, ws, turns, rope)
+    for round_no in range(4):
+        fill(round_no)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            graph.replay()
+        side.synchronize()
+        step(buffers, eager, None, turns, rope)
+        torch.cuda.synchronize()
+        flat = lambda s: [x.view(torch.uint8) for x in (*s[0], *s[1:])]  # noqa: E731
+        for a, b in zip(flat(captured), flat(eager)):
+            assert torch.equal(a, b)
