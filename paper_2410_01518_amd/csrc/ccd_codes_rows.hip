@@ -271,10 +271,10 @@ __global__ __launch_bounds__(512, 4) void append_blocks_kernel(Paged P, Codes C,
           else if (turned) load_partners(R, row, e0, x[g], z[g]);
         }
         if (turned) {
-          const int pairs = R.rot / 2, tokens = n - part < kPart ? n - part : kPart;
+          const int tokens = n - part < kPart ? n - part : kPart;
           __syncthreads();
-          for (int k = threadIdx.x; k < tokens * pairs; k += blockDim.x)
-            angles[k / pairs][k % pairs] = angle_of(R, k % pairs, N.positions[t + part + k / pairs], N.turns);
+          for (int i = wave; i < tokens; i += waves)
+            if (lane < R.rot / 2) angles[i][lane] = angle_of(R, lane, N.positions[t + part + i], N.turns);
           __syncthreads();
         }
 #pragma unroll
