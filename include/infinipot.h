@@ -383,7 +383,8 @@ CCD_API size_t ccd_codes_workspace_bytes(const ccd_paged_t* paged, const ccd_cod
 
 /* ccd_paged_attend over codes: k_t and v_t are the numbers that the codes stand for.  Keys and values that a row does not see do not reach it, whatever their
  * codes and scales.  Products of codes are exact: codes are bf16 numbers.  With bf16 queries the weights of a tile of tokens, times the scales of
- * the values, are rounded to bf16 for their product with the codes; fp32 queries and weights enter as sums of three bf16 numbers. */
+ * the values, are rounded to bf16 for their product with the codes; fp32 queries and weights enter as sums of three bf16 numbers.  (What a
+ * weight times a scale has below 2^-126 is rounded more coarsely.) */
 CCD_API int ccd_paged_attend_codes(const ccd_paged_t* paged, const ccd_codes_t* codes, const void* Q, const void* K_codes, const void* V_codes,
                            const float* K_scales, const float* V_scales, const int32_t* block_table, const int32_t* q_start, const int32_t* kv_len,
                            void* out, float* lse, void* workspace, size_t workspace_bytes, void* hip_stream);

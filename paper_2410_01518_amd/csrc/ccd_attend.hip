@@ -16,11 +16,14 @@ int attend_compute_units();
 //   rows kernel, d 128, 32 heads of 8 groups, 8192 tokens, for 1, 2, 3, 4 stretches:  512 new tokens 160, 102, 101, 91;  1024: 162, 160, 168, 167;
 //   1536: 213, 235, 250, 237;  64 new tokens, for 4, 8, 16, 32: 52, 35, 29, 33
 //   fp32, 16 heads of 4 groups, 4096 tokens, for 1, 2, 3, 4, 6, 8:  d 64, 256 new tokens 111, 64, 71, 58, 77, 64;  d 128, 300: 167, 174, 128, 139, 140, 133
-static double grid_time(const Paged& P, int by_rows, int64_t units, int64_t len, int64_t parts, int64_t cus) {
-  const double token = by_rows ? (P.d == 64 ? 12 : 20) : (P.d == 64 ? 26 : 40), shared = by_rows || P.d == 64 ? 1.6 : 2.0;
+//   rows kernel over codes (int8; two workgroups on a compute unit stand in each other's way less), d 128, 8192 tokens, for 1, 2, 3, 4 stretches:  512 new tokens 226, 140, 126, 107;
+//   1024: 230, 188, 200, 195;  four of 128 over 4096: 124, 88, 84, 75;  64 new tokens, for 4, 8, 16, 32: 72, 46, 36, 42;  d 64, 512: 167, 104, 94, 77
+static double grid_time(const Paged& P, int by_rows, bool codes, int64_t units, int64_t len, int64_t parts, int64_t cus) {
+  codes = codes && by_rows;
+  const double token = codes ? (P.d == 64 ? 20 : 26.5) : by_rows ? (P.d == 64 ? 12 : 20) : (P.d == 64 ? 26 : 40), shared = codes ? 1.4 : by_rows || P.d == 64 ? 1.6 : 2.0;
   const int64_t wgs = units * parts, rounds = wgs / (2 * cus), rest = wgs % (2 * cus);
   const double last = rest == 0 ? 0 : rest <= cus ? 1 : by_rows && 2 * rest <= 3 * cus ? (1 + 3 * shared) / 4 : shared;
-  const double sums = parts == 1 ? 0 : 8000 + (double)wgs * (by_rows ? 128 : 32) * P.d * 8 / 4000;
+  const double sums = parts == 1 ? 0 : 8000 + (codes ? (double)P.tokens * P.Hq * parts : (double)wgs * (by_rows ? 128 : 32)) * P.d * 8 / 4000;
   return (rounds * shared + last) * ((double)len / parts + 250) * token + sums;
 }
 
@@ -80,7 +83,10 @@ AttendCuts plan_attend(const Paged& P, int dtype, bool codes, int max_new, int m
     const int64_t filled = ((int64_t)P.tokens * P.G + g.rows - 1) / g.rows, of_all = (int64_t)P.B * g.row_blocks;
     const int64_t listed = most_blocks(P.B, P.tokens, P.G, g.rows, g.few);
     if (of_all > listed) g.blocks = (int)listed;
-    const int64_t units = P.Hkv * (filled < 1 ? 1 : filled < of_all ? filled : of_all);
+    // (over codes: as many tokens for every pot, as those of the catalyst prompt, are so many blocks, filled or not.  16 tokens over 32 pots, a block of 64 rows each, 119 us; 127 when taken for
+    // half as many.  Lengths of sequences with several pages differ, and the longest decides: there more, shorter stretches are the safer choice, 17 of 519 .. 8192 201, 243 so)
+    const bool alike = codes && g.by_rows && P.table_width == 1 && P.tokens == (int64_t)P.B * max_new;
+    const int64_t units = P.Hkv * (alike ? of_all : filled < 1 ? 1 : filled < of_all ? filled : of_all);
     if (P.window > 0 && len > (int64_t)P.window + g.rows / P.G + 1) len = (int64_t)P.window + g.rows / P.G + 1;      // of one block
     const int64_t held = most_parts((of_all < listed ? of_all : listed) * P.Hkv, c.even.parts);
     int64_t most = len < 256 * 64 ? (len + 255) / 256 : 64;
@@ -88,7 +94,7 @@ AttendCuts plan_attend(const Paged& P, int dtype, bool codes, int max_new, int m
     int64_t parts = 1;
     double least = 0;
     for (int64_t p = 1; p <= most; ++p) {
-      const double t = grid_time(P, g.by_rows, units, len, p, cus);
+      const double t = grid_time(P, g.by_rows, codes, units, len, p, cus);
       if (p == 1 || t < least) { least = t; parts = p; }
     }
     // Whether the products are put right by the sums of the weights as rounded (add_rounded).  That takes some of the error off at any length, and costs more the longer
