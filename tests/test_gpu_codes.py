@@ -702,6 +702,26 @@ def test_compact(kind, pots, Hkv, page, d, k, novelty):
         np.testing.assert_array_equal(g, w)
 
 
+@pytest.mark.parametrize("pots,Hkv,page,d,k", [(32, 8, 300, 128, 131), (129, 1, 1000, 128, 513), (40, 4, 128, 128, 128), (150, 1, 700, 64, 257)])
+def test_compact_of_many_pots(pots, Hkv, page, d, k):
+    """Whole rows by one workgroup, scales with strides of their own, kept rows side by side and far apart."""
+    rng = np.random.default_rng(k)
+    K, V, Ks, Vs = _random_cache("int8", pots, Hkv, page, d, 1, k)
+    wide = torch.zeros((2, pots, 3, Hkv, page + 5), device="cuda")
+    for w, s in zip(wide, (Ks, Vs)):
+        w[:, 1, :, :page] = s
+    Ks, Vs = (w[:, 1, :, :page] for w in wide)
+    nov = torch.rand((pots, Hkv, page), device="cuda")
+    keep = np.stack([np.sort(rng.permutation(page)[:k]) if u % 3 else np.arange(page - k, page) for u in range(pots * Hkv)]).reshape(pots, Hkv, k).astype(np.int32)
+    want = [C.compact(_bytes(x), keep) for x in (K, V)] + [C.compact(x.cpu().numpy(), keep) for x in (Ks, Vs, nov)]
+    paged = ip.make_paged(K, tokens=0, dtype=torch.bfloat16)
+    assert ip.ccd_paged_compact_codes(paged, ip.make_codes(K, Ks), K, V, Ks, Vs, _dev(keep), novelty=nov) == ip.CCD_OK
+    torch.cuda.synchronize()
+    for g, w in zip([_bytes(K), _bytes(V), Ks.cpu().numpy(), Vs.cpu().numpy(), nov.cpu().numpy()], want):
+        np.testing.assert_array_equal(g, w)
+    assert (wide[:, :, 0] == 0).all() and (wide[:, :, 2] == 0).all() and (wide[..., page:] == 0).all()
+
+
 def test_compact_leaves_rows_whose_entry_is_outside_the_page():
     K, V, Ks, Vs = _random_cache("int8", 1, 1, 64, 64, 1, 1)
     keep = np.array([[[0, 5, 64, 9, -1, 2 ** 31 - 1, 40]]], np.int32)
