@@ -72,12 +72,14 @@ struct TurnEight {
 };
 // where the partners of a lane's eight elements begin (kPieces)
 __device__ __forceinline__ int partners_at(const Rotary& R, int e0) { return e0 >= R.rot ? e0 : e0 < R.rot / 2 ? e0 + R.rot / 2 : e0 - R.rot / 2; }
-// ... and otherwise, one by one: x's neighbours, or from the row
+// ... and otherwise, one by one: x's neighbours, or from the row.  An element that is not turned is its own partner in any layout: taken 0 times, another's that is no number
+// would make it none.
 template <class T>
 __device__ __forceinline__ void load_partners(const Rotary& R, const T* row, int e0, const float (&x)[kPer], float (&z)[kPer]) {
   const int pairs = R.rot / 2;
 #pragma unroll
-  for (int j = 0; j < kPer; ++j) z[j] = R.half ? load_elem(row + (e0 + j >= R.rot ? e0 + j : e0 + j < pairs ? e0 + j + pairs : e0 + j - pairs)) : x[j ^ 1];
+  for (int j = 0; j < kPer; ++j)
+    z[j] = R.half ? load_elem(row + (e0 + j >= R.rot ? e0 + j : e0 + j < pairs ? e0 + j + pairs : e0 + j - pairs)) : e0 + j >= R.rot ? x[j] : x[j ^ 1];
 }
 
 // the largest |x|, as bits: an infinite value or a NaN is larger than all numbers

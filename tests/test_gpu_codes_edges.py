@@ -1,0 +1,43 @@
+"""The cache in 8 bits at its edges: elements that are no numbers beside ones that are not turned.  Tolerances as in test_gpu_codes; codes and scales bit for bit wherever nothing is rotated.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import codes_oracle as C
+from oracle import paged_oracle as O
+from paper_2410_01518_amd import infinipot as ip
+from tests.test_gpu_codes import _bytes, _empty_cache
+from tests.test_gpu_paged import DT, _dev, _f64
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("kind,rows", [("int8", 1), ("e4m3", 1), ("e4m3", 8)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("layout", [ip.CCD_ROPE_HALF, ip.CCD_ROPE_PAIRS])
+@pytest.mark.parametrize("d,rot", [(64, 32), (128, 12), (128, 96)])
+def test_append_beside_what_is_no_number(kind, rows, dtype, layout, d, rot):
+    """Infinities and NaN among the elements that are not turned are the codes of those elements alone; what is not turned keeps its sign, zeros too.  The largest elements stand there,
+    so scales and codes of the elements that are not turned are known bit for bit."""
+    T, Hkv, page = 16, 3, 8
+    new = torch.randn((T, Hkv, d), generator=torch.Generator(device="cuda").manual_seed(rot), device="cuda").to(DT[dtype])
+    new[..., rot:] *= 16.0
+    new[..., rot + 4] = 50.0
+    new[..., rot + 6], new[..., rot + 7] = -0.0, 1.0
+    new[3, 0, rot], new[3, 1, rot + 1] = float("inf"), float("-inf")
+    new[5, 2, d - 1], new[6, 2, d - 2] = float("nan"), float("inf")
+    K, V, Ks, Vs = _empty_cache(kind, 2, Hkv, page, d, rows)
+    bits, scales = _bytes(K), Ks.cpu().numpy()
+    rope = ip.make_rope(new, rot=rot, layout=layout)
+    slots, positions = np.arange(T, dtype=np.int32), np.arange(T, dtype=np.int32) * 1001
+    paged, codes = ip.make_paged(K, tokens=T, dtype=DT[dtype], K_new=new), ip.make_codes(K, Ks)
+    ip.ccd_paged_append_codes(paged, codes, new, new, _dev(slots), K, V, Ks, Vs, rope=rope, positions=_dev(positions), turns=ip.rope_turns(rope))
+    torch.cuda.synchronize()
+    C.append(O.rope(_f64(new), positions, O.frequencies(rot, 10000.0), half=layout == ip.CCD_ROPE_HALF), slots, bits, scales, kind, rows)
+    np.testing.assert_array_equal(Ks.cpu().numpy(), scales)
+    got = _bytes(K)
+    known = np.broadcast_to(np.isfinite(np.repeat(scales, rows, axis=2))[..., None], got.shape)[..., rot:]      # (int8: rows that are no numbers have no codes to speak of)
+    np.testing.assert_array_equal(got[..., rot:][known], bits[..., rot:][known])
+    assert known.sum() < known.size if kind == "int8" else (bits[..., rot:] == 0x7F).sum() == 4
+    np.testing.assert_array_equal(np.isnan(C.decode(got, scales, kind, rows)), np.isnan(C.decode(bits, scales, kind, rows)))
