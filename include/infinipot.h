@@ -345,7 +345,8 @@ CCD_API int ccd_paged_attend(const ccd_paged_t* paged, const void* Q, const void
  * Tokens that share a scale are a block: rows scale_rows * j .. scale_rows * (j + 1) - 1 of a page.  A call that writes the first row of a block begins it
  * anew: what the block held is gone.  Otherwise the block's scale is the larger of its own and what the new rows need, and where it grows, the rows before the
  * first new one are rounded again to the new scale (of a power of two: only what falls below 2^-6 of it changes).  Rows of the block that lie behind the
- * first new one and are not written by the call count as not yet written.
+ * first new one and are not written by the call count as not yet written.  Every call takes any scales, those of a cache quantised elsewhere too; the own scale of a block that an
+ * append goes on in is taken as the next power of two, at most 2^120 (0 where it is negative or no number), and the rows before are rounded again from what they read as.
  *
  *   ccd_paged_append_codes   quantises new keys and values (embedded on the way, if asked for) and writes them to their rows
  *   ccd_paged_read_codes     cached tokens back as numbers: for the scores of a distillation, or to hand a sequence on

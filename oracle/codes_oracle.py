@@ -49,6 +49,11 @@ def encode(x, scale, kind):
     return np.where(np.isfinite(x), c + np.where(np.signbit(y), 128, 0), 0x7F).astype(np.uint8)
 
 
+def own_scale(s):
+    """A block's scale as it was found: the power of two at or above it, 2^120 at most; 0 where it is negative or no number."""
+    return min(2.0 ** math.ceil(math.log2(s)), 2.0 ** 120) if math.isfinite(s) and s > 0.0 else 0.0
+
+
 def append(x, slots, codes, scales, kind, rows):
     """x [tokens, Hkv, d] (64 bits) to the rows of slots (negative or outside: not written), changing codes and scales.  Returns nothing."""
     n_pages, Hkv, page, _ = codes.shape
@@ -61,11 +66,13 @@ def append(x, slots, codes, scales, kind, rows):
         first = min(r for r, _ in new)
         for h in range(Hkv):
             fresh = np.stack([x[t, h] for _, t in new])
-            need, old = scale_for(fresh, kind), float(scales[p, h, j])
-            s = need if first == 0 else max(old, need)
-            if first > 0 and s > old:
+            need, old = scale_for(fresh, kind), scales[p, h, j]
+            s = need if first == 0 else max(own_scale(float(old)), need)
+            if first > 0 and s != old:
                 r = slice(j * rows, j * rows + first)
-                codes[p, h, r] = encode(NUMBERS[kind][codes[p, h, r]] * old, s, kind)
+                with np.errstate(over="ignore", invalid="ignore"):
+                    was = NUMBERS[kind][codes[p, h, r]].astype(np.float32) * old            # (what the rows read as, in fp32)
+                codes[p, h, r] = encode(was, s, kind)
             for r, t in new:
                 codes[p, h, j * rows + r] = encode(x[t, h], s, kind)
             scales[p, h, j] = math.nan if kind == "int8" and not np.isfinite(fresh).all() else s

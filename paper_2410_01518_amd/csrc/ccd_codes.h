@@ -51,7 +51,13 @@ __device__ __forceinline__ float scale_for(float top) {
   const int e = (int)(bits >> 23) - 8 + ((bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);          // biased
   return __uint_as_float((uint32_t)(e < 7 ? 7 : e) << 23);                                  // (7: 2^-120)
 }
-// 1 / scale: exact for a power of two, 2^-22 of it off at most otherwise
+// The scale of a block that a call finds, as one that e4m3 codes are rounded to: the smallest power of two that is not below it, 2^120 at most (no fp32 number needs more; a scale
+// from elsewhere may be any number), 0 where it is negative or none, as no row then reads as what a scale could keep.
+__device__ __forceinline__ float power_of_two_scale(float scale) {
+  const uint32_t bits = __float_as_uint(scale);
+  return bits >= 0x7F800000u ? 0.f : fminf(__uint_as_float((bits + 0x7FFFFFu) & 0x7F800000u), 1.329227995784916e36f);
+}
+// 1 / scale: exact for a power of two, 2^-22 of it off at most otherwise (int8; e4m3 takes powers of two alone)
 template <int CODE>
 __device__ __forceinline__ float inverse_scale(float scale) {
   if constexpr (CODE == kInt8) return __builtin_amdgcn_rcpf(scale);

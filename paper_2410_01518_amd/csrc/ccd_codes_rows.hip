@@ -303,8 +303,9 @@ __global__ __launch_bounds__(512, 4) void append_blocks_kernel(Paged P, Codes C,
       }
 #pragma unroll
       for (int k = 32; k; k >>= 1) { const uint32_t y = __shfl_xor(top, k); top = y > top ? y : top; }
-      const float scale = fmaxf(old, scale_for<kE4m3>(__uint_as_float(top))), inverse = inverse_scale<kE4m3>(scale);
-      if (there && !anew && scale > old)
+      const float scale = fmaxf(power_of_two_scale(old), scale_for<kE4m3>(__uint_as_float(top))), inverse = inverse_scale<kE4m3>(scale);
+      // (what stands before is rounded again wherever its scale becomes another one, NaN among them)
+      if (there && !anew && scale != old)
         for (int r0 = block << C.shift; r0 < first; r0 += kPart) {
           uint2 w[kKeep];
 #pragma unroll

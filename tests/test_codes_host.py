@@ -292,3 +292,12 @@ def test_a_block_of_the_reference_worked_by_hand():
     C.append(np.array([[[0.25]]]), [0], codes, scales, "e4m3", 2)
     assert scales[0, 0, 0] == 2.0 ** -10 and scales[0, 0, 1] == 7.0
     assert math.isclose(C.decode(codes, scales, "e4m3", 2)[0, 0, 0, 0], 0.25)
+
+
+def test_a_block_of_the_reference_quantised_elsewhere():
+    """Scale 3: rows read as 3 and -6, and go on under 4 as 3 and -6; under a scale that is none they read as NaN and stay so."""
+    for held, scale, rows in ((3.0, 4.0, [3.0, -6.0]), (math.nan, 2.0 ** -8, [math.nan, math.nan]), (2.0 ** 127, 2.0 ** 120, [2.0 ** 127, math.nan]), (0.0, 2.0 ** -8, [0.0, 0.0])):
+        codes, scales = np.array([0x38, 0xC0, 0x55, 0x55], np.uint8).reshape(1, 1, 4, 1), np.full((1, 1, 1), held, np.float32)
+        C.append(np.array([[[1.0]]]), [2], codes, scales, "e4m3", 4)
+        assert scales[0, 0, 0] == scale
+        np.testing.assert_array_equal(C.decode(codes, scales, "e4m3", 4)[0, 0, :3, 0], rows + [1.0 if scale < 2.0 ** 100 else 0.0])

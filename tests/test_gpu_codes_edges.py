@@ -1,4 +1,4 @@
-"""The cache in 8 bits at its edges: elements that are no numbers beside ones that are not turned.  Tolerances as in test_gpu_codes; codes and scales bit for bit wherever nothing is rotated.
+"""The cache in 8 bits at its edges: elements that are no numbers beside ones that are not turned, blocks quantised elsewhere.  Tolerances as in test_gpu_codes; codes and scales bit for bit wherever nothing is rotated.
 """
 import numpy as np
 import pytest
@@ -41,3 +41,31 @@ def test_append_beside_what_is_no_number(kind, rows, dtype, layout, d, rot):
     np.testing.assert_array_equal(got[..., rot:][known], bits[..., rot:][known])
     assert known.sum() < known.size if kind == "int8" else (bits[..., rot:] == 0x7F).sum() == 4
     np.testing.assert_array_equal(np.isnan(C.decode(got, scales, kind, rows)), np.isnan(C.decode(bits, scales, kind, rows)))
+
+
+@pytest.mark.parametrize("rows,first", [(8, 3), (32, 17)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_append_into_blocks_quantised_elsewhere(rows, first, dtype):
+    """A block's own scale may be any number: the rows before the new ones are rounded again from what they read as, to a scale that is a power of two."""
+    d, page, Hkv = 64, 32, 1
+    held = np.array([3.0, 0.75, 1.0 / 3.0, 5e-7, 1e-40, 0.0, 2.0 ** 120, 1.5 * 2.0 ** 120, 2.0 ** 127, 3.4e38, np.inf, np.nan, 2.0 ** -9, 1.0 + 2.0 ** -23, 2.0 - 2.0 ** -23], np.float32)
+    n = len(held)
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    K, V, Ks, Vs = _empty_cache("e4m3", n, Hkv, page, d, rows)
+    for x in (K, V):
+        x.view(torch.uint8).copy_(torch.randint(0, 256, x.shape, generator=g, device="cuda").to(torch.uint8))
+    for s in (Ks, Vs):
+        s.copy_(_dev(held)[:, None, None].expand(s.shape))
+    new = (torch.randn((2 * n, 2, Hkv, d), generator=g, device="cuda") * 0.01).to(DT[dtype])
+    slots = np.concatenate([[p * page + first, p * page + first + 1] for p in range(n)]).astype(np.int32)
+    want = [(_bytes(x), s.cpu().numpy()) for x, s in ((K, Ks), (V, Vs))]
+    paged, codes = ip.make_paged(K, tokens=2 * n, dtype=DT[dtype], K_new=new[:, 0]), ip.make_codes(K, Ks)
+    assert ip.ccd_paged_append_codes(paged, codes, new[:, 0], new[:, 1], _dev(slots), K, V, Ks, Vs) == ip.CCD_OK
+    torch.cuda.synchronize()
+    for j, (x, s) in enumerate(((K, Ks), (V, Vs))):
+        C.append(_f64(new[:, j]), slots, *want[j], "e4m3", rows)
+        np.testing.assert_array_equal(s.cpu().numpy(), want[j][1])
+        got, bits = (C.E4M3[b] for b in (_bytes(x), want[j][0]))           # (a code that is no number has two signs)
+        np.testing.assert_array_equal(got, bits)
+        fin = np.isfinite(bits)
+        np.testing.assert_array_equal(_bytes(x)[fin], want[j][0][fin])
