@@ -228,6 +228,12 @@ __device__ __forceinline__ bool attend_stretch_codes(const Paged& P, const Atten
     // (by lanes, all that have the token)
     const uint64_t there = __ballot(own_there);
     const bool whole = there == ~(uint64_t)0 && t0 + Tl::kTokens - 1 <= pos_min && t0 >= low_max;
+    // (a value's scale that is no number makes a weight of 0 none: of tokens that are seen it has to, of others it must not)
+    const bool guarded = !whole && __any(!(fabsf(vs) < INFINITY));
+    auto unseen = [&](int j, int h, int i) {
+      const int t = t0 + Tl::token_of(h, 4 * group + i);
+      return !((there >> Tl::lane_of(h, 4 * group + i)) & 1u) || t > pos[j] || t < low[j];
+    };
     const char* values_lds = keys_lds + Tl::kSide + slot;
     Tl::store_keys(keys, keys_lds, lane);
     scales_lds[own] = ks;
@@ -256,10 +262,7 @@ __device__ __forceinline__ bool attend_stretch_codes(const Paged& P, const Atten
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           x[j][h][i] *= scale_of(sk, h, i);
-          if (!whole) {
-            const int t = t0 + Tl::token_of(h, 4 * group + i);
-            if (!((there >> Tl::lane_of(h, 4 * group + i)) & 1u) || t > pos[j] || t < low[j]) x[j][h][i] = -INFINITY;
-          }
+          if (!whole && unseen(j, h, i)) x[j][h][i] = -INFINITY;
           top = fmaxf(top, x[j][h][i]);
         }
       top *= P.scale_log2;
@@ -281,9 +284,13 @@ __device__ __forceinline__ bool attend_stretch_codes(const Paged& P, const Atten
         const float weight = fast_exp2(fmaf(x[j][h][i], P.scale_log2, -ref));
         l[j] += weight;
         e[k] = weight * scale_of(sv, h, i);
-        if (!whole) e[k] = weight == 0.f ? 0.f : e[k];      // (the scale of a token that is not seen may be no number)
-        ls[j] += e[k];
       }
+      if (__builtin_expect(guarded, 0)) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) e[k] = unseen(j, k >> 2, k & 3) ? 0.f : e[k];
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) ls[j] += e[k];
       cut(e, w[j].w);
       if constexpr (Tl::kParts == 1) {
 #pragma unroll

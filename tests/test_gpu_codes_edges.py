@@ -1,4 +1,4 @@
-"""The cache in 8 bits at its edges: elements that are no numbers beside ones that are not turned, blocks quantised elsewhere.  Tolerances as in test_gpu_codes; codes and scales bit for bit wherever nothing is rotated.
+"""The cache in 8 bits at its edges: elements that are no numbers beside ones that are not turned, blocks quantised elsewhere, weights of 0 in fp32.  Tolerances as in test_gpu_codes; codes and scales bit for bit wherever nothing is rotated.
 """
 import numpy as np
 import pytest
@@ -7,7 +7,7 @@ import torch
 from oracle import codes_oracle as C
 from oracle import paged_oracle as O
 from paper_2410_01518_amd import infinipot as ip
-from tests.test_gpu_codes import _bytes, _empty_cache
+from tests.test_gpu_codes import _bytes, _empty_cache, _numbers, _paged_problem, _run_attend
 from tests.test_gpu_paged import DT, _dev, _f64
 
 pytestmark = pytest.mark.gpu
@@ -69,3 +69,37 @@ def test_append_into_blocks_quantised_elsewhere(rows, first, dtype):
         np.testing.assert_array_equal(got, bits)
         fin = np.isfinite(bits)
         np.testing.assert_array_equal(_bytes(x)[fin], want[j][0][fin])
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("pos", [10, 40, 66])
+@pytest.mark.parametrize("news", [[1], [3], [40], [1, 40], [2, 1, 1]])
+@pytest.mark.parametrize("length,max_len", [(70, None), (70 + 32 * 40, None), (70 + 32 * 40, 64)])
+def test_a_value_that_is_no_number_and_is_seen(kind, dtype, pos, news, length, max_len):
+    """A row that sees such a value has it, whatever is left of its weight: here 0 in fp32, in tiles that are seen whole and in others, however the call is cut."""
+    lens = [length] * len(news)
+    p = _paged_problem(21, kind, 1, dtype, lens, news, 4, 2, 64, 16)
+    at = length - 70 + pos
+    p["Q"].copy_(p["Q"].abs() + 1.0)
+    for b in range(len(news)):
+        page, row = int(p["table"][b, at // 16]), at % 16
+        if kind == "int8":                                                     # the key: a logit far below all others, about -127 * 64 * 1.8 * 8 / 8
+            p["K"].view(torch.uint8)[page, :, row] = 0x81
+            p["Ks"][page, :, row] = 8.0
+            p["Vs"][page, :, row] = float("nan")
+        else:
+            p["K"].view(torch.uint8)[page, :, row] = 0xFE
+            p["Ks"][page, :, row] = 8.0
+            p["V"].view(torch.uint8)[page, 0, row, 5] = 0x7F
+            p["V"].view(torch.uint8)[page, 1, row] = 0x7F
+    out, lse = _run_attend(p, max_len=max_len)
+    K, V = _numbers(p)
+    with np.errstate(invalid="ignore"):
+        want, want_lse, _, _ = O.attend(_f64(p["Q"]), K, V, p["table"], p["q_start"], p["lens"])
+    np.testing.assert_array_equal(np.isnan(_f64(out)), np.isnan(want))
+    assert np.isnan(want).any() and np.isfinite(want_lse).all()
+    for b in range(len(news)):
+        K[int(p["table"][b, at // 16]), :, at % 16] = 0.0                      # (the sizes of the logits that have weights)
+    logit = O.attend(_f64(p["Q"]), K, np.zeros_like(V), p["table"], p["q_start"], p["lens"])[3]
+    assert (np.abs(_f64(lse) - want_lse) <= (3 * 64 + 12) * 2.0 ** -24 * logit + length * 2.0 ** -24 + 2.0 ** -20 + 2.0 ** -22 * np.abs(want_lse)).all()
