@@ -1,4 +1,5 @@
-"""The cache in 8 bits at its edges: elements that are no numbers beside ones that are not turned, blocks quantised elsewhere, weights of 0 in fp32.  Tolerances as in test_gpu_codes; codes and scales bit for bit wherever nothing is rotated.
+"""The cache in 8 bits at its edges: elements that are no numbers beside ones that are not turned, blocks quantised elsewhere, weights of 0 in fp32, stretches of more than
+64 tiles, odd pages of long caches.  Tolerances as in test_gpu_codes; codes and scales bit for bit wherever nothing is rotated.
 """
 import numpy as np
 import pytest
@@ -7,7 +8,7 @@ import torch
 from oracle import codes_oracle as C
 from oracle import paged_oracle as O
 from paper_2410_01518_amd import infinipot as ip
-from tests.test_gpu_codes import _bytes, _empty_cache, _numbers, _paged_problem, _run_attend
+from tests.test_gpu_codes import _bytes, _check_attend, _empty_cache, _numbers, _paged_problem, _run_attend
 from tests.test_gpu_paged import DT, _dev, _f64
 
 pytestmark = pytest.mark.gpu
@@ -103,3 +104,24 @@ def test_a_value_that_is_no_number_and_is_seen(kind, dtype, pos, news, length, m
         K[int(p["table"][b, at // 16]), :, at % 16] = 0.0                      # (the sizes of the logits that have weights)
     logit = O.attend(_f64(p["Q"]), K, np.zeros_like(V), p["table"], p["q_start"], p["lens"])[3]
     assert (np.abs(_f64(lse) - want_lse) <= (3 * 64 + 12) * 2.0 ** -24 * logit + length * 2.0 ** -24 + 2.0 ** -20 + 2.0 ** -22 * np.abs(want_lse)).all()
+
+
+@pytest.mark.parametrize("kind,rows", [("int8", 1), ("e4m3", 16)])
+@pytest.mark.parametrize("dtype,length,new,page,d,max_len", [
+    ("bf16", 9200, 9, 16, 128, 64), ("bf16", 9200, 17, 48, 64, 64), ("bf16", 9200, 10, 4096, 128, 64), ("fp32", 9200, 9, 16, 64, 64),      # a stretch of 144 tiles
+    ("bf16", 24000, 9, 64, 64, 1100), ("bf16", 9200, 9, 16, 128, None),                # stretches of 75 tiles or more, without the sums of rounded weights; many short ones
+])
+def test_stretches_of_more_than_64_tiles(kind, rows, dtype, length, new, page, d, max_len):
+    """Shuffled pages, by few stretches (the hint says so): pages are looked up for 64 tiles at once."""
+    p = _paged_problem(23, kind, rows, dtype, [length], [new], 4, 1, d, page)
+    out, lse = _run_attend(p, max_len=max_len)
+    _check_attend(p, out, lse, dtype)
+
+
+@pytest.mark.parametrize("kind,rows", [("int8", 1), ("e4m3", 1), ("e4m3", 4)])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("lens,news,page", [([1800, 1300], [9, 17], 37), ([2500], [17], 100), ([4300], [9], 100)])
+def test_chunks_over_odd_pages_of_long_caches(kind, rows, d, lens, news, page):
+    p = _paged_problem(29, kind, rows if page % rows == 0 else 1, "bf16", lens, news, 8, 2, d, page)
+    out, lse = _run_attend(p)
+    _check_attend(p, out, lse, "bf16")
