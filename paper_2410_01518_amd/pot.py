@@ -67,6 +67,8 @@ def _pool(shape, dtype, codes, scale_rows, device):
         return K, torch.zeros_like(K), None, None
     if codes not in ip.CODE_TYPES:
         raise TypeError(f"unsupported code type {codes}")
+    if scale_rows < 1 or scale_rows & (scale_rows - 1) or shape[-2] % scale_rows or (scale_rows > 1 and codes is not torch.float8_e4m3fn):
+        raise ValueError("scale_rows is a power of two that divides the page, and 1 with codes of torch.int8")
     K = torch.zeros(shape, dtype=torch.uint8, device=device).view(codes)
     scales = torch.zeros((*shape[:-2], shape[-2] // scale_rows), dtype=torch.float32, device=device)
     return K, torch.zeros_like(K.view(torch.uint8)).view(codes), scales, torch.zeros_like(scales)
