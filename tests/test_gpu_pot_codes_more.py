@@ -1,0 +1,73 @@
+"""Distillation of pots and pools in 8 bits: log-sum-exps handed in, novelty with strides of its own, groups of pots, refusals.
+
+Scores with log-sum-exps are compared with a plain pot's that holds the numbers read back and takes the same log-sum-exps: the same keys and normalisers in other kernels' order of sums,
+so 3e-5 relative as in test_gpu_pot_codes (fp32 2e-3).
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import codes_oracle as C
+from paper_2410_01518_amd import infinipot as ip
+from paper_2410_01518_amd.pot import MemoryPot
+from tests import gpu_util as gu
+from tests.test_gpu_codes import CODE, _bytes
+from tests.test_gpu_paged import DT
+from tests.test_gpu_pot_codes import _fill
+
+pytestmark = pytest.mark.gpu
+
+
+def _plain(pot, kind):
+    """A pot of numbers that holds what `pot` stands for."""
+    plain = MemoryPot(pot.B, pot.L, pot.Hkv, pot.d, pot.n_cap, pot.k, pot.T, dtype=pot.dtype)
+    for to, x, s in ((plain.K, pot.K, pot.K_scales), (plain.V, pot.V, pot.V_scales)):
+        to.copy_(torch.from_numpy(C.decode(_bytes(x.flatten(0, 1)), s.flatten(0, 1).cpu().numpy(), kind, 1)).view(to.shape).cuda().to(pot.dtype))
+    plain.novelty.copy_(pot.novelty)
+    plain.n_valid = pot.n_valid
+    return plain
+
+
+def _off(a, b):
+    """The largest relative difference of finite scores; infinite ones are in the same places."""
+    a, b = (x.cpu().numpy().astype(np.float64) for x in (a, b))
+    assert (np.isinf(a) == np.isinf(b)).all()
+    fin = np.isfinite(b)
+    return (np.abs(a[fin] - b[fin]) / (np.abs(b[fin]) + 1e-30)).max()
+
+
+def _compacted(pot, before, keep):
+    """Codes, scales and novelty are the kept rows of `before`, in order, and behind them what stood there."""
+    after = [_bytes(pot.K), _bytes(pot.V), pot.K_scales.cpu().numpy(), pot.V_scales.cpu().numpy(), pot.novelty.cpu().numpy()]
+    flat = keep.reshape(-1, pot.Hkv, pot.k)
+    for x, y in zip(after, before):
+        np.testing.assert_array_equal(x.reshape(-1, pot.Hkv, *x.shape[3:]), C.compact(y.reshape(-1, pot.Hkv, *y.shape[3:]), flat))
+
+
+def _held(pot):
+    return [_bytes(pot.K), _bytes(pot.V), pot.K_scales.cpu().numpy(), pot.V_scales.cpu().numpy(), pot.novelty.cpu().numpy()]
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype,d,P", [("bf16", 128, 32), ("bf16", 64, 5), ("fp32", 64, 9)])
+def test_distillation_takes_the_log_sum_exps_it_is_given(kind, dtype, d, P):
+    B, L, Hkv, Hq, n, k = 2, 3, 2, 8, 512, 200
+    g = torch.Generator(device="cuda").manual_seed(7)
+    pot = MemoryPot(B, L, Hkv, d, n, k, 40, dtype=DT[dtype], codes=CODE[kind])
+    _fill(pot, n, g)
+    plain, before = _plain(pot, kind), _held(pot)
+    Q = torch.randn((B, L, Hq, P, d), generator=g, device="cuda").to(DT[dtype])
+    lse = pot.attend(Q, behind=True)[1]
+    scores = [torch.zeros((B, L, Hkv, n), device="cuda") for _ in range(3)]
+    assert pot.distill(Q, scores=scores[0], lse=lse) == ip.CCD_OK
+    shape = ip.make_shape(Q, plain.K, plain.novelty, k=k, T=40, pool_w=7)
+    ip.ccd_score_lse(shape, Q, plain.K, lse.flip(1).contiguous(), plain.novelty, scores[2], ip.alloc_workspace(shape))
+    assert plain.distill(Q, scores=scores[1], lse=lse) == ip.CCD_OK
+    torch.cuda.synchronize()
+    tol = 3e-5 if dtype == "bf16" else 2e-3
+    assert _off(scores[0], scores[1]) <= tol
+    assert not torch.allclose(scores[2], scores[0], rtol=0.05)            # (other rows' log-sum-exps give other scores)
+    keep, a = gu.to_host(pot.keep_idx), scores[0].cpu().numpy()
+    np.testing.assert_array_equal(keep, gu.replay_select(a, k))
+    gu.assert_keep_matches(keep, gu.to_host(plain.keep_idx), scores[1].cpu().numpy(), k)
+    _compacted(pot, before, keep)
