@@ -95,7 +95,13 @@ def _distil_codes(K, V, K_scales, V_scales, Q_cat, novelty, keep_idx, workspace,
     else:
         ip.ccd_score_lse(shape, Q_cat, numbers, lse, novelty, scores, workspace)
     ip.ccd_select(shape, scores, keep_idx)
-    return ip.ccd_paged_compact_codes(paged, codes, *flat, keep_idx, novelty=novelty if novelty is not None and novelty.dim() == 4 else None)
+    # (carried per head, as the shape has it; compacted where it stands if it is dense, else by way of a copy)
+    carried = novelty if novelty is not None and (shape.nov_stride_l or shape.nov_stride_h) else None
+    dense = carried if carried is None else carried.contiguous()
+    rc = ip.ccd_paged_compact_codes(paged, codes, *flat, keep_idx, novelty=dense)
+    if dense is not carried:
+        carried[..., :k].copy_(dense[..., :k])
+    return rc
 
 
 class MemoryPot:

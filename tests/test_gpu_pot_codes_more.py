@@ -9,7 +9,7 @@ import torch
 
 from oracle import codes_oracle as C
 from paper_2410_01518_amd import infinipot as ip
-from paper_2410_01518_amd.pot import MemoryPot
+from paper_2410_01518_amd.pot import MemoryPot, PagedPots
 from tests import gpu_util as gu
 from tests.test_gpu_codes import CODE, _bytes
 from tests.test_gpu_paged import DT
@@ -71,3 +71,51 @@ def test_distillation_takes_the_log_sum_exps_it_is_given(kind, dtype, d, P):
     np.testing.assert_array_equal(keep, gu.replay_select(a, k))
     gu.assert_keep_matches(keep, gu.to_host(plain.keep_idx), scores[1].cpu().numpy(), k)
     _compacted(pot, before, keep)
+
+
+def _full_pool(kind, pots=1, L=2, Hkv=2, n=256, d=64, Hq=4, P=16, **kw):
+    """A pool of pots whose first sequence's is full, and what a distillation of it takes."""
+    pool = PagedPots(pots + 1, pots + 2, n, n, n, L, Hq, Hkv, d, codes=CODE[kind], **kw)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    assert pool.step([n] + [0] * pots) == n
+    for layer in range(L):
+        pool.append(layer, *(torch.randn((n, Hkv, d), generator=g, device="cuda").bfloat16() for _ in range(2)))
+    return pool, int(pool.table[0, 0]), torch.randn((1, L, Hq, P, d), generator=g, device="cuda").bfloat16()
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("how", ["dense", "layers first", "wide rows", "shared", "shared by expansion"])
+def test_a_pool_takes_novelty_of_any_strides(kind, how):
+    """The same tokens are kept and the same novelty stands beside them, however it is laid out; what lies between its rows is left alone."""
+    L, Hkv, n, k = 2, 2, 256, 96
+    pool, page, Q_cat = _full_pool(kind)
+    values = torch.rand((1, L, Hkv, n), generator=torch.Generator(device="cuda").manual_seed(4), device="cuda")
+    if "shared" in how:
+        values = values[:, :1, :1].expand(1, L, Hkv, n)
+    dense = values.contiguous()
+    room = torch.full((L, 3, Hkv, n + 8), -1.0, device="cuda")
+    nov = dense.clone()
+    if how == "layers first":
+        nov = room[..., :n].transpose(0, 1)[1:2]
+        nov.copy_(dense)
+    elif how == "wide rows":
+        nov = room.transpose(0, 1)[:1, ..., :n]
+        nov.copy_(dense)
+    elif how == "shared":
+        nov = dense[:, 0, 0].contiguous()
+    elif how == "shared by expansion":
+        nov = dense[:, :1, :1].contiguous().expand(1, L, Hkv, n)
+    keep = torch.empty((1, L, Hkv, k), dtype=torch.int32, device="cuda")
+    assert pool.distill(0, page, Q_cat, nov, keep, None, k=k, T=30) == ip.CCD_OK
+    other, other_page, _ = _full_pool(kind)
+    want, want_keep = dense.clone(), torch.empty_like(keep)
+    assert other.distill(0, other_page, Q_cat, want, want_keep, None, k=k, T=30) == ip.CCD_OK
+    torch.cuda.synchronize()
+    assert torch.equal(keep, want_keep)
+    assert torch.equal(nov, {"shared": values[:, 0, 0], "shared by expansion": values}.get(how, want))
+    assert torch.equal(want, torch.cat([torch.gather(dense, 3, want_keep.long()), dense[..., k:]], 3))
+    for a, b in ((pool.K, other.K), (pool.V, other.V), (pool.K_scales, other.K_scales), (pool.V_scales, other.V_scales)):
+        assert torch.equal(a[page].view(torch.uint8), b[other_page].view(torch.uint8))
+    if how in ("layers first", "wide rows"):
+        nov.fill_(-1.0)
+        assert (room == -1.0).all()
