@@ -335,7 +335,8 @@ CCD_API int ccd_paged_attend(const ccd_paged_t* paged, const void* Q, const void
 /* ---- The same cache in 8 bits ---------------------------------------------------------------------------------------
  *
  * K_codes and V_codes [n_pages, Hkv, page, d] hold a byte per element, K_scales and V_scales (fp32) [n_pages, Hkv, page / scale_rows]
- * what a code of 1 stands for, not negative: x = code * scale.  Decoding reads half the bytes of a bf16 cache, and a memory pot takes half of the memory.
+ * what a code of 1 stands for, not negative: x = code * scale.  Decoding reads half the bytes of a bf16 cache, and a memory pot takes half of the memory
+ * (the scores of a distillation need its keys as numbers meanwhile: ccd_paged_read_codes, for as many pots at a time as there is room for).
  *   CCD_INT8   scale_rows = 1, a scale for every token and head: scale = max(|x| / 127, 2^-120) over the head's d elements, code = x / scale rounded to
  *              nearest, halves to even (of the exact quotient).  A token and head that holds an infinite value or a NaN has a scale of NaN, and reads as NaN.
  *   CCD_E4M3   (four bits of exponent, three of mantissa, the largest number 448, no infinities) a scale for every scale_rows tokens and head: the

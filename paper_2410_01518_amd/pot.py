@@ -12,8 +12,9 @@ Only buffer bookkeeping happens here; appending, attention, scoring, selection a
 page is a whole pot, a sequence's pot is distilled as soon as it is full, whatever the others hold.
 
 Either holds its cache in 8 bits if it is given a type of code (`codes`: torch.int8 or torch.float8_e4m3fn): half of a bf16 pot's memory and of the bytes that
-decoding reads.  Keys and values are quantised as they are appended, attention reads the codes; a distillation reads the keys back into a buffer of its own for their
-scores, and moves codes and scales of what it keeps.
+decoding reads.  Keys and values are quantised as they are appended, attention reads the codes; a distillation reads keys back into a buffer of its own for their
+scores, and moves codes and scales of what it keeps.  The buffer has the keys of about 256 heads at a time, however many sequences and layers there are (32 layers of 8
+heads, 4096 tokens of 128 in bf16: 256 MiB, while one distillation runs, next to 264 MiB of codes and scales for every sequence).
 """
 from __future__ import annotations
 
@@ -74,26 +75,54 @@ def _pool(shape, dtype, codes, scale_rows, device):
     return K, torch.zeros_like(K.view(torch.uint8)).view(codes), scales, torch.zeros_like(scales)
 
 
+# Units (pots and heads) of which a distillation over codes reads the keys back at a time: about one for every compute unit, so that the score kernels take no longer than over all at
+# once.  8 heads, 4096 tokens of 128, us: 4 sequences of 32 layers 1095 over all 1024 units, 1065 by 256, 1249 by 128, 1551 by 64; one of 48 layers 459 at once, 431 by 192; but 36 layers 351 and 420 by 144.
+READ_UNITS = 256
+
+
+def _read_groups(B, L, Hkv):
+    """(b0, b1, l0, l1): sequences and layers whose keys are read back at a time, side by side in memory."""
+    parts = (L * Hkv + READ_UNITS // 2) // READ_UNITS       # of a sequence's layers
+    if parts > 1:
+        each = -(-L // parts)
+        return [(b, b + 1, l, min(L, l + each)) for b in range(B) for l in range(0, L, each)]
+    each = max(1, READ_UNITS // (L * Hkv))
+    return [(b, min(B, b + each), 0, L) for b in range(0, B, each)]
+
+
 def _distil_codes(K, V, K_scales, V_scales, Q_cat, novelty, keep_idx, workspace, *, dtype, n_valid, k, T, pool_w, pool_mode, scores=None, lse=None) -> int:
     """ccd_compress (ccd_compress_lse with lse) over codes K, V [B, L, Hkv, n_cap, d]: the keys are read back for their scores.  workspace: of ccd_score, or None."""
     B, L, Hkv, n_cap, d = K.shape
     if n_valid < n_cap or n_valid <= k:
         return ip.CCD_NOOP
-    pages, device = B * L, K.device
-    numbers = torch.empty(K.shape, dtype=dtype, device=device)
-    table = torch.arange(pages, dtype=torch.int32, device=device)[:, None]
-    q_start, kv_len = torch.arange(pages + 1, dtype=torch.int32, device=device) * n_cap, torch.full((pages,), n_cap, dtype=torch.int32, device=device)
+    device, groups = K.device, _read_groups(B, L, Hkv)
+    most = max((b1 - b0) * (l1 - l0) for b0, b1, l0, l1 in groups)
+    buffer = torch.empty((most, Hkv, n_cap, d), dtype=dtype, device=device)
+    table = torch.arange(B * L, dtype=torch.int32, device=device)[:, None]
+    q_start, kv_len = torch.arange(most + 1, dtype=torch.int32, device=device) * n_cap, torch.full((most,), n_cap, dtype=torch.int32, device=device)
     flat = [x.flatten(0, 1) for x in (K, V, K_scales, V_scales)]
     codes = ip.make_codes(flat[0], flat[2])
-    paged = ip.make_paged(flat[0], tokens=pages * n_cap, dtype=dtype, block_table=table, out=numbers.flatten(0, 1))
-    ip.ccd_paged_read_codes(paged, codes, flat[0], None, flat[2], None, table, q_start, kv_len, numbers.flatten(0, 1), None)
-    shape = ip.make_shape(Q_cat, numbers, novelty, k=k, T=T, pool_w=pool_w, pool_mode=pool_mode, n_valid=n_valid)
     scores = torch.empty((B, L, Hkv, n_valid), dtype=torch.float32, device=device) if scores is None else scores
-    workspace = ip.alloc_workspace(shape, device) if workspace is None else workspace
-    if lse is None:
-        ip.ccd_score(shape, Q_cat, numbers, novelty, scores, workspace)
-    else:
-        ip.ccd_score_lse(shape, Q_cat, numbers, lse, novelty, scores, workspace)
+    for b0, b1, l0, l1 in groups:
+        numbers, own, queries, sums, new, into = buffer, table, Q_cat, lse, novelty, scores
+        if len(groups) > 1:
+            pots, first = (b1 - b0) * (l1 - l0), b0 * L + l0
+            numbers, own, queries, into = buffer[:pots], table[first: first + pots], Q_cat[b0:b1, l0:l1], scores[b0:b1, l0:l1]
+            new = None if novelty is None else novelty[b0:b1] if novelty.dim() == 2 else novelty[b0:b1, l0:l1]
+            if lse is not None:
+                sums = lse[b0:b1, l0:l1]
+                sums = sums if sums.data_ptr() % 16 == 0 else sums.clone()
+        paged = ip.make_paged(flat[0], tokens=own.shape[0] * n_cap, dtype=dtype, block_table=own, out=numbers)
+        ip.ccd_paged_read_codes(paged, codes, flat[0], None, flat[2], None, own, q_start, kv_len, numbers, None)
+        numbers = numbers.view(b1 - b0, l1 - l0, Hkv, n_cap, d)
+        shape = ip.make_shape(queries, numbers, new, k=k, T=T, pool_w=pool_w, pool_mode=pool_mode, n_valid=n_valid)
+        if workspace is None or (len(groups) > 1 and workspace.numel() < ip.ccd_workspace_bytes(shape)):
+            workspace = ip.alloc_workspace(shape, device)
+        if lse is None:
+            ip.ccd_score(shape, queries, numbers, new, into, workspace)
+        else:
+            ip.ccd_score_lse(shape, queries, numbers, sums, new, into, workspace)
+    shape.B, shape.L = B, L                                 # of all: what the selection reads
     ip.ccd_select(shape, scores, keep_idx)
     # (carried per head, as the shape has it; compacted where it stands if it is dense, else by way of a copy)
     carried = novelty if novelty is not None and (shape.nov_stride_l or shape.nov_stride_h) else None

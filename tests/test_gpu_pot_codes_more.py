@@ -119,3 +119,29 @@ def test_a_pool_takes_novelty_of_any_strides(kind, how):
     if how in ("layers first", "wide rows"):
         nov.fill_(-1.0)
         assert (room == -1.0).all()
+
+
+@pytest.mark.parametrize("B,L,Hkv,d,P", [(2, 40, 16, 64, 4), (5, 3, 32, 128, 2), (2, 150, 5, 64, 1)])         # layers by 14, sequences by two, layers by 50 (log-sum-exps not on 16 bytes)
+@pytest.mark.parametrize("with_lse", [False, True])
+def test_keys_are_read_back_some_pots_at_a_time(B, L, Hkv, d, P, with_lse):
+    """Scores, kept rows and what is left as of a plain pot that holds the same numbers; no buffer for all keys at once."""
+    n, k = 64, 24
+    pot = MemoryPot(B, L, Hkv, d, n, k, 6, codes=torch.int8)
+    g = torch.Generator(device="cuda").manual_seed(B)
+    _fill(pot, n, g)
+    plain, before = _plain(pot, "int8"), _held(pot)
+    Q = torch.randn((B, L, Hkv, P, d), generator=g, device="cuda").bfloat16()
+    lse = pot.attend(Q, behind=True)[1] if with_lse else None
+    scores = [torch.zeros((B, L, Hkv, n), device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    held = torch.cuda.memory_allocated()
+    torch.cuda.reset_peak_memory_stats()
+    assert pot.distill(Q, scores=scores[0], lse=lse) == ip.CCD_OK
+    assert torch.cuda.max_memory_allocated() - held < 0.6 * 2 * pot.K.numel()
+    assert plain.distill(Q, scores=scores[1], lse=lse) == ip.CCD_OK
+    torch.cuda.synchronize()
+    assert _off(*scores) <= 3e-5
+    keep = gu.to_host(pot.keep_idx)
+    np.testing.assert_array_equal(keep, gu.replay_select(scores[0].cpu().numpy(), k))
+    gu.assert_keep_matches(keep, gu.to_host(plain.keep_idx), scores[1].cpu().numpy(), k)
+    _compacted(pot, before, keep)
