@@ -606,8 +606,8 @@ def _check_append_codes(paged, codes, rope, K_new, V_new, slots, K_codes, V_code
         full = -(-tokens // codes.new_rows)
         _holds(K_new, (full, Hkv, codes.new_rows, d), (codes.new_stride_b, paged.new_stride_h, paged.new_stride_t, 1))
     else:
-        if codes.new_rows > 0:
-            raise AssertionError("new keys [B, Hkv, m, d] needed")
+        if codes.new_rows > 0 or (K_new.dim() != 3 and tokens > 0):
+            raise AssertionError("new keys [B, Hkv, m, d] needed" if codes.new_rows > 0 else "new keys [tokens, Hkv, d] needed, or a descriptor made for [B, Hkv, m, d]")
         _holds(K_new, (tokens, Hkv, d), (paged.new_stride_t, paged.new_stride_h, 1))
     _check_cache(paged, codes, K_codes, V_codes, K_scales, V_scales)
     _int32(tokens, slots)

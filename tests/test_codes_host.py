@@ -301,3 +301,19 @@ def test_a_block_of_the_reference_quantised_elsewhere():
         C.append(np.array([[[1.0]]]), [2], codes, scales, "e4m3", 4)
         assert scales[0, 0, 0] == scale
         np.testing.assert_array_equal(C.decode(codes, scales, "e4m3", 4)[0, 0, :3, 0], rows + [1.0 if scale < 2.0 ** 100 else 0.0])
+
+
+def test_new_keys_in_an_order_that_the_descriptor_does_not_know(launches):  # noqa: F811
+    """[B, Hkv, m, d] with a descriptor made without them, and the other way round; no tokens in either order are nothing to refuse."""
+    for batched in (True, False):
+        t, call = _append_call(batched)
+        paged = ip.make_paged(t["K_codes"], tokens=TOKENS, dtype=torch.bfloat16, K_new=t["K_new"])
+        other = ip.make_codes(t["K_codes"], t["K_scales"], K_new=_append_call(not batched)[0]["K_new"])
+        with pytest.raises(AssertionError, match="needed"):
+            ip.ccd_paged_append_codes(paged, other, rope=None, **{x: t[x] for x in t if x not in ("positions", "turns")})
+        assert launches.calls == 0
+        assert call(t) == ip.CCD_OK and launches.calls == 1
+        launches.calls = 0
+    none = _bf16(B, HKV, 0, D)
+    paged, codes = ip.make_paged(t["K_codes"], tokens=0, dtype=torch.bfloat16, K_new=none), ip.make_codes(t["K_codes"], t["K_scales"], K_new=none)
+    assert ip.ccd_paged_append_codes(paged, codes, none, none, _ints(0), *(t[x] for x in ("K_codes", "V_codes", "K_scales", "V_scales"))) == ip.CCD_OK
