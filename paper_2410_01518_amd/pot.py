@@ -338,6 +338,7 @@ class PagedPots:
         [1, page] or [1, L, Hkv, page], keep_idx [1, L, Hkv, k].  Returns the library's code; after CCD_OK the sequence has k tokens, as of the
         next step."""
         assert self.table.shape[1] == 1, "distillation needs pages that are whole pots"
+        assert self.codes is None or self.K_scales.shape[-1] == self.page, "distillation needs a scale per token"
         K, V = self.K[page_id: page_id + 1], self.V[page_id: page_id + 1]
         if self.codes is not None:
             rc = _distil_codes(K, V, self.K_scales[page_id: page_id + 1], self.V_scales[page_id: page_id + 1], Q_cat, novelty, keep_idx, workspace, dtype=self.dtype,

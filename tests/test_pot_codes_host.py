@@ -1,8 +1,9 @@
-"""Pools in 8 bits on the host: what their constructors refuse."""
+"""Pools in 8 bits on the host: what they refuse before anything is launched."""
 import pytest
 import torch
 
 from paper_2410_01518_amd.pot import PagedPots
+from tests.test_paged_binding import launches  # noqa: F401  (a fixture)
 
 
 @pytest.mark.parametrize("codes,page,rows", [(torch.float8_e4m3fn, 16, 12), (torch.float8_e4m3fn, 16, 32), (torch.float8_e4m3fn, 48, 3), (torch.float8_e4m3fn, 37, 2), (torch.float8_e4m3fn, 16, 0),
@@ -16,3 +17,14 @@ def test_scale_rows_that_there_cannot_be(codes, page, rows):
 def test_scales_of_a_pool(codes, page, rows):
     pool = PagedPots(2, 4, page, 100, 20, 3, 2, 1, 64, device="cpu", codes=codes, scale_rows=rows)
     assert pool.K.dtype is codes and pool.K.shape == (4, 3, 1, page, 64) and pool.K_scales.shape == (4, 3, 1, page // rows) and not pool.V_scales.any()
+
+
+def test_a_pot_whose_tokens_share_scales_is_not_distilled(launches):  # noqa: F811
+    """Refused before its scores are worked out."""
+    n, L, Hkv, d = 64, 2, 1, 64
+    pool = PagedPots(2, 4, n, n, n, L, 2, Hkv, d, device="cpu", codes=torch.float8_e4m3fn, scale_rows=16)
+    pool.lengths[0] = n
+    keep, workspace = torch.full((1, L, Hkv, 20), -5, dtype=torch.int32), torch.zeros(1 << 16, dtype=torch.uint8)
+    with pytest.raises(AssertionError, match="scale per token"):
+        pool.distill(0, 0, torch.zeros((1, L, 2, 3, d), dtype=torch.bfloat16), torch.zeros((1, n)), keep, workspace, k=20, T=4)
+    assert launches.calls == 0 and pool.lengths[0] == n and (keep == -5).all()
