@@ -366,8 +366,8 @@ typedef struct {
 } ccd_codes_t;
 
 /* ccd_paged_append into codes; slots, positions, rope and turns as there.  With scale_rows > 1 the new tokens of one block have to stand side by side
- * in the call, in any order (the plan numbers them so), and no two calls at once may write to one block.  The rotation is fp32 and not rounded before it is
- * quantised. */
+ * in the call, in any order (the plan numbers them so), and no two calls at once may write to one block.  They are the work of one workgroup: with scale_rows of 16
+ * or 32 a prompt fills the chip, with hundreds it is left to a few compute units.  The rotation is fp32 and not rounded before it is quantised. */
 CCD_API int ccd_paged_append_codes(const ccd_paged_t* paged, const ccd_codes_t* codes, const ccd_rope_t* rope, const void* K_new, const void* V_new,
                            const int32_t* slots, const int32_t* positions, const uint64_t* turns, void* K_codes, void* V_codes,
                            float* K_scales, float* V_scales, void* hip_stream);

@@ -8,7 +8,7 @@
 //
 // Bound by the reading of the cache, d bytes and four of scale per token, head and side, and by the waves that are there to wait for it: a tile is half the bytes
 // of a bf16 one.  So values take no registers on their way, and three waves share a SIMD.  Measured, bf16 queries, 32 heads on 8 of 128, int8: one sequence of 131072 tokens
-// 59 - 61 us (4.5 - 4.7 TB/s), 64 of 500 .. 8192 101 us (4.35 TB/s; 115 with values through registers and two waves), 256 of them 323 us (4.8 TB/s; 357 so).  Tiles of 64 tokens spill: 135 us for the 64;
+// 59 - 61 us (4.5 - 4.7 TB/s), 64 of 500 .. 8192 100 us (4.4 TB/s; 115 with values through registers and two waves), 256 of them 316 us (4.9 TB/s; 357 so); fp32 queries, the 64 114 us, e4m3 105.  Tiles of 64 tokens spill: 135 us for the 64;
 // tiles asked for two ahead change nothing.
 #pragma once
 

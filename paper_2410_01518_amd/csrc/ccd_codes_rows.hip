@@ -219,6 +219,7 @@ __global__ __launch_bounds__(256, 4) void append_tokens_kernel(Paged P, Codes C,
 // A scale per block of 2^shift tokens: a workgroup per `each` tokens, at most 64, takes those that begin a run, tokens of one block side by side, and the run with them.  A
 // wave per head; lanes side by side have a token's row, kKeep times four or eight tokens at a time.  First the run's largest element, then the codes; a run of that many tokens
 // stays in registers in between, longer ones are read twice.  Measured, 16384 tokens of 8 heads of 128, bf16: blocks of 16 25 us (4.0 TB/s), embedded 35; of 64, read twice, 36.
+// A block has one scale, so a run is one workgroup's (of keys, and one of values): 4096 tokens in blocks of 16, 64, 256, 4096: 13, 42, 117, 698 us.
 template <class T, int D, Turned MODE>
 __global__ __launch_bounds__(512, 4) void append_blocks_kernel(Paged P, Codes C, Rotary R, Append<T> N, int each) {
   constexpr int kLanes = D / kPer, kTokens = 64 / kLanes, kKeep = 4, kPart = kKeep * kTokens;
