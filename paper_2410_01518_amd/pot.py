@@ -95,6 +95,10 @@ def _distil_codes(K, V, K_scales, V_scales, Q_cat, novelty, keep_idx, workspace,
     B, L, Hkv, n_cap, d = K.shape
     if n_valid < n_cap or n_valid <= k:
         return ip.CCD_NOOP
+    # (carried per head, as the shape has it: compacted, with rows of its own for every head)
+    carried = novelty if novelty is not None and novelty.dim() == 4 and (novelty.stride(1) or novelty.stride(2)) else None
+    if carried is not None and any(step == 0 and size > 1 for step, size in zip(carried.stride(), carried.shape)):
+        raise AssertionError("novelty that is carried per head and shared by some of them")
     device, groups = K.device, _read_groups(B, L, Hkv)
     most = max((b1 - b0) * (l1 - l0) for b0, b1, l0, l1 in groups)
     buffer = torch.empty((most, Hkv, n_cap, d), dtype=dtype, device=device)
@@ -124,8 +128,7 @@ def _distil_codes(K, V, K_scales, V_scales, Q_cat, novelty, keep_idx, workspace,
             ip.ccd_score_lse(shape, queries, numbers, sums, new, into, workspace)
     shape.B, shape.L = B, L                                 # of all: what the selection reads
     ip.ccd_select(shape, scores, keep_idx)
-    # (carried per head, as the shape has it; compacted where it stands if it is dense, else by way of a copy)
-    carried = novelty if novelty is not None and (shape.nov_stride_l or shape.nov_stride_h) else None
+    # (compacted where it stands if it is dense, else by way of a copy)
     dense = carried if carried is None else carried.contiguous()
     rc = ip.ccd_paged_compact_codes(paged, codes, *flat, keep_idx, novelty=dense)
     if dense is not carried:

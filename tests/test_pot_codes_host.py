@@ -28,3 +28,15 @@ def test_a_pot_whose_tokens_share_scales_is_not_distilled(launches):  # noqa: F8
     with pytest.raises(AssertionError, match="scale per token"):
         pool.distill(0, 0, torch.zeros((1, L, 2, 3, d), dtype=torch.bfloat16), torch.zeros((1, n)), keep, workspace, k=20, T=4)
     assert launches.calls == 0 and pool.lengths[0] == n and (keep == -5).all()
+
+
+@pytest.mark.parametrize("shared", [1, 2])
+def test_novelty_carried_per_head_that_some_heads_share(launches, shared):  # noqa: F811
+    """Rows that are compacted cannot be those of two layers, or of two heads; refused before anything is moved."""
+    n, L, Hkv, d = 64, 2, 3, 64
+    pool = PagedPots(2, 4, n, n, n, L, 3, Hkv, d, device="cpu", codes=torch.int8)
+    pool.lengths[0] = n
+    novelty = torch.zeros((1, 1, Hkv, n) if shared == 1 else (1, L, 1, n)).expand(1, L, Hkv, n)
+    with pytest.raises(AssertionError, match="shared by some"):
+        pool.distill(0, 0, torch.zeros((1, L, 3, 3, d), dtype=torch.bfloat16), novelty, torch.zeros((1, L, Hkv, 20), dtype=torch.int32), None, k=20, T=4)
+    assert launches.calls == 0 and pool.lengths[0] == n
